@@ -72,7 +72,7 @@ typedef enum {
     TFNO_ERR_ALIAS = 4,       /* y overlaps x or W                                        */
     TFNO_ERR_WORKSPACE = 5,   /* workspace missing or smaller than tfno_workspace_bytes() */
     TFNO_ERR_HIP = 6,         /* the HIP runtime reported a launch error                  */
-    TFNO_ERR_ALIGN = 7        /* x, W or y is not aligned to 8 bytes                      */
+    TFNO_ERR_ALIGN = 7        /* a tensor is not aligned: x, W, y to 8 bytes, others to their elements */
 } tfno_status;
 
 /*
@@ -298,6 +298,107 @@ tfno_status tfno_spectral_conv1d_gemm_ifft(const void *x, const void *W, void *y
  */
 tfno_status tfno_spectral_conv1d_auto(const void *x, const void *W, void *y,
                                       int B, int C_in, int C_out, int N, int K, void *stream);
+
+/*
+ * Operators along time
+ * --------------------
+ * The layers above mix a field over the whole transformed axis.  The two operators below mix a trajectory of fields causally along
+ * time and can be advanced by one frame at constant cost: the gated delta rule, a matrix-valued state per head that each token
+ * corrects, and the norm of its queries and keys with the rotation by position.
+ *
+ *  - Tensors are [batch, token, head, value] with the last axis contiguous and the other strides given, in elements and not negative; inputs
+ *    may repeat elements (stride 0), outputs may not.  So slices of one fused projection are taken as they are.
+ *  - Types: float32, or BF16 (tfno_dtype) for what the descriptor says; weights, tables, gates, states and their gradients are float32.
+ *    Sums, norms and states are held in float32 whatever the type.
+ *  - Pointers are aligned to the size of an element (TFNO_ERR_ALIGN); every size, stride and alignment gives the same result, tensors whose
+ *    rows are aligned to 16 bytes the faster one.
+ *  - An output that overlaps an input or another output is TFNO_ERR_ALIAS; slices that interleave in one buffer do not overlap.
+ *  - Streams, ownership, workspace and the detection of errors before anything is launched are as above.  The descriptor is read during the call alone.
+ *  - Equal calls give equal bits: no sum depends on the order in which workgroups run.
+ */
+typedef enum { TFNO_F32 = 0, TFNO_BF16 = 1 } tfno_dtype;
+
+typedef struct { long long batch, token, head; } tfno_strides;   /* in elements */
+
+/*
+ * Norm of queries and keys for each head with the rotation by position, in one pass:
+ *
+ *   y[b,t,h,:] = Rot(p) ( x[b,t,h,:] w / sqrt(mean_d x[b,t,h,d]^2 + eps) ),    p = positions[b,t], or t without positions
+ *
+ * for x = q [B, T, Hq, D] with w = wq and x = k [B, T, Hk, D] with w = wk (float32 [D]; NULL: ones).  Rot turns the first R values of a
+ * head in pairs, (a, b) -> (a c - b s, a s + b c) with c = cos[p, i] and s = sin[p, i] (float32 [P, R / 2], contiguous): pair i is
+ * values i and i + R / 2, or 2 i and 2 i + 1 where `interleaved` is set.  The other D - R values are not turned; R = 0 is the norm alone.
+ * A position outside 0 .. P-1 gives NaN in the values that it would turn.  y may be x itself (the same pointer and strides).
+ *
+ * The backward call takes the gradients of the results (at the places of q_out, k_out) and gives those of q, k and, where the pointers are
+ * not NULL, of the weights.  It needs tfno_head_norm_rope_workspace_bytes(D) bytes of workspace.  dq may be q or dq_out itself.
+ *
+ * Sizes: 1 <= D <= 512, R even, 0 <= R <= D, Hq + Hk >= 1, eps > 0, P >= T without positions (TFNO_ERR_SHAPE); B = 0 or T = 0 is an empty call,
+ * whose weights' gradients are zeros.
+ */
+typedef struct {
+    int dtype;                    /* tfno_dtype of q, k and of their results and gradients */
+    int B, T, Hq, Hk, D, R, P;
+    int interleaved;
+    float eps;
+    long long positions_batch;    /* stride of positions, int32 [B, T] */
+    tfno_strides q, k, q_out, k_out;
+    tfno_strides dq, dk;          /* backward only */
+} tfno_head_norm_desc;
+
+tfno_status tfno_head_norm_rope(const tfno_head_norm_desc *d, const void *q, const void *k, const float *wq, const float *wk,
+                                const float *cos, const float *sin, const int *positions, void *q_out, void *k_out, void *stream);
+tfno_status tfno_head_norm_rope_backward(const tfno_head_norm_desc *d, const void *q, const void *k, const float *wq, const float *wk,
+                                         const float *cos, const float *sin, const int *positions, const void *dq_out,
+                                         const void *dk_out, void *dq, void *dk, float *dwq, float *dwk, void *stream);
+size_t tfno_head_norm_rope_workspace_bytes(int D);
+
+/*
+ * Gated delta rule.  A head's state S [Dk, Dv] starts from `initial` (NULL: zeros) and for every token
+ *
+ *   Sb = exp(g) S,    S = Sb + beta k (v - Sb' k)',    o = scale S' q
+ *
+ * with q, k [B, T, Hk, Dk], v, o [B, T, Hv, Dv], g and beta float32 [B, T, Hv] (g NULL: no decay; g = -inf forgets the state) and states
+ * float32 [B, Hv, Dk, Dv], contiguous.  Hv is a multiple of Hk: value head h uses key head h / (Hv / Hk).  `lengths` (int32 [B] on the device, or
+ * NULL) says how many tokens of each sequence count, as if cut to 0 .. T: the others are not read, their outputs and gradients are zeros, and
+ * final is the state after the last one that counts.  Any decay and any beta are right; with |beta k'k| < 2 and g <= 0 the state stays bounded.
+ * A NaN or an infinity in a token that counts makes its head's results NaN from the chunk of that token on (64 tokens, 32 for float32).
+ *
+ * The whole sequence: o, and final where it is not NULL.  With a tape (tfno_gated_delta_rule_tape_bytes bytes, aligned to 256) the call leaves
+ * there what the backward call needs, else it needs tfno_gated_delta_rule_workspace_bytes(d, 0) bytes of workspace.
+ *
+ * The backward call takes the same inputs, the tape (which it only reads), the gradient d_o of o and d_final of final (NULL: zeros), and gives the
+ * gradients of q, k, v, beta and, where not NULL, of g and initial.  Value heads that share a key head add up in dq and dk.  It needs
+ * tfno_gated_delta_rule_workspace_bytes(d, 1) bytes of workspace.
+ *
+ * Sizes: B >= 0, T >= 0, Hk, Hv, Dk, Dv >= 1 (TFNO_ERR_SHAPE), Dk <= 128, Dv <= 256 (else TFNO_ERR_UNSUPPORTED).
+ */
+typedef struct {
+    int dtype;                    /* tfno_dtype of q, k, v, o and of their gradients */
+    int B, T, Hk, Hv, Dk, Dv;
+    float scale;
+    tfno_strides q, k, v, o;      /* backward: o is d_o's */
+    tfno_strides g, beta;
+    tfno_strides dq, dk, dv, dg, dbeta;   /* backward only */
+} tfno_delta_rule_desc;
+
+tfno_status tfno_gated_delta_rule(const tfno_delta_rule_desc *d, const void *q, const void *k, const void *v, const float *g,
+                                  const float *beta, const int *lengths, const float *initial, void *o, float *final, void *tape,
+                                  void *stream);
+tfno_status tfno_gated_delta_rule_backward(const tfno_delta_rule_desc *d, const void *q, const void *k, const void *v, const float *g,
+                                           const float *beta, const int *lengths, const float *initial, const void *tape,
+                                           const void *d_o, const float *d_final, void *dq, void *dk, void *dv, float *dg,
+                                           float *dbeta, float *d_initial, void *stream);
+size_t tfno_gated_delta_rule_tape_bytes(const tfno_delta_rule_desc *d);
+size_t tfno_gated_delta_rule_workspace_bytes(const tfno_delta_rule_desc *d, int backward);
+
+/*
+ * One token of B sequences: the states [pool, Hv, Dk, Dv] (float32, contiguous) are advanced in place, and o is written.  Sequence b has the state
+ * slots[b] (int32 [B] on the device; NULL: b).  A negative slot is a place without a sequence (o = 0), one that the pool does not hold gives NaN;
+ * no state is touched for either.  A slot may not be given twice.  Descriptor, sizes and gates as above with T = 1; strides of tokens are not used.
+ */
+tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void *q, const void *k, const void *v, const float *g,
+                                       const float *beta, float *states, const int *slots, int pool, void *o, void *stream);
 
 /*
  * Workspace (device memory for intermediates) that an entry point needs for a

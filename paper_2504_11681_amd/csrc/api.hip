@@ -7,6 +7,7 @@
 #include "matdft.h"
 #include "pruned1d.h"
 #include "staged.h"
+#include "workspace.h"
 
 #include <atomic>
 #include <cstdlib>
@@ -622,6 +623,16 @@ size_t workspace_for(const Shape &req, int variant, int B, int C_in, int C_out)
 
 }  // namespace
 
+namespace tfno {
+
+RegisteredWorkspace registered_workspace()
+{
+    void *p = g_ws_ptr.load();
+    return RegisteredWorkspace{p, g_ws_bytes.load()};
+}
+
+}  // namespace tfno
+
 extern "C" {
 
 tfno_status tfno_spectral_conv1d(const void *x, const void *W, void *y, int B, int C_in, int C_out, int N, int K,
@@ -768,10 +779,10 @@ const char *tfno_status_string(tfno_status s)
     case TFNO_ERR_NULL: return "a required pointer is NULL";
     case TFNO_ERR_SHAPE: return "a size argument is out of range";
     case TFNO_ERR_UNSUPPORTED: return "no fused kernel for this shape (use the staged entry point)";
-    case TFNO_ERR_ALIAS: return "y or the workspace overlaps another buffer";
+    case TFNO_ERR_ALIAS: return "an output or the workspace overlaps another buffer";
     case TFNO_ERR_WORKSPACE: return "workspace missing or too small (see tfno_workspace_bytes), or the shape needs more than the built-in scratch";
     case TFNO_ERR_HIP: return "the HIP runtime reported an error at launch";
-    case TFNO_ERR_ALIGN: return "x, W or y is not aligned to 8 bytes";
+    case TFNO_ERR_ALIGN: return "a tensor is not aligned (x, W, y: 8 bytes; operators along time: an element)";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,439 @@
+// Gradient of the gated delta rule, from the tape of the forward pass (the names are those of the forward kernels).  With dO already
+// times scale and dS' the gradient of a chunk's outgoing state:
+//
+//   dU = P' dO + e^(GL-G) (K dS'),   Y = T' (beta dU) = dV,
+//   dS = e^GL dS' + Q' (e^G dO) - K' (e^G Y)                                        (k_delta_scan_back, from the last chunk to the first)
+//
+// and for every chunk by itself (k_delta_gradients), with C = Y E', D = dO E', X = P . D - A . C and strict() resp. tril() of M:
+//
+//   dbeta_j = sum_i X_ij + e^(GL-G_j) k_j (dS' E_j),
+//   dq = e^G (dO S') + (M . D beta) K,
+//   dk = -e^G (Y S') + e^(GL-G) beta (E dS'') + (M . D beta)' Q - (W + W') K,   W = strict(M . C beta),
+//   dG_i = sum_j X_ij beta_j - beta_i sum_j X_ji + q_i e^G (dO S')_i - k_i e^G (Y S')_i - c_i,   c_i = e^(GL-G_i) beta_i k_i (dS' E_i),
+//   dG_L += sum c + e^GL <S, dS'>,   dg = sum of dG from the token on.
+//
+// Value heads that share a key head are summed by the workgroup of that key head, in their order.
+#pragma once
+#include "deltarule_kernel.h"
+
+namespace tfno {
+
+template <class E, int KB, int NC>
+__global__ __launch_bounds__(256) void k_delta_scan_back(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PM = DELTA_PM;
+    // LDS in units: K | P' , gates, T' | K', Q'
+    constexpr int K_UNITS = U::Q, PT_UNITS = U::TRI * PM, T_UNITS = U::KEY_TAPE - U::KT;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    unsigned char *ldsK = lds, *ldsPT = ldsK + K_UNITS * 1024, *ldsG = ldsPT + PT_UNITS * 1024, *ldsTT = ldsG + 1024,
+                  *ldsKT = ldsTT + PT_UNITS * 1024;
+    const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsG;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int m = lane & 15, g = lane >> 4;
+    const int block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
+    const int len = sequence_length(a, b), n = (len + L - 1) / L;
+    const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
+    const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
+    const int col0 = (block * waves + wave) * 16 * NC;
+
+    floatx4 S[NC][DT];          // dS', laid out as the state is
+    load_state<NC, DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col0, lane, S);
+    const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + h * a.sdo.head);
+    E *dv = (E *)a.dv + (b * a.sdv.batch + h * a.sdv.head);
+
+    auto load_first = [&](int chunk) {
+        const unsigned char *v = value + (long long)chunk * mem.value_units * 1024;
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, ldsK, K_UNITS, wave, waves, lane);
+        units_to_lds(v + U::PT * 1024, ldsPT, PT_UNITS, wave, waves, lane);
+    };
+    if (n > 0) load_first(n - 1);
+    for (int chunk = n - 1; chunk >= 0; --chunk) {
+        const int t0 = chunk * L;
+        loads_done_and_barrier();
+        {
+            const unsigned char *v = value + (long long)chunk * mem.value_units * 1024;
+            units_to_lds(v + U::GATES * 1024, ldsG, 1, wave, waves, lane);
+            units_to_lds(v + U::TT * 1024, ldsTT, PT_UNITS, wave, waves, lane);
+            units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, ldsKT, T_UNITS, wave, waves, lane);
+        }
+        float x[NC][LB][8];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 16 * c + m;
+            load_columns<E, LB>(d_o + (long long)t0 * a.sdo.token, a.sdo.token, col, a.Dv, g, len - t0, x[c]);
+            if (col < mem.dvp) {
+                float *to = mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp + col;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) to[tile_index(t, 4 * g + r) * mem.dvp] = S[c][t][r];
+            }
+        }
+        floatx4 KS[NC][NT], PO_[NC][NT];
+        {
+            Frag<PM> Sf[NC][KB];
+            Frag<PI> Of[NC][LB];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    float u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] = S[c][2 * kb + (e >> 2)][e & 3];
+                    Sf[c][kb] = make_frag<PM>(u);
+                }
+#pragma unroll
+                for (int s = 0; s < LB; ++s) Of[c][s] = make_frag<PI>(x[c][s]);
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) KS[c][i] = PO_[c][i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const Frag<PI> kf = load_frag<PI>(ldsK + (i * KB + kb) * PI * 1024, lane);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) KS[c][i] = mm<3>(kf, Sf[c][kb], KS[c][i]);
+                }
+#pragma unroll
+                for (int kb = i / 2; kb < LB; ++kb) {
+                    const Frag<PM> pf = load_frag<PM>(ldsPT + U::upper(i, kb) * PM * 1024, lane);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) PO_[c][i] = mm<3>(pf, Of[c][kb], PO_[c][i]);
+                }
+            }
+        }
+        loads_done_and_barrier();
+        if (chunk > 0) load_first(chunk - 1);
+
+        // Y = T' (beta dU)
+        floatx4 Y[NC][NT];
+        {
+            Frag<PM> R[NC][LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float be[8], left[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) be[e] = gates->beta[32 * s + 8 * g + e], left[e] = gates->left[32 * s + 8 * g + e];
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    float u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        u[e] = be[e] * fmaf(left[e], KS[c][2 * s + (e >> 2)][e & 3], a.scale * PO_[c][2 * s + (e >> 2)][e & 3]);
+                    R[c][s] = make_frag<PM>(u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) Y[c][i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+                for (int kb = i / 2; kb < LB; ++kb) {
+                    const Frag<PM> tf = load_frag<PM>(ldsTT + U::upper(i, kb) * PM * 1024, lane);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) Y[c][i] = mm<3>(tf, R[c][kb], Y[c][i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 16 * c + m;
+            if (col < mem.dvp) {
+                float *to = mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp + col;
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = tile_index(i, 4 * g + r);
+                        to[row * mem.dvp] = Y[c][i][r];
+                        if (t0 + row < a.T && col < a.Dv) store_element(dv + (long long)(t0 + row) * a.sdv.token + col, Y[c][i][r]);
+                    }
+            }
+        }
+        Frag<PM> Wo[NC][LB], Wy[NC][LB];
+#pragma unroll
+        for (int s = 0; s < LB; ++s) {
+            float decay[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) decay[e] = gates->decay[32 * s + 8 * g + e];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                float u[8], w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    u[e] = a.scale * decay[e] * x[c][s][e];
+                    w[e] = -decay[e] * Y[c][2 * s + (e >> 2)][e & 3];
+                }
+                Wo[c][s] = make_frag<PM>(u);
+                Wy[c][s] = make_frag<PM>(w);
+            }
+        }
+        const float whole = gates->whole;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[c][t] *= whole;
+#pragma unroll
+            for (int kb = 0; kb < LB; ++kb) {
+                const Frag<PI> kf = load_frag<PI>(ldsKT + (t * LB + kb) * PI * 1024, lane);
+                const Frag<PI> qf = load_frag<PI>(ldsKT + ((DT + t) * LB + kb) * PI * 1024, lane);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    S[c][t] = mm<3>(kf, Wy[c][kb], S[c][t]);
+                    S[c][t] = mm<3>(qf, Wo[c][kb], S[c][t]);
+                }
+            }
+        }
+    }
+    for (int t = n * L + g; t < a.T; t += 4)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 16 * c + m;
+            if (col < a.Dv) store_element(dv + (long long)t * a.sdv.token + col, 0.0f);
+        }
+    if (a.d_initial) store_state<NC, DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col0, lane, S);
+}
+
+// One workgroup for a chunk of a key head, a wave for each 16 tokens of it.
+template <class E, int KB>
+__global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PM = DELTA_PM, COL = L + 4;
+    constexpr int PANEL = DT * PM * 1024 * 2, MATRICES = 2 * L * COL * 4;
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[PANEL > MATRICES ? PANEL : MATRICES];
+    unsigned char *panelS = shared, *panelD = shared + PANEL / 2;    // 32 columns of S and dS' as operand blocks
+    float *Mq = (float *)shared, *Mk = Mq + L * COL;                 // after the last of them
+    __shared__ double G[L];
+    __shared__ float beta[L], left[L], column_sums[NT][L], row_sums[L], token_g[L], token_beta[L], inner[NT];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int chunk = blockIdx.x % mem.chunks, kh = blockIdx.x / mem.chunks;
+    const int b = kh / a.Hk, hk = kh - b * a.Hk, group = a.Hv / a.Hk;
+    const int len = sequence_length(a, b), t0 = chunk * L;
+    const int i = wave, token = t0 + tile_index(i, m);               // the lane's token where tokens are columns
+    E *dq = (E *)a.dq + (b * a.sdq.batch + (long long)token * a.sdq.token + hk * a.sdq.head);
+    E *dk = (E *)a.dk + (b * a.sdk.batch + (long long)token * a.sdk.token + hk * a.sdk.head);
+
+    if (t0 >= len) {                     // past the sequence's end
+        const float zero[8] = {};
+        if (token < a.T)
+#pragma unroll
+            for (int s = 0; s < KB; ++s) {
+                store8(dq + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dq, zero);
+                store8(dk + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dk, zero);
+            }
+        for (int x = tid; x < L * group; x += 64 * NT) {
+            const int t = t0 + x % L, h = hk * group + x / L;
+            if (t < a.T) {
+                if (a.dg) a.dg[b * a.sdg.batch + (long long)t * a.sdg.token + h * a.sdg.head] = 0.0f;
+                a.dbeta[b * a.sdbeta.batch + (long long)t * a.sdbeta.token + h * a.sdbeta.head] = 0.0f;
+            }
+        }
+        return;
+    }
+
+    const unsigned char *key = mem.key + ((long long)kh * mem.chunks + chunk) * mem.key_units * 1024;
+    Frag<PI> kf[KB], qf[KB];
+    floatx4 kk[NT], qk[NT], mq[NT], mk[NT], accq[DT], acck[DT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) kk[j] = qk[j] = mq[j] = mk[j] = floatx4{0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < DT; ++t) accq[t] = acck[t] = floatx4{0, 0, 0, 0};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        kf[kb] = load_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane);
+        qf[kb] = load_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            if (j <= (i | 1)) {
+                const Frag<PI> other = load_frag<PI>(key + (U::K + (j * KB + kb) * PI) * 1024, lane);
+                kk[j] = mm<3>(kf[kb], other, kk[j]);
+                qk[j] = mm<3>(qf[kb], other, qk[j]);
+            }
+    }
+
+    for (int member = 0; member < group; ++member) {
+        const int h = hk * group + member;
+        const long long at = ((long long)(b * a.Hv + h)) * mem.chunks + chunk;
+        const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
+        const float *states = mem.states + at * DKP * mem.dvp, *d_states = mem.d_states + at * DKP * mem.dvp;
+        const float *errors = mem.errors + at * L * mem.dvp, *d_values = mem.d_values + at * L * mem.dvp;
+        const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + (long long)token * a.sdo.token + h * a.sdo.head);
+        __syncthreads();
+        if (tid < L) G[tid] = mem.G[at * L + tid], beta[tid] = gates->beta[tid], left[tid] = gates->left[tid];
+
+        floatx4 D[NT], C[NT], hq[DT], hy[DT], he[DT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) D[j] = C[j] = floatx4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < DT; ++t) hq[t] = hy[t] = he[t] = floatx4{0, 0, 0, 0};
+        float dot = 0.0f;
+        for (int kb = 0; kb < mem.dvp / 32; ++kb) {
+            const int c0 = 32 * kb + 8 * g;
+            __syncthreads();
+            for (int t = wave; t < DT; t += NT) {
+                const long long row = (long long)tile_index(t, m) * mem.dvp + c0;
+                float u[8], w[8];
+                load8(states + row, 8, true, u);
+                load8(d_states + row, 8, true, w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot = fmaf(u[e], w[e], dot);
+                store_frag<PM>(panelS + t * PM * 1024, lane, make_frag<PM>(u));
+                store_frag<PM>(panelD + t * PM * 1024, lane, make_frag<PM>(w));
+            }
+            float u[8];
+            load8(d_o + c0, token < len ? a.Dv - c0 : 0, vec.d_o, u);
+            const Frag<PI> of = make_frag<PI>(u);
+            load8(d_values + tile_index(i, m) * mem.dvp + c0, 8, true, u);
+            const Frag<PM> yf = make_frag<PM>(u);
+            Frag<PM> ef{};
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                if (j <= (i | 1)) {
+                    load8(errors + tile_index(j, m) * mem.dvp + c0, 8, true, u);
+                    const Frag<PM> f = make_frag<PM>(u);
+                    D[j] = mm<3>(of, f, D[j]);
+                    C[j] = mm<3>(yf, f, C[j]);
+                    if (j == i) ef = f;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const Frag<PM> sf = load_frag<PM>(panelS + t * PM * 1024, lane), df = load_frag<PM>(panelD + t * PM * 1024, lane);
+                hq[t] = mm<3>(sf, of, hq[t]);
+                hy[t] = mm<3>(sf, yf, hy[t]);
+                he[t] = mm<3>(df, ef, he[t]);
+            }
+        }
+        dot = group_sum(dot, 64);
+        if (lane == 0) inner[wave] = dot;
+
+        // matrices of token pairs: rows tile_index(i, 4 g + r), column tile_index(j, m)
+        float rows[4] = {};
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float column = 0.0f;
+            if (j <= (i | 1)) {
+                const int col = tile_index(j, m);
+                const float be = beta[col];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = tile_index(i, 4 * g + r);
+                    const float M = col <= row ? expf((float)(G[row] - G[col])) : 0.0f, strict = col < row ? M : 0.0f;
+                    const float Dm = a.scale * M * D[j][r], Cm = strict * C[j][r];
+                    const float x = qk[j][r] * Dm - kk[j][r] * Cm;
+                    rows[r] = fmaf(x, be, rows[r]);
+                    column += x;
+                    mq[j][r] = fmaf(Dm, be, mq[j][r]);
+                    mk[j][r] = fmaf(-Cm, be, mk[j][r]);
+                }
+            }
+            column += __shfl_xor(column, 16, 64);
+            column += __shfl_xor(column, 32, 64);
+            if (g == 0) column_sums[wave][tile_index(j, m)] = column;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            rows[r] = group_sum(rows[r], 16);
+            if (m == 0) row_sums[tile_index(i, 4 * g + r)] = rows[r];
+        }
+        // terms with the states: token in columns
+        {
+            const int tok = tile_index(i, m);
+            const float decay = gates->decay[tok], fq = a.scale * decay, fe = left[tok], be = beta[tok];
+            float tg = 0.0f, tb = 0.0f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int e = 4 * (t & 1) + r;
+                    const float q = frag_value<PI>(qf[t >> 1], e), k = frag_value<PI>(kf[t >> 1], e);
+                    const float vq = fq * hq[t][r], vy = decay * hy[t][r], ve = fe * he[t][r];
+                    tg = fmaf(q, vq, fmaf(-k, vy, tg));
+                    tb = fmaf(k, ve, tb);
+                    accq[t][r] += vq;
+                    acck[t][r] += fmaf(be, ve, -vy);
+                }
+            tg += __shfl_xor(tg, 16, 64), tg += __shfl_xor(tg, 32, 64);
+            tb += __shfl_xor(tb, 16, 64), tb += __shfl_xor(tb, 32, 64);
+            if (g == 0) token_g[tok] = tg, token_beta[tok] = tb;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const int tok = lane < L ? lane : 0;
+            float column = 0.0f, whole = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NT; ++w) column += column_sums[w][tok], whole += inner[w];
+            const float c = lane < L ? beta[tok] * token_beta[tok] : 0.0f;
+            float dG = lane < L ? row_sums[tok] - beta[tok] * column + token_g[tok] - c : 0.0f;
+            const float all = group_sum(c, 64);
+            if (lane == L - 1) dG += all + gates->whole * whole;
+            for (int step = 1; step < 64; step <<= 1) {
+                const float u = __shfl_down(dG, step, 64);
+                if (lane + step < 64) dG += u;
+            }
+            const int t = t0 + lane;
+            if (lane < L && t < a.T) {
+                const bool live = t < len;
+                if (a.dg) a.dg[b * a.sdg.batch + (long long)t * a.sdg.token + h * a.sdg.head] = live ? dG : 0.0f;
+                a.dbeta[b * a.sdbeta.batch + (long long)t * a.sdbeta.token + h * a.sdbeta.head] = live ? column + token_beta[tok] : 0.0f;
+            }
+        }
+    }
+    __syncthreads();
+
+    // products of token pairs with K and Q, once for the group
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+        if (j <= (i | 1))
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = tile_index(i, 4 * g + r) * COL + tile_index(j, m);
+                Mq[at] = mq[j][r], Mk[at] = mk[j][r];
+            }
+    __syncthreads();
+    const int row = tile_index(i, m);
+#pragma unroll
+    for (int kb = 0; kb < LB; ++kb) {
+        float u[8];
+        Frag<PM> lowq{}, highq{}, sym{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = 0.0f;
+        if (kb <= i / 2) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = Mq[row * COL + 32 * kb + 8 * g + e], u[e] += Mk[row * COL + 32 * kb + 8 * g + e];
+            lowq = make_frag<PM>(w);
+        }
+        if (kb >= i / 2) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = Mq[(32 * kb + 8 * g + e) * COL + row], u[e] += Mk[(32 * kb + 8 * g + e) * COL + row];
+            highq = make_frag<PM>(w);
+        }
+        sym = make_frag<PM>(u);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            const Frag<PI> kt = load_frag<PI>(key + (U::KT + (t * LB + kb) * PI) * 1024, lane);
+            acck[t] = mm<3>(kt, sym, acck[t]);
+            if (kb <= i / 2) accq[t] = mm<3>(kt, lowq, accq[t]);
+            if (kb >= i / 2) acck[t] = mm<3>(load_frag<PI>(key + (U::QT + (t * LB + kb) * PI) * 1024, lane), highq, acck[t]);
+        }
+    }
+    if (token < a.T)
+#pragma unroll
+        for (int s = 0; s < KB; ++s) {
+            float u[8], w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = accq[2 * s + (e >> 2)][e & 3], w[e] = acck[2 * s + (e >> 2)][e & 3];
+            store8(dq + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dq, u);
+            store8(dk + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dk, w);
+        }
+}
+
+}  // namespace tfno

@@ -1,0 +1,142 @@
+// Launches of the gated delta rule over sequences.
+#include "deltagrad_kernel.h"
+
+namespace tfno {
+
+namespace {
+
+size_t pad(size_t n) { return (n + 255) / 256 * 256; }
+
+// Layout of the tape, or of the workspace of a forward pass without one; `base` may be NULL for its size alone.
+template <class E, int KB>
+size_t forward_memory(const DeltaArgs &a, unsigned char *base, bool tape, DeltaMemory *m)
+{
+    typedef DeltaUnits<E, KB> U;
+    m->chunks = (a.T + U::L - 1) / U::L;
+    m->dvp = (a.Dv + 31) / 32 * 32;
+    m->key_units = tape ? U::KEY_TAPE : U::KEY_FORWARD;
+    m->value_units = tape ? U::VALUE_TAPE : U::VALUE_FORWARD;
+    const size_t keys = (size_t)a.B * a.Hk * m->chunks, values = (size_t)a.B * a.Hv * m->chunks;
+    size_t at = 0;
+    m->key = base + at, at += keys * m->key_units * 1024;
+    m->value = base + at, at += values * m->value_units * 1024;
+    if (tape) {
+        m->G = (double *)(base + at), at += pad(values * U::L * sizeof(double));
+        m->states = (float *)(base + at), at += values * U::DKP * m->dvp * sizeof(float);
+        m->errors = (float *)(base + at), at += values * U::L * m->dvp * sizeof(float);
+    }
+    return at;
+}
+template <class E, int KB>
+size_t backward_memory(const DeltaArgs &a, unsigned char *base, DeltaMemory *m)
+{
+    typedef DeltaUnits<E, KB> U;
+    const size_t values = (size_t)a.B * a.Hv * ((a.T + U::L - 1) / U::L), dvp = (a.Dv + 31) / 32 * 32;
+    size_t at = 0;
+    m->d_states = (float *)(base + at), at += values * U::DKP * dvp * sizeof(float);
+    m->d_values = (float *)(base + at), at += values * U::L * dvp * sizeof(float);
+    return at;
+}
+
+// Rows whose elements may be read or written eight at a time.
+bool rows_of_8(const void *p, const Strides &s, bool bf16)
+{
+    const long long unit = bf16 ? 8 : 4;
+    return ((uintptr_t)p & 15) == 0 && s.batch % unit == 0 && s.token % unit == 0 && s.head % unit == 0;
+}
+
+// Waves of a scan's workgroup and column tiles of a wave: two tiles and four waves where there are heads enough to fill the chip.
+struct ScanShape { int waves, nc, blocks; };
+ScanShape scan_shape(const DeltaArgs &a, int dvp)
+{
+    const int tiles = dvp / 16;
+    const long long heads = (long long)a.B * a.Hv;
+    ScanShape s;
+    s.nc = heads * tiles >= 2048 ? 2 : 1;
+    s.waves = 4;
+    while (s.waves > 1 && (heads * tiles < 256LL * s.waves * s.nc || s.waves * s.nc > tiles)) s.waves >>= 1;
+    s.blocks = (tiles + s.waves * s.nc - 1) / (s.waves * s.nc);
+    return s;
+}
+
+template <class E, int KB, int NC, bool TAPE>
+hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int bytes = (U::QT + U::VALUE_FORWARD) * 1024;
+    static LdsLimitOnce limit;
+    if (hipError_t e = limit.set({(const void *)k_delta_scan<E, KB, NC, TAPE>}, bytes); e != hipSuccess) return e;
+    k_delta_scan<E, KB, NC, TAPE><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    return hipGetLastError();
+}
+template <class E, int KB, int NC>
+hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int bytes = (U::Q + 2 * U::TRI * DELTA_PM + 1 + U::KEY_TAPE - U::KT) * 1024;
+    static LdsLimitOnce limit;
+    if (hipError_t e = limit.set({(const void *)k_delta_scan_back<E, KB, NC>}, bytes); e != hipSuccess) return e;
+    k_delta_scan_back<E, KB, NC><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    return hipGetLastError();
+}
+
+template <class E, int KB>
+hipError_t forward(const DeltaArgs &a, hipStream_t s)
+{
+    typedef DeltaUnits<E, KB> U;
+    DeltaMemory m{};
+    const bool tape = a.tape != nullptr;
+    forward_memory<E, KB>(a, tape ? a.tape : a.workspace, tape, &m);
+    DeltaVec vec{};
+    vec.q = rows_of_8(a.q, a.sq, a.bf16), vec.k = rows_of_8(a.k, a.sk, a.bf16);
+    const unsigned grid = (unsigned)(a.B * a.Hv * m.chunks);
+    if (grid && tape) k_delta_prepare<E, KB, true><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
+    else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const ScanShape sh = scan_shape(a, m.dvp);
+    if (tape) return sh.nc == 2 ? scan<E, KB, 2, true>(a, m, sh, s) : scan<E, KB, 1, true>(a, m, sh, s);
+    return sh.nc == 2 ? scan<E, KB, 2, false>(a, m, sh, s) : scan<E, KB, 1, false>(a, m, sh, s);
+}
+
+template <class E, int KB>
+hipError_t backward(const DeltaArgs &a, hipStream_t s)
+{
+    typedef DeltaUnits<E, KB> U;
+    DeltaMemory m{};
+    forward_memory<E, KB>(a, a.tape, true, &m);
+    backward_memory<E, KB>(a, a.workspace, &m);
+    DeltaVec vec{};
+    vec.d_o = rows_of_8(a.d_o, a.sdo, a.bf16), vec.dq = rows_of_8(a.dq, a.sdq, a.bf16), vec.dk = rows_of_8(a.dk, a.sdk, a.bf16);
+    const ScanShape sh = scan_shape(a, m.dvp);
+    if (hipError_t e = sh.nc == 2 ? scan_back<E, KB, 2>(a, m, sh, s) : scan_back<E, KB, 1>(a, m, sh, s); e != hipSuccess) return e;
+    if (m.chunks == 0) return hipSuccess;
+    k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 64 * U::NT, 0, s>>>(a, m, vec);
+    return hipGetLastError();
+}
+
+template <class E, class F>
+auto by_size(const DeltaArgs &a, F f)
+{
+    return a.Dk <= 32 ? f.template operator()<E, 1>() : a.Dk <= 64 ? f.template operator()<E, 2>() : f.template operator()<E, 4>();
+}
+struct Forward { const DeltaArgs &a; hipStream_t s; template <class E, int KB> hipError_t operator()() const { return forward<E, KB>(a, s); } };
+struct Backward { const DeltaArgs &a; hipStream_t s; template <class E, int KB> hipError_t operator()() const { return backward<E, KB>(a, s); } };
+struct ForwardBytes {
+    const DeltaArgs &a; bool tape;
+    template <class E, int KB> size_t operator()() const { DeltaMemory m{}; return forward_memory<E, KB>(a, nullptr, tape, &m); }
+};
+struct BackwardBytes {
+    const DeltaArgs &a;
+    template <class E, int KB> size_t operator()() const { DeltaMemory m{}; return backward_memory<E, KB>(a, nullptr, &m); }
+};
+template <class F>
+auto by_kind(const DeltaArgs &a, F f) { return a.bf16 ? by_size<bf16>(a, f) : by_size<float>(a, f); }
+
+}  // namespace
+
+size_t delta_tape_bytes(const DeltaArgs &a) { return by_kind(a, ForwardBytes{a, true}); }
+size_t delta_workspace_bytes(const DeltaArgs &a, bool backward) { return backward ? by_kind(a, BackwardBytes{a}) : by_kind(a, ForwardBytes{a, false}); }
+hipError_t delta_forward_launch(const DeltaArgs &a, hipStream_t s) { return by_kind(a, Forward{a, s}); }
+hipError_t delta_backward_launch(const DeltaArgs &a, hipStream_t s) { return by_kind(a, Backward{a, s}); }
+
+}  // namespace tfno

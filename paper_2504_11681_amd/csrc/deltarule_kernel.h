@@ -1,0 +1,662 @@
+// The gated delta rule over whole sequences, by chunks of L tokens.  Token by token a head's state S [Dk, Dv] follows
+//
+//   Sb = exp(g_t) S,   e_t = v_t - Sb' k_t,   S <- Sb + k_t (beta_t e_t)',   o_t = scale S' q_t.
+//
+// With a chunk's incoming state S, G the running sum of g in it, M_ij = exp(G_i - G_j) for j <= i (no exponent of a sum is ever
+// taken apart, so nothing overflows where decays are strong):
+//
+//   A = strict(M . K K'),   T = (I + A diag(beta))^-1,   P = M . Q K',
+//   E = T (V - e^G (K S)),   U = beta E,
+//   O = scale (e^G (Q S) + P U),   S <- e^GL S + K' (e^(GL-G) U).
+//
+// k_delta_prepare forms what does not depend on S for all chunks at once, k_delta_scan walks through the chunks.  Everything of it
+// that the scan reads is laid out as operands of the matrix instructions.
+//
+// An operand block is 16 rows by 32 columns: lane (m, g) = (lane % 16, lane / 16) holds row m, columns 8 g .. 8 g + 7.  A result tile
+// has its column in m and rows 4 g .. 4 g + 3.  Rows of tiles 2 s and 2 s + 1 are taken in the order
+//
+//   row r of tile 2 s + p  <->  index 32 s + 8 (r / 4) + 4 p + r % 4,
+//
+// so that the two results of a pair hold in each lane just the eight consecutive indexes that an operand block needs: a result becomes
+// an operand without leaving its registers.
+//
+// Float32 values (the state, E, T, P, and float32 inputs) are operands as three BF16 parts that add up to them, and products of parts
+// below 2^-24 are left out, so sums have float32's accuracy.  BF16 inputs are one part.  What goes into a BF16 output alone (P, and S as
+// the outputs read it) is taken in two parts, 2^-16 off, which the output's own 2^-9 hides.
+#pragma once
+#include "bf16x3.h"
+#include "deltarule.h"
+
+namespace tfno {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+template <int P>
+struct Frag { bf16x8 p[P]; };
+
+template <int P>
+__device__ __forceinline__ Frag<P> make_frag(const float (&x)[8])
+{
+    Frag<P> f;
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        uintx4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
+        f.p[p] = __builtin_bit_cast(bf16x8, w);
+        if (p + 1 < P)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r[e] -= __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);
+    }
+    return f;
+}
+
+// c + A B with the products of parts i, j that have i + j < CUT
+template <int CUT, int PA, int PB>
+__device__ __forceinline__ floatx4 mm(const Frag<PA> &a, const Frag<PB> &b, floatx4 c)
+{
+#pragma unroll
+    for (int sum = CUT - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (sum - i >= 0 && sum - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[sum - i], c, 0, 0, 0);
+    return c;
+}
+
+template <int P>
+__device__ __forceinline__ Frag<P> load_frag(const unsigned char *unit, int lane)
+{
+    Frag<P> f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(unit + p * 1024 + lane * 16);
+    return f;
+}
+template <int P>
+__device__ __forceinline__ void store_frag(unsigned char *unit, int lane, const Frag<P> &f)
+{
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<bf16x8 *>(unit + p * 1024 + lane * 16) = f.p[p];
+}
+// The value that the parts of element e add up to.
+template <int P>
+__device__ __forceinline__ float frag_value(const Frag<P> &f, int e)
+{
+    float v = 0.0f;
+#pragma unroll
+    for (int p = P - 1; p >= 0; --p) v += (float)f.p[p][e];
+    return v;
+}
+
+// index of row r of tile i
+__device__ __forceinline__ int tile_index(int i, int r) { return 32 * (i >> 1) + 8 * (r >> 2) + 4 * (i & 1) + (r & 3); }
+
+// What the kernels are built for.  BF16: chunks of 64, one part an input; float32: chunks of 32 (its operands are three times as large),
+// three parts.
+template <class E> struct DeltaKind;
+template <> struct DeltaKind<bf16> { static constexpr int L = 64, PI = 1, PO = 2; };
+template <> struct DeltaKind<float> { static constexpr int L = 32, PI = 3, PO = 3; };
+
+constexpr int DELTA_PM = 3;      // parts of float32 operands
+
+// Memory of a chunk, in units of 1024 bytes (one part of an operand block).  KB = ceil(Dk / 32).
+template <class E, int KB>
+struct DeltaUnits {
+    static constexpr int L = DeltaKind<E>::L, PI = DeltaKind<E>::PI, PO = DeltaKind<E>::PO;
+    static constexpr int NT = L / 16, LB = L / 32, DT = 2 * KB, DKP = 32 * KB;
+    static constexpr int TRI = NT == 2 ? 2 : 6;                    // blocks on and below the diagonal
+    // of a key head: K, Q [NT][KB], K', Q' [DT][LB]
+    static constexpr int K = 0, Q = NT * KB * PI, KT = 2 * NT * KB * PI, QT = KT + DT * LB * PI;
+    static constexpr int KEY_FORWARD = QT, KEY_TAPE = QT + DT * LB * PI;
+    // of a value head: gates, T, P; with a tape T', P'
+    static constexpr int GATES = 0, T = 1, P = T + TRI * DELTA_PM, VALUE_FORWARD = P + TRI * PO;
+    static constexpr int TT = VALUE_FORWARD, PT = TT + TRI * DELTA_PM, VALUE_TAPE = PT + TRI * DELTA_PM;
+    static constexpr int lower(int i, int kb) { return NT == 2 ? i : i < 2 ? i : 2 + 2 * (i - 2) + kb; }   // kb <= i / 2
+    static constexpr int upper(int i, int kb) { return NT == 2 ? i : i < 2 ? 2 * i + kb : 4 + (i - 2); }   // kb >= i / 2
+};
+
+// Gates of a chunk of a value head, as they lie in its first unit.
+template <int L>
+struct DeltaGates {
+    float decay[L];        // exp(G)
+    float beta[L];
+    float left[L];         // exp(GL - G)
+    float whole;           // exp(GL)
+};
+
+// Where the parts of a call's memory lie.
+struct DeltaMemory {
+    unsigned char *key, *value;      // units of the key heads' and of the value heads' chunks, [b][head][chunk]
+    double *G;                       // [b][hv][chunk][L] running sums (tape)
+    float *states, *errors;          // tape: S before each chunk [DKP][DVP], E [L][DVP]
+    float *d_states, *d_values;      // backward: gradient of the state after each chunk, Y [L][DVP]
+    int chunks, dvp, key_units, value_units;
+};
+
+__device__ __forceinline__ int sequence_length(const DeltaArgs &a, int b)
+{
+    if (!a.lengths) return a.T;
+    const int n = a.lengths[b];
+    return n < 0 ? 0 : n < a.T ? n : a.T;
+}
+
+// Eight neighbouring elements of which the first n count (the others are 0); one access where `vec` says that addresses allow it.
+__device__ __forceinline__ void load8(const float *p, int n, bool vec, float (&x)[8])
+{
+    if (vec && n >= 8) {
+        const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
+        x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+    } else if (n > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p[e < n ? e : 0];       // loads without branches between them
+#pragma unroll
+        for (int e = 1; e < 8; ++e) x[e] = e < n ? x[e] : 0.0f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const bf16 *p, int n, bool vec, float (&x)[8])
+{
+    if (vec && n >= 8) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(p);
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    } else if (n > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = to_float(p[e < n ? e : 0]);       // loads without branches between them
+#pragma unroll
+        for (int e = 1; e < 8; ++e) x[e] = e < n ? x[e] : 0.0f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+    }
+}
+__device__ __forceinline__ void store8(float *p, int n, bool vec, const float (&x)[8])
+{
+    if (vec && n >= 8) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = x[e];
+    }
+}
+__device__ __forceinline__ void store8(bf16 *p, int n, bool vec, const float (&x)[8])
+{
+    if (vec && n >= 8) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) store_element(p + e, x[e]);
+    }
+}
+
+struct DeltaVec { bool q, k, d_o, dq, dk; };       // which tensors' rows may be read eight elements at a time
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// One workgroup for a chunk of a value head: L / 16 waves.  The inverse T of the unit lower triangular matrix is found by blocks of 16:
+// each diagonal block by substitution, the blocks below it from T_IJ = -T_II sum_{J<=M<I} N_IM T_MJ, one wave for a block column.
+// Substitution and not the product (I - N)(I + N^2)(I + N^4)..: its powers grow like binomials where keys are alike, and cancel.
+template <class E, int KB, bool TAPE>
+__global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PO = U::PO;
+    constexpr int ROW = DKP + 16 / sizeof(E), COL = L + 4;
+    __shared__ __attribute__((aligned(16))) E Ks[L * ROW];
+    __shared__ __attribute__((aligned(16))) E Qs[L * ROW];
+    __shared__ __attribute__((aligned(16))) float N[L * COL];
+    __shared__ __attribute__((aligned(16))) float X[L * COL];      // P, then T
+    __shared__ double G[L];
+    __shared__ float beta[L];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+    const int chunk = blockIdx.x % mem.chunks, head = blockIdx.x / mem.chunks;
+    const int b = head / a.Hv, h = head - b * a.Hv, group = a.Hv / a.Hk, hk = h / group;
+    const bool first = h == hk * group;                             // this workgroup writes the key head's blocks too
+    const int len = sequence_length(a, b), t0 = chunk * L;
+    if (t0 >= len) return;
+    unsigned char *key = mem.key + ((long long)(b * a.Hk + hk) * mem.chunks + chunk) * mem.key_units * 1024;
+    unsigned char *value = mem.value + ((long long)head * mem.chunks + chunk) * mem.value_units * 1024;
+
+    for (int x = tid; x < L * DKP / 8; x += 64 * NT) {
+        const int row = x / (DKP / 8), d = x % (DKP / 8) * 8, n = t0 + row < len ? a.Dk - d : 0;
+        float u[8];
+        load8((const E *)a.k + (b * a.sk.batch + (long long)(t0 + row) * a.sk.token + hk * a.sk.head + d), n, vec.k, u);
+        store8(Ks + row * ROW + d, 8, true, u);
+        load8((const E *)a.q + (b * a.sq.batch + (long long)(t0 + row) * a.sq.token + hk * a.sq.head + d), n, vec.q, u);
+        store8(Qs + row * ROW + d, 8, true, u);
+    }
+    if (wave == 0) {
+        // running sums of g in 64 bits; what is below any exponent counts as -1e5 each, so that differences past a reset stay exact
+        double s = 0.0;
+        const bool live = lane < L && t0 + lane < len;
+        if (live && a.g) {
+            const float v = a.g[b * a.sg.batch + (long long)(t0 + lane) * a.sg.token + h * a.sg.head];
+            s = v < -1e5f ? -1e5 : (double)v;
+        }
+        for (int step = 1; step < 64; step <<= 1) {
+            const double u = __shfl_up(s, step, 64);
+            if (lane >= step) s += u;
+        }
+        const double all = __shfl(s, L - 1, 64);
+        if (lane < L) {
+            const float be = live ? a.beta[b * a.sbeta.batch + (long long)(t0 + lane) * a.sbeta.token + h * a.sbeta.head] : 0.0f;
+            G[lane] = s;
+            beta[lane] = be;
+            DeltaGates<L> *gates = (DeltaGates<L> *)value;
+            gates->decay[lane] = expf((float)s);
+            gates->beta[lane] = be;
+            gates->left[lane] = expf((float)(all - s));
+            if (lane == 0) gates->whole = expf((float)all);
+            if (TAPE) mem.G[((long long)head * mem.chunks + chunk) * L + lane] = s;
+        }
+    }
+    __syncthreads();
+
+    // N = A diag(beta) and P; a wave takes a tile of rows
+    {
+        const int i = wave;
+        floatx4 kk[NT], qk[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) kk[j] = qk[j] = floatx4{0, 0, 0, 0};
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            float u[8];
+            load8(Ks + tile_index(i, m) * ROW + 32 * kb + 8 * g, 8, true, u);
+            const Frag<PI> kf = make_frag<PI>(u);
+            load8(Qs + tile_index(i, m) * ROW + 32 * kb + 8 * g, 8, true, u);
+            const Frag<PI> qf = make_frag<PI>(u);
+            if (first) {
+                store_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane, kf);
+                store_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane, qf);
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                if (j <= (i | 1)) {
+                    load8(Ks + tile_index(j, m) * ROW + 32 * kb + 8 * g, 8, true, u);
+                    const Frag<PI> other = make_frag<PI>(u);
+                    kk[j] = mm<3>(kf, other, kk[j]);
+                    qk[j] = mm<3>(qf, other, qk[j]);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            if (j <= (i | 1)) {
+                const int col = tile_index(j, m);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = tile_index(i, 4 * g + r);
+                    const float decay = col <= row ? expf((float)(G[row] - G[col])) : 0.0f;
+                    N[row * COL + col] = col < row ? decay * kk[j][r] * beta[col] : 0.0f;
+                    X[row * COL + col] = col <= row ? decay * qk[j][r] : 0.0f;
+                }
+            }
+        if (first) {       // K' and Q': tiles of Dk rows, blocks of 32 tokens
+            for (int x = wave; x < DT * LB; x += NT) {
+                const int t = x / LB, kb = x % LB, d = tile_index(t, m);
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = to_float(Ks[(32 * kb + 8 * g + e) * ROW + d]);
+                store_frag<PI>(key + (U::KT + x * PI) * 1024, lane, make_frag<PI>(u));
+                if (TAPE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] = to_float(Qs[(32 * kb + 8 * g + e) * ROW + d]);
+                    store_frag<PI>(key + (U::QT + x * PI) * 1024, lane, make_frag<PI>(u));
+                }
+            }
+        }
+    }
+    __syncthreads();
+    {
+        const int i = wave, row = tile_index(i, m);
+        for (int kb = 0; kb < LB; ++kb) {
+            float u[8];
+            if (kb <= i / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = X[row * COL + 32 * kb + 8 * g + e];
+                store_frag<PO>(value + (U::P + U::lower(i, kb) * PO) * 1024, lane, make_frag<PO>(u));
+            }
+            if (TAPE && kb >= i / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = X[(32 * kb + 8 * g + e) * COL + row];
+                store_frag<DELTA_PM>(value + (U::PT + U::upper(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
+            }
+        }
+    }
+    __syncthreads();
+
+    // the diagonal block of a wave: lane n has its column n
+    const int J = wave;
+    {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == m ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j = 0; j < i; ++j) s = fmaf(-N[(16 * J + i) * COL + 16 * J + j], x[j], s);
+            x[i] = s;
+        }
+        if (g == 0) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) X[(16 * J + i) * COL + 16 * J + m] = x[i];
+        } else if (g == 1 && (J & 1)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) X[(16 * (J - 1) + i) * COL + 16 * J + m] = 0.0f;     // right of the pair's first diagonal block
+        }
+    }
+    __syncthreads();
+    {
+        floatx4 col[NT];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) col[0][r] = X[(16 * J + 4 * g + r) * COL + 16 * J + m];
+#pragma unroll
+        for (int step = 1; step < NT; ++step) {
+            const int I = J + step;
+            if (I >= NT) break;
+            floatx4 sum = {0, 0, 0, 0}, out = {0, 0, 0, 0};
+#pragma unroll
+            for (int M = 0; M < step; ++M)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(N[(16 * I + m) * COL + 16 * (J + M) + 4 * g + r], col[M][r], sum, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                out = __builtin_amdgcn_mfma_f32_16x16x4f32(X[(16 * I + m) * COL + 16 * I + 4 * g + r], sum[r], out, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                col[step][r] = -out[r];
+                X[(16 * I + 4 * g + r) * COL + 16 * J + m] = -out[r];
+            }
+        }
+    }
+    __syncthreads();
+    {
+        const int i = wave, row = tile_index(i, m);
+        for (int kb = 0; kb < LB; ++kb) {
+            float u[8];
+            if (kb <= i / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = X[row * COL + 32 * kb + 8 * g + e];
+                store_frag<DELTA_PM>(value + (U::T + U::lower(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
+            }
+            if (TAPE && kb >= i / 2) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = X[(32 * kb + 8 * g + e) * COL + row];
+                store_frag<DELTA_PM>(value + (U::TT + U::upper(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------------------
+// Units of 1024 bytes from global memory to LDS, shared out over the waves of the workgroup; they are there after the wave's own
+// loads_done() and a barrier.
+__device__ __forceinline__ void units_to_lds(const unsigned char *from, unsigned char *to, int units, int wave, int waves, int lane)
+{
+    for (int u = wave; u < units; u += waves)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned int *)(from + u * 1024 + lane * 16),
+                                         (__attribute__((address_space(3))) unsigned int *)(to + u * 1024), 16, 0, 0);
+}
+__device__ __forceinline__ void loads_done_and_barrier()
+{
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+}
+
+// A wave's columns of one chunk: eight consecutive tokens of a column for each pair of tiles, from a tensor [token, column] whose first token
+// counts (what does not count is read there instead: loads without branches between them).
+template <class E, int LB>
+__device__ __forceinline__ void load_columns(const E *p, long long token, int col, int columns, int g, int count, float (&x)[LB][8])
+{
+    p += col < columns ? col : 0;
+    E u[LB][8];
+#pragma unroll
+    for (int s = 0; s < LB; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int t = 32 * s + 8 * g + e;
+            u[s][e] = p[(t < count ? t : 0) * token];
+        }
+#pragma unroll
+    for (int s = 0; s < LB; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[s][e] = col < columns && 32 * s + 8 * g + e < count ? to_float(u[s][e]) : 0.0f;
+}
+
+// Element r of tile t of a wave's state is row tile_index(t, 4 g + r), column col0 + 16 c + m.
+template <int NC, int DT>
+__device__ __forceinline__ void load_state(const float *p, int Dk, int Dv, int col0, int lane, floatx4 (&S)[NC][DT])
+{
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int t = 0; t < DT; ++t) S[c][t] = floatx4{0, 0, 0, 0};
+    if (!p) return;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = tile_index(t, 4 * g + r), col = col0 + 16 * c + m;
+                S[c][t][r] = p[d < Dk && col < Dv ? d * Dv + col : 0];
+            }
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (tile_index(t, 4 * g + r) >= Dk || col0 + 16 * c + m >= Dv) S[c][t][r] = 0.0f;
+}
+template <int NC, int DT>
+__device__ __forceinline__ void store_state(float *p, int Dk, int Dv, int col0, int lane, const floatx4 (&S)[NC][DT])
+{
+    const int m = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = tile_index(t, 4 * g + r), col = col0 + 16 * c + m;
+                if (d < Dk && col < Dv) p[(long long)d * Dv + col] = S[c][t][r];
+            }
+}
+
+// A workgroup walks through the chunks of one head with 16 NC columns of its state a wave, which stay in the wave's registers.  The
+// chunk's blocks come to LDS in two halves, each on its way while the other one is computed with.
+template <class E, int KB, int NC, bool TAPE>
+__global__ __launch_bounds__(256) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PO = U::PO, PM = DELTA_PM;
+    constexpr int CUT_O = PO;
+    // LDS in units: K, Q | K' | gates, T, P
+    constexpr int A_UNITS = U::KT, KT_UNITS = U::QT - U::KT, B_UNITS = U::VALUE_FORWARD;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    unsigned char *ldsA = lds, *ldsKT = lds + A_UNITS * 1024, *ldsB = ldsKT + KT_UNITS * 1024;
+    const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int m = lane & 15, g = lane >> 4;
+    const int block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
+    const int len = sequence_length(a, b), n = (len + L - 1) / L;
+    const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
+    const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
+    const int col0 = (block * waves + wave) * 16 * NC;
+
+    floatx4 S[NC][DT];
+    load_state<NC, DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col0, lane, S);
+    const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
+    E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
+
+    if (n > 0) units_to_lds(key + U::K * 1024, ldsA, A_UNITS, wave, waves, lane);
+    for (int chunk = 0; chunk < n; ++chunk) {
+        const int t0 = chunk * L;
+        loads_done_and_barrier();
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, ldsKT, KT_UNITS, wave, waves, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, ldsB, B_UNITS, wave, waves, lane);
+        float x[NC][LB][8];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 16 * c + m;
+            load_columns<E, LB>(v + (long long)t0 * a.sv.token, a.sv.token, col, a.Dv, g, len - t0, x[c]);
+            if (TAPE && col < mem.dvp) {
+                float *to = mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp + col;
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) to[tile_index(t, 4 * g + r) * mem.dvp] = S[c][t][r];
+            }
+        }
+        Frag<PM> Sf[NC][KB];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = S[c][2 * kb + (e >> 2)][e & 3];
+                Sf[c][kb] = make_frag<PM>(u);
+            }
+        // K S with tokens in rows, (Q S)' with tokens in columns
+        floatx4 KS[NC][NT], QS[NC][NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) KS[c][i] = QS[c][i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const Frag<PI> kf = load_frag<PI>(ldsA + (U::K + (i * KB + kb) * PI) * 1024, lane);
+                const Frag<PI> qf = load_frag<PI>(ldsA + (U::Q + (i * KB + kb) * PI) * 1024, lane);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    KS[c][i] = mm<3>(kf, Sf[c][kb], KS[c][i]);
+                    QS[c][i] = mm<CUT_O>(Sf[c][kb], qf, QS[c][i]);
+                }
+            }
+        }
+        loads_done_and_barrier();
+        if (chunk + 1 < n) units_to_lds(key + ((long long)(chunk + 1) * mem.key_units + U::K) * 1024, ldsA, A_UNITS, wave, waves, lane);
+
+        // E = T (V - e^G K S)
+        floatx4 Ee[NC][NT];
+        {
+            Frag<PM> R[NC][LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float decay[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) decay[e] = gates->decay[32 * s + 8 * g + e];
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    float u[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[c][2 * s + (e >> 2)][e & 3], x[c][s][e]);
+                    R[c][s] = make_frag<PM>(u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c) Ee[c][i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+                for (int kb = 0; kb <= i / 2; ++kb) {
+                    const Frag<PM> tf = load_frag<PM>(ldsB + (U::T + U::lower(i, kb) * PM) * 1024, lane);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) Ee[c][i] = mm<3>(tf, R[c][kb], Ee[c][i]);
+                }
+            }
+        }
+        if (TAPE) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int col = col0 + 16 * c + m;
+                if (col < mem.dvp) {
+                    float *to = mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp + col;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) to[tile_index(i, 4 * g + r) * mem.dvp] = Ee[c][i][r];
+                }
+            }
+        }
+        // U = beta E: for the outputs, and times e^(GL-G) for the state
+        Frag<PM> W[NC][LB];
+        {
+            Frag<PO> Uf[NC][LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float be[8], left[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) be[e] = gates->beta[32 * s + 8 * g + e], left[e] = gates->left[32 * s + 8 * g + e];
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    float u[8], w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        u[e] = be[e] * Ee[c][2 * s + (e >> 2)][e & 3];
+                        w[e] = left[e] * u[e];
+                    }
+                    Uf[c][s] = make_frag<PO>(u);
+                    W[c][s] = make_frag<PM>(w);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const float decay = gates->decay[tile_index(i, m)];
+#pragma unroll
+                for (int c = 0; c < NC; ++c) QS[c][i] *= decay;
+#pragma unroll
+                for (int kb = 0; kb <= i / 2; ++kb) {
+                    const Frag<PO> pf = load_frag<PO>(ldsB + (U::P + U::lower(i, kb) * PO) * 1024, lane);
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) QS[c][i] = mm<CUT_O>(Uf[c][kb], pf, QS[c][i]);
+                }
+                // token tile_index(i, m), columns col0 + 16 c + 4 g ..
+                const int t = t0 + tile_index(i, m);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int col = col0 + 16 * c + 4 * g;
+                    E *to = o + (long long)t * a.so.token + col;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (t < a.T && col + r < a.Dv) store_element(to + r, a.scale * QS[c][i][r]);
+                }
+            }
+        }
+        // S <- e^GL S + K' (e^(GL-G) U)
+        const float whole = gates->whole;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[c][t] *= whole;
+#pragma unroll
+            for (int kb = 0; kb < LB; ++kb) {
+                const Frag<PI> kf = load_frag<PI>(ldsKT + (t * LB + kb) * PI * 1024, lane);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) S[c][t] = mm<3>(kf, W[c][kb], S[c][t]);
+            }
+        }
+    }
+    // past the sequence's end
+    for (int t = n * L + (lane >> 4); t < a.T; t += 4)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = col0 + 16 * c + m;
+            if (col < a.Dv) store_element(o + (long long)t * a.so.token + col, 0.0f);
+        }
+    if (a.final_state) store_state<NC, DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col0, lane, S);
+}
+
+}  // namespace tfno

@@ -1,0 +1,225 @@
+"""What the operators along time refuse, on the host before anything is launched (no call here needs a GPU)."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2504_11681_amd import binding as tfno
+
+FAKE = 0x10000000      # never dereferenced: every call fails its checks, or has nothing to do
+MB = 1 << 20
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(tfno.LIB_PATH):
+        from paper_2504_11681_amd import build
+        build.build(verbose=False)
+    return tfno.lib()
+
+
+def strides(T, H, D):
+    return tfno._Strides(T * H * D, H * D, D)
+
+
+def norm_desc(**kw):
+    d = tfno._HeadNormDesc(1, 2, 8, 4, 2, 64, 32, 8, 0, 1e-6, 0)
+    for n, H in (("q", 4), ("k", 2), ("q_out", 4), ("k_out", 2), ("dq", 4), ("dk", 2)):
+        setattr(d, n, strides(8, H, 64))
+    for n, v in kw.items():
+        setattr(d, n, v)
+    return d
+
+
+def rule_desc(**kw):
+    d = tfno._DeltaRuleDesc(1, 2, 8, 2, 4, 64, 64, 0.125)
+    for n, H, D in (("q", 2, 64), ("k", 2, 64), ("v", 4, 64), ("o", 4, 64), ("g", 4, 1), ("beta", 4, 1), ("dq", 2, 64), ("dk", 2, 64), ("dv", 4, 64),
+                    ("dg", 4, 1), ("dbeta", 4, 1)):
+        setattr(d, n, strides(8, H, D))
+    for n, v in kw.items():
+        setattr(d, n, v)
+    return d
+
+
+def call(fn, desc, args, **kw):
+    a = dict(args, **kw)
+    return fn(ctypes.addressof(desc) if desc is not None else None, *a.values(), None)
+
+
+def pointers(*names):
+    return {n: FAKE + i * MB for i, n in enumerate(names)}
+
+
+NORM = pointers("q", "k", "wq", "wk", "cos", "sin", "positions", "q_out", "k_out")
+NORM_BACK = pointers("q", "k", "wq", "wk", "cos", "sin", "positions", "dq_out", "dk_out", "dq", "dk", "dwq", "dwk")
+RULE = pointers("q", "k", "v", "g", "beta", "lengths", "initial", "o", "final", "tape")
+RULE_BACK = pointers("q", "k", "v", "g", "beta", "lengths", "initial", "tape", "d_o", "d_final", "dq", "dk", "dv", "dg", "dbeta", "d_initial")
+
+
+def test_norm_refuses(L):
+    for fn, args, needed in ((L.tfno_head_norm_rope, NORM, ("q", "k", "cos", "sin", "q_out", "k_out")),
+                             (L.tfno_head_norm_rope_backward, NORM_BACK, ("q", "k", "cos", "sin", "dq_out", "dk_out", "dq", "dk"))):
+        assert call(fn, None, args) == tfno.ERR_NULL
+        for n in needed:
+            assert call(fn, norm_desc(), args, **{n: None}) == tfno.ERR_NULL, n
+        for bad in (dict(dtype=2), dict(dtype=-1), dict(B=-1), dict(T=-1), dict(Hq=-1), dict(Hq=0, Hk=0), dict(D=0), dict(D=513), dict(R=-2), dict(R=3),
+                    dict(R=66), dict(eps=0.0), dict(eps=float("nan")), dict(P=-1), dict(positions_batch=-1), dict(B=1 << 30, T=1 << 10),
+                    dict(q=tfno._Strides(-1, 256, 64)), dict(k=tfno._Strides(1 << 40, 128, 64))):
+            assert call(fn, norm_desc(**bad), args) == tfno.ERR_SHAPE, bad
+        assert call(fn, norm_desc(P=7), args, positions=None) == tfno.ERR_SHAPE
+        for n in needed:
+            assert call(fn, norm_desc(), args, **{n: args[n] + 1}) == tfno.ERR_ALIGN, n
+        assert call(fn, norm_desc(), args, cos=args["cos"] + 2) == tfno.ERR_ALIGN
+        assert call(fn, norm_desc(B=0), dict.fromkeys(args)) == tfno.OK
+        first, second = ("q_out", "k_out") if fn is L.tfno_head_norm_rope else ("dq", "dk")
+        assert call(fn, norm_desc(), args, **{first: args[second]}) == tfno.ERR_ALIAS          # results over each other
+        assert call(fn, norm_desc(), args, **{first: args["cos"]}) == tfno.ERR_ALIAS
+        assert call(fn, norm_desc(), args, **{first: args["q"] + 2}) == tfno.ERR_ALIAS         # in place, but not at the same place
+        assert call(fn, norm_desc(**{first: tfno._Strides(8 * 256, 256, 32)}), args) == tfno.ERR_ALIAS   # heads that overlap each other
+        assert call(fn, norm_desc(**{first: tfno._Strides(0, 256, 64)}), args) == tfno.ERR_ALIAS         # one place for the whole batch
+
+
+def test_norm_gradient_needs_its_workspace(L):
+    need = L.tfno_head_norm_rope_workspace_bytes(64)
+    assert need > 0 and L.tfno_head_norm_rope_workspace_bytes(0) == 0 and L.tfno_head_norm_rope_workspace_bytes(513) == 0
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    assert call(L.tfno_head_norm_rope_backward, norm_desc(), NORM_BACK) == tfno.ERR_WORKSPACE
+    assert L.tfno_set_workspace(FAKE + 64 * MB, need - 1) == tfno.OK
+    assert call(L.tfno_head_norm_rope_backward, norm_desc(), NORM_BACK) == tfno.ERR_WORKSPACE
+    assert L.tfno_set_workspace(NORM_BACK["dq_out"], need) == tfno.OK
+    assert call(L.tfno_head_norm_rope_backward, norm_desc(), NORM_BACK) == tfno.ERR_ALIAS
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+
+
+def test_rule_refuses(L):
+    for fn, args, needed, outputs in (
+            (L.tfno_gated_delta_rule, RULE, ("q", "k", "v", "beta", "o"), ("o", "final", "tape")),
+            (L.tfno_gated_delta_rule_backward, RULE_BACK, ("q", "k", "v", "beta", "tape", "d_o", "dq", "dk", "dv", "dbeta"), ("dq", "dk", "dv", "dg", "dbeta", "d_initial"))):
+        assert call(fn, None, args) == tfno.ERR_NULL
+        for n in needed:
+            assert call(fn, rule_desc(), args, **{n: None}) == tfno.ERR_NULL, n
+        for bad in (dict(dtype=2), dict(B=-1), dict(T=-1), dict(Hk=0), dict(Hv=0), dict(Hv=3), dict(Dk=0), dict(Dv=0), dict(q=tfno._Strides(1024, -128, 64)),
+                    dict(v=tfno._Strides(1 << 41, 256, 64)), dict(B=1 << 20, Hk=64, Hv=64), dict(T=2147483647, B=4)):
+            assert call(fn, rule_desc(**bad), args) == tfno.ERR_SHAPE, bad
+        for bad in (dict(Dk=129), dict(Dv=257)):
+            assert call(fn, rule_desc(**bad), args) == tfno.ERR_UNSUPPORTED, bad
+        for n in args:
+            if n != "tape":
+                assert call(fn, rule_desc(), args, **{n: args[n] + 1}) == tfno.ERR_ALIGN, n
+        assert call(fn, rule_desc(), args, tape=args["tape"] + 128) == tfno.ERR_ALIGN
+        for n in outputs:
+            other = "k" if n != "tape" else "q"
+            assert call(fn, rule_desc(), args, **{n: args[other]}) == tfno.ERR_ALIAS, n
+        assert call(fn, rule_desc(**{"o" if fn is L.tfno_gated_delta_rule else "dv": tfno._Strides(2048, 0, 64)}), args) == tfno.ERR_ALIAS
+        assert call(fn, rule_desc(B=0), dict.fromkeys(args)) == tfno.OK
+        assert call(fn, rule_desc(T=0), dict.fromkeys(args)) == tfno.OK
+
+
+def test_slices_of_one_projection_are_no_aliases(L):
+    """q, k, v and the result interleaved in rows of one buffer: refused for the workspace alone; one value closer together, as an alias."""
+    d = rule_desc()
+    for n, H in (("q", 2), ("k", 2), ("v", 4), ("o", 4)):
+        setattr(d, n, tfno._Strides(8 * 12 * 64, 12 * 64, 64))
+    at = dict(RULE, q=FAKE, k=FAKE + 2 * 128, v=FAKE + 4 * 128, o=FAKE + 8 * 128, tape=None)
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    assert call(L.tfno_gated_delta_rule, d, at) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 8 * 128 - 2) == tfno.ERR_ALIAS
+    assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 8 * 128 + 2) == tfno.ERR_ALIAS
+
+
+    # one buffer [B, 4, T, H, D]
+    for n, H in (("q", 2), ("k", 2), ("v", 4), ("o", 4)):
+        setattr(d, n, tfno._Strides(4 * 8 * 256, H * 64, 64))
+    at = dict(RULE, q=FAKE, k=FAKE + 2 * 8 * 256, v=FAKE + 4 * 8 * 256, o=FAKE + 6 * 8 * 256, tape=None)
+    assert call(L.tfno_gated_delta_rule, d, at) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 6 * 8 * 256 - 2) == tfno.ERR_ALIAS
+    assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 6 * 8 * 256 + 2) == tfno.ERR_ALIAS
+
+
+def test_rule_memory(L):
+    d = rule_desc()
+    tape, forward, backward = L.tfno_gated_delta_rule_tape_bytes(ctypes.addressof(d)), *(L.tfno_gated_delta_rule_workspace_bytes(ctypes.addressof(d), b) for b in (0, 1))
+    assert tape > forward > 0 and backward > 0
+    longer = rule_desc(T=8 * 64)
+    assert L.tfno_gated_delta_rule_tape_bytes(ctypes.addressof(longer)) >= 7 * tape
+    for bad in (dict(Dk=129), dict(Hv=3), dict(B=-1)):
+        bad = rule_desc(**bad)
+        assert L.tfno_gated_delta_rule_tape_bytes(ctypes.addressof(bad)) == 0
+        assert L.tfno_gated_delta_rule_workspace_bytes(ctypes.addressof(bad), 1) == 0
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    assert call(L.tfno_gated_delta_rule, d, RULE, tape=None) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_gated_delta_rule_backward, d, RULE_BACK) == tfno.ERR_WORKSPACE
+    assert L.tfno_set_workspace(FAKE + 64 * MB, forward - 1) == tfno.OK
+    assert call(L.tfno_gated_delta_rule, d, RULE, tape=None) == tfno.ERR_WORKSPACE
+    assert L.tfno_set_workspace(RULE["q"], forward) == tfno.OK
+    assert call(L.tfno_gated_delta_rule, d, RULE, tape=None) == tfno.ERR_ALIAS
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+
+
+def test_step_refuses(L):
+    args = pointers("q", "k", "v", "g", "beta", "states", "slots", "pool", "o")
+    args["pool"] = 5
+    args["states"] = FAKE + 100 * MB
+    fn, d = L.tfno_gated_delta_rule_step, lambda **kw: rule_desc(**{"T": 1, **kw})
+    assert call(fn, None, args) == tfno.ERR_NULL
+    for n in ("q", "k", "v", "beta", "states", "o"):
+        assert call(fn, d(), args, **{n: None}) == tfno.ERR_NULL, n
+    for bad in (dict(T=2), dict(T=0), dict(Hv=5), dict(dtype=7), dict(B=-2)):
+        assert call(fn, d(**bad), args) == tfno.ERR_SHAPE, bad
+    assert call(fn, d(), args, pool=-1) == tfno.ERR_SHAPE
+    assert call(fn, d(), args, slots=None, pool=1) == tfno.ERR_SHAPE
+    assert call(fn, d(Dk=200), args) == tfno.ERR_UNSUPPORTED
+    for n in ("q", "k", "v", "g", "beta", "states", "slots", "o"):
+        assert call(fn, d(), args, **{n: args[n] + 1}) == tfno.ERR_ALIGN, n
+    assert call(fn, d(), args, o=args["states"]) == tfno.ERR_ALIAS
+    assert call(fn, d(), args, v=args["states"]) == tfno.ERR_ALIAS
+    assert call(fn, d(B=0), args) == tfno.OK
+
+
+def test_binding_refuses_what_is_not_on_the_device_or_has_another_type():
+    q = torch.zeros(2, 8, 2, 16)
+    g = torch.zeros(2, 8, 2)
+    with pytest.raises(TypeError):
+        tfno.gated_delta_rule(q, q, q, g, g, q)
+    with pytest.raises(TypeError):
+        tfno.gated_delta_rule(q, q.double(), q, g, g, q)
+    with pytest.raises(TypeError):
+        tfno.gated_delta_rule(q, q, q, g.double(), g, q)
+    with pytest.raises(TypeError):
+        tfno.head_norm_rope(q, q.bfloat16(), None, None, None, None, q, q)
+    with pytest.raises(TypeError):
+        tfno.head_norm_rope(q, q, None, None, None, None, q, q, positions=torch.zeros(2, 8))
+    with pytest.raises(TypeError):
+        tfno.gated_delta_rule_step(q[:, 0], q[:, 0], q[:, 0], g[:, 0], g[:, 0], torch.zeros(2, 2, 16, 16), q[:, 0], slots=torch.zeros(2))
+
+
+def layouts(*tensors):
+    return [tfno._layout(t) for t in tensors]
+
+
+def test_binding_refuses_shapes_that_do_not_fit():
+    q, v, g = torch.zeros(2, 8, 2, 16), torch.zeros(2, 8, 4, 24), torch.zeros(2, 8, 4)
+    none = [None] * 5
+    assert tfno._rule_desc(q.dtype, *layouts(q, q, v, v, g, g), *none, None)[0].scale == 0.25
+    for bad in ((q[:, :7], q, v, v, g, g), (q, q[..., :8], v, v, g, g), (q, q, v, q, g, g), (q, q, v, v, g[..., :2], g), (q, q, v, v, g, g[:1]), (q[0], q[0], v, v, g, g),
+                (q, q, v, v[..., ::2].repeat(1, 1, 1, 2)[..., ::1].transpose(2, 3), g, g)):
+        with pytest.raises(ValueError):
+            tfno._rule_desc(q.dtype, *layouts(*bad), *none, None)
+    with pytest.raises(ValueError):      # the last axis has to be contiguous
+        tfno._rule_desc(q.dtype, *layouts(torch.zeros(2, 8, 2, 32)[..., ::2], q, v, v, g, g), *none, None)
+    with pytest.raises(TypeError):
+        tfno._rule_desc(torch.float16, *layouts(q, q, v, v, g, g), *none, None)
+    w, cos = torch.zeros(16), torch.zeros(8, 4)
+    more = (None, None, None)
+    assert tfno._head_norm_desc(q.dtype, *layouts(q, q, q, q), *more, *layouts(w, w), None, None, *layouts(cos, cos), 1e-6, False)[0].R == 8
+    for qq, kk, ww, cc in ((q, q[:1], w, cos), (q, q[..., :8], w, cos), (q, q, w[:8], cos), (q, q, w, cos[0]), (q[0], q[0], w, cos)):
+        with pytest.raises(ValueError):
+            tfno._head_norm_desc(q.dtype, *layouts(qq, kk, qq, kk), *more, *layouts(ww, ww), None, None, *layouts(cc, cc), 1e-6, False)
+    with pytest.raises(ValueError):
+        tfno._head_norm_desc(q.dtype, *layouts(q, q, q, q), *more, *layouts(w, w), None, None, tfno._layout(cos), None, 1e-6, False)
+    s = torch.zeros(3, 4, 16, 24)
+    assert tfno._step_desc(q.dtype, *layouts(q[:, 0], q[:, 0], v[:, 0], v[:, 0], g[:, 0], g[:, 0]), s.shape, None)[0].T == 1
+    for bad in (s[:, :2], s[0], s[..., :8]):
+        with pytest.raises(ValueError):
+            tfno._step_desc(q.dtype, *layouts(q[:, 0], q[:, 0], v[:, 0], v[:, 0], g[:, 0], g[:, 0]), bad.shape, None)

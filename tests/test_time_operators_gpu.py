@@ -1,0 +1,468 @@
+"""The norm of heads with rotation and the gated delta rule on the GPU against float64."""
+import pytest
+import torch
+
+import time_oracle as oracle
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def tfno():
+    from paper_2504_11681_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    binding.lib()
+    return binding
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def near(name, got, want, bound):
+    off = oracle.rel(got, want)
+    say(f"   {name}: {off:.3g} of {bound:.3g}")
+    assert off <= bound, name
+
+
+def inputs(dtype, B, T, Hk, Hv, Dk, Dv, seed=0, state=True, decay=1.0, alike=0.5):
+    gen = torch.Generator("cuda").manual_seed(1000 + seed)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    def unit(x):
+        return x / x.norm(dim=-1, keepdim=True)
+
+    x = {"q": unit(normal(B, T, Hk, Dk)).to(dtype), "k": unit(normal(B, T, Hk, Dk) + alike * normal(1, 1, Hk, Dk)).to(dtype),
+         "v": normal(B, T, Hv, Dv).to(dtype), "g": -decay * torch.rand(B, T, Hv, generator=gen, device="cuda") * 0.3,
+         "beta": torch.sigmoid(normal(B, T, Hv)), "scale": Dk ** -0.5, "initial": normal(B, Hv, Dk, Dv) if state else None, "lengths": None}
+    x["d_o"], x["d_final"] = normal(B, T, Hv, Dv).to(dtype), normal(B, Hv, Dk, Dv)
+    return x
+
+
+def names(x, *n):
+    return [x[i] for i in n]
+
+
+def forward(tfno, x, tape=None, o=None):
+    v, k = x["v"], x["k"]
+    o = torch.full(v.shape, 7.0, dtype=v.dtype, device="cuda") if o is None else o
+    final = torch.full((v.shape[0], v.shape[2], k.shape[3], v.shape[3]), 7.0, device="cuda")
+    tfno.gated_delta_rule(*names(x, "q", "k", "v", "g", "beta"), o, scale=x["scale"], initial_state=x["initial"], final_state=final, lengths=x["lengths"],
+                          tape=tape)
+    return o, final
+
+
+def backward(tfno, x, tape, grads=None, initial=True):
+    d = grads or {n: None if x[n] is None else torch.full(x[n].shape, 7.0, dtype=x[n].dtype, device="cuda") for n in ("q", "k", "v", "g", "beta")}
+    d["initial"] = torch.full((x["v"].shape[0], x["v"].shape[2], x["k"].shape[3], x["v"].shape[3]), 7.0, device="cuda") if initial else None
+    tfno.gated_delta_rule_backward(*names(x, "q", "k", "v", "g", "beta", "d_o"), *names(d, "q", "k", "v", "g", "beta"), tape, scale=x["scale"],
+                                   initial_state=x["initial"], d_final_state=x["d_final"], d_initial_state=d["initial"], lengths=x["lengths"])
+    return d
+
+
+def want(x, grads):
+    a = names(x, "q", "k", "v", "g", "beta", "scale", "initial", "lengths")
+    return oracle.rule(*a, *names(x, "d_o", "d_final")) if grads else oracle.rule(*a)
+
+
+def check_forward(tfno, x, what):
+    say(what)
+    o, final = forward(tfno, x)
+    wo, wfinal = want(x, False)
+    near("o", o, wo, oracle.REL[o.dtype])
+    near("final", final, wfinal, oracle.REL[F32])
+    return o, final
+
+
+def check_both(tfno, x, what):
+    say(what)
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    o, final = forward(tfno, x, tape)
+    d = backward(tfno, x, tape)
+    w = want(x, True)
+    near("o", o, w[0], oracle.REL[o.dtype])
+    near("final", final, w[1], oracle.REL[F32])
+    for n, v in zip(("q", "k", "v", "g", "beta", "initial"), w[2:]):
+        if d[n] is not None:
+            near("d" + n, d[n], v, oracle.REL_GATES if n in ("g", "beta") else oracle.REL[d[n].dtype])
+    return o, final, d
+
+
+# one token, around the sizes of tiles and chunks, several chunks; head sizes from 1, odd, around the sizes of blocks; shared key heads
+SIZES = [(1, 1, 1, 1, 64, 64), (2, 2, 1, 1, 1, 1), (3, 15, 2, 2, 16, 16), (2, 17, 1, 3, 7, 5), (2, 31, 2, 4, 32, 33), (2, 33, 1, 1, 33, 32),
+         (1, 63, 2, 2, 64, 17), (2, 64, 1, 2, 65, 64), (2, 65, 3, 3, 100, 130), (1, 129, 1, 1, 128, 256), (2, 200, 2, 4, 128, 128), (1, 300, 1, 4, 48, 80),
+         (5, 96, 2, 2, 31, 31)]
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", SIZES)
+def test_rule_and_gradient(tfno, dtype, size):
+    check_both(tfno, inputs(dtype, *size), f"[case] rule {dtype} {size}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", SIZES)
+def test_rule_without_tape_gives_what_it_gives_with_one(tfno, dtype, size):
+    x = inputs(dtype, *size, seed=1, state=False)
+    o, final = check_forward(tfno, x, f"[case] no tape {dtype} {size}")
+    o2, final2 = forward(tfno, x, tfno.gated_delta_rule_tape(x["q"], x["v"]))
+    near("o with a tape", o2, o.double(), oracle.REL[dtype])
+    near("final with a tape", final2, final.double(), oracle.REL[F32])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(1, 700, 1, 1, 64, 64), (40, 70, 8, 16, 128, 128), (64, 70, 8, 8, 64, 64), (9, 90, 32, 32, 32, 256), (2, 1500, 1, 2, 128, 64)])
+def test_rule_of_many_heads_and_of_long_sequences(tfno, dtype, size):
+    check_both(tfno, inputs(dtype, *size, seed=2), f"[case] large {dtype} {size}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_gates_at_their_ends(tfno, dtype):
+    x = inputs(dtype, 2, 150, 2, 2, 64, 48, seed=3)
+    g, beta = x["g"], x["beta"]
+    g[0, ::7] = float("-inf")                                  # forgets
+    g[0, 3::11] = torch.finfo(F32).min
+    g[1, :, 0] = 0.0                                           # never forgets
+    g[1, ::5, 1] = -200.0
+    beta[0, ::3] = 0.0                                         # writes nothing
+    beta[1, ::4] = 1.0
+    check_both(tfno, x, f"[case] gates {dtype}")
+    x["g"][:] = float("-inf")
+    check_both(tfno, x, f"[case] everything forgotten {dtype}")
+    x["beta"][:] = 0.0
+    check_both(tfno, x, f"[case] nothing written {dtype}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_no_decay(tfno, dtype):
+    x = inputs(dtype, 2, 130, 1, 2, 32, 32, seed=4)
+    x["g"] = None
+    check_both(tfno, x, f"[case] g None {dtype}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_keys_that_are_all_alike(tfno, dtype):
+    """The matrix of a chunk is then full below its diagonal: the inverse is well behaved, the powers of the matrix are not."""
+    x = inputs(dtype, 1, 200, 2, 2, 64, 64, seed=5, decay=0.0)
+    x["k"][:] = x["k"][:, :1]
+    x["beta"][:] = 1.0
+    check_both(tfno, x, f"[case] alike {dtype}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("bad", (float("nan"), float("inf"), float("-inf")))
+def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
+    B, T = 7, 140
+    x = inputs(dtype, B, T, 2, 4, 48, 40, seed=6)
+    x["lengths"] = torch.tensor([T, 0, 1, 64, 65, T + 50, -3], dtype=torch.int32, device="cuda")
+    live = oracle.tokens_of(x["lengths"], B, T, "cuda")
+    for n in ("q", "k", "v", "g", "beta", "d_o"):
+        x[n][~live] = bad
+    o, final, d = check_both(tfno, x, f"[case] lengths {dtype} {bad}")
+    for t in (o, d["q"], d["k"], d["v"], d["g"], d["beta"]):
+        assert (t[~live] == 0).all()
+    assert torch.equal(final[1], x["initial"][1]) and torch.equal(final[6], x["initial"][6])
+    assert torch.equal(d["initial"][1], x["d_final"][1])
+    check_forward(tfno, x, "without tape")
+
+
+def test_no_tokens_at_all(tfno):
+    x = inputs(F32, 3, 0, 2, 2, 16, 16, seed=7)
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    assert torch.equal(forward(tfno, x, tape)[1], x["initial"])
+    assert torch.equal(backward(tfno, x, tape)["initial"], x["d_final"])
+    x = inputs(F32, 0, 5, 2, 2, 16, 16, seed=7)
+    forward(tfno, x)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("way", ("fused", "heads first", "one element off", "repeated", "wide rows"))
+def test_strides(tfno, dtype, way):
+    B, T, Hk, Hv, Dk, Dv = 2, 77, 2, 4, 64, 64
+    x = inputs(dtype, B, T, Hk, Hv, Dk, Dv, seed=8)
+    plain = dict(x)
+    o, grads = None, None
+    if way == "fused":          # slices of one projection, and gradients into slices of one tensor
+        def fused():
+            w = torch.empty(B, T, (2 * Hk + Hv) * Dk, dtype=dtype, device="cuda")
+            q, k, v = w.split((Hk * Dk, Hk * Dk, Hv * Dv), -1)
+            return q.unflatten(-1, (Hk, Dk)), k.unflatten(-1, (Hk, Dk)), v.unflatten(-1, (Hv, Dv))
+        parts, dparts = fused(), fused()
+        for n, p in zip("qkv", parts):
+            p.copy_(x[n])
+            x[n] = p
+        gates = torch.empty(B, T, 2 * Hv, device="cuda")
+        gates[..., :Hv], gates[..., Hv:] = x["g"], x["beta"]
+        x["g"], x["beta"] = gates[..., :Hv], gates[..., Hv:]
+        grads = {**dict(zip("qkv", dparts)), "g": torch.empty_like(plain["g"]), "beta": torch.empty_like(plain["g"])}
+    elif way == "heads first":
+        for n in ("q", "k", "v", "d_o", "g", "beta"):
+            x[n] = x[n].transpose(1, 2).contiguous().transpose(1, 2)
+        o = torch.empty(B, Hv, T, Dv, dtype=dtype, device="cuda").transpose(1, 2)
+    elif way == "one element off":
+        for n in ("q", "k", "v", "d_o", "g", "beta"):
+            w = torch.empty(x[n].numel() + 1, dtype=x[n].dtype, device="cuda")[1:].view(x[n].shape)
+            x[n] = w.copy_(x[n])
+        o = torch.empty(plain["v"].numel() + 1, dtype=dtype, device="cuda")[1:].view(plain["v"].shape)
+    elif way == "repeated":     # one trajectory's queries for the whole batch, one gate for all heads
+        x["q"] = x["q"][:1].expand(B, -1, -1, -1)
+        x["beta"] = x["beta"][..., :1].expand(-1, -1, Hv)
+        x["d_o"] = x["d_o"][:, :1].expand(-1, T, -1, -1)
+        grads = {n: torch.empty_like(plain[n]) for n in ("q", "k", "v", "g", "beta")}
+    else:
+        for n in ("q", "k", "v"):
+            w = torch.empty(*x[n].shape[:-1], x[n].shape[-1] + 3, dtype=dtype, device="cuda")[..., :-3]
+            x[n] = w.copy_(x[n])
+    say(f"[case] strides {dtype} {way}")
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    got = forward(tfno, x, tape, o)
+    d = backward(tfno, x, tape, grads)
+    w = want(x, True)
+    near("o", got[0], w[0], oracle.REL[dtype])
+    near("final", got[1], w[1], oracle.REL[F32])
+    for n, v in zip(("q", "k", "v", "g", "beta", "initial"), w[2:]):
+        near("d" + n, d[n], v, oracle.REL_GATES if n in ("g", "beta") else oracle.REL[d[n].dtype])
+
+
+def test_offsets_past_32_bits(tfno):
+    """Two trajectories further apart than 2^31 elements."""
+    far, T, H, D = 2 ** 31 + 64, 70, 2, 64
+    memory = torch.empty(far + 4 * T * H * D, dtype=BF16, device="cuda")
+    x = inputs(BF16, 2, T, H, H, D, D, seed=9)
+    views = [memory[i * T * H * D:].as_strided((2, T, H, D), (far, H * D, D, 1)) for i in range(4)]
+    for n, w in zip(("q", "k", "v"), views):
+        x[n] = w.copy_(x[n])
+    say("[case] far apart")
+    o, final = forward(tfno, x, o=views[3])
+    wo, wfinal = want(x, False)
+    near("o", o, wo, oracle.REL[BF16])
+    near("final", final, wfinal, oracle.REL[F32])
+    cos = torch.ones(T, D // 2, device="cuda")
+    tfno.head_norm_rope(x["q"], x["k"], None, None, cos, torch.zeros_like(cos), views[3], views[2])
+    near("norm", views[3], oracle.norm(x["q"], None, None, None, None, 1e-6, False), oracle.REL[BF16])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_gradient_against_differences(tfno, dtype):
+    x = inputs(dtype, 2, 90, 1, 2, 24, 20, seed=10)
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    forward(tfno, x, tape)
+    d = backward(tfno, x, tape)
+    gen = torch.Generator("cuda").manual_seed(5)
+    for n in ("q", "k", "v", "g", "beta", "initial"):
+        way = torch.randn(x[n].shape, generator=gen, device="cuda", dtype=torch.float64)
+
+        def loss(h):
+            o, final = want({**x, n: x[n].double() + h * way}, False)
+            return float((o * x["d_o"].double()).sum() + (final * x["d_final"].double()).sum())
+
+        slope = (loss(1e-4) - loss(-1e-4)) / 2e-4
+        got = float((d[n].double() * way).sum())
+        # the error of a sum with a random direction is about the L2 error of the gradient: four standard deviations, and 1e-6 for the differences
+        bound = 4 * oracle.REL_GATES if d[n].dtype == F32 else 4 * oracle.REL[BF16]
+        say(f"   d{n}: {got:.8g}, by differences {slope:.8g}")
+        assert abs(got - slope) <= bound * float(d[n].double().norm()) + 1e-6 * abs(slope)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_equal_calls_give_equal_bits_and_the_past_does_not_see_the_future(tfno, dtype):
+    x = inputs(dtype, 3, 180, 2, 4, 64, 64, seed=11)
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    first, again = forward(tfno, x, tape), forward(tfno, x, tape)
+    d, d2 = backward(tfno, x, tape), backward(tfno, x, tape)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    assert all(torch.equal(d[n], d2[n]) for n in d)
+    for n in ("q", "k", "v", "g", "beta"):
+        x[n][:, 100:] = x[n][:, 100:] * 0.5
+    assert torch.equal(first[0][:, :100], forward(tfno, x)[0][:, :100])
+
+
+def test_another_stream_and_a_graph(tfno):
+    x = inputs(BF16, 2, 100, 2, 2, 64, 64, seed=12)
+    cos = torch.rand(100, 32, device="cuda")
+    w = torch.rand(64, device="cuda")
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    qn, kn, o, final = torch.empty_like(x["q"]), torch.empty_like(x["k"]), torch.empty_like(x["v"]), torch.empty_like(x["initial"])
+    d = {n: torch.empty_like(x[n]) for n in ("q", "k", "v", "g", "beta", "initial")}
+    dw = torch.empty(2, 64, device="cuda")
+    states, so = x["initial"].clone(), torch.empty_like(x["v"][:, 0])
+
+    def work():
+        tfno.head_norm_rope(x["q"], x["k"], w, w, cos, cos, qn, kn)
+        tfno.gated_delta_rule(qn, kn, x["v"], x["g"], x["beta"], o, scale=0.1, initial_state=x["initial"], final_state=final, tape=tape)
+        tfno.gated_delta_rule_backward(qn, kn, x["v"], x["g"], x["beta"], x["d_o"], d["q"], d["k"], d["v"], d["g"], d["beta"], tape, scale=0.1,
+                                       initial_state=x["initial"], d_final_state=x["d_final"], d_initial_state=d["initial"])
+        tfno.head_norm_rope_backward(x["q"], x["k"], w, w, cos, cos, d["q"], d["k"], d["q"], d["k"], dw[0], dw[1])
+        states.copy_(x["initial"])
+        tfno.gated_delta_rule_step(qn[:, 0], kn[:, 0], x["v"][:, 0], x["g"][:, 0], x["beta"][:, 0], states, so, scale=0.1)
+
+    results = [qn, kn, o, final, dw, states, so, *d.values()]
+    work()
+    torch.cuda.synchronize()
+    eager = [r.clone() for r in results]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for r in results:
+            r.fill_(7.0)
+        work()
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(eager, results))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work()
+    for step in range(4):
+        for n in ("q", "v", "d_o"):
+            x[n].mul_(-1.0)
+        for r in results:
+            r.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [r.clone() for r in results]
+        work()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, results)), step
+
+
+# ---------------------------------------------------------------- one token
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(1, 1, 1, 1, 1), (1, 4, 8, 64, 64), (3, 2, 2, 7, 5), (5, 1, 3, 33, 20), (2, 2, 4, 128, 256), (70, 4, 8, 100, 48), (2, 1, 1, 128, 130),
+                                  (200, 4, 4, 128, 128), (1, 1, 2, 16, 3)])
+def test_step(tfno, dtype, size):
+    B, Hk, Hv, Dk, Dv = size
+    x = inputs(dtype, B, 1, Hk, Hv, Dk, Dv, seed=20)
+    pool = B + 3
+    states = torch.randn(pool, Hv, Dk, Dv, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    slots = torch.randperm(pool, generator=torch.Generator("cuda").manual_seed(2), device="cuda")[:B].to(torch.int32)
+    if B > 2:
+        slots[1], slots[2] = -1, pool
+        x["g"][0], x["beta"][0] = float("-inf"), 1.0
+    before = states.clone()
+    o = torch.full((B, Hv, Dv), 7.0, dtype=dtype, device="cuda")
+    say(f"[case] step {dtype} {size}")
+    tfno.gated_delta_rule_step(*(x[n][:, 0] for n in ("q", "k", "v", "g", "beta")), states, o, slots=slots, scale=x["scale"])
+    live = [b for b in range(B) if 0 <= int(slots[b]) < pool]
+    rows = slots[live].long()
+    wo, wS = oracle.rule(*(x[n][live] for n in ("q", "k", "v", "g", "beta")), x["scale"], before[rows])
+    near("o", o[live], wo[:, 0], oracle.REL[dtype])
+    near("states", states[rows], wS, oracle.REL[F32])
+    rest = [s for s in range(pool) if s not in set(rows.tolist())]
+    assert torch.equal(states[rest], before[rest])
+    if B > 2:
+        assert (o[1] == 0).all() and torch.isnan(o[2]).all()
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_steps_follow_the_whole_sequence(tfno, dtype):
+    x = inputs(dtype, 2, 70, 2, 4, 64, 40, seed=21)
+    states, outputs = x["initial"].clone(), []
+    for t in range(70):
+        o = torch.empty(2, 4, 40, dtype=dtype, device="cuda")
+        tfno.gated_delta_rule_step(*(x[n][:, t] for n in ("q", "k", "v", "g", "beta")), states, o, scale=x["scale"])
+        outputs.append(o)
+    wo, wS = want(x, False)
+    near("o", torch.stack(outputs, 1), wo, oracle.REL[dtype])
+    near("state", states, wS, oracle.REL[F32])
+    o = torch.empty(2, 4, 40, dtype=dtype, device="cuda")
+    tfno.gated_delta_rule_step(x["q"][:, 0], x["k"][:, 0], x["v"][:, 0], None, x["beta"][:, 0], states, o)       # no decay, the default scale
+    again = oracle.rule(x["q"][:, :1], x["k"][:, :1], x["v"][:, :1], None, x["beta"][:, :1], 64 ** -0.5, wS)
+    near("o without decay", o, again[0][:, 0], oracle.REL[dtype])
+
+
+# ---------------------------------------------------------------- norm with rotation
+
+NORMS = [(1, 1, 1, 1, 1, 0), (2, 3, 2, 1, 2, 2), (1, 5, 3, 2, 3, 2), (2, 7, 4, 2, 7, 4), (1, 1, 8, 8, 64, 64), (3, 37, 6, 2, 80, 40), (2, 33, 2, 2, 96, 96),
+         (2, 100, 16, 4, 128, 128), (1, 9, 5, 1, 128, 30), (2, 9, 1, 3, 200, 8), (1, 17, 2, 2, 256, 256), (1, 3, 1, 1, 511, 510), (2, 4, 2, 2, 512, 64),
+         (4, 5, 0, 3, 64, 32), (4, 5, 3, 0, 64, 64)]
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("size", NORMS)
+def test_norm(tfno, dtype, interleaved, size):
+    B, T, Hq, Hk, D, R = size
+    gen = torch.Generator("cuda").manual_seed(30)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    qk = (normal(B, T, Hq + Hk, D) * 3).to(dtype)
+    dqk = normal(B, T, Hq + Hk, D).to(dtype)
+    q, k, dy, dz = qk[:, :, :Hq], qk[:, :, Hq:], dqk[:, :, :Hq], dqk[:, :, Hq:]
+    if T > 2 and Hq:
+        q[:, 1, 0] = 0.0                              # a row of zeros has a norm too
+    wq, wk = 1 + 0.3 * normal(D), 1 + 0.3 * normal(D)
+    P = 3 * T
+    angle = 6.3 * torch.rand(P, R // 2, generator=gen, device="cuda")
+    cos, sin = (torch.cos(angle), torch.sin(angle)) if R else (None, None)
+    for positions in (None, torch.randint(0, P, (B, T), generator=gen, device="cuda", dtype=torch.int32)):
+        say(f"[case] norm {dtype} {interleaved} {size} {positions is not None}")
+        yq, yk = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+        tfno.head_norm_rope(q, k, wq, wk, cos, sin, yq, yk, positions=positions, eps=1e-4, interleaved=interleaved)
+        dq, dk, dwq, dwk = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(wq, 7.0), torch.full_like(wk, 7.0)
+        tfno.head_norm_rope_backward(q, k, wq, wk, cos, sin, dy, dz, dq, dk, dwq, dwk, positions=positions, eps=1e-4, interleaved=interleaved)
+        for n, x, w, d, got, dx, dw in (("q", q, wq, dy, yq, dq, dwq), ("k", k, wk, dz, yk, dk, dwk)):
+            a = oracle.norm(x, w, cos, sin, positions, 1e-4, interleaved, d)
+            near(n, got, a[0], oracle.REL[dtype])
+            # one value a head: its gradient is the small difference of two that cancel
+            near("d" + n, dx.double() + (x.double() if D == 1 else 0), a[1] + (x.double() if D == 1 else 0), oracle.REL[dtype])
+            near("dw" + n, dw, a[2], oracle.REL[F32])
+
+
+def test_norm_in_place_without_weights_and_with_strides(tfno):
+    gen = torch.Generator("cuda").manual_seed(31)
+    cos, sin = torch.rand(9, 16, generator=gen, device="cuda"), torch.rand(9, 16, generator=gen, device="cuda")
+    for dtype in (F32, BF16):
+        w = torch.randn(2, 9, 4 * 32 + 5, generator=gen, device="cuda").to(dtype)
+        for off in (0, 1, 4):                          # slices of wide rows, at odd places too
+            q, k = w[..., off:off + 64].unflatten(-1, (2, 32)), w[..., off + 64:off + 128].unflatten(-1, (2, 32))
+            wants = [oracle.norm(x, None, cos, sin, None, 1e-6, False) for x in (q, k)]
+            dx = [oracle.norm(x, None, cos, sin, None, 1e-6, False, x)[1] for x in (q, k)]
+            dq, dk = q.clone(), k.clone()              # gradients over the gradients that they come from
+            tfno.head_norm_rope_backward(q, k, None, None, cos, sin, dq, dk, dq, dk)
+            near("dq", dq, dx[0], oracle.REL[dtype])
+            near("dk", dk, dx[1], oracle.REL[dtype])
+            tfno.head_norm_rope(q, k, None, None, cos, sin, q, k)
+            near("q", q, wants[0], oracle.REL[dtype])
+            near("k", k, wants[1], oracle.REL[dtype])
+
+
+def test_norm_of_positions_that_the_tables_do_not_hold(tfno):
+    q = torch.randn(1, 4, 2, 12, device="cuda")
+    out, k_out = torch.zeros_like(q), torch.zeros_like(q)
+    cos = torch.ones(5, 4, device="cuda")
+    positions = torch.tensor([[0, 5, -1, 4]], dtype=torch.int32, device="cuda")
+    tfno.head_norm_rope(q, q, None, None, cos, torch.zeros_like(cos), out, k_out, positions=positions)
+    assert torch.isnan(out[:, 1:3, :, :8]).all() and torch.isfinite(out[:, 1:3, :, 8:]).all()
+    assert torch.isfinite(out[:, (0, 3)]).all()
+
+
+def test_norm_gradient_against_differences(tfno):
+    gen = torch.Generator("cuda").manual_seed(33)
+    q, dy = torch.randn(2, 5, 3, 24, generator=gen, device="cuda"), torch.randn(2, 5, 3, 24, generator=gen, device="cuda")
+    w = 1 + 0.2 * torch.randn(24, generator=gen, device="cuda")
+    angle = torch.rand(5, 6, generator=gen, device="cuda")
+    cos, sin = torch.cos(angle), torch.sin(angle)
+    d = {"x": torch.empty_like(q), "w": torch.empty_like(w)}
+    tfno.head_norm_rope_backward(q, q, w, w, cos, sin, dy, dy, d["x"], torch.empty_like(q), d["w"], None)
+    for n in ("x", "w"):
+        way = torch.randn(d[n].shape, generator=gen, device="cuda", dtype=torch.float64)
+
+        def loss(h):
+            return float((oracle.norm(q.double() + (h * way if n == "x" else 0), w.double() + (h * way if n == "w" else 0), cos, sin, None, 1e-6, False) * dy).sum())
+
+        slope = (loss(1e-4) - loss(-1e-4)) / 2e-4
+        assert abs(float((d[n].double() * way).sum()) - slope) <= 4 * oracle.REL_GATES * float(d[n].norm()) + 1e-6 * abs(slope)
+
+
+def test_norm_of_nothing(tfno):
+    q = torch.zeros(0, 4, 2, 16, device="cuda")
+    dw = torch.full((16,), 7.0, device="cuda")
+    tfno.head_norm_rope(q, q, None, None, None, None, q.clone(), q.clone())
+    tfno.head_norm_rope_backward(q, q, None, None, None, None, q.clone(), q.clone(), q.clone(), q.clone(), dw, None)
+    assert (dw == 0).all()
