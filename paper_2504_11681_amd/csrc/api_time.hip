@@ -173,12 +173,16 @@ tfno_status rule_sizes(const tfno_delta_rule_desc *d)
     return TFNO_OK;
 }
 
+// The kernels reach the tokens of a chunk of v, o and their gradients with 32-bit offsets.
+bool tokens_near(const DeltaArgs &a, const Strides &s) { return a.T <= 1 || s.token < (1 << 24); }
+
 DeltaArgs rule_args(const tfno_delta_rule_desc *d)
 {
     DeltaArgs a{};
     a.sq = strides(d->q), a.sk = strides(d->k), a.sv = strides(d->v), a.so = strides(d->o), a.sg = strides(d->g), a.sbeta = strides(d->beta);
     a.sdo = a.so, a.sdq = strides(d->dq), a.sdk = strides(d->dk), a.sdv = strides(d->dv), a.sdg = strides(d->dg), a.sdbeta = strides(d->dbeta);
     a.B = d->B, a.T = d->T, a.Hk = d->Hk, a.Hv = d->Hv, a.Dk = d->Dk, a.Dv = d->Dv, a.scale = d->scale, a.bf16 = d->dtype == TFNO_BF16;
+    if (a.T == 1) a.sv.token = a.so.token = a.sdo.token = a.sdv.token = 0;      // whatever it is, no second token is reached with it
     return a;
 }
 
@@ -209,6 +213,7 @@ tfno_status tfno_gated_delta_rule(const tfno_delta_rule_desc *d, const void *q, 
     if (d->B == 0 || (d->T == 0 && !final)) return TFNO_OK;
     if (d->T > 0 && (!q || !k || !v || !beta || !o)) return TFNO_ERR_NULL;
     DeltaArgs a = rule_args(d);
+    if (!tokens_near(a, a.sv) || !tokens_near(a, a.so)) return TFNO_ERR_UNSUPPORTED;
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.Hv * a.Dk * a.Dv;
     const bool t = a.T > 0;
@@ -239,6 +244,7 @@ tfno_status tfno_gated_delta_rule_backward(const tfno_delta_rule_desc *d, const 
     if (d->B == 0 || (d->T == 0 && !d_initial)) return TFNO_OK;
     if (d->T > 0 && (!q || !k || !v || !beta || !tape || !d_o || !dq || !dk || !dv || !dbeta)) return TFNO_ERR_NULL;
     DeltaArgs a = rule_args(d);
+    if (!tokens_near(a, a.sdo) || !tokens_near(a, a.sdv)) return TFNO_ERR_UNSUPPORTED;
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.Hv * a.Dk * a.Dv;
     const bool t = a.T > 0;

@@ -18,184 +18,200 @@
 
 namespace tfno {
 
-template <class E, int KB, int NC>
-__global__ __launch_bounds__(256) void k_delta_scan_back(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+// LDS of a chunk: K, gates, P', T' | K', Q'
+template <class E, int KB>
+struct BackwardLds : ScanLds<DeltaUnits<E, KB>::Q + 1 + 2 * DeltaUnits<E, KB>::TRI * DELTA_PM, DeltaUnits<E, KB>::KEY_TAPE - DeltaUnits<E, KB>::KT> {};
+
+template <class E, int KB>
+__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan_back(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
     typedef DeltaUnits<E, KB> U;
     constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PM = DELTA_PM;
-    // LDS in units: K | P' , gates, T' | K', Q'
-    constexpr int K_UNITS = U::Q, PT_UNITS = U::TRI * PM, T_UNITS = U::KEY_TAPE - U::KT;
+    typedef BackwardLds<E, KB> Lds;
+    constexpr int K_UNITS = U::Q, TRI_UNITS = U::TRI * PM;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    unsigned char *ldsK = lds, *ldsPT = ldsK + K_UNITS * 1024, *ldsG = ldsPT + PT_UNITS * 1024, *ldsTT = ldsG + 1024,
-                  *ldsKT = ldsTT + PT_UNITS * 1024;
-    const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsG;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int m = lane & 15, g = lane >> 4;
-    const int block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int block = id % blocks_per_head, head = id / blocks_per_head;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
     const int len = sequence_length(a, b), n = (len + L - 1) / L;
     const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
     const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
-    const int col0 = (block * waves + wave) * 16 * NC;
+    const int col0 = (block * waves + wave) * 16, col = col0 + m;
+    const bool all_columns = a.Dv % 32 == 0;
 
-    floatx4 S[NC][DT];          // dS', laid out as the state is
-    load_state<NC, DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col0, lane, S);
+    floatx4 S[DT];          // dS', laid out as the state is
+    load_state<DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + h * a.sdo.head);
     E *dv = (E *)a.dv + (b * a.sdv.batch + h * a.sdv.head);
+    const unsigned at_do = 8 * g * (unsigned)a.sdo.token + (col < a.Dv ? col : 0);
+    const unsigned at_dv = 8 * g * (unsigned)a.sdv.token + col, at_tape = 8 * g * (unsigned)mem.dvp + col;
 
-    auto load_first = [&](int chunk) {
+    auto load_first = [&](int chunk, int parity) {
+        unsigned char *to = Lds::first(lds, parity);
         const unsigned char *v = value + (long long)chunk * mem.value_units * 1024;
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, ldsK, K_UNITS, wave, waves, lane);
-        units_to_lds(v + U::PT * 1024, ldsPT, PT_UNITS, wave, waves, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, wave, waves, lane);
+        units_to_lds(v + U::GATES * 1024, to + K_UNITS * 1024, 1, wave, waves, lane);
+        units_to_lds(v + U::PT * 1024, to + (K_UNITS + 1) * 1024, TRI_UNITS, wave, waves, lane);
+        units_to_lds(v + U::TT * 1024, to + (K_UNITS + 1 + TRI_UNITS) * 1024, TRI_UNITS, wave, waves, lane);
     };
-    if (n > 0) load_first(n - 1);
+    auto load_last = [&](int chunk, int parity) {
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, wave, waves, lane);
+    };
+    E next[LB][8];
+    auto load_do = [&](int chunk) { load_columns<E, LB>(d_o + (long long)chunk * L * a.sdo.token, a.sdo.token, at_do, g, len - chunk * L, next); };
+    if (n > 0) {
+        load_first(n - 1, (n - 1) & 1);
+        if (Lds::DOUBLE) load_last(n - 1, (n - 1) & 1);
+        load_do(n - 1);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
     for (int chunk = n - 1; chunk >= 0; --chunk) {
-        const int t0 = chunk * L;
-        loads_done_and_barrier();
-        {
-            const unsigned char *v = value + (long long)chunk * mem.value_units * 1024;
-            units_to_lds(v + U::GATES * 1024, ldsG, 1, wave, waves, lane);
-            units_to_lds(v + U::TT * 1024, ldsTT, PT_UNITS, wave, waves, lane);
-            units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, ldsKT, T_UNITS, wave, waves, lane);
+        const int t0 = chunk * L, parity = chunk & 1;
+        const unsigned char *ldsK = Lds::first(lds, parity), *ldsG = ldsK + K_UNITS * 1024, *ldsPT = ldsG + 1024, *ldsTT = ldsPT + TRI_UNITS * 1024,
+                            *ldsKT = Lds::last(lds, parity);
+        const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsG;
+        __syncthreads();
+        float x[LB][8];
+        columns_to_float<E, LB>(next, all_columns, col < a.Dv, g, len - t0, x);
+        const int before = chunk > 0 ? chunk - 1 : 0;
+        if (!Lds::DOUBLE) load_last(chunk, parity);
+        if (chunk > 0) {
+            load_first(before, parity ^ 1);
+            if (Lds::DOUBLE) load_last(before, parity ^ 1);
         }
-        float x[NC][LB][8];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = col0 + 16 * c + m;
-            load_columns<E, LB>(d_o + (long long)t0 * a.sdo.token, a.sdo.token, col, a.Dv, g, len - t0, x[c]);
-            if (col < mem.dvp) {
-                float *to = mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp + col;
-#pragma unroll
-                for (int t = 0; t < DT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) to[tile_index(t, 4 * g + r) * mem.dvp] = S[c][t][r];
-            }
-        }
-        floatx4 KS[NC][NT], PO_[NC][NT];
+        load_do(before);
+        if (col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        // K dS' and P' dO, a pair of tiles of tokens at a time
+        floatx4 KS[NT], PO_[NT];
         {
-            Frag<PM> Sf[NC][KB];
-            Frag<PI> Of[NC][LB];
+            Frag<PI> Of[LB];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) {
-                    float u[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = S[c][2 * kb + (e >> 2)][e & 3];
-                    Sf[c][kb] = make_frag<PM>(u);
-                }
-#pragma unroll
-                for (int s = 0; s < LB; ++s) Of[c][s] = make_frag<PI>(x[c][s]);
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                for (int c = 0; c < NC; ++c) KS[c][i] = PO_[c][i] = floatx4{0, 0, 0, 0};
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) {
-                    const Frag<PI> kf = load_frag<PI>(ldsK + (i * KB + kb) * PI * 1024, lane);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) KS[c][i] = mm<3>(kf, Sf[c][kb], KS[c][i]);
-                }
-#pragma unroll
-                for (int kb = i / 2; kb < LB; ++kb) {
-                    const Frag<PM> pf = load_frag<PM>(ldsPT + U::upper(i, kb) * PM * 1024, lane);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) PO_[c][i] = mm<3>(pf, Of[c][kb], PO_[c][i]);
-                }
-            }
-        }
-        loads_done_and_barrier();
-        if (chunk > 0) load_first(chunk - 1);
-
-        // Y = T' (beta dU)
-        floatx4 Y[NC][NT];
-        {
-            Frag<PM> R[NC][LB];
+            for (int s = 0; s < LB; ++s) Of[s] = make_frag<PI>(x[s]);
 #pragma unroll
             for (int s = 0; s < LB; ++s) {
-                float be[8], left[8];
+                Frag<PM> pf[LB][2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) be[e] = gates->beta[32 * s + 8 * g + e], left[e] = gates->left[32 * s + 8 * g + e];
+                for (int kb = s; kb < LB; ++kb)
 #pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    float u[8];
+                    for (int p = 0; p < 2; ++p) pf[kb][p] = load_frag<PM>(ldsPT + U::upper(2 * s + p, kb) * PM * 1024, lane);
+                PO_[2 * s] = PO_[2 * s + 1] = floatx4{0, 0, 0, 0};
+                floatx4 *to[2] = {&PO_[2 * s], &PO_[2 * s + 1]};
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        u[e] = be[e] * fmaf(left[e], KS[c][2 * s + (e >> 2)][e & 3], a.scale * PO_[c][2 * s + (e >> 2)][e & 3]);
-                    R[c][s] = make_frag<PM>(u);
-                }
+                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(pf[kb], Of[kb], to);
             }
+            Frag<PM> Sf[KB];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
+            for (int kb = 0; kb < KB; ++kb) {
+                float u[8];
 #pragma unroll
-                for (int c = 0; c < NC; ++c) Y[c][i] = floatx4{0, 0, 0, 0};
-#pragma unroll
-                for (int kb = i / 2; kb < LB; ++kb) {
-                    const Frag<PM> tf = load_frag<PM>(ldsTT + U::upper(i, kb) * PM * 1024, lane);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) Y[c][i] = mm<3>(tf, R[c][kb], Y[c][i]);
-                }
+                for (int e = 0; e < 8; ++e) u[e] = S[2 * kb + (e >> 2)][e & 3];
+                Sf[kb] = make_frag<PM>(u);
             }
-        }
+            Frag<PI> kf[2][2];
+            auto read = [&](int step, int to) {
+                const int i = step / KB * 2, kb = step % KB;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = col0 + 16 * c + m;
-            if (col < mem.dvp) {
-                float *to = mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp + col;
+                for (int p = 0; p < 2; ++p) kf[to][p] = load_frag<PI>(ldsK + ((i + p) * KB + kb) * PI * 1024, lane);
+            };
+            read(0, 0);
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int row = tile_index(i, 4 * g + r);
-                        to[row * mem.dvp] = Y[c][i][r];
-                        if (t0 + row < a.T && col < a.Dv) store_element(dv + (long long)(t0 + row) * a.sdv.token + col, Y[c][i][r]);
-                    }
+            for (int step = 0; step < LB * KB; ++step) {
+                const int i = step / KB * 2, kb = step % KB, at = step & 1;
+                if (step + 1 < LB * KB) read(step + 1, at ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kb == 0) KS[i] = KS[i + 1] = floatx4{0, 0, 0, 0};
+                floatx4 *to[2] = {&KS[i], &KS[i + 1]};
+                mm_many<3, false>(kf[at], Sf[kb], to);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        Frag<PM> Wo[NC][LB], Wy[NC][LB];
+
+        // Y = T' (beta dU)
+        floatx4 Y[NT];
+        {
+            Frag<PM> R[LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float be[8], left[8], u[8];
+                load_gates(gates->beta + 32 * s + 8 * g, be);
+                load_gates(gates->left + 32 * s + 8 * g, left);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = be[e] * fmaf(left[e], KS[2 * s + (e >> 2)][e & 3], a.scale * PO_[2 * s + (e >> 2)][e & 3]);
+                R[s] = make_frag<PM>(u);
+            }
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                Frag<PM> tf[LB][2];
+#pragma unroll
+                for (int kb = s; kb < LB; ++kb)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) tf[kb][p] = load_frag<PM>(ldsTT + U::upper(2 * s + p, kb) * PM * 1024, lane);
+                Y[2 * s] = Y[2 * s + 1] = floatx4{0, 0, 0, 0};
+                floatx4 *to[2] = {&Y[2 * s], &Y[2 * s + 1]};
+#pragma unroll
+                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(tf[kb], R[kb], to);
+            }
+        }
+        Frag<PM> Wo[LB], Wy[LB];
 #pragma unroll
         for (int s = 0; s < LB; ++s) {
-            float decay[8];
+            float decay[8], u[8], w[8];
+            load_gates(gates->decay + 32 * s + 8 * g, decay);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) decay[e] = gates->decay[32 * s + 8 * g + e];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                float u[8], w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    u[e] = a.scale * decay[e] * x[c][s][e];
-                    w[e] = -decay[e] * Y[c][2 * s + (e >> 2)][e & 3];
-                }
-                Wo[c][s] = make_frag<PM>(u);
-                Wy[c][s] = make_frag<PM>(w);
+            for (int e = 0; e < 8; ++e) {
+                u[e] = a.scale * decay[e] * x[s][e];
+                w[e] = -decay[e] * Y[2 * s + (e >> 2)][e & 3];
             }
+            Wo[s] = make_frag<PM>(u);
+            Wy[s] = make_frag<PM>(w);
         }
         const float whole = gates->whole;
+        if (!Lds::DOUBLE) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+        }
+        {
+            Frag<PI> kf[2][2], qf[2][2];
+            auto read = [&](int step, int to) {
+                const int t = step / LB * 2, kb = step % LB;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) S[c][t] *= whole;
-#pragma unroll
-            for (int kb = 0; kb < LB; ++kb) {
-                const Frag<PI> kf = load_frag<PI>(ldsKT + (t * LB + kb) * PI * 1024, lane);
-                const Frag<PI> qf = load_frag<PI>(ldsKT + ((DT + t) * LB + kb) * PI * 1024, lane);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    S[c][t] = mm<3>(kf, Wy[c][kb], S[c][t]);
-                    S[c][t] = mm<3>(qf, Wo[c][kb], S[c][t]);
+                for (int p = 0; p < 2; ++p) {
+                    kf[to][p] = load_frag<PI>(ldsKT + ((t + p) * LB + kb) * PI * 1024, lane);
+                    qf[to][p] = load_frag<PI>(ldsKT + ((DT + t + p) * LB + kb) * PI * 1024, lane);
                 }
+            };
+            read(0, 0);
+#pragma unroll
+            for (int step = 0; step < KB * LB; ++step) {
+                const int t = step / LB * 2, kb = step % LB, at = step & 1;
+                if (step + 1 < KB * LB) read(step + 1, at ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
+                floatx4 *to[2] = {&S[t], &S[t + 1]};
+                mm_many<3, false>(kf[at], Wy[kb], to);
+                mm_many<3, false>(qf[at], Wo[kb], to);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        }
+        if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);      // what the next chunk needs is there; the stores have its time
+        if (col0 < mem.dvp) {
+            store_tiles<NT>(mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Y);
+            const bool whole_chunk = t0 + L <= a.T;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = t0 + 32 * (i >> 1) + 4 * (i & 1) + r;
+                    if (col < a.Dv && (whole_chunk || row + 8 * g < a.T)) store_element(dv + row * a.sdv.token + at_dv, Y[i][r]);
+                }
         }
     }
     for (int t = n * L + g; t < a.T; t += 4)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = col0 + 16 * c + m;
-            if (col < a.Dv) store_element(dv + (long long)t * a.sdv.token + col, 0.0f);
-        }
-    if (a.d_initial) store_state<NC, DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col0, lane, S);
+        if (col < a.Dv) store_element(dv + t * a.sdv.token + col, 0.0f);
+    if (a.d_initial) store_state<DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
 }
 
 // One workgroup for a chunk of a key head, a wave for each 16 tokens of it.

@@ -45,38 +45,34 @@ bool rows_of_8(const void *p, const Strides &s, bool bf16)
     return ((uintptr_t)p & 15) == 0 && s.batch % unit == 0 && s.token % unit == 0 && s.head % unit == 0;
 }
 
-// Waves of a scan's workgroup and column tiles of a wave: two tiles and four waves where there are heads enough to fill the chip.
-struct ScanShape { int waves, nc, blocks; };
+// Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few heads.
+struct ScanShape { int waves, blocks; };
 ScanShape scan_shape(const DeltaArgs &a, int dvp)
 {
     const int tiles = dvp / 16;
     const long long heads = (long long)a.B * a.Hv;
-    ScanShape s;
-    s.nc = heads * tiles >= 2048 ? 2 : 1;
-    s.waves = 4;
-    while (s.waves > 1 && (heads * tiles < 256LL * s.waves * s.nc || s.waves * s.nc > tiles)) s.waves >>= 1;
-    s.blocks = (tiles + s.waves * s.nc - 1) / (s.waves * s.nc);
+    ScanShape s{SCAN_THREADS / 64, 0};
+    while (s.waves > 2 && (heads * tiles < 256LL * s.waves || s.waves > tiles)) s.waves >>= 1;
+    s.blocks = (tiles + s.waves - 1) / s.waves;
     return s;
 }
 
-template <class E, int KB, int NC, bool TAPE>
+template <class E, int KB, bool TAPE>
 hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
 {
-    typedef DeltaUnits<E, KB> U;
-    constexpr int bytes = (U::QT + U::VALUE_FORWARD) * 1024;
+    constexpr int bytes = ForwardLds<E, KB>::BYTES;
     static LdsLimitOnce limit;
-    if (hipError_t e = limit.set({(const void *)k_delta_scan<E, KB, NC, TAPE>}, bytes); e != hipSuccess) return e;
-    k_delta_scan<E, KB, NC, TAPE><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    if (hipError_t e = limit.set({(const void *)k_delta_scan<E, KB, TAPE>}, bytes); e != hipSuccess) return e;
+    k_delta_scan<E, KB, TAPE><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
-template <class E, int KB, int NC>
+template <class E, int KB>
 hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
 {
-    typedef DeltaUnits<E, KB> U;
-    constexpr int bytes = (U::Q + 2 * U::TRI * DELTA_PM + 1 + U::KEY_TAPE - U::KT) * 1024;
+    constexpr int bytes = BackwardLds<E, KB>::BYTES;
     static LdsLimitOnce limit;
-    if (hipError_t e = limit.set({(const void *)k_delta_scan_back<E, KB, NC>}, bytes); e != hipSuccess) return e;
-    k_delta_scan_back<E, KB, NC><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    if (hipError_t e = limit.set({(const void *)k_delta_scan_back<E, KB>}, bytes); e != hipSuccess) return e;
+    k_delta_scan_back<E, KB><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 
@@ -89,13 +85,13 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s)
     forward_memory<E, KB>(a, tape ? a.tape : a.workspace, tape, &m);
     DeltaVec vec{};
     vec.q = rows_of_8(a.q, a.sq, a.bf16), vec.k = rows_of_8(a.k, a.sk, a.bf16);
+    m.vec_o = a.Dv % 4 == 0 && ((uintptr_t)a.o & (a.bf16 ? 7 : 15)) == 0 && a.so.batch % 4 == 0 && a.so.token % 4 == 0 && a.so.head % 4 == 0;
     const unsigned grid = (unsigned)(a.B * a.Hv * m.chunks);
     if (grid && tape) k_delta_prepare<E, KB, true><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const ScanShape sh = scan_shape(a, m.dvp);
-    if (tape) return sh.nc == 2 ? scan<E, KB, 2, true>(a, m, sh, s) : scan<E, KB, 1, true>(a, m, sh, s);
-    return sh.nc == 2 ? scan<E, KB, 2, false>(a, m, sh, s) : scan<E, KB, 1, false>(a, m, sh, s);
+    return tape ? scan<E, KB, true>(a, m, sh, s) : scan<E, KB, false>(a, m, sh, s);
 }
 
 template <class E, int KB>
@@ -108,7 +104,7 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s)
     DeltaVec vec{};
     vec.d_o = rows_of_8(a.d_o, a.sdo, a.bf16), vec.dq = rows_of_8(a.dq, a.sdq, a.bf16), vec.dk = rows_of_8(a.dk, a.sdk, a.bf16);
     const ScanShape sh = scan_shape(a, m.dvp);
-    if (hipError_t e = sh.nc == 2 ? scan_back<E, KB, 2>(a, m, sh, s) : scan_back<E, KB, 1>(a, m, sh, s); e != hipSuccess) return e;
+    if (hipError_t e = scan_back<E, KB>(a, m, sh, s); e != hipSuccess) return e;
     if (m.chunks == 0) return hipSuccess;
     k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 64 * U::NT, 0, s>>>(a, m, vec);
     return hipGetLastError();

@@ -34,6 +34,23 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 template <int P>
 struct Frag { bf16x8 p[P]; };
 
+// x minus the low (high) one of the two BF16 values in w: a dot product of pairs with (-1, 0) resp. (0, -1), exact, one instruction instead of a mask
+// and a subtraction.  The constants are held in registers behind the compiler's back: as an inline constant -1.0 means the high half alone.
+__device__ __forceinline__ float minus_low(unsigned w, float x)
+{
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    unsigned c = 0x0000bf80u;
+    asm("" : "+s"(c));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, c), x, false);
+}
+__device__ __forceinline__ float minus_high(unsigned w, float x)
+{
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    unsigned c = 0xbf800000u;
+    asm("" : "+s"(c));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, c), x, false);
+}
+
 template <int P>
 __device__ __forceinline__ Frag<P> make_frag(const float (&x)[8])
 {
@@ -45,11 +62,11 @@ __device__ __forceinline__ Frag<P> make_frag(const float (&x)[8])
     for (int p = 0; p < P; ++p) {
         uintx4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
+        for (int e = 0; e < 4; ++e) {
+            w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
+            if (p + 1 < P) r[2 * e] = minus_low(w[e], r[2 * e]), r[2 * e + 1] = minus_high(w[e], r[2 * e + 1]);
+        }
         f.p[p] = __builtin_bit_cast(bf16x8, w);
-        if (p + 1 < P)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] -= __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);
     }
     return f;
 }
@@ -64,6 +81,22 @@ __device__ __forceinline__ floatx4 mm(const Frag<PA> &a, const Frag<PB> &b, floa
         for (int i = 0; i < PA; ++i)
             if (sum - i >= 0 && sum - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[sum - i], c, 0, 0, 0);
     return c;
+}
+
+// The same for N accumulators that do not depend on each other, so that their products follow at the rate of the matrix pipe and not at its latency:
+// c[n] + A[n] B, or with SWAP c[n] + B A[n].
+template <int CUT, bool SWAP, int N, int PA, int PB>
+__device__ __forceinline__ void mm_many(const Frag<PA> (&a)[N], const Frag<PB> &b, floatx4 *const (&c)[N])
+{
+#pragma unroll
+    for (int sum = CUT - 1; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (sum - i >= 0 && sum - i < PB)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    *c[n] = SWAP ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.p[sum - i], a[n].p[i], *c[n], 0, 0, 0)
+                                 : __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n].p[i], b.p[sum - i], *c[n], 0, 0, 0);
 }
 
 template <int P>
@@ -133,6 +166,7 @@ struct DeltaMemory {
     float *states, *errors;          // tape: S before each chunk [DKP][DVP], E [L][DVP]
     float *d_states, *d_values;      // backward: gradient of the state after each chunk, Y [L][DVP]
     int chunks, dvp, key_units, value_units;
+    bool vec_o;                      // rows of o take four elements at a time
 };
 
 __device__ __forceinline__ int sequence_length(const DeltaArgs &a, int b)
@@ -410,253 +444,303 @@ __device__ __forceinline__ void loads_done_and_barrier()
     __syncthreads();
 }
 
-// A wave's columns of one chunk: eight consecutive tokens of a column for each pair of tiles, from a tensor [token, column] whose first token
-// counts (what does not count is read there instead: loads without branches between them).
+// A wave's column of one chunk, eight consecutive tokens for each pair of tiles, from a tensor [token, column] whose first token counts.  `at`
+// is the lane's offset (8 g token + its column, or column 0 past the last one); distances of tokens are uniform.  In a chunk that ends early, the
+// first token is read in place of those that do not count: loads without branches between them.
 template <class E, int LB>
-__device__ __forceinline__ void load_columns(const E *p, long long token, int col, int columns, int g, int count, float (&x)[LB][8])
+__device__ __forceinline__ void load_columns(const E *p, long long token, unsigned at, int g, int count, E (&u)[LB][8])
 {
-    p += col < columns ? col : 0;
-    E u[LB][8];
+    if (count >= 32 * LB) {
+#pragma unroll
+        for (int s = 0; s < LB; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[s][e] = (p + (32 * s + e) * token)[at];
+    } else {
+        p += (long long)at - 8 * g * token;
+#pragma unroll
+        for (int s = 0; s < LB; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[s][e] = p[32 * s + 8 * g + e < count ? (32 * s + 8 * g + e) * token : 0];
+    }
+}
+template <class E, int LB>
+__device__ __forceinline__ void columns_to_float(const E (&u)[LB][8], bool all_columns, bool column, int g, int count, float (&x)[LB][8])
+{
 #pragma unroll
     for (int s = 0; s < LB; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int t = 32 * s + 8 * g + e;
-            u[s][e] = p[(t < count ? t : 0) * token];
-        }
+        for (int e = 0; e < 8; ++e) x[s][e] = to_float(u[s][e]);
+    if (!all_columns || count < 32 * LB)
 #pragma unroll
-    for (int s = 0; s < LB; ++s)
+        for (int s = 0; s < LB; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = col < columns && 32 * s + 8 * g + e < count ? to_float(u[s][e]) : 0.0f;
+            for (int e = 0; e < 8; ++e) x[s][e] = column && 32 * s + 8 * g + e < count ? x[s][e] : 0.0f;
 }
 
-// Element r of tile t of a wave's state is row tile_index(t, 4 g + r), column col0 + 16 c + m.
-template <int NC, int DT>
-__device__ __forceinline__ void load_state(const float *p, int Dk, int Dv, int col0, int lane, floatx4 (&S)[NC][DT])
+// A wave's state: element r of tile t is row tile_index(t, 4 g + r), column `col`.
+template <int DT>
+__device__ __forceinline__ void load_state(const float *p, int Dk, int Dv, int col, int g, floatx4 (&S)[DT])
 {
-    const int m = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int t = 0; t < DT; ++t) S[c][t] = floatx4{0, 0, 0, 0};
+    for (int t = 0; t < DT; ++t) S[t] = floatx4{0, 0, 0, 0};
     if (!p) return;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int r = 0; r < 4; ++r) {
+            const int d = tile_index(t, 4 * g + r);
+            S[t][r] = p[d < Dk && col < Dv ? d * Dv + col : 0];
+        }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = tile_index(t, 4 * g + r), col = col0 + 16 * c + m;
-                S[c][t][r] = p[d < Dk && col < Dv ? d * Dv + col : 0];
-            }
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (tile_index(t, 4 * g + r) >= Dk || col0 + 16 * c + m >= Dv) S[c][t][r] = 0.0f;
+        for (int r = 0; r < 4; ++r)
+            if (tile_index(t, 4 * g + r) >= Dk || col >= Dv) S[t][r] = 0.0f;
 }
-template <int NC, int DT>
-__device__ __forceinline__ void store_state(float *p, int Dk, int Dv, int col0, int lane, const floatx4 (&S)[NC][DT])
+template <int DT>
+__device__ __forceinline__ void store_state(float *p, int Dk, int Dv, int col, int g, const floatx4 (&S)[DT])
 {
-    const int m = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int r = 0; r < 4; ++r) {
+            const int d = tile_index(t, 4 * g + r);
+            if (d < Dk && col < Dv) p[d * Dv + col] = S[t][r];
+        }
+}
+// Tiles of rows tile_index(t, 4 g + r) of a matrix of `stride` columns in the memory between the kernels; `at` = 8 g stride + column.
+template <int N>
+__device__ __forceinline__ void store_tiles(float *p, int stride, unsigned at, const floatx4 (&x)[N])
+{
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = tile_index(t, 4 * g + r), col = col0 + 16 * c + m;
-                if (d < Dk && col < Dv) p[(long long)d * Dv + col] = S[c][t][r];
-            }
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) (p + (32 * (t >> 1) + 4 * (t & 1) + r) * stride)[at] = x[t][r];
 }
 
-// A workgroup walks through the chunks of one head with 16 NC columns of its state a wave, which stay in the wave's registers.  The
-// chunk's blocks come to LDS in two halves, each on its way while the other one is computed with.
-template <class E, int KB, int NC, bool TAPE>
-__global__ __launch_bounds__(256) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+// Eight float32 values of a chunk's gates for tokens 8 g .. 8 g + 7.
+__device__ __forceinline__ void load_gates(const float *p, float (&x)[8])
+{
+    const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+}
+
+// LDS of a scan, in units: what a chunk needs first (FIRST) for two chunks, what its last products need (LAST) for two where that fits into 160,
+// else for one.
+template <int FIRST_, int LAST_>
+struct ScanLds {
+    static constexpr int FIRST = FIRST_, LAST = LAST_;
+    static constexpr bool DOUBLE = 2 * (FIRST + LAST) <= 160;
+    static constexpr int BYTES = (2 * FIRST + (DOUBLE ? 2 : 1) * LAST) * 1024;
+    static __device__ __forceinline__ unsigned char *first(unsigned char *lds, int parity) { return lds + parity * FIRST * 1024; }
+    static __device__ __forceinline__ unsigned char *last(unsigned char *lds, int parity) { return lds + (2 * FIRST + (DOUBLE ? parity * LAST : 0)) * 1024; }
+};
+template <class E, int KB>
+struct ForwardLds : ScanLds<DeltaUnits<E, KB>::KT + DeltaUnits<E, KB>::VALUE_FORWARD, DeltaUnits<E, KB>::QT - DeltaUnits<E, KB>::KT> {};
+
+constexpr int SCAN_THREADS = 512;
+
+// A workgroup walks through the chunks of one head with 16 columns of its state a wave, which stay in the wave's registers.  A chunk's blocks come
+// to LDS while the chunk before it is computed with; K', where two do not fit, while the chunk's first products are.  Blocks are read from
+// LDS one group ahead of their products, and a group has several accumulators, so that products follow at the rate of the matrix pipe.  Two waves
+// a SIMD (256 registers each, none of them accumulation registers, whose copies would cost as much as the splits): one splits while the other multiplies.
+template <class E, int KB, bool TAPE>
+__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
     typedef DeltaUnits<E, KB> U;
     constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PO = U::PO, PM = DELTA_PM;
-    constexpr int CUT_O = PO;
-    // LDS in units: K, Q | K' | gates, T, P
-    constexpr int A_UNITS = U::KT, KT_UNITS = U::QT - U::KT, B_UNITS = U::VALUE_FORWARD;
+    typedef ForwardLds<E, KB> Lds;               // K, Q, gates, T, P | K'
+    constexpr int A_UNITS = U::KT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    unsigned char *ldsA = lds, *ldsKT = lds + A_UNITS * 1024, *ldsB = ldsKT + KT_UNITS * 1024;
-    const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int m = lane & 15, g = lane >> 4;
-    const int block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);       // the blocks of a head, and heads that share keys, on one XCD
+    const int block = id % blocks_per_head, head = id / blocks_per_head;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
     const int len = sequence_length(a, b), n = (len + L - 1) / L;
     const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
     const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
-    const int col0 = (block * waves + wave) * 16 * NC;
+    const int col0 = (block * waves + wave) * 16, col = col0 + m;
+    const bool all_columns = a.Dv % 32 == 0;
 
-    floatx4 S[NC][DT];
-    load_state<NC, DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col0, lane, S);
+    floatx4 S[DT];
+    load_state<DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
     E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
+    const unsigned at_v = 8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0);
+    const unsigned at_tape = 8 * g * (unsigned)mem.dvp + col;
 
-    if (n > 0) units_to_lds(key + U::K * 1024, ldsA, A_UNITS, wave, waves, lane);
+    auto load_first = [&](int chunk, int parity) {
+        unsigned char *to = Lds::first(lds, parity);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, wave, waves, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, U::VALUE_FORWARD, wave, waves, lane);
+    };
+    auto load_last = [&](int chunk, int parity) {
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, wave, waves, lane);
+    };
+    E next[LB][8];
+    auto load_v = [&](int chunk) { load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next); };
+    if (n > 0) {
+        load_first(0, 0);
+        if (Lds::DOUBLE) load_last(0, 0);
+        load_v(0);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
     for (int chunk = 0; chunk < n; ++chunk) {
-        const int t0 = chunk * L;
-        loads_done_and_barrier();
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, ldsKT, KT_UNITS, wave, waves, lane);
-        units_to_lds(value + (long long)chunk * mem.value_units * 1024, ldsB, B_UNITS, wave, waves, lane);
-        float x[NC][LB][8];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = col0 + 16 * c + m;
-            load_columns<E, LB>(v + (long long)t0 * a.sv.token, a.sv.token, col, a.Dv, g, len - t0, x[c]);
-            if (TAPE && col < mem.dvp) {
-                float *to = mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp + col;
-#pragma unroll
-                for (int t = 0; t < DT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) to[tile_index(t, 4 * g + r) * mem.dvp] = S[c][t][r];
-            }
+        const int t0 = chunk * L, parity = chunk & 1;
+        const unsigned char *ldsA = Lds::first(lds, parity), *ldsB = ldsA + A_UNITS * 1024, *ldsKT = Lds::last(lds, parity);
+        const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
+        __syncthreads();
+        float x[LB][8];
+        columns_to_float<E, LB>(next, all_columns, col < a.Dv, g, len - t0, x);
+        const int after = chunk + 1 < n ? chunk + 1 : chunk;
+        if (!Lds::DOUBLE) load_last(chunk, parity);
+        if (chunk + 1 < n) {
+            load_first(after, parity ^ 1);
+            if (Lds::DOUBLE) load_last(after, parity ^ 1);
         }
-        Frag<PM> Sf[NC][KB];
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
+        load_v(after);
+        if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        // K S with tokens in rows, (Q S)' with tokens in columns: two tiles of tokens at a time
+        floatx4 KS[NT], QS[NT];
+        {
+            Frag<PM> Sf[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 float u[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = S[c][2 * kb + (e >> 2)][e & 3];
-                Sf[c][kb] = make_frag<PM>(u);
+                for (int e = 0; e < 8; ++e) u[e] = S[2 * kb + (e >> 2)][e & 3];
+                Sf[kb] = make_frag<PM>(u);
             }
-        // K S with tokens in rows, (Q S)' with tokens in columns
-        floatx4 KS[NC][NT], QS[NC][NT];
+            Frag<PI> kf[2][2], qf[2][2];
+            auto read = [&](int step, int to) {
+                const int i = step / KB * 2, kb = step % KB;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    kf[to][p] = load_frag<PI>(ldsA + (U::K + ((i + p) * KB + kb) * PI) * 1024, lane);
+                    qf[to][p] = load_frag<PI>(ldsA + (U::Q + ((i + p) * KB + kb) * PI) * 1024, lane);
+                }
+            };
+            read(0, 0);
+#pragma unroll
+            for (int step = 0; step < LB * KB; ++step) {
+                const int i = step / KB * 2, kb = step % KB, at = step & 1;
+                if (step + 1 < LB * KB) read(step + 1, at ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kb == 0) KS[i] = KS[i + 1] = QS[i] = QS[i + 1] = floatx4{0, 0, 0, 0};
+                floatx4 *ks[2] = {&KS[i], &KS[i + 1]}, *qs[2] = {&QS[i], &QS[i + 1]};
+                mm_many<3, false>(kf[at], Sf[kb], ks);
+                mm_many<PO, true>(qf[at], Sf[kb], qs);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+
+        // E = T (V - e^G K S): a pair of tiles of tokens at a time
+        floatx4 Ee[NT];
+        {
+            Frag<PM> R[LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float decay[8], u[8];
+                load_gates(gates->decay + 32 * s + 8 * g, decay);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[2 * s + (e >> 2)][e & 3], x[s][e]);
+                R[s] = make_frag<PM>(u);
+            }
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                Frag<PM> tf[LB][2];
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) tf[kb][p] = load_frag<PM>(ldsB + (U::T + U::lower(2 * s + p, kb) * PM) * 1024, lane);
+                Ee[2 * s] = Ee[2 * s + 1] = floatx4{0, 0, 0, 0};
+                floatx4 *to[2] = {&Ee[2 * s], &Ee[2 * s + 1]};
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb) mm_many<3, false>(tf[kb], R[kb], to);
+            }
+        }
+        if (TAPE && col0 < mem.dvp) store_tiles<NT>(mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Ee);
+        // U = beta E: for the outputs, and times e^(GL-G) for the state
+        Frag<PM> W[LB];
+        {
+            Frag<PO> Uf[LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float be[8], left[8], u[8], w[8];
+                load_gates(gates->beta + 32 * s + 8 * g, be);
+                load_gates(gates->left + 32 * s + 8 * g, left);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    u[e] = be[e] * Ee[2 * s + (e >> 2)][e & 3];
+                    w[e] = left[e] * u[e];
+                }
+                Uf[s] = make_frag<PO>(u);
+                W[s] = make_frag<PM>(w);
+            }
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                Frag<PO> pf[LB][2];
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) pf[kb][p] = load_frag<PO>(ldsB + (U::P + U::lower(2 * s + p, kb) * PO) * 1024, lane);
+#pragma unroll
+                for (int p = 0; p < 2; ++p) QS[2 * s + p] *= gates->decay[tile_index(2 * s + p, m)];
+                floatx4 *to[2] = {&QS[2 * s], &QS[2 * s + 1]};
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb) mm_many<PO, true>(pf[kb], Uf[kb], to);
+            }
+        }
+        // S <- e^GL S + K' (e^(GL-G) U): a pair of tiles of the state at a time
+        const float whole = gates->whole;
+        if (!Lds::DOUBLE) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+        }
+        {
+            Frag<PI> kf[2][2];
+            auto read = [&](int step, int to) {
+                const int t = step / LB * 2, kb = step % LB;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) kf[to][p] = load_frag<PI>(ldsKT + ((t + p) * LB + kb) * PI * 1024, lane);
+            };
+            read(0, 0);
+#pragma unroll
+            for (int step = 0; step < KB * LB; ++step) {
+                const int t = step / LB * 2, kb = step % LB, at = step & 1;
+                if (step + 1 < KB * LB) read(step + 1, at ^ 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
+                floatx4 *to[2] = {&S[t], &S[t + 1]};
+                mm_many<3, false>(kf[at], W[kb], to);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        // what the next chunk needs is there; the outputs are stored behind that wait and have the next chunk's time
+        if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
+        // token t0 + tile_index(i, m), columns col0 + 4 g ..
+        const int lane_token = 8 * (m >> 2) + (m & 3);
+        const unsigned at_o = lane_token * (unsigned)a.so.token + col0 + 4 * g;
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
+            const int tile_token = t0 + 32 * (i >> 1) + 4 * (i & 1);
+            E *to = o + tile_token * a.so.token;
+            const float u[4] = {a.scale * QS[i][0], a.scale * QS[i][1], a.scale * QS[i][2], a.scale * QS[i][3]};
+            if (mem.vec_o) {
+                if (tile_token + lane_token < a.T && col0 + 4 * g < a.Dv) store4(to + at_o, u);
+            } else {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) KS[c][i] = QS[c][i] = floatx4{0, 0, 0, 0};
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const Frag<PI> kf = load_frag<PI>(ldsA + (U::K + (i * KB + kb) * PI) * 1024, lane);
-                const Frag<PI> qf = load_frag<PI>(ldsA + (U::Q + (i * KB + kb) * PI) * 1024, lane);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    KS[c][i] = mm<3>(kf, Sf[c][kb], KS[c][i]);
-                    QS[c][i] = mm<CUT_O>(Sf[c][kb], qf, QS[c][i]);
-                }
-            }
-        }
-        loads_done_and_barrier();
-        if (chunk + 1 < n) units_to_lds(key + ((long long)(chunk + 1) * mem.key_units + U::K) * 1024, ldsA, A_UNITS, wave, waves, lane);
-
-        // E = T (V - e^G K S)
-        floatx4 Ee[NC][NT];
-        {
-            Frag<PM> R[NC][LB];
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                float decay[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) decay[e] = gates->decay[32 * s + 8 * g + e];
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    float u[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[c][2 * s + (e >> 2)][e & 3], x[c][s][e]);
-                    R[c][s] = make_frag<PM>(u);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                for (int c = 0; c < NC; ++c) Ee[c][i] = floatx4{0, 0, 0, 0};
-#pragma unroll
-                for (int kb = 0; kb <= i / 2; ++kb) {
-                    const Frag<PM> tf = load_frag<PM>(ldsB + (U::T + U::lower(i, kb) * PM) * 1024, lane);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) Ee[c][i] = mm<3>(tf, R[c][kb], Ee[c][i]);
-                }
-            }
-        }
-        if (TAPE) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int col = col0 + 16 * c + m;
-                if (col < mem.dvp) {
-                    float *to = mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp + col;
-#pragma unroll
-                    for (int i = 0; i < NT; ++i)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) to[tile_index(i, 4 * g + r) * mem.dvp] = Ee[c][i][r];
-                }
-            }
-        }
-        // U = beta E: for the outputs, and times e^(GL-G) for the state
-        Frag<PM> W[NC][LB];
-        {
-            Frag<PO> Uf[NC][LB];
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                float be[8], left[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) be[e] = gates->beta[32 * s + 8 * g + e], left[e] = gates->left[32 * s + 8 * g + e];
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    float u[8], w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        u[e] = be[e] * Ee[c][2 * s + (e >> 2)][e & 3];
-                        w[e] = left[e] * u[e];
-                    }
-                    Uf[c][s] = make_frag<PO>(u);
-                    W[c][s] = make_frag<PM>(w);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const float decay = gates->decay[tile_index(i, m)];
-#pragma unroll
-                for (int c = 0; c < NC; ++c) QS[c][i] *= decay;
-#pragma unroll
-                for (int kb = 0; kb <= i / 2; ++kb) {
-                    const Frag<PO> pf = load_frag<PO>(ldsB + (U::P + U::lower(i, kb) * PO) * 1024, lane);
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) QS[c][i] = mm<CUT_O>(Uf[c][kb], pf, QS[c][i]);
-                }
-                // token tile_index(i, m), columns col0 + 16 c + 4 g ..
-                const int t = t0 + tile_index(i, m);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int col = col0 + 16 * c + 4 * g;
-                    E *to = o + (long long)t * a.so.token + col;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (t < a.T && col + r < a.Dv) store_element(to + r, a.scale * QS[c][i][r]);
-                }
-            }
-        }
-        // S <- e^GL S + K' (e^(GL-G) U)
-        const float whole = gates->whole;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) {
-#pragma unroll
-            for (int c = 0; c < NC; ++c) S[c][t] *= whole;
-#pragma unroll
-            for (int kb = 0; kb < LB; ++kb) {
-                const Frag<PI> kf = load_frag<PI>(ldsKT + (t * LB + kb) * PI * 1024, lane);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) S[c][t] = mm<3>(kf, W[c][kb], S[c][t]);
+                for (int r = 0; r < 4; ++r)
+                    if (tile_token + lane_token < a.T && col0 + 4 * g + r < a.Dv) store_element(to + at_o + r, u[r]);
             }
         }
     }
     // past the sequence's end
-    for (int t = n * L + (lane >> 4); t < a.T; t += 4)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int col = col0 + 16 * c + m;
-            if (col < a.Dv) store_element(o + (long long)t * a.so.token + col, 0.0f);
-        }
-    if (a.final_state) store_state<NC, DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col0, lane, S);
+    for (int t = n * L + g; t < a.T; t += 4)
+        if (col < a.Dv) store_element(o + t * a.so.token + col, 0.0f);
+    if (a.final_state) store_state<DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
 }
 
 }  // namespace tfno
