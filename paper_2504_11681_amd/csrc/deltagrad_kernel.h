@@ -224,8 +224,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
     __shared__ __attribute__((aligned(1024))) unsigned char shared[PANEL > MATRICES ? PANEL : MATRICES];
     unsigned char *panelS = shared, *panelD = shared + PANEL / 2;    // 32 columns of S and dS' as operand blocks
     float *Mq = (float *)shared, *Mk = Mq + L * COL;                 // after the last of them
-    __shared__ double G[L];
-    __shared__ float beta[L], left[L], column_sums[NT][L], row_sums[L], token_g[L], token_beta[L], inner[NT];
+    __shared__ float hi[L], lo[L], beta[L], left[L], column_sums[NT][L], row_sums[L], token_g[L], token_beta[L], inner[NT];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
     const int chunk = blockIdx.x % mem.chunks, kh = blockIdx.x / mem.chunks;
@@ -281,7 +280,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
         const float *errors = mem.errors + at * L * mem.dvp, *d_values = mem.d_values + at * L * mem.dvp;
         const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + (long long)token * a.sdo.token + h * a.sdo.head);
         __syncthreads();
-        if (tid < L) G[tid] = mem.G[at * L + tid], beta[tid] = gates->beta[tid], left[tid] = gates->left[tid];
+        if (tid < L) hi[tid] = mem.logs[at * 2 * L + tid], lo[tid] = mem.logs[at * 2 * L + L + tid], beta[tid] = gates->beta[tid], left[tid] = gates->left[tid];
 
         floatx4 D[NT], C[NT], hq[DT], hy[DT], he[DT];
 #pragma unroll
@@ -340,7 +339,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = tile_index(i, 4 * g + r);
-                    const float M = col <= row ? expf((float)(G[row] - G[col])) : 0.0f, strict = col < row ? M : 0.0f;
+                    const float M = col <= row ? decay_between(hi[row], lo[row], hi[col], lo[col]) : 0.0f, strict = col < row ? M : 0.0f;
                     const float Dm = a.scale * M * D[j][r], Cm = strict * C[j][r];
                     const float x = qk[j][r] * Dm - kk[j][r] * Cm;
                     rows[r] = fmaf(x, be, rows[r]);

@@ -21,7 +21,7 @@ size_t forward_memory(const DeltaArgs &a, unsigned char *base, bool tape, DeltaM
     m->key = base + at, at += keys * m->key_units * 1024;
     m->value = base + at, at += values * m->value_units * 1024;
     if (tape) {
-        m->G = (double *)(base + at), at += pad(values * U::L * sizeof(double));
+        m->logs = (float *)(base + at), at += pad(values * 2 * U::L * sizeof(float));
         m->states = (float *)(base + at), at += values * U::DKP * m->dvp * sizeof(float);
         m->errors = (float *)(base + at), at += values * U::L * m->dvp * sizeof(float);
     }

@@ -162,7 +162,7 @@ struct DeltaGates {
 // Where the parts of a call's memory lie.
 struct DeltaMemory {
     unsigned char *key, *value;      // units of the key heads' and of the value heads' chunks, [b][head][chunk]
-    double *G;                       // [b][hv][chunk][L] running sums (tape)
+    float *logs;                     // tape: [b][hv][chunk][2][L] running sums of g in powers of two, as sums of two floats
     float *states, *errors;          // tape: S before each chunk [DKP][DVP], E [L][DVP]
     float *d_states, *d_values;      // backward: gradient of the state after each chunk, Y [L][DVP]
     int chunks, dvp, key_units, value_units;
@@ -231,151 +231,215 @@ __device__ __forceinline__ void store8(bf16 *p, int n, bool vec, const float (&x
     }
 }
 
+// Eight float32 values of LDS whose address is a multiple of 16.
+__device__ __forceinline__ void load_gates(const float *p, float (&x)[8])
+{
+    const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+}
+
 struct DeltaVec { bool q, k, d_o, dq, dk; };       // which tensors' rows may be read eight elements at a time
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// One workgroup for a chunk of a value head: L / 16 waves.  The inverse T of the unit lower triangular matrix is found by blocks of 16:
-// each diagonal block by substitution, the blocks below it from T_IJ = -T_II sum_{J<=M<I} N_IM T_MJ, one wave for a block column.
+// An operand block from LDS: eight elements of one row.
+template <int P>
+__device__ __forceinline__ Frag<P> row_frag(const float *p)
+{
+    float u[8];
+    load8(p, 8, true, u);
+    return make_frag<P>(u);
+}
+template <int P>
+__device__ __forceinline__ Frag<P> row_frag(const bf16 *p)
+{
+    static_assert(P == 1, "BF16 is one part");
+    Frag<P> f;
+    f.p[0] = *reinterpret_cast<const bf16x8 *>(p);
+    return f;
+}
+// The same of one column, rows `stride` apart.
+template <int P>
+__device__ __forceinline__ Frag<P> column_frag(const float *p, int stride)
+{
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = p[e * stride];
+    return make_frag<P>(u);
+}
+template <int P>
+__device__ __forceinline__ Frag<P> column_frag(const bf16 *p, int stride)
+{
+    static_assert(P == 1, "BF16 is one part");
+    uintx4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = p[2 * e * stride].bits | (unsigned)p[(2 * e + 1) * stride].bits << 16;
+    Frag<P> f;
+    f.p[0] = __builtin_bit_cast(bf16x8, w);
+    return f;
+}
+// Eight elements of a row of memory to LDS, zeros past the n-th.
+template <class E>
+__device__ __forceinline__ void row_to_lds(const E *p, int n, bool vec, E *to)
+{
+    if (vec && n >= 8) {
+        constexpr int W = 8 * sizeof(E) / 16;
+#pragma unroll
+        for (int w = 0; w < W; ++w) reinterpret_cast<uint4 *>(to)[w] = reinterpret_cast<const uint4 *>(p)[w];
+    } else {
+        float u[8];
+        load8(p, n, false, u);
+        store8(to, 8, true, u);
+    }
+}
+
+// exp(G_i - G_j) from running sums in powers of two that are sums of two floats: exact differences also after a reset.
+__device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return __builtin_amdgcn_exp2f((hi_i - hi_j) + (lo_i - lo_j)); }
+
+// One workgroup for a chunk of a value head: L / 16 waves.  Bound by its instructions and barriers (what it moves, 54 KiB for heads of 64, is the
+// smaller part), so nothing passes through LDS that need not: a wave takes the pairs of tokens whose column is in its own tile, and
+// P comes out as an operand block as it is.  The inverse T of the unit lower triangular matrix I + N is found by blocks of 16: each diagonal
+// block by substitution, a column after the other, the blocks below it from T_IJ = -T_II sum_{J<=M<I} N_IM T_MJ, one wave for a block column.
 // Substitution and not the product (I - N)(I + N^2)(I + N^4)..: its powers grow like binomials where keys are alike, and cancel.
 template <class E, int KB, bool TAPE>
 __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
 {
     typedef DeltaUnits<E, KB> U;
-    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PO = U::PO;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PO = U::PO, PM = DELTA_PM;
     constexpr int ROW = DKP + 16 / sizeof(E), COL = L + 4;
-    __shared__ __attribute__((aligned(16))) E Ks[L * ROW];
-    __shared__ __attribute__((aligned(16))) E Qs[L * ROW];
-    __shared__ __attribute__((aligned(16))) float N[L * COL];
-    __shared__ __attribute__((aligned(16))) float X[L * COL];      // P, then T
-    __shared__ double G[L];
-    __shared__ float beta[L];
+    constexpr int ROWS_BYTES = 2 * L * ROW * sizeof(E), MATRIX_BYTES = L * COL * 4;
+    __shared__ __attribute__((aligned(16))) unsigned char shared[ROWS_BYTES > MATRIX_BYTES ? ROWS_BYTES : MATRIX_BYTES];
+    __shared__ __attribute__((aligned(16))) float N[L * COL];      // its columns: N[j * COL + i] is row i, column j
+    __shared__ float hi[L], lo[L], beta[L];
+    E *Ks = (E *)shared, *Qs = Ks + L * ROW;
+    float *X = (float *)shared;                                    // T, once K and Q are done with
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
-    const int chunk = blockIdx.x % mem.chunks, head = blockIdx.x / mem.chunks;
-    const int b = head / a.Hv, h = head - b * a.Hv, group = a.Hv / a.Hk, hk = h / group;
-    const bool first = h == hk * group;                             // this workgroup writes the key head's blocks too
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int group = a.Hv / a.Hk, member = id % group, at = id / group;   // value heads that share keys are neighbours
+    const int chunk = at % mem.chunks, kh = at / mem.chunks, b = kh / a.Hk, hk = kh - b * a.Hk, h = hk * group + member;
+    const long long head = (long long)b * a.Hv + h;
+    const bool first = member == 0;                                 // this workgroup writes the key head's blocks too
     const int len = sequence_length(a, b), t0 = chunk * L;
     if (t0 >= len) return;
-    unsigned char *key = mem.key + ((long long)(b * a.Hk + hk) * mem.chunks + chunk) * mem.key_units * 1024;
-    unsigned char *value = mem.value + ((long long)head * mem.chunks + chunk) * mem.value_units * 1024;
+    unsigned char *key = mem.key + ((long long)kh * mem.chunks + chunk) * mem.key_units * 1024;
+    unsigned char *value = mem.value + (head * mem.chunks + chunk) * mem.value_units * 1024;
 
-    for (int x = tid; x < L * DKP / 8; x += 64 * NT) {
-        const int row = x / (DKP / 8), d = x % (DKP / 8) * 8, n = t0 + row < len ? a.Dk - d : 0;
-        float u[8];
-        load8((const E *)a.k + (b * a.sk.batch + (long long)(t0 + row) * a.sk.token + hk * a.sk.head + d), n, vec.k, u);
-        store8(Ks + row * ROW + d, 8, true, u);
-        load8((const E *)a.q + (b * a.sq.batch + (long long)(t0 + row) * a.sq.token + hk * a.sq.head + d), n, vec.q, u);
-        store8(Qs + row * ROW + d, 8, true, u);
+    const E *k = (const E *)a.k + (b * a.sk.batch + (long long)t0 * a.sk.token + hk * a.sk.head);
+    const E *q = (const E *)a.q + (b * a.sq.batch + (long long)t0 * a.sq.token + hk * a.sq.head);
+#pragma unroll
+    for (int x = 0; x < L * DKP / 8 / (64 * NT); ++x) {
+        const int s = tid + x * 64 * NT, row = s / (DKP / 8), d = s % (DKP / 8) * 8, n = t0 + row < len ? a.Dk - d : 0;
+        row_to_lds(k + row * a.sk.token + d, n, vec.k, Ks + row * ROW + d);
+        row_to_lds(q + row * a.sq.token + d, n, vec.q, Qs + row * ROW + d);
     }
     if (wave == 0) {
         // running sums of g in 64 bits; what is below any exponent counts as -1e5 each, so that differences past a reset stay exact
         double s = 0.0;
         const bool live = lane < L && t0 + lane < len;
-        if (live && a.g) {
-            const float v = a.g[b * a.sg.batch + (long long)(t0 + lane) * a.sg.token + h * a.sg.head];
-            s = v < -1e5f ? -1e5 : (double)v;
+        float be = 0.0f;
+        if (live) {
+            be = a.beta[b * a.sbeta.batch + (long long)(t0 + lane) * a.sbeta.token + h * a.sbeta.head];
+            if (a.g) {
+                const float v = a.g[b * a.sg.batch + (long long)(t0 + lane) * a.sg.token + h * a.sg.head];
+                s = v < -1e5f ? -1e5 : (double)v;
+            }
         }
-        for (int step = 1; step < 64; step <<= 1) {
+        for (int step = 1; step < L; step <<= 1) {
             const double u = __shfl_up(s, step, 64);
             if (lane >= step) s += u;
         }
+        s *= 1.4426950408889634;
         const double all = __shfl(s, L - 1, 64);
         if (lane < L) {
-            const float be = live ? a.beta[b * a.sbeta.batch + (long long)(t0 + lane) * a.sbeta.token + h * a.sbeta.head] : 0.0f;
-            G[lane] = s;
+            const float h0 = (float)s, l0 = (float)(s - (double)h0);
+            hi[lane] = h0, lo[lane] = l0;
             beta[lane] = be;
             DeltaGates<L> *gates = (DeltaGates<L> *)value;
-            gates->decay[lane] = expf((float)s);
+            gates->decay[lane] = __builtin_amdgcn_exp2f((float)s);
             gates->beta[lane] = be;
-            gates->left[lane] = expf((float)(all - s));
-            if (lane == 0) gates->whole = expf((float)all);
-            if (TAPE) mem.G[((long long)head * mem.chunks + chunk) * L + lane] = s;
+            gates->left[lane] = __builtin_amdgcn_exp2f((float)(all - s));
+            if (lane == 0) gates->whole = __builtin_amdgcn_exp2f((float)all);
+            if (TAPE) {
+                float *logs = mem.logs + (head * mem.chunks + chunk) * 2 * L;
+                logs[lane] = h0, logs[L + lane] = l0;
+            }
         }
     }
     __syncthreads();
 
-    // N = A diag(beta) and P; a wave takes a tile of rows
     {
-        const int i = wave;
-        floatx4 kk[NT], qk[NT];
+        const int w = wave, own = tile_index(w, m);                 // the lane's token
+        floatx4 kk[NT], qk[NT], kq[NT];                             // k_row.k_own, q_row.k_own and k_row.q_own
 #pragma unroll
-        for (int j = 0; j < NT; ++j) kk[j] = qk[j] = floatx4{0, 0, 0, 0};
+        for (int i = 0; i < NT; ++i) kk[i] = qk[i] = kq[i] = floatx4{0, 0, 0, 0};
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            float u[8];
-            load8(Ks + tile_index(i, m) * ROW + 32 * kb + 8 * g, 8, true, u);
-            const Frag<PI> kf = make_frag<PI>(u);
-            load8(Qs + tile_index(i, m) * ROW + 32 * kb + 8 * g, 8, true, u);
-            const Frag<PI> qf = make_frag<PI>(u);
+            const Frag<PI> kf = row_frag<PI>(Ks + own * ROW + 32 * kb + 8 * g), qf = row_frag<PI>(Qs + own * ROW + 32 * kb + 8 * g);
             if (first) {
-                store_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane, kf);
-                store_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane, qf);
+                store_frag<PI>(key + (U::K + (w * KB + kb) * PI) * 1024, lane, kf);
+                store_frag<PI>(key + (U::Q + (w * KB + kb) * PI) * 1024, lane, qf);
             }
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (j <= (i | 1)) {
-                    load8(Ks + tile_index(j, m) * ROW + 32 * kb + 8 * g, 8, true, u);
-                    const Frag<PI> other = make_frag<PI>(u);
-                    kk[j] = mm<3>(kf, other, kk[j]);
-                    qk[j] = mm<3>(qf, other, qk[j]);
-                }
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-            if (j <= (i | 1)) {
-                const int col = tile_index(j, m);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = tile_index(i, 4 * g + r);
-                    const float decay = col <= row ? expf((float)(G[row] - G[col])) : 0.0f;
-                    N[row * COL + col] = col < row ? decay * kk[j][r] * beta[col] : 0.0f;
-                    X[row * COL + col] = col <= row ? decay * qk[j][r] : 0.0f;
-                }
-            }
-        if (first) {       // K' and Q': tiles of Dk rows, blocks of 32 tokens
-            for (int x = wave; x < DT * LB; x += NT) {
-                const int t = x / LB, kb = x % LB, d = tile_index(t, m);
-                float u[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = to_float(Ks[(32 * kb + 8 * g + e) * ROW + d]);
-                store_frag<PI>(key + (U::KT + x * PI) * 1024, lane, make_frag<PI>(u));
-                if (TAPE) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[e] = to_float(Qs[(32 * kb + 8 * g + e) * ROW + d]);
-                    store_frag<PI>(key + (U::QT + x * PI) * 1024, lane, make_frag<PI>(u));
-                }
+            for (int i = 0; i < NT; ++i) {
+                const int at = tile_index(i, m) * ROW + 32 * kb + 8 * g;
+                const Frag<PI> other = row_frag<PI>(Ks + at);
+                if (i >= (w & ~1)) kk[i] = mm<3>(other, kf, kk[i]);
+                if (i <= (w | 1)) kq[i] = mm<3>(other, qf, kq[i]);
+                if (TAPE && i >= (w & ~1)) qk[i] = mm<3>(row_frag<PI>(Qs + at), kf, qk[i]);
             }
         }
-    }
-    __syncthreads();
-    {
-        const int i = wave, row = tile_index(i, m);
-        for (int kb = 0; kb < LB; ++kb) {
-            float u[8];
-            if (kb <= i / 2) {
+        const float hi_own = hi[own], lo_own = lo[own], beta_own = beta[own];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = X[row * COL + 32 * kb + 8 * g + e];
-                store_frag<PO>(value + (U::P + U::lower(i, kb) * PO) * 1024, lane, make_frag<PO>(u));
+        for (int s = 0; s < LB; ++s) {
+            float h8[8], l8[8], u[8];
+            load_gates(hi + 32 * s + 8 * g, h8);
+            load_gates(lo + 32 * s + 8 * g, l8);
+            if (s >= w / 2) {           // the lane's token is the column: N, and with a tape P'
+                float n[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int row = 32 * s + 8 * g + e;
+                    const float decay = decay_between(h8[e], l8[e], hi_own, lo_own);
+                    n[e] = own < row ? decay * kk[2 * s + (e >> 2)][e & 3] * beta_own : 0.0f;
+                    u[e] = own <= row ? decay * qk[2 * s + (e >> 2)][e & 3] : 0.0f;
+                }
+                store8(N + own * COL + 32 * s + 8 * g, 8, true, n);
+                if (TAPE) store_frag<PM>(value + (U::PT + U::upper(w, s) * PM) * 1024, lane, make_frag<PM>(u));
             }
-            if (TAPE && kb >= i / 2) {
+            if (s <= w / 2) {           // the lane's token is the row: P
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = X[(32 * kb + 8 * g + e) * COL + row];
-                store_frag<DELTA_PM>(value + (U::PT + U::upper(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
+                for (int e = 0; e < 8; ++e)
+                    u[e] = 32 * s + 8 * g + e <= own ? decay_between(hi_own, lo_own, h8[e], l8[e]) * kq[2 * s + (e >> 2)][e & 3] : 0.0f;
+                store_frag<PO>(value + (U::P + U::lower(w, s) * PO) * 1024, lane, make_frag<PO>(u));
             }
         }
+        if (first)         // K' and Q': tiles of Dk rows, blocks of 32 tokens
+#pragma unroll
+            for (int x = 0; x < DT * LB / NT; ++x) {
+                const int y = w + x * NT, t = y / LB, kb = y % LB, from = (32 * kb + 8 * g) * ROW + tile_index(t, m);
+                store_frag<PI>(key + (U::KT + y * PI) * 1024, lane, column_frag<PI>(Ks + from, ROW));
+                if (TAPE) store_frag<PI>(key + (U::QT + y * PI) * 1024, lane, column_frag<PI>(Qs + from, ROW));
+            }
     }
     __syncthreads();
 
-    // the diagonal block of a wave: lane n has its column n
+    // the diagonal block of a wave: lane m has its column m, and takes row after row off the ones below it
     const int J = wave;
+    floatx4 col[NT];
     {
         float x[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float s = i == m ? 1.0f : 0.0f;
+        for (int i = 0; i < 16; ++i) x[i] = i == m ? 1.0f : 0.0f;
 #pragma unroll
-            for (int j = 0; j < i; ++j) s = fmaf(-N[(16 * J + i) * COL + 16 * J + j], x[j], s);
-            x[i] = s;
+        for (int j = 0; j < 15; ++j) {
+            float n[16];
+#pragma unroll
+            for (int i = (j + 1) & ~3; i < 16; i += 4) {
+                const float4 u = *reinterpret_cast<const float4 *>(N + (16 * J + j) * COL + 16 * J + i);
+                n[i] = u.x, n[i + 1] = u.y, n[i + 2] = u.z, n[i + 3] = u.w;
+            }
+#pragma unroll
+            for (int i = j + 1; i < 16; ++i) x[i] = fmaf(-n[i], x[j], x[i]);
         }
         if (g == 0) {
 #pragma unroll
@@ -384,47 +448,37 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
 #pragma unroll
             for (int i = 0; i < 16; ++i) X[(16 * (J - 1) + i) * COL + 16 * J + m] = 0.0f;     // right of the pair's first diagonal block
         }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) col[0][r] = g == 0 ? x[r] : g == 1 ? x[4 + r] : g == 2 ? x[8 + r] : x[12 + r];
     }
     __syncthreads();
-    {
-        floatx4 col[NT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) col[0][r] = X[(16 * J + 4 * g + r) * COL + 16 * J + m];
+    for (int step = 1; step < NT; ++step) {
+        const int I = J + step;
+        if (I >= NT) break;
+        floatx4 sum = {0, 0, 0, 0}, out = {0, 0, 0, 0};
 #pragma unroll
-        for (int step = 1; step < NT; ++step) {
-            const int I = J + step;
-            if (I >= NT) break;
-            floatx4 sum = {0, 0, 0, 0}, out = {0, 0, 0, 0};
-#pragma unroll
-            for (int M = 0; M < step; ++M)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(N[(16 * I + m) * COL + 16 * (J + M) + 4 * g + r], col[M][r], sum, 0, 0, 0);
+        for (int M = 0; M < step; ++M)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                out = __builtin_amdgcn_mfma_f32_16x16x4f32(X[(16 * I + m) * COL + 16 * I + 4 * g + r], sum[r], out, 0, 0, 0);
+                sum = __builtin_amdgcn_mfma_f32_16x16x4f32(N[(16 * (J + M) + 4 * g + r) * COL + 16 * I + m], col[M][r], sum, 0, 0, 0);
+        const float4 diagonal = *reinterpret_cast<const float4 *>(X + (16 * I + m) * COL + 16 * I + 4 * g);
+        const float d[4] = {diagonal.x, diagonal.y, diagonal.z, diagonal.w};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                col[step][r] = -out[r];
-                X[(16 * I + 4 * g + r) * COL + 16 * J + m] = -out[r];
-            }
+        for (int r = 0; r < 4; ++r) out = __builtin_amdgcn_mfma_f32_16x16x4f32(d[r], sum[r], out, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            col[step][r] = -out[r];
+            X[(16 * I + 4 * g + r) * COL + 16 * J + m] = -out[r];
         }
     }
     __syncthreads();
     {
         const int i = wave, row = tile_index(i, m);
+#pragma unroll
         for (int kb = 0; kb < LB; ++kb) {
-            float u[8];
-            if (kb <= i / 2) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = X[row * COL + 32 * kb + 8 * g + e];
-                store_frag<DELTA_PM>(value + (U::T + U::lower(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
-            }
-            if (TAPE && kb >= i / 2) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = X[(32 * kb + 8 * g + e) * COL + row];
-                store_frag<DELTA_PM>(value + (U::TT + U::upper(i, kb) * DELTA_PM) * 1024, lane, make_frag<DELTA_PM>(u));
-            }
+            if (kb <= i / 2) store_frag<PM>(value + (U::T + U::lower(i, kb) * PM) * 1024, lane, row_frag<PM>(X + row * COL + 32 * kb + 8 * g));
+            if (TAPE && kb >= i / 2) store_frag<PM>(value + (U::TT + U::upper(i, kb) * PM) * 1024, lane, column_frag<PM>(X + (32 * kb + 8 * g) * COL + row, COL));
         }
     }
 }
@@ -516,13 +570,6 @@ __device__ __forceinline__ void store_tiles(float *p, int stride, unsigned at, c
     for (int t = 0; t < N; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) (p + (32 * (t >> 1) + 4 * (t & 1) + r) * stride)[at] = x[t][r];
-}
-
-// Eight float32 values of a chunk's gates for tokens 8 g .. 8 g + 7.
-__device__ __forceinline__ void load_gates(const float *p, float (&x)[8])
-{
-    const float4 u = reinterpret_cast<const float4 *>(p)[0], v = reinterpret_cast<const float4 *>(p)[1];
-    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
 }
 
 // LDS of a scan, in units: what a chunk needs first (FIRST) for two chunks, what its last products need (LAST) for two where that fits into 160,
