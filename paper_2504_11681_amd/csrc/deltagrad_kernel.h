@@ -46,8 +46,8 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     load_state<DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + h * a.sdo.head);
     E *dv = (E *)a.dv + (b * a.sdv.batch + h * a.sdv.head);
-    const unsigned at_do = 8 * g * (unsigned)a.sdo.token + (col < a.Dv ? col : 0);
-    const unsigned at_dv = 8 * g * (unsigned)a.sdv.token + col, at_tape = 8 * g * (unsigned)mem.dvp + col;
+    const unsigned at_do = (8 * g * (unsigned)a.sdo.token + (col < a.Dv ? col : 0)) * sizeof(E);
+    const unsigned at_dv = (8 * g * (unsigned)a.sdv.token + col) * sizeof(E), at_tape = (8 * g * (unsigned)mem.dvp + col) * 4;
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
@@ -74,8 +74,12 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                             *ldsKT = Lds::last(lds, parity);
         const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsG;
         __syncthreads();
+        mask_columns<E, LB>(next, all_columns, col < a.Dv, g, len - t0);
         float x[LB][8];
-        columns_to_float<E, LB>(next, all_columns, col < a.Dv, g, len - t0, x);
+#pragma unroll
+        for (int s = 0; s < LB; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = to_float(next[s][e]);
         const int before = chunk > 0 ? chunk - 1 : 0;
         if (!Lds::DOUBLE) load_last(chunk, parity);
         if (chunk > 0) {
@@ -100,7 +104,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 PO_[2 * s] = PO_[2 * s + 1] = floatx4{0, 0, 0, 0};
                 floatx4 *to[2] = {&PO_[2 * s], &PO_[2 * s + 1]};
 #pragma unroll
-                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(pf[kb], Of[kb], to);
+                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(pf[kb], Of[kb], to, NoWeave());
             }
             Frag<PM> Sf[KB];
 #pragma unroll
@@ -124,7 +128,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 __builtin_amdgcn_sched_barrier(0);
                 if (kb == 0) KS[i] = KS[i + 1] = floatx4{0, 0, 0, 0};
                 floatx4 *to[2] = {&KS[i], &KS[i + 1]};
-                mm_many<3, false>(kf[at], Sf[kb], to);
+                mm_many<3, false>(kf[at], Sf[kb], to, NoWeave());
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -152,7 +156,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 Y[2 * s] = Y[2 * s + 1] = floatx4{0, 0, 0, 0};
                 floatx4 *to[2] = {&Y[2 * s], &Y[2 * s + 1]};
 #pragma unroll
-                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(tf[kb], R[kb], to);
+                for (int kb = s; kb < LB; ++kb) mm_many<3, false>(tf[kb], R[kb], to, NoWeave());
             }
         }
         Frag<PM> Wo[LB], Wy[LB];
@@ -191,8 +195,8 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 __builtin_amdgcn_sched_barrier(0);
                 if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
                 floatx4 *to[2] = {&S[t], &S[t + 1]};
-                mm_many<3, false>(kf[at], Wy[kb], to);
-                mm_many<3, false>(qf[at], Wo[kb], to);
+                mm_many<3, false>(kf[at], Wy[kb], to, NoWeave());
+                mm_many<3, false>(qf[at], Wo[kb], to, NoWeave());
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int row = t0 + 32 * (i >> 1) + 4 * (i & 1) + r;
-                    if (col < a.Dv && (whole_chunk || row + 8 * g < a.T)) store_element(dv + row * a.sdv.token + at_dv, Y[i][r]);
+                    if (col < a.Dv && (whole_chunk || row + 8 * g < a.T)) store_element(behind(dv + row * a.sdv.token, at_dv), Y[i][r]);
                 }
         }
     }
@@ -264,12 +268,11 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
         kf[kb] = load_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane);
         qf[kb] = load_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane);
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-            if (j <= (i | 1)) {
-                const Frag<PI> other = load_frag<PI>(key + (U::K + (j * KB + kb) * PI) * 1024, lane);
-                kk[j] = mm<3>(kf[kb], other, kk[j]);
-                qk[j] = mm<3>(qf[kb], other, qk[j]);
-            }
+        for (int j = 0; j < NT; ++j) {            // all tiles, the unused ones too: no branches between the products
+            const Frag<PI> other = load_frag<PI>(key + (U::K + (j * KB + kb) * PI) * 1024, lane);
+            kk[j] = mm<3>(kf[kb], other, kk[j]);
+            qk[j] = mm<3>(qf[kb], other, qk[j]);
+        }
     }
 
     for (int member = 0; member < group; ++member) {
@@ -308,14 +311,13 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
             const Frag<PM> yf = make_frag<PM>(u);
             Frag<PM> ef{};
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
-                if (j <= (i | 1)) {
-                    load8(errors + tile_index(j, m) * mem.dvp + c0, 8, true, u);
-                    const Frag<PM> f = make_frag<PM>(u);
-                    D[j] = mm<3>(of, f, D[j]);
-                    C[j] = mm<3>(yf, f, C[j]);
-                    if (j == i) ef = f;
-                }
+            for (int j = 0; j < NT; ++j) {
+                load8(errors + tile_index(j, m) * mem.dvp + c0, 8, true, u);
+                const Frag<PM> f = make_frag<PM>(u);
+                D[j] = mm<3>(of, f, D[j]);
+                C[j] = mm<3>(yf, f, C[j]);
+                if (j == i) ef = f;
+            }
             __syncthreads();
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
@@ -436,8 +438,8 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
         for (int t = 0; t < DT; ++t) {
             const Frag<PI> kt = load_frag<PI>(key + (U::KT + (t * LB + kb) * PI) * 1024, lane);
             acck[t] = mm<3>(kt, sym, acck[t]);
-            if (kb <= i / 2) accq[t] = mm<3>(kt, lowq, accq[t]);
-            if (kb >= i / 2) acck[t] = mm<3>(load_frag<PI>(key + (U::QT + (t * LB + kb) * PI) * 1024, lane), highq, acck[t]);
+            accq[t] = mm<3>(kt, lowq, accq[t]);           // zeros where the block lies above the diagonal
+            acck[t] = mm<3>(load_frag<PI>(key + (U::QT + (t * LB + kb) * PI) * 1024, lane), highq, acck[t]);
         }
     }
     if (token < a.T)

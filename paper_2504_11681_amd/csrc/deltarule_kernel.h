@@ -31,8 +31,12 @@ namespace tfno {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
+// An operand block: a lane's eight values in P parts of BF16 each.
 template <int P>
-struct Frag { bf16x8 p[P]; };
+struct Frag {
+    uintx4 w[P];
+    __device__ __forceinline__ bf16x8 part(int i) const { return __builtin_bit_cast(bf16x8, w[i]); }
+};
 
 // x minus the low (high) one of the two BF16 values in w: a dot product of pairs with (-1, 0) resp. (0, -1), exact, one instruction instead of a mask
 // and a subtraction.  The constants are held in registers behind the compiler's back: as an inline constant -1.0 means the high half alone.
@@ -51,23 +55,24 @@ __device__ __forceinline__ float minus_high(unsigned w, float x)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, c), x, false);
 }
 
+// Values 4 e .. 4 e + 3: two pairs in step, since a dot product's result is not there for the next instruction.
+template <int P>
+__device__ __forceinline__ void set_four(Frag<P> &f, int e, const float (&x)[4])
+{
+    float r[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const unsigned u = pack_bf16(r[0], r[1]), v = pack_bf16(r[2], r[3]);
+        if (p + 1 < P) r[0] = minus_low(u, r[0]), r[1] = minus_high(u, r[1]), r[2] = minus_low(v, r[2]), r[3] = minus_high(v, r[3]);
+        f.w[p][2 * e] = u, f.w[p][2 * e + 1] = v;
+    }
+}
 template <int P>
 __device__ __forceinline__ Frag<P> make_frag(const float (&x)[8])
 {
     Frag<P> f;
-    float r[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = x[e];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        uintx4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            w[e] = pack_bf16(r[2 * e], r[2 * e + 1]);
-            if (p + 1 < P) r[2 * e] = minus_low(w[e], r[2 * e]), r[2 * e + 1] = minus_high(w[e], r[2 * e + 1]);
-        }
-        f.p[p] = __builtin_bit_cast(bf16x8, w);
-    }
+    set_four<P>(f, 0, {x[0], x[1], x[2], x[3]});
+    set_four<P>(f, 1, {x[4], x[5], x[6], x[7]});
     return f;
 }
 
@@ -79,14 +84,40 @@ __device__ __forceinline__ floatx4 mm(const Frag<PA> &a, const Frag<PB> &b, floa
     for (int sum = CUT - 1; sum >= 0; --sum)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
-            if (sum - i >= 0 && sum - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[sum - i], c, 0, 0, 0);
+            if (sum - i >= 0 && sum - i < PB) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.part(i), b.part(sum - i), c, 0, 0, 0);
     return c;
 }
 
-// The same for N accumulators that do not depend on each other, so that their products follow at the rate of the matrix pipe and not at its latency:
-// c[n] + A[n] B, or with SWAP c[n] + B A[n].
-template <int CUT, bool SWAP, int N, int PA, int PB>
-__device__ __forceinline__ void mm_many(const Frag<PA> (&a)[N], const Frag<PB> &b, floatx4 *const (&c)[N])
+// Work that is spread over the matrix instructions of a region: piece(k) after every EVERY of them, in exactly that order.  A wave issues in order
+// and a matrix instruction runs for 16 cycles, so what stands between two of them costs nothing until it fills those.
+template <int EVERY, int PIECES, class F>
+struct Weave {
+    F piece;
+    int count = 0;
+    __device__ __forceinline__ explicit Weave(F f) : piece(f) {}
+    __device__ __forceinline__ void step()
+    {
+        if (++count % EVERY == 0 && count / EVERY <= PIECES) {
+            __builtin_amdgcn_sched_barrier(0);
+            piece(count / EVERY - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    __device__ __forceinline__ void rest()
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            if (k >= count / EVERY) piece(k);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+};
+template <int EVERY, int PIECES, class F>
+__device__ __forceinline__ Weave<EVERY, PIECES, F> weave(F f) { return Weave<EVERY, PIECES, F>(f); }
+struct NoWeave { __device__ __forceinline__ void step() {} };
+
+// c[n] + A[n] B (with SWAP c[n] + B A[n]) for N accumulators that do not depend on each other.
+template <int CUT, bool SWAP, int N, int PA, int PB, class W>
+__device__ __forceinline__ void mm_many(const Frag<PA> (&a)[N], const Frag<PB> &b, floatx4 *const (&c)[N], W &&between)
 {
 #pragma unroll
     for (int sum = CUT - 1; sum >= 0; --sum)
@@ -94,9 +125,28 @@ __device__ __forceinline__ void mm_many(const Frag<PA> (&a)[N], const Frag<PB> &
         for (int i = 0; i < PA; ++i)
             if (sum - i >= 0 && sum - i < PB)
 #pragma unroll
-                for (int n = 0; n < N; ++n)
-                    *c[n] = SWAP ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.p[sum - i], a[n].p[i], *c[n], 0, 0, 0)
-                                 : __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n].p[i], b.p[sum - i], *c[n], 0, 0, 0);
+                for (int n = 0; n < N; ++n) {
+                    *c[n] = SWAP ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part(sum - i), a[n].part(i), *c[n], 0, 0, 0)
+                                 : __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n].part(i), b.part(sum - i), *c[n], 0, 0, 0);
+                    between.step();
+                }
+}
+// Matrix instructions of a product of PA and PB parts.
+constexpr int products(int PA, int PB, int CUT)
+{
+    int n = 0;
+    for (int i = 0; i < PA; ++i)
+        for (int j = 0; j < PB; ++j) n += i + j < CUT;
+    return n;
+}
+constexpr int at_least_1(int n) { return n > 0 ? n : 1; }
+__device__ __forceinline__ void region_end() { __builtin_amdgcn_sched_barrier(0); }
+// Values that are wanted here and not where the compiler would rather compute them, behind the branches that follow.
+template <int P>
+__device__ __forceinline__ void hold(Frag<P> &f)
+{
+#pragma unroll
+    for (int p = 0; p < P; ++p) asm volatile("" : "+v"(f.w[p]));
 }
 
 template <int P>
@@ -104,14 +154,14 @@ __device__ __forceinline__ Frag<P> load_frag(const unsigned char *unit, int lane
 {
     Frag<P> f;
 #pragma unroll
-    for (int p = 0; p < P; ++p) f.p[p] = *reinterpret_cast<const bf16x8 *>(unit + p * 1024 + lane * 16);
+    for (int p = 0; p < P; ++p) f.w[p] = *reinterpret_cast<const uintx4 *>(unit + p * 1024 + lane * 16);
     return f;
 }
 template <int P>
 __device__ __forceinline__ void store_frag(unsigned char *unit, int lane, const Frag<P> &f)
 {
 #pragma unroll
-    for (int p = 0; p < P; ++p) *reinterpret_cast<bf16x8 *>(unit + p * 1024 + lane * 16) = f.p[p];
+    for (int p = 0; p < P; ++p) *reinterpret_cast<uintx4 *>(unit + p * 1024 + lane * 16) = f.w[p];
 }
 // The value that the parts of element e add up to.
 template <int P>
@@ -119,7 +169,7 @@ __device__ __forceinline__ float frag_value(const Frag<P> &f, int e)
 {
     float v = 0.0f;
 #pragma unroll
-    for (int p = P - 1; p >= 0; --p) v += (float)f.p[p][e];
+    for (int p = P - 1; p >= 0; --p) v += __uint_as_float(e & 1 ? f.w[p][e >> 1] & 0xffff0000u : f.w[p][e >> 1] << 16);
     return v;
 }
 
@@ -254,7 +304,7 @@ __device__ __forceinline__ Frag<P> row_frag(const bf16 *p)
 {
     static_assert(P == 1, "BF16 is one part");
     Frag<P> f;
-    f.p[0] = *reinterpret_cast<const bf16x8 *>(p);
+    f.w[0] = *reinterpret_cast<const uintx4 *>(p);
     return f;
 }
 // The same of one column, rows `stride` apart.
@@ -270,11 +320,9 @@ template <int P>
 __device__ __forceinline__ Frag<P> column_frag(const bf16 *p, int stride)
 {
     static_assert(P == 1, "BF16 is one part");
-    uintx4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = p[2 * e * stride].bits | (unsigned)p[(2 * e + 1) * stride].bits << 16;
     Frag<P> f;
-    f.p[0] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.w[0][e] = p[2 * e * stride].bits | (unsigned)p[(2 * e + 1) * stride].bits << 16;
     return f;
 }
 // Eight elements of a row of memory to LDS, zeros past the n-th.
@@ -380,12 +428,12 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
                 store_frag<PI>(key + (U::Q + (w * KB + kb) * PI) * 1024, lane, qf);
             }
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
+            for (int i = 0; i < NT; ++i) {            // all tiles, the unused ones too: no branches between the products
                 const int at = tile_index(i, m) * ROW + 32 * kb + 8 * g;
                 const Frag<PI> other = row_frag<PI>(Ks + at);
-                if (i >= (w & ~1)) kk[i] = mm<3>(other, kf, kk[i]);
-                if (i <= (w | 1)) kq[i] = mm<3>(other, qf, kq[i]);
-                if (TAPE && i >= (w & ~1)) qk[i] = mm<3>(row_frag<PI>(Qs + at), kf, qk[i]);
+                kk[i] = mm<3>(other, kf, kk[i]);
+                kq[i] = mm<3>(other, qf, kq[i]);
+                if (TAPE) qk[i] = mm<3>(row_frag<PI>(Qs + at), kf, qk[i]);
             }
         }
         const float hi_own = hi[own], lo_own = lo[own], beta_own = beta[own];
@@ -488,47 +536,55 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
 // loads_done() and a barrier.
 __device__ __forceinline__ void units_to_lds(const unsigned char *from, unsigned char *to, int units, int wave, int waves, int lane)
 {
-    for (int u = wave; u < units; u += waves)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned int *)(from + u * 1024 + lane * 16),
+    const unsigned at = lane * 16;          // a uniform address and 32 bits a lane: no vector instruction but the load
+    for (int u = wave; u < units; u += waves) {
+        const unsigned char *p = from + u * 1024;
+        unsigned off = at;
+        asm("" : "+s"(p), "+v"(off));
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned int *)(p + off),
                                          (__attribute__((address_space(3))) unsigned int *)(to + u * 1024), 16, 0, 0);
-}
-__device__ __forceinline__ void loads_done_and_barrier()
-{
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
+    }
 }
 
+// The element `bytes` behind a uniform address: 32 bits a lane, so that the address stays scalar.
+template <class E>
+__device__ __forceinline__ const E *behind(const E *p, unsigned bytes) { return (const E *)((const char *)p + bytes); }
+template <class E>
+__device__ __forceinline__ E *behind(E *p, unsigned bytes) { return (E *)((char *)p + bytes); }
+
 // A wave's column of one chunk, eight consecutive tokens for each pair of tiles, from a tensor [token, column] whose first token counts.  `at`
-// is the lane's offset (8 g token + its column, or column 0 past the last one); distances of tokens are uniform.  In a chunk that ends early, the
+// is the lane's offset in bytes (8 g tokens and its column, or column 0 past the last one); distances of tokens are uniform.  In a chunk that ends early, the
 // first token is read in place of those that do not count: loads without branches between them.
 template <class E, int LB>
 __device__ __forceinline__ void load_columns(const E *p, long long token, unsigned at, int g, int count, E (&u)[LB][8])
 {
     if (count >= 32 * LB) {
+        asm("" : "+v"(at));
 #pragma unroll
         for (int s = 0; s < LB; ++s)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[s][e] = (p + (32 * s + e) * token)[at];
+            for (int e = 0; e < 8; ++e) {
+                const E *q = p + (32 * s + e) * token;
+                asm("" : "+s"(q));
+                u[s][e] = *behind(q, at);
+            }
     } else {
-        p += (long long)at - 8 * g * token;
+        p = behind(p, at) - 8 * g * token;
 #pragma unroll
         for (int s = 0; s < LB; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[s][e] = p[32 * s + 8 * g + e < count ? (32 * s + 8 * g + e) * token : 0];
     }
 }
+// Zeros in place of what does not count.
 template <class E, int LB>
-__device__ __forceinline__ void columns_to_float(const E (&u)[LB][8], bool all_columns, bool column, int g, int count, float (&x)[LB][8])
+__device__ __forceinline__ void mask_columns(E (&u)[LB][8], bool all_columns, bool column, int g, int count)
 {
+    if (all_columns && count >= 32 * LB) return;
 #pragma unroll
     for (int s = 0; s < LB; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[s][e] = to_float(u[s][e]);
-    if (!all_columns || count < 32 * LB)
-#pragma unroll
-        for (int s = 0; s < LB; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[s][e] = column && 32 * s + 8 * g + e < count ? x[s][e] : 0.0f;
+        for (int e = 0; e < 8; ++e) u[s][e] = column && 32 * s + 8 * g + e < count ? u[s][e] : E{};
 }
 
 // A wave's state: element r of tile t is row tile_index(t, 4 g + r), column `col`.
@@ -562,14 +618,14 @@ __device__ __forceinline__ void store_state(float *p, int Dk, int Dv, int col, i
             if (d < Dk && col < Dv) p[d * Dv + col] = S[t][r];
         }
 }
-// Tiles of rows tile_index(t, 4 g + r) of a matrix of `stride` columns in the memory between the kernels; `at` = 8 g stride + column.
+// Tiles of rows tile_index(t, 4 g + r) of a matrix of `stride` columns in the memory between the kernels; `at` = 8 g rows and the column, in bytes.
 template <int N>
 __device__ __forceinline__ void store_tiles(float *p, int stride, unsigned at, const floatx4 (&x)[N])
 {
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) (p + (32 * (t >> 1) + 4 * (t & 1) + r) * stride)[at] = x[t][r];
+        for (int r = 0; r < 4; ++r) *behind(p + (32 * (t >> 1) + 4 * (t & 1) + r) * stride, at) = x[t][r];
 }
 
 // LDS of a scan, in units: what a chunk needs first (FIRST) for two chunks, what its last products need (LAST) for two where that fits into 160,
@@ -615,8 +671,10 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     load_state<DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
     E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
-    const unsigned at_v = 8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0);
-    const unsigned at_tape = 8 * g * (unsigned)mem.dvp + col;
+    const unsigned at_v = (8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0)) * sizeof(E);
+    const unsigned at_tape = (8 * g * (unsigned)mem.dvp + col) * 4;
+    const int lane_token = 8 * (m >> 2) + (m & 3);              // where tokens are columns: token lane_token of a tile, columns col0 + 4 g ..
+    const unsigned at_o = (lane_token * (unsigned)a.so.token + 4 * g) * sizeof(E);
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
@@ -633,154 +691,205 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         if (Lds::DOUBLE) load_last(0, 0);
         load_v(0);
     }
+    Frag<PM> Sf[KB];            // the state as operand
+    auto split_s = [&](int kb) {
+        float u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = S[2 * kb + (e >> 2)][e & 3];
+        Sf[kb] = make_frag<PM>(u);
+    };
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) split_s(kb);
     __builtin_amdgcn_s_waitcnt(0);
     for (int chunk = 0; chunk < n; ++chunk) {
         const int t0 = chunk * L, parity = chunk & 1;
         const unsigned char *ldsA = Lds::first(lds, parity), *ldsB = ldsA + A_UNITS * 1024, *ldsKT = Lds::last(lds, parity);
         const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
         __syncthreads();
-        float x[LB][8];
-        columns_to_float<E, LB>(next, all_columns, col < a.Dv, g, len - t0, x);
+        mask_columns<E, LB>(next, all_columns, col < a.Dv, g, len - t0);
         const int after = chunk + 1 < n ? chunk + 1 : chunk;
         if (!Lds::DOUBLE) load_last(chunk, parity);
         if (chunk + 1 < n) {
             load_first(after, parity ^ 1);
             if (Lds::DOUBLE) load_last(after, parity ^ 1);
         }
-        load_v(after);
         if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
-        // K S with tokens in rows, (Q S)' with tokens in columns: two tiles of tokens at a time
+        region_end();
+
+        // K S, tokens in rows; then (Q S)', tokens in columns, and meanwhile R = V - e^G K S as operand
         floatx4 KS[NT], QS[NT];
+        Frag<PM> R[LB];
         {
-            Frag<PM> Sf[KB];
+            Frag<PI> kf[2][NT];
+            auto read = [&](int unit, int kb, int to) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) kf[to][i] = load_frag<PI>(ldsA + (unit + (i * KB + kb) * PI) * 1024, lane);
+            };
+            floatx4 *ks[NT], *qs[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) KS[i] = QS[i] = floatx4{0, 0, 0, 0}, ks[i] = &KS[i], qs[i] = &QS[i];
+            read(U::K, 0, 0);
+            float decay[LB][8];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) load_gates(gates->decay + 32 * s + 8 * g, decay[s]);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                float u[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = S[2 * kb + (e >> 2)][e & 3];
-                Sf[kb] = make_frag<PM>(u);
+                if (kb + 1 < KB) read(U::K, kb + 1, (kb + 1) & 1);
+                else read(U::Q, 0, (kb + 1) & 1);
+                region_end();
+                mm_many<3, false>(kf[kb & 1], Sf[kb], ks, NoWeave());
+                region_end();
             }
-            Frag<PI> kf[2][2], qf[2][2];
-            auto read = [&](int step, int to) {
-                const int i = step / KB * 2, kb = step % KB;
+            constexpr int MFMA = KB * NT * products(PI, PM, PO);
+            auto pieces = weave<at_least_1(MFMA / (2 * LB)), 2 * LB>([&](int k) {
+                const int s = k >> 1, e = k & 1;
+                float u[4];
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    kf[to][p] = load_frag<PI>(ldsA + (U::K + ((i + p) * KB + kb) * PI) * 1024, lane);
-                    qf[to][p] = load_frag<PI>(ldsA + (U::Q + ((i + p) * KB + kb) * PI) * 1024, lane);
-                }
-            };
-            read(0, 0);
+                for (int r = 0; r < 4; ++r) u[r] = fmaf(-decay[s][4 * e + r], KS[2 * s + e][r], to_float(next[s][4 * e + r]));
+                set_four<PM>(R[s], e, u);
+            });
 #pragma unroll
-            for (int step = 0; step < LB * KB; ++step) {
-                const int i = step / KB * 2, kb = step % KB, at = step & 1;
-                if (step + 1 < LB * KB) read(step + 1, at ^ 1);
-                __builtin_amdgcn_sched_barrier(0);
-                if (kb == 0) KS[i] = KS[i + 1] = QS[i] = QS[i + 1] = floatx4{0, 0, 0, 0};
-                floatx4 *ks[2] = {&KS[i], &KS[i + 1]}, *qs[2] = {&QS[i], &QS[i + 1]};
-                mm_many<3, false>(kf[at], Sf[kb], ks);
-                mm_many<PO, true>(qf[at], Sf[kb], qs);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int kb = 0; kb < KB; ++kb) {
+                if (kb + 1 < KB) read(U::Q, kb + 1, (KB + kb + 1) & 1);
+                region_end();
+                mm_many<PO, true>(kf[(KB + kb) & 1], Sf[kb], qs, pieces);
+                region_end();
             }
+            pieces.rest();
+#pragma unroll
+            for (int s = 0; s < LB; ++s) hold(R[s]);
         }
+        load_v(after);
 
-        // E = T (V - e^G K S): a pair of tiles of tokens at a time
+        // E = T R, the tokens of one pair of tiles after the other, and U = beta E as operand, for the outputs and times e^(GL-G) for the state, while
+        // the products of the next pair run; then the outputs' P U and the first part of S <- e^GL S + K' (e^(GL-G) U) while the last pair is split
         floatx4 Ee[NT];
+        Frag<PM> W[LB];
+        Frag<PO> Uf[LB];
+        float be[LB][8], left[LB][8], decay_o[NT];
+        Frag<PM> tf[2][2];
+        auto read_t = [&](int s, int kb, int to) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) tf[to][p] = load_frag<PM>(ldsB + (U::T + U::lower(2 * s + p, kb) * PM) * 1024, lane);
+        };
+        read_t(0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) decay_o[i] = gates->decay[tile_index(i, m)], Ee[i] = floatx4{0, 0, 0, 0};
+        const float whole = gates->whole;
+        auto split_u = [&](int s, int e) {
+            float u[4], w[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                u[r] = be[s][4 * e + r] * Ee[2 * s + e][r];
+                w[r] = left[s][4 * e + r] * u[r];
+            }
+            set_four<PO>(Uf[s], e, u);
+            set_four<PM>(W[s], e, w);
+        };
+        Frag<PO> pf[2][2];
+        auto read_p = [&](int s, int kb, int to) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) pf[to][p] = load_frag<PO>(ldsB + (U::P + U::lower(2 * s + p, kb) * PO) * 1024, lane);
+        };
         {
-            Frag<PM> R[LB];
+            floatx4 *to[2] = {&Ee[0], &Ee[1]};
+            if (LB > 1) read_t(1, 0, 1);
+            load_gates(gates->beta + 8 * g, be[0]);
+            load_gates(gates->left + 8 * g, left[0]);
+            region_end();
+            auto pieces = weave<1, NT + DT>([&](int k) {
+                if (k < NT) QS[k] *= decay_o[k];
+                else S[k - NT] *= whole;
+            });
+            mm_many<3, false>(tf[0], R[0], to, pieces);
+            if (LB > 1) read_t(1, 1, 0);
+            read_p(0, 0, 0);
+            pieces.rest();
+        }
+        if constexpr (LB > 1) {
+            floatx4 *to[2] = {&Ee[2], &Ee[3]};
+            auto pieces = weave<8, 2>([&](int e) { split_u(0, e); });
+            mm_many<3, false>(tf[1], R[0], to, pieces);
+            load_gates(gates->beta + 32 * (LB - 1) + 8 * g, be[LB - 1]);
+            load_gates(gates->left + 32 * (LB - 1) + 8 * g, left[LB - 1]);
+            mm_many<3, false>(tf[0], R[LB - 1], to, pieces);
+            pieces.rest();
+        } else {
 #pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                float decay[8], u[8];
-                load_gates(gates->decay + 32 * s + 8 * g, decay);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[2 * s + (e >> 2)][e & 3], x[s][e]);
-                R[s] = make_frag<PM>(u);
-            }
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                Frag<PM> tf[LB][2];
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) tf[kb][p] = load_frag<PM>(ldsB + (U::T + U::lower(2 * s + p, kb) * PM) * 1024, lane);
-                Ee[2 * s] = Ee[2 * s + 1] = floatx4{0, 0, 0, 0};
-                floatx4 *to[2] = {&Ee[2 * s], &Ee[2 * s + 1]};
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb) mm_many<3, false>(tf[kb], R[kb], to);
-            }
+            for (int e = 0; e < 2; ++e) split_u(0, e);
         }
         if (TAPE && col0 < mem.dvp) store_tiles<NT>(mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Ee);
-        // U = beta E: for the outputs, and times e^(GL-G) for the state
-        Frag<PM> W[LB];
-        {
-            Frag<PO> Uf[LB];
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                float be[8], left[8], u[8], w[8];
-                load_gates(gates->beta + 32 * s + 8 * g, be);
-                load_gates(gates->left + 32 * s + 8 * g, left);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    u[e] = be[e] * Ee[2 * s + (e >> 2)][e & 3];
-                    w[e] = left[e] * u[e];
-                }
-                Uf[s] = make_frag<PO>(u);
-                W[s] = make_frag<PM>(w);
-            }
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                Frag<PO> pf[LB][2];
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) pf[kb][p] = load_frag<PO>(ldsB + (U::P + U::lower(2 * s + p, kb) * PO) * 1024, lane);
-#pragma unroll
-                for (int p = 0; p < 2; ++p) QS[2 * s + p] *= gates->decay[tile_index(2 * s + p, m)];
-                floatx4 *to[2] = {&QS[2 * s], &QS[2 * s + 1]};
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb) mm_many<PO, true>(pf[kb], Uf[kb], to);
-            }
-        }
-        // S <- e^GL S + K' (e^(GL-G) U): a pair of tiles of the state at a time
-        const float whole = gates->whole;
         if (!Lds::DOUBLE) {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
         }
-        {
-            Frag<PI> kf[2][2];
-            auto read = [&](int step, int to) {
-                const int t = step / LB * 2, kb = step % LB;
+        // the updates of the state's pairs of tiles, first with tokens 0 .. 31, then with the others: blocks are read two updates ahead
+        Frag<PI> kf[2][2];
+        auto read_k = [&](int update) {
+            if (update >= LB * KB) return;
 #pragma unroll
-                for (int p = 0; p < 2; ++p) kf[to][p] = load_frag<PI>(ldsKT + ((t + p) * LB + kb) * PI * 1024, lane);
-            };
-            read(0, 0);
+            for (int p = 0; p < 2; ++p) kf[update & 1][p] = load_frag<PI>(ldsKT + ((2 * (update % KB) + p) * LB + update / KB) * PI * 1024, lane);
+        };
+        floatx4 *o0[2] = {&QS[0], &QS[1]};
+        read_k(0);
+        read_k(1);
+        if constexpr (LB > 1) {
+            constexpr int MFMA = 4 * products(PO, PO, PO) + KB * 2 * products(PI, PM, 3);
+            floatx4 *o1[2] = {&QS[2], &QS[3]};
+            auto pieces = weave<MFMA / 3, 2>([&](int e) { split_u(1, e); });
+            read_p(1, 0, 1);
+            region_end();
+            mm_many<PO, true>(pf[0], Uf[0], o0, pieces);
+            read_p(1, 1, 0);
+            region_end();
+            mm_many<PO, true>(pf[1], Uf[0], o1, pieces);
 #pragma unroll
-            for (int step = 0; step < KB * LB; ++step) {
-                const int t = step / LB * 2, kb = step % LB, at = step & 1;
-                if (step + 1 < KB * LB) read(step + 1, at ^ 1);
-                __builtin_amdgcn_sched_barrier(0);
-                if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
-                floatx4 *to[2] = {&S[t], &S[t + 1]};
-                mm_many<3, false>(kf[at], W[kb], to);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int pair = 0; pair < KB; ++pair) {
+                floatx4 *to[2] = {&S[2 * pair], &S[2 * pair + 1]};
+                mm_many<3, false>(kf[pair & 1], W[0], to, pieces);
+                read_k(pair + 2);
+                region_end();
             }
+            pieces.rest();
+        }
+        // the last tokens' products; a pair of tiles of the state is split for the next chunk while those of the next pair run, then of the outputs
+        {
+            constexpr int LAST = (LB - 1) * KB;
+            auto split_s = [&](int pair, int e) {
+                const floatx4 &x = S[2 * pair + e];
+                set_four<PM>(Sf[pair], e, {x[0], x[1], x[2], x[3]});
+            };
+#pragma unroll
+            for (int pair = 0; pair < KB; ++pair) {
+                floatx4 *to[2] = {&S[2 * pair], &S[2 * pair + 1]};
+                auto pieces = weave<2, 2>([&](int e) {
+                    if (pair > 0) split_s(pair - 1, e);
+                });
+                mm_many<3, false>(kf[(LAST + pair) & 1], W[LB - 1], to, pieces);
+                read_k(LAST + pair + 2);
+                region_end();
+            }
+            auto pieces = weave<2, 2>([&](int e) { split_s(KB - 1, e); });
+            floatx4 *to[2] = {&QS[NT - 2], &QS[NT - 1]};
+            mm_many<PO, true>(pf[0], Uf[LB - 1], to, pieces);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) hold(Sf[kb]);
+            region_end();
         }
         // what the next chunk needs is there; the outputs are stored behind that wait and have the next chunk's time
         if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
-        // token t0 + tile_index(i, m), columns col0 + 4 g ..
-        const int lane_token = 8 * (m >> 2) + (m & 3);
-        const unsigned at_o = lane_token * (unsigned)a.so.token + col0 + 4 * g;
+        const bool plain = mem.vec_o && t0 + L <= a.T && (all_columns || col0 + 16 <= a.Dv);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const int tile_token = t0 + 32 * (i >> 1) + 4 * (i & 1);
-            E *to = o + tile_token * a.so.token;
+            E *to = o + tile_token * a.so.token + col0;
             const float u[4] = {a.scale * QS[i][0], a.scale * QS[i][1], a.scale * QS[i][2], a.scale * QS[i][3]};
-            if (mem.vec_o) {
-                if (tile_token + lane_token < a.T && col0 + 4 * g < a.Dv) store4(to + at_o, u);
+            if (plain) {
+                if (col0 < a.Dv) store4(behind(to, at_o), u);
             } else {
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (tile_token + lane_token < a.T && col0 + 4 * g + r < a.Dv) store_element(to + at_o + r, u[r]);
+                    if (tile_token + lane_token < a.T && col0 + 4 * g + r < a.Dv) store_element(behind(to, at_o) + r, u[r]);
             }
         }
     }

@@ -28,14 +28,23 @@ hipError_t launch(const HeadNormArgs &a, int lpr, hipStream_t s)
 {
     HeadNormShape g;
     g.lpr = lpr;
-    g.chunks = (a.Hq + a.Hk + NH - 1) / NH;
-    g.items = (unsigned)a.B * (unsigned)a.T * g.chunks;
-    const unsigned groups = HEAD_NORM_THREADS / lpr;
-    unsigned blocks = (g.items + groups - 1) / groups;
-    if (BACKWARD && blocks > HEAD_NORM_BLOCKS) blocks = HEAD_NORM_BLOCKS;
-    if (blocks) k_head_norm<E, VEC, ITER, NH, INTER, BACKWARD><<<blocks, HEAD_NORM_THREADS, 0, s>>>(a, g);
+    const unsigned tokens = (unsigned)a.B * (unsigned)a.T, groups = HEAD_NORM_THREADS / lpr;
+    const int heads[2] = {a.Hq, a.Hk};
+    unsigned blocks[2];
+    for (int i = 0; i < 2; ++i) {
+        g.chunks[i] = heads[i] > 0 ? (heads[i] + NH - 1) / NH : 1;
+        g.items[i] = heads[i] > 0 ? tokens * g.chunks[i] : 0;
+        blocks[i] = (g.items[i] + groups - 1) / groups;
+    }
+    const unsigned long long all = (unsigned long long)blocks[0] + blocks[1];
+    if (BACKWARD && all > HEAD_NORM_BLOCKS)      // shared out as the work is, each kind that has work its own
+        for (int i = 0; i < 2; ++i)
+            if (blocks[i]) blocks[i] = 1 + (unsigned)((unsigned long long)blocks[i] * (HEAD_NORM_BLOCKS - 2) / all);
+    g.blocks_q = blocks[0];
+    const unsigned grid = blocks[0] + blocks[1];
+    if (grid) k_head_norm<E, VEC, ITER, NH, INTER, BACKWARD><<<grid, HEAD_NORM_THREADS, 0, s>>>(a, g);
     if (BACKWARD && (a.dwq || a.dwk))
-        k_head_norm_weights<<<(2 * a.D + 15) / 16, 1024, 0, s>>>(a.partial, blocks, a.D, a.dwq, a.dwk);
+        k_head_norm_weights<<<dim3((a.D + 15) / 16, 2), 1024, 0, s>>>(a.partial, blocks[0], grid, a.D, a.dwq, a.dwk);
     return hipGetLastError();
 }
 
@@ -65,6 +74,6 @@ hipError_t typed(const HeadNormArgs &a, hipStream_t s)
 
 hipError_t head_norm_launch(const HeadNormArgs &a, hipStream_t s) { return typed<false>(a, s); }
 hipError_t head_norm_backward_launch(const HeadNormArgs &a, hipStream_t s) { return typed<true>(a, s); }
-size_t head_norm_workspace_bytes(int D) { return sizeof(float) * (size_t)HEAD_NORM_BLOCKS * 2 * D; }
+size_t head_norm_workspace_bytes(int D) { return sizeof(float) * (size_t)HEAD_NORM_BLOCKS * D; }
 
 }  // namespace tfno
