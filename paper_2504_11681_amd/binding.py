@@ -405,6 +405,24 @@ def fno1d_real(x, W, y, stream=None):
 
 
 # ---------------------------------------------------------------- operators along time
+#
+# A call's descriptor and all checks of its arguments depend on types, devices, shapes and strides alone.  They are made once for each such
+# combination (_plan) and looked up afterwards: what a call costs on the host is its rate for one token.
+
+_plans = {}
+
+
+def _of(t):
+    """What a plan depends on of a tensor."""
+    return None if t is None else (t.dtype, t.get_device(), t.shape, t.stride())
+
+
+def _plan(key, make, *args):
+    if len(_plans) >= 4096:
+        _plans.clear()
+    plan = _plans[key] = make(*args)
+    return plan
+
 
 def _element_type(dtype) -> int:
     torch = _torch or _load_torch()
@@ -415,80 +433,77 @@ def _element_type(dtype) -> int:
     raise TypeError("q, k and v must be float32 or bfloat16")
 
 
-def _tensors(first, others, **named):
-    """Checks what the operators along time take: device tensors of the type of `first` (others) or of the type given (named; None passes),
-    whose last axis is contiguous."""
-    for name, t in others.items():
-        if t.dtype is not first.dtype:
-            raise TypeError(f"{name} must have the type of q")
-    checks = list(others.items())
-    for name, (t, dtype) in named.items():
-        if t is not None:
-            if t.dtype is not dtype:
+def _check_types(first, same, f32=(), i32=(), u8=()):
+    """Device tensors on one device: `same` of the type of the first one, the others of the types named; each given as (name, _of(tensor))."""
+    torch = _torch or _load_torch()
+    _element_type(first[0])
+    for dtype, tensors in ((first[0], same), (torch.float32, f32), (torch.int32, i32), (torch.uint8, u8)):
+        for name, t in tensors:
+            if t is None:
+                continue
+            if t[0] is not dtype:
                 raise TypeError(f"{name} must be {dtype}")
-            checks.append((name, t))
-    for name, t in checks:
-        if not t.is_cuda or t.device != first.device:
-            raise TypeError(f"{name} must be a tensor on the device of q")
+            if t[1] < 0 or t[1] != first[1]:
+                raise TypeError(f"{name} must be a tensor on the device of q")
 
 
-def _layout(t):
-    return None if t is None else (t.shape, t.stride())
-
-
-def _strides4(name, layout, shape):
+def _strides4(name, t, shape):
     """Strides of a [B, T, H, D] tensor with its last axis contiguous."""
-    if tuple(layout[0]) != shape:
-        raise ValueError(f"{name} must be {list(shape)}, not {list(layout[0])}")
-    if shape[3] > 1 and layout[1][3] != 1:
+    if tuple(t[2]) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t[2])}")
+    if shape[3] > 1 and t[3][3] != 1:
         raise ValueError(f"the last axis of {name} must be contiguous")
-    return _Strides(*layout[1][:3])
+    return _Strides(*t[3][:3])
 
 
-def _contiguous(**tensors):
-    for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
+def _check_contiguous(shape, *tensors):
+    for name, t in tensors:
+        if t is None:
+            continue
+        if tuple(t[2]) != tuple(shape):
+            raise ValueError(f"{name} must be {list(shape)}, not {list(t[2])}")
+        step = 1
+        for size, stride in zip(reversed(t[2]), reversed(t[3])):
+            if size > 1 and stride != step:
+                raise ValueError(f"{name} must be contiguous")
+            step *= size
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-@functools.lru_cache(maxsize=1024)
-def _head_norm_desc(dtype, q, k, q_out, k_out, dq, dk, positions, wq, wk, dwq, dwk, cos, sin, eps, interleaved):
-    if len(q[0]) != 4 or len(k[0]) != 4 or q[0][:2] != k[0][:2] or q[0][3] != k[0][3]:
+def _head_norm_plan(q, k, q_out, k_out, dq, dk, positions, wq, wk, dwq, dwk, cos, sin, eps, interleaved):
+    names = (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("dq", dq), ("dk", dk))
+    _check_types(q, names, f32=(("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk), ("cos", cos), ("sin", sin)), i32=(("positions", positions),))
+    if len(q[2]) != 4 or len(k[2]) != 4 or q[2][:2] != k[2][:2] or q[2][3] != k[2][3]:
         raise ValueError("q and k must be [B, T, Hq, D] and [B, T, Hk, D]")
-    B, T, Hq, D = q[0]
-    Hk = k[0][2]
-    for name, w in (("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk)):
-        if w is not None and tuple(w[0]) != (D,):
-            raise ValueError(f"{name} must be [D]")
-    if (cos is None) != (sin is None) or (cos is not None and (len(cos[0]) != 2 or cos[0] != sin[0])):
+    B, T, Hq, D = q[2]
+    Hk = k[2][2]
+    _check_contiguous((D,), ("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk))
+    if (cos is None) != (sin is None) or (cos is not None and (len(cos[2]) != 2 or cos[2] != sin[2])):
         raise ValueError("cos and sin must both be [P, R / 2], or both None")
-    P, R = (0, 0) if cos is None else (cos[0][0], 2 * cos[0][1])
-    d = _HeadNormDesc(_element_type(dtype), B, T, Hq, Hk, D, R, P, int(interleaved), eps, 0)
+    P, R = (0, 0) if cos is None else (cos[2][0], 2 * cos[2][1])
+    _check_contiguous((P, R // 2), ("cos", cos), ("sin", sin))
+    d = _HeadNormDesc(_element_type(q[0]), B, T, Hq, Hk, D, R, P, int(interleaved), eps, 0)
     if positions is not None:
-        if tuple(positions[0]) != (B, T) or (T > 1 and positions[1][1] != 1):
+        if tuple(positions[2]) != (B, T) or (T > 1 and positions[3][1] != 1):
             raise ValueError("positions must be [B, T] with contiguous rows")
-        d.positions_batch = positions[1][0]
-    for name, t, H in (("q", q, Hq), ("k", k, Hk), ("q_out", q_out, Hq), ("k_out", k_out, Hk), ("dq", dq, Hq), ("dk", dk, Hk)):
+        d.positions_batch = positions[3][0]
+    for (name, t), H in zip(names, (Hq, Hk) * 3):
         if t is not None:
             setattr(d, name, _strides4(name, t, (B, T, H, D)))
-    return d, ctypes.addressof(d)
+    return ctypes.addressof(d), _entry("tfno_head_norm_rope_workspace_bytes")(D), d
 
 
 def head_norm_rope(q, k, wq, wk, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6, interleaved: bool = False, stream=None):
     """Norm of queries and keys for each head with the rotation by position: q [B, T, Hq, D] and k [B, T, Hk, D] (float32 or bfloat16, any
     strides with the last axis contiguous) into q_out and k_out, which may be q and k themselves.  wq, wk: float32 [D] or None (ones);
     cos, sin: float32 [P, R / 2] or None (no rotation); positions: int32 [B, T] or None (0 .. T - 1)."""
-    f32, i32 = (_torch or _load_torch()).float32, _torch.int32
-    _tensors(q, {"q": q, "k": k, "q_out": q_out, "k_out": k_out}, wq=(wq, f32), wk=(wk, f32), cos=(cos, f32), sin=(sin, f32), positions=(positions, i32))
-    _contiguous(wq=wq, wk=wk, cos=cos, sin=sin)
-    d = _head_norm_desc(q.dtype, _layout(q), _layout(k), _layout(q_out), _layout(k_out), None, None, _layout(positions), _layout(wq), _layout(wk),
-                        None, None, _layout(cos), _layout(sin), eps, interleaved)
-    st = _entry("tfno_head_norm_rope")(d[1], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
-                                       q_out.data_ptr(), k_out.data_ptr(), _raw_stream(q.device.index) if stream is None else stream)
+    key = (_of(q), _of(k), _of(q_out), _of(k_out), None, None, _of(positions), _of(wq), _of(wk), None, None, _of(cos), _of(sin), eps, interleaved)
+    plan = _plans.get(key) or _plan(key, _head_norm_plan, *key)
+    st = _entry("tfno_head_norm_rope")(plan[0], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
+                                       q_out.data_ptr(), k_out.data_ptr(), _raw_stream(key[0][1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_head_norm_rope")
     return q_out, k_out
@@ -497,73 +512,65 @@ def head_norm_rope(q, k, wq, wk, cos, sin, q_out, k_out, positions=None, eps: fl
 def head_norm_rope_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq, dk, dwq=None, dwk=None, positions=None, eps: float = 1e-6,
                             interleaved: bool = False, stream=None):
     """Gradients dq, dk and, where given, dwq, dwk (float32 [D]) of head_norm_rope from those of its results, dq_out and dk_out."""
-    f32, i32 = (_torch or _load_torch()).float32, _torch.int32
-    _tensors(q, {"q": q, "k": k, "dq_out": dq_out, "dk_out": dk_out, "dq": dq, "dk": dk}, wq=(wq, f32), wk=(wk, f32), cos=(cos, f32), sin=(sin, f32),
-             positions=(positions, i32), dwq=(dwq, f32), dwk=(dwk, f32))
-    _contiguous(wq=wq, wk=wk, cos=cos, sin=sin, dwq=dwq, dwk=dwk)
-    d = _head_norm_desc(q.dtype, _layout(q), _layout(k), _layout(dq_out), _layout(dk_out), _layout(dq), _layout(dk), _layout(positions), _layout(wq),
-                        _layout(wk), _layout(dwq), _layout(dwk), _layout(cos), _layout(sin), eps, interleaved)
-    ensure_workspace(_need("tfno_head_norm_rope_workspace_bytes", d[0].D), q.device)
-    st = _entry("tfno_head_norm_rope_backward")(d[1], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
+    key = (_of(q), _of(k), _of(dq_out), _of(dk_out), _of(dq), _of(dk), _of(positions), _of(wq), _of(wk), _of(dwq), _of(dwk), _of(cos), _of(sin), eps,
+           interleaved)
+    plan = _plans.get(key) or _plan(key, _head_norm_plan, *key)
+    ensure_workspace(plan[1], q.device)
+    st = _entry("tfno_head_norm_rope_backward")(plan[0], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
                                                 dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk),
-                                                _raw_stream(q.device.index) if stream is None else stream)
+                                                _raw_stream(key[0][1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_head_norm_rope_backward")
     return dq, dk
 
 
-@functools.lru_cache(maxsize=1024)
-def _rule_desc(dtype, q, k, v, o, g, beta, dq, dk, dv, dg, dbeta, scale):
-    """The descriptor of a call, its address, the shape of its states, and the bytes of its tape and workspaces."""
-    if len(q[0]) != 4 or len(v[0]) != 4 or q[0][:2] != v[0][:2]:
+def _rule_plan(q, k, v, o, g, beta, dq, dk, dv, dg, dbeta, lengths, tape, initial, final, other, scale):
+    names = (("q", q), ("k", k), ("v", v), ("o", o), ("dq", dq), ("dk", dk), ("dv", dv))
+    gates = (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta))
+    states = (("the initial state", initial), ("the final state or its gradient", final), ("the gradient of the initial state", other))
+    _check_types(q, names, f32=gates + states, i32=(("lengths", lengths),), u8=(("the tape", tape),))
+    if len(q[2]) != 4 or len(v[2]) != 4 or q[2][:2] != v[2][:2]:
         raise ValueError("q, k must be [B, T, Hk, Dk] and v [B, T, Hv, Dv]")
-    B, T, Hk, Dk = q[0]
-    Hv, Dv = v[0][2:]
-    d = _DeltaRuleDesc(_element_type(dtype), B, T, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale)
-    for name, t, shape in (("q", q, (Hk, Dk)), ("k", k, (Hk, Dk)), ("v", v, (Hv, Dv)), ("o", o, (Hv, Dv)), ("dq", dq, (Hk, Dk)), ("dk", dk, (Hk, Dk)),
-                           ("dv", dv, (Hv, Dv))):
+    B, T, Hk, Dk = q[2]
+    Hv, Dv = v[2][2:]
+    d = _DeltaRuleDesc(_element_type(q[0]), B, T, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale)
+    for (name, t), shape in zip(names, ((Hk, Dk), (Hk, Dk), (Hv, Dv), (Hv, Dv), (Hk, Dk), (Hk, Dk), (Hv, Dv))):
         if t is not None:
             setattr(d, name, _strides4(name, t, (B, T, *shape)))
-    for name, t in (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)):
+    for name, t in gates:
         if t is not None:
-            if tuple(t[0]) != (B, T, Hv):
+            if tuple(t[2]) != (B, T, Hv):
                 raise ValueError(f"{name} must be [B, T, Hv]")
-            setattr(d, name, _Strides(*t[1]))
+            setattr(d, name, _Strides(*t[3]))
+    _check_contiguous((B, Hv, Dk, Dv), *states)
+    _check_contiguous((B,), ("lengths", lengths))
     at = ctypes.addressof(d)
-    ask = _entry("tfno_gated_delta_rule_workspace_bytes")
-    return d, at, (B, Hv, Dk, Dv), _entry("tfno_gated_delta_rule_tape_bytes")(at), ask(at, 0), ask(at, 1)
-
-
-def _check_states(shape, B, tape, need, lengths, **states):
-    for name, t in states.items():
-        if t is not None and (tuple(t.shape) != shape or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {list(shape)}")
-    if lengths is not None and (tuple(lengths.shape) != (B,) or not lengths.is_contiguous()):
-        raise ValueError("lengths must be a contiguous [B]")
-    if tape is not None and (not tape.is_contiguous() or tape.numel() * tape.element_size() < need):
+    need = _entry("tfno_gated_delta_rule_tape_bytes")(at)
+    if tape is not None and (len(tape[2]) != 1 or tape[3][0] != 1 or tape[2][0] < need):
         raise ValueError(f"the tape must be contiguous and hold {need} bytes")
+    ask = _entry("tfno_gated_delta_rule_workspace_bytes")
+    return at, need, ask(at, 0), ask(at, 1), d
 
 
 def gated_delta_rule_tape(q, v):
     """A tape for gated_delta_rule and gated_delta_rule_backward on tensors of the sizes of q [B, T, Hk, Dk] and v [B, T, Hv, Dv]."""
     torch = _torch or _load_torch()
-    d = _rule_desc(q.dtype, _layout(q), _layout(q), _layout(v), None, None, None, None, None, None, None, None, None)
-    return torch.empty(d[3], dtype=torch.uint8, device=q.device)
+    key = ("tape", _of(q), _of(v))
+    plan = _plans.get(key) or _plan(key, lambda: _rule_plan(key[1], key[1], key[2], *(None,) * 14))
+    return torch.empty(plan[1], dtype=torch.uint8, device=q.device)
 
 
 def gated_delta_rule(q, k, v, g, beta, o, scale=None, initial_state=None, final_state=None, lengths=None, tape=None, stream=None):
     """The gated delta rule over whole sequences: q, k [B, T, Hk, Dk], v, o [B, T, Hv, Dv] (float32 or bfloat16, any strides with the last axis
     contiguous), g (log decay, or None) and beta float32 [B, T, Hv], states float32 [B, Hv, Dk, Dv], lengths int32 [B].  scale is Dk ** -0.5
     where it is not given.  With a tape (gated_delta_rule_tape) the gradient can be taken afterwards."""
-    f32, i32 = (_torch or _load_torch()).float32, _torch.int32
-    _tensors(q, {"q": q, "k": k, "v": v, "o": o}, g=(g, f32), beta=(beta, f32), initial_state=(initial_state, f32), final_state=(final_state, f32),
-             lengths=(lengths, i32), tape=(tape, _torch.uint8))
-    d = _rule_desc(q.dtype, _layout(q), _layout(k), _layout(v), _layout(o), _layout(g), _layout(beta), None, None, None, None, None, scale)
-    _check_states(d[2], d[2][0], tape, d[3], lengths, initial_state=initial_state, final_state=final_state)
+    key = (_of(q), _of(k), _of(v), _of(o), _of(g), _of(beta), None, None, None, None, None, _of(lengths), _of(tape), _of(initial_state),
+           _of(final_state), None, scale)
+    plan = _plans.get(key) or _plan(key, _rule_plan, *key)
     if tape is None:
-        ensure_workspace(d[4], q.device)
-    st = _entry("tfno_gated_delta_rule")(d[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state),
-                                         o.data_ptr(), _ptr(final_state), _ptr(tape), _raw_stream(q.device.index) if stream is None else stream)
+        ensure_workspace(plan[2], q.device)
+    st = _entry("tfno_gated_delta_rule")(plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state),
+                                         o.data_ptr(), _ptr(final_state), _ptr(tape), _raw_stream(key[0][1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule")
     return o
@@ -573,54 +580,50 @@ def gated_delta_rule_backward(q, k, v, g, beta, d_o, dq, dk, dv, dg, dbeta, tape
                               d_initial_state=None, lengths=None, stream=None):
     """Gradients of gated_delta_rule with the same inputs, from its tape and the gradients d_o of o and d_final_state of the final state
     (None: zeros).  dg and d_initial_state may be None."""
-    f32, i32 = (_torch or _load_torch()).float32, _torch.int32
-    _tensors(q, {"q": q, "k": k, "v": v, "d_o": d_o, "dq": dq, "dk": dk, "dv": dv}, g=(g, f32), beta=(beta, f32), dg=(dg, f32), dbeta=(dbeta, f32),
-             initial_state=(initial_state, f32), d_final_state=(d_final_state, f32), d_initial_state=(d_initial_state, f32), lengths=(lengths, i32),
-             tape=(tape, _torch.uint8))
-    d = _rule_desc(q.dtype, _layout(q), _layout(k), _layout(v), _layout(d_o), _layout(g), _layout(beta), _layout(dq), _layout(dk), _layout(dv),
-                   _layout(dg), _layout(dbeta), scale)
-    _check_states(d[2], d[2][0], tape, d[3], lengths, initial_state=initial_state, d_final_state=d_final_state, d_initial_state=d_initial_state)
-    ensure_workspace(d[5], q.device)
+    key = (_of(q), _of(k), _of(v), _of(d_o), _of(g), _of(beta), _of(dq), _of(dk), _of(dv), _of(dg), _of(dbeta), _of(lengths), _of(tape),
+           _of(initial_state), _of(d_final_state), _of(d_initial_state), scale)
+    plan = _plans.get(key) or _plan(key, _rule_plan, *key)
+    ensure_workspace(plan[3], q.device)
     st = _entry("tfno_gated_delta_rule_backward")(
-        d[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state), tape.data_ptr(), d_o.data_ptr(),
+        plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state), tape.data_ptr(), d_o.data_ptr(),
         _ptr(d_final_state), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dg), dbeta.data_ptr(), _ptr(d_initial_state),
-        _raw_stream(q.device.index) if stream is None else stream)
+        _raw_stream(key[0][1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule_backward")
     return dq, dk, dv, dg, dbeta
 
 
-@functools.lru_cache(maxsize=1024)
-def _step_desc(dtype, q, k, v, o, g, beta, states, scale):
-    if len(q[0]) != 3 or len(v[0]) != 3 or q[0][0] != v[0][0]:
+def _step_plan(q, k, v, o, g, beta, states, slots, scale):
+    names = (("q", q), ("k", k), ("v", v), ("o", o))
+    _check_types(q, names, f32=(("g", g), ("beta", beta), ("states", states)), i32=(("slots", slots),))
+    if len(q[2]) != 3 or len(v[2]) != 3 or q[2][0] != v[2][0]:
         raise ValueError("q, k must be [B, Hk, Dk] and v [B, Hv, Dv]")
-    B, Hk, Dk = q[0]
-    Hv, Dv = v[0][1:]
-    if len(states) != 4 or tuple(states[1:]) != (Hv, Dk, Dv):
+    B, Hk, Dk = q[2]
+    Hv, Dv = v[2][1:]
+    if len(states[2]) != 4:
         raise ValueError("states must be [pool, Hv, Dk, Dv]")
-    d = _DeltaRuleDesc(_element_type(dtype), B, 1, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale)
-    for name, t, shape in (("q", q, (Hk, Dk)), ("k", k, (Hk, Dk)), ("v", v, (Hv, Dv)), ("o", o, (Hv, Dv))):
-        s = t[1]
-        setattr(d, name, _strides4(name, ((B, 1, *t[0][1:]) if t[0][0] == B else t[0], (s[0], 0, s[1], s[2])), (B, 1, *shape)))
+    _check_contiguous((states[2][0], Hv, Dk, Dv), ("states", states))
+    _check_contiguous((B,), ("slots", slots))
+    d = _DeltaRuleDesc(_element_type(q[0]), B, 1, Hk, Hv, Dk, Dv, Dk ** -0.5 if scale is None else scale)
+    for (name, t), shape in zip(names, ((Hk, Dk), (Hk, Dk), (Hv, Dv), (Hv, Dv))):
+        if tuple(t[2]) != (B, *shape):
+            raise ValueError(f"{name} must be {[B, *shape]}, not {list(t[2])}")
+        setattr(d, name, _strides4(name, (t[0], t[1], (B, 1, *shape), (t[3][0], 0, t[3][1], t[3][2])), (B, 1, *shape)))
     for name, t in (("g", g), ("beta", beta)):
         if t is not None:
-            if tuple(t[0]) != (B, Hv):
+            if tuple(t[2]) != (B, Hv):
                 raise ValueError(f"{name} must be [B, Hv]")
-            setattr(d, name, _Strides(t[1][0], 0, t[1][1]))
-    return d, ctypes.addressof(d)
+            setattr(d, name, _Strides(t[3][0], 0, t[3][1]))
+    return ctypes.addressof(d), d
 
 
 def gated_delta_rule_step(q, k, v, g, beta, states, o, slots=None, scale=None, stream=None):
     """One token of the gated delta rule: q, k [B, Hk, Dk], v, o [B, Hv, Dv], g (or None) and beta float32 [B, Hv]; the states float32
     [pool, Hv, Dk, Dv] of the slots int32 [B] (None: 0 .. B - 1; negative: no sequence) are advanced in place."""
-    f32, i32 = (_torch or _load_torch()).float32, _torch.int32
-    _tensors(q, {"q": q, "k": k, "v": v, "o": o}, g=(g, f32), beta=(beta, f32), states=(states, f32), slots=(slots, i32))
-    d = _step_desc(q.dtype, _layout(q), _layout(k), _layout(v), _layout(o), _layout(g), _layout(beta), states.shape, scale)
-    _contiguous(states=states, slots=slots)
-    if slots is not None and tuple(slots.shape) != (q.shape[0],):
-        raise ValueError("slots must be [B]")
-    st = _entry("tfno_gated_delta_rule_step")(d[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), states.data_ptr(), _ptr(slots),
-                                              states.shape[0], o.data_ptr(), _raw_stream(q.device.index) if stream is None else stream)
+    key = (_of(q), _of(k), _of(v), _of(o), _of(g), _of(beta), _of(states), _of(slots), scale)
+    plan = _plans.get(key) or _plan(key, _step_plan, *key)
+    st = _entry("tfno_gated_delta_rule_step")(plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), states.data_ptr(), _ptr(slots),
+                                              key[6][2][0], o.data_ptr(), _raw_stream(key[0][1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule_step")
     return o

@@ -178,7 +178,7 @@ def test_step_refuses(L):
 
 
 def test_binding_refuses_what_is_not_on_the_device_or_has_another_type():
-    q = torch.zeros(2, 8, 2, 16)
+    q = torch.zeros(2, 8, 2, 16)          # on the CPU
     g = torch.zeros(2, 8, 2)
     with pytest.raises(TypeError):
         tfno.gated_delta_rule(q, q, q, g, g, q)
@@ -194,32 +194,68 @@ def test_binding_refuses_what_is_not_on_the_device_or_has_another_type():
         tfno.gated_delta_rule_step(q[:, 0], q[:, 0], q[:, 0], g[:, 0], g[:, 0], torch.zeros(2, 2, 16, 16), q[:, 0], slots=torch.zeros(2))
 
 
-def layouts(*tensors):
-    return [tfno._layout(t) for t in tensors]
+def plans(*tensors):
+    """What a plan depends on of these tensors, as if they lay on device 0."""
+    return [None if t is None else (t.dtype, 0, t.shape, t.stride()) for t in tensors]
 
 
 def test_binding_refuses_shapes_that_do_not_fit():
     q, v, g = torch.zeros(2, 8, 2, 16), torch.zeros(2, 8, 4, 24), torch.zeros(2, 8, 4)
-    none = [None] * 5
-    assert tfno._rule_desc(q.dtype, *layouts(q, q, v, v, g, g), *none, None)[0].scale == 0.25
+    none = [None] * 10
+    good = (q, q, v, v, g, g)
+    plan = tfno._rule_plan(*plans(*good), *none, None)
+    assert plan[-1].scale == 0.25 and plan[1] > plan[2] > 0
     for bad in ((q[:, :7], q, v, v, g, g), (q, q[..., :8], v, v, g, g), (q, q, v, q, g, g), (q, q, v, v, g[..., :2], g), (q, q, v, v, g, g[:1]), (q[0], q[0], v, v, g, g),
-                (q, q, v, v[..., ::2].repeat(1, 1, 1, 2)[..., ::1].transpose(2, 3), g, g)):
+                (q, q, v, v.transpose(2, 3), g, g)):
         with pytest.raises(ValueError):
-            tfno._rule_desc(q.dtype, *layouts(*bad), *none, None)
+            tfno._rule_plan(*plans(*bad), *none, None)
     with pytest.raises(ValueError):      # the last axis has to be contiguous
-        tfno._rule_desc(q.dtype, *layouts(torch.zeros(2, 8, 2, 32)[..., ::2], q, v, v, g, g), *none, None)
+        tfno._rule_plan(*plans(torch.zeros(2, 8, 2, 32)[..., ::2], q, v, v, g, g), *none, None)
     with pytest.raises(TypeError):
-        tfno._rule_desc(torch.float16, *layouts(q, q, v, v, g, g), *none, None)
+        tfno._rule_plan(*plans(q.half(), q.half(), v.half(), v.half(), g, g), *none, None)
+    with pytest.raises(TypeError):
+        tfno._rule_plan(*plans(q, q.double(), v, v, g, g), *none, None)
+    with pytest.raises(TypeError):
+        tfno._rule_plan(*plans(q, q, v, v, g, g.double()), *none, None)
+    more = dict(lengths=torch.zeros(2, dtype=torch.int32), tape=torch.zeros(plan[1], dtype=torch.uint8), initial=torch.zeros(2, 4, 16, 24), final=torch.zeros(2, 4, 16, 24),
+                other=torch.zeros(2, 4, 16, 24))
+
+    def with_more(**kw):
+        return tfno._rule_plan(*plans(*good), *[None] * 5, *plans(*{**more, **kw}.values()), None)
+
+    assert with_more()[1] == plan[1]
+    for kw in (dict(lengths=torch.zeros(3, dtype=torch.int32)), dict(tape=more["tape"][1:]), dict(tape=torch.zeros(2, plan[1], dtype=torch.uint8)),
+               dict(initial=torch.zeros(2, 4, 24, 16)), dict(final=torch.zeros(2, 4, 24, 16).transpose(2, 3)), dict(other=torch.zeros(1, 4, 16, 24))):
+        with pytest.raises(ValueError):
+            with_more(**kw)
+    for kw in (dict(lengths=torch.zeros(2)), dict(tape=torch.zeros(plan[1])), dict(initial=torch.zeros(2, 4, 16, 24, dtype=torch.bfloat16))):
+        with pytest.raises(TypeError):
+            with_more(**kw)
+
+
+def test_binding_refuses_shapes_of_the_norm_and_the_step_that_do_not_fit():
+    q, v, g = torch.zeros(2, 8, 2, 16), torch.zeros(2, 8, 4, 24), torch.zeros(2, 8, 4)
     w, cos = torch.zeros(16), torch.zeros(8, 4)
-    more = (None, None, None)
-    assert tfno._head_norm_desc(q.dtype, *layouts(q, q, q, q), *more, *layouts(w, w), None, None, *layouts(cos, cos), 1e-6, False)[0].R == 8
-    for qq, kk, ww, cc in ((q, q[:1], w, cos), (q, q[..., :8], w, cos), (q, q, w[:8], cos), (q, q, w, cos[0]), (q[0], q[0], w, cos)):
+
+    def norm(q, k, w, cos, sin, positions=None):
+        return tfno._head_norm_plan(*plans(q, k, q, k, None, None, positions, w, w, None, None, cos, sin), 1e-6, False)
+
+    assert norm(q, q, w, cos, cos)[-1].R == 8
+    for bad in ((q, q[:1], w, cos, cos), (q, q[..., :8], w, cos, cos), (q, q, w[:8], cos, cos), (q, q, w, cos[0], cos[0]), (q[0], q[0], w, cos, cos), (q, q, w, cos, None),
+                (q, q, torch.zeros(32)[::2], cos, cos), (q, q, w, cos, cos[:4]), (q, q, w, cos, cos, torch.zeros(2, 7, dtype=torch.int32)),
+                (q, q, w, torch.zeros(8, 8)[:, ::2], cos)):
         with pytest.raises(ValueError):
-            tfno._head_norm_desc(q.dtype, *layouts(qq, kk, qq, kk), *more, *layouts(ww, ww), None, None, *layouts(cc, cc), 1e-6, False)
-    with pytest.raises(ValueError):
-        tfno._head_norm_desc(q.dtype, *layouts(q, q, q, q), *more, *layouts(w, w), None, None, tfno._layout(cos), None, 1e-6, False)
-    s = torch.zeros(3, 4, 16, 24)
-    assert tfno._step_desc(q.dtype, *layouts(q[:, 0], q[:, 0], v[:, 0], v[:, 0], g[:, 0], g[:, 0]), s.shape, None)[0].T == 1
-    for bad in (s[:, :2], s[0], s[..., :8]):
+            norm(*bad)
+    with pytest.raises(TypeError):
+        norm(q, q, w, cos, cos, torch.zeros(2, 8))
+    s, slots = torch.zeros(3, 4, 16, 24), torch.zeros(2, dtype=torch.int32)
+
+    def step(states, slots=None, o=v[:, 0], beta=g[:, 0]):
+        return tfno._step_plan(*plans(q[:, 0], q[:, 0], v[:, 0], o, g[:, 0], beta, states, slots), None)
+
+    assert step(s, slots)[-1].T == 1
+    for bad in ((s[:, :2],), (s[0],), (s[..., :8],), (s, torch.zeros(3, dtype=torch.int32)), (s, slots, v[:1, 0]), (s, slots, v[:, 0], g[:, 0, :2]), (s.transpose(2, 3).contiguous(),)):
         with pytest.raises(ValueError):
-            tfno._step_desc(q.dtype, *layouts(q[:, 0], q[:, 0], v[:, 0], v[:, 0], g[:, 0], g[:, 0]), bad.shape, None)
+            step(*bad)
+    with pytest.raises(TypeError):
+        step(s, torch.zeros(2))
