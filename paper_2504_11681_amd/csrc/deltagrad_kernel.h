@@ -22,7 +22,8 @@ namespace tfno {
 template <class E, int KB>
 struct BackwardLds : ScanLds<DeltaUnits<E, KB>::Q + 1 + 2 * DeltaUnits<E, KB>::TRI * DELTA_PM, DeltaUnits<E, KB>::KEY_TAPE - DeltaUnits<E, KB>::KT> {};
 
-template <class E, int KB>
+// EFFECTS: what each segment but the first adds to the gradient of the state before it, without anything else.
+template <class E, int KB, bool EFFECTS>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan_back(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
     typedef DeltaUnits<E, KB> U;
@@ -34,16 +35,21 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int block = id % blocks_per_head, head = id / blocks_per_head;
+    const int some = EFFECTS ? mem.segments - 1 : mem.segments;
+    const int block = id % blocks_per_head, part = id / blocks_per_head, segment = part % some + (EFFECTS ? 1 : 0), head = part / some;
+    const long long at = (long long)head * mem.segments + segment;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
-    const int len = sequence_length(a, b), n = (len + L - 1) / L;
+    const int len = sequence_length(a, b), all = (len + L - 1) / L;
+    const int begin = segment * mem.segment_chunks, n = all < begin + mem.segment_chunks ? all : begin + mem.segment_chunks;   // chunks begin .. n - 1
     const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
     const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
     const int col0 = (block * waves + wave) * 16, col = col0 + m;
     const bool all_columns = a.Dv % 32 == 0;
 
     floatx4 S[DT];          // dS', laid out as the state is
-    load_state<DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
+    if (EFFECTS) load_state<DT>(nullptr, 0, 0, col, g, S);
+    else if (mem.segments > 1) load_state<DT>(mem.segment_d_states + at * U::DKP * mem.dvp, U::DKP, mem.dvp, col, g, S);
+    else load_state<DT>(a.d_final ? a.d_final + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + h * a.sdo.head);
     E *dv = (E *)a.dv + (b * a.sdv.batch + h * a.sdv.head);
     const unsigned at_do = (8 * g * (unsigned)a.sdo.token + (col < a.Dv ? col : 0)) * sizeof(E);
@@ -62,13 +68,13 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     };
     E next[LB][8];
     auto load_do = [&](int chunk) { load_columns<E, LB>(d_o + (long long)chunk * L * a.sdo.token, a.sdo.token, at_do, g, len - chunk * L, next); };
-    if (n > 0) {
+    if (n > begin) {
         load_first(n - 1, (n - 1) & 1);
         if (Lds::DOUBLE) load_last(n - 1, (n - 1) & 1);
         load_do(n - 1);
     }
     __builtin_amdgcn_s_waitcnt(0);
-    for (int chunk = n - 1; chunk >= 0; --chunk) {
+    for (int chunk = n - 1; chunk >= begin; --chunk) {
         const int t0 = chunk * L, parity = chunk & 1;
         const unsigned char *ldsK = Lds::first(lds, parity), *ldsG = ldsK + K_UNITS * 1024, *ldsPT = ldsG + 1024, *ldsTT = ldsPT + TRI_UNITS * 1024,
                             *ldsKT = Lds::last(lds, parity);
@@ -80,14 +86,14 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         for (int s = 0; s < LB; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[s][e] = to_float(next[s][e]);
-        const int before = chunk > 0 ? chunk - 1 : 0;
+        const int before = chunk > begin ? chunk - 1 : begin;
         if (!Lds::DOUBLE) load_last(chunk, parity);
-        if (chunk > 0) {
+        if (chunk > begin) {
             load_first(before, parity ^ 1);
             if (Lds::DOUBLE) load_last(before, parity ^ 1);
         }
         load_do(before);
-        if (col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        if (!EFFECTS && col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
         // K dS' and P' dO, a pair of tiles of tokens at a time
         floatx4 KS[NT], PO_[NT];
         {
@@ -201,7 +207,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             }
         }
         if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);      // what the next chunk needs is there; the stores have its time
-        if (col0 < mem.dvp) {
+        if (!EFFECTS && col0 < mem.dvp) {
             store_tiles<NT>(mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Y);
             const bool whole_chunk = t0 + L <= a.T;
 #pragma unroll
@@ -213,9 +219,14 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 }
         }
     }
-    for (int t = n * L + g; t < a.T; t += 4)
+    if (EFFECTS) {
+        if (col0 < mem.dvp) store_tiles<DT>(mem.back_effects + at * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        return;
+    }
+    const int last = segment + 1 < mem.segments ? (begin + mem.segment_chunks) * L : a.T;
+    for (int t = (n > begin ? n : begin) * L + g; t < last; t += 4)
         if (col < a.Dv) store_element(dv + t * a.sdv.token + col, 0.0f);
-    if (a.d_initial) store_state<DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
+    if (a.d_initial && segment == 0) store_state<DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
 }
 
 // One workgroup for a chunk of a key head, a wave for each 16 tokens of it.

@@ -1,11 +1,25 @@
 // Launches of the gated delta rule over sequences.
 #include "deltagrad_kernel.h"
 
+#include <algorithm>
+
 namespace tfno {
 
 namespace {
 
+constexpr int SEGMENT_MAX_WAVES = 512, SEGMENT_WAVES = 2048, SEGMENT_MIN_CHUNKS = 8;
+
 size_t pad(size_t n) { return (n + 255) / 256 * 256; }
+
+// Segments of a head's chunks that are walked through at once.  They cost: the effect of each is walked through beforehand with Dk more columns.
+// So they are for few heads, whose columns leave most of the chip idle, and many chunks.
+int segments_of(const DeltaArgs &a, int chunks)
+{
+    const long long waves = (long long)a.B * a.Hv * ((a.Dv + 31) / 32 * 2);
+    if (waves == 0 || waves > SEGMENT_MAX_WAVES) return 1;
+    const long long n = std::min<long long>(SEGMENT_WAVES / waves, chunks / SEGMENT_MIN_CHUNKS);
+    return n < 2 ? 1 : (int)n;
+}
 
 // Layout of the tape, or of the workspace of a forward pass without one; `base` may be NULL for its size alone.
 template <class E, int KB>
@@ -16,7 +30,9 @@ size_t forward_memory(const DeltaArgs &a, unsigned char *base, bool tape, DeltaM
     m->dvp = (a.Dv + 31) / 32 * 32;
     m->key_units = tape ? U::KEY_TAPE : U::KEY_FORWARD;
     m->value_units = tape ? U::VALUE_TAPE : U::VALUE_FORWARD;
-    const size_t keys = (size_t)a.B * a.Hk * m->chunks, values = (size_t)a.B * a.Hv * m->chunks;
+    m->segments = segments_of(a, m->chunks);
+    m->segment_chunks = (m->chunks + m->segments - 1) / m->segments;
+    const size_t keys = (size_t)a.B * a.Hk * m->chunks, values = (size_t)a.B * a.Hv * m->chunks, parts = (size_t)a.B * a.Hv * m->segments;
     size_t at = 0;
     m->key = base + at, at += keys * m->key_units * 1024;
     m->value = base + at, at += values * m->value_units * 1024;
@@ -25,16 +41,25 @@ size_t forward_memory(const DeltaArgs &a, unsigned char *base, bool tape, DeltaM
         m->states = (float *)(base + at), at += values * U::DKP * m->dvp * sizeof(float);
         m->errors = (float *)(base + at), at += values * U::L * m->dvp * sizeof(float);
     }
+    if (m->segments > 1) {
+        m->effects = (float *)(base + at), at += parts * U::DKP * (m->dvp + U::DKP) * sizeof(float);
+        m->segment_states = (float *)(base + at), at += parts * U::DKP * m->dvp * sizeof(float);
+    }
     return at;
 }
 template <class E, int KB>
 size_t backward_memory(const DeltaArgs &a, unsigned char *base, DeltaMemory *m)
 {
     typedef DeltaUnits<E, KB> U;
-    const size_t values = (size_t)a.B * a.Hv * ((a.T + U::L - 1) / U::L), dvp = (a.Dv + 31) / 32 * 32;
+    const int chunks = (a.T + U::L - 1) / U::L, segments = segments_of(a, chunks);
+    const size_t values = (size_t)a.B * a.Hv * chunks, dvp = (a.Dv + 31) / 32 * 32, parts = (size_t)a.B * a.Hv * segments;
     size_t at = 0;
     m->d_states = (float *)(base + at), at += values * U::DKP * dvp * sizeof(float);
     m->d_values = (float *)(base + at), at += values * U::L * dvp * sizeof(float);
+    if (segments > 1) {
+        m->back_effects = (float *)(base + at), at += parts * U::DKP * dvp * sizeof(float);
+        m->segment_d_states = (float *)(base + at), at += parts * U::DKP * dvp * sizeof(float);
+    }
     return at;
 }
 
@@ -45,34 +70,53 @@ bool rows_of_8(const void *p, const Strides &s, bool bf16)
     return ((uintptr_t)p & 15) == 0 && s.batch % unit == 0 && s.token % unit == 0 && s.head % unit == 0;
 }
 
-// Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few heads.
+// Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few.
 struct ScanShape { int waves, blocks; };
-ScanShape scan_shape(const DeltaArgs &a, int dvp)
+ScanShape scan_shape(long long walks, int tiles)
 {
-    const int tiles = dvp / 16;
-    const long long heads = (long long)a.B * a.Hv;
     ScanShape s{SCAN_THREADS / 64, 0};
-    while (s.waves > 2 && (heads * tiles < 256LL * s.waves || s.waves > tiles)) s.waves >>= 1;
+    while (s.waves > 2 && (walks * tiles < 256LL * s.waves || s.waves > tiles)) s.waves >>= 1;
     s.blocks = (tiles + s.waves - 1) / s.waves;
     return s;
 }
 
+template <class... Kernels>
+hipError_t allow_lds(LdsLimitOnce &limit, int bytes, Kernels... k) { return limit.set({(const void *)k...}, bytes); }
+
 template <class E, int KB, bool TAPE>
-hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
+hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
-    constexpr int bytes = ForwardLds<E, KB>::BYTES;
-    static LdsLimitOnce limit;
-    if (hipError_t e = limit.set({(const void *)k_delta_scan<E, KB, TAPE>}, bytes); e != hipSuccess) return e;
-    k_delta_scan<E, KB, TAPE><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    constexpr int bytes = ForwardLds<E, KB>::BYTES, effect_bytes = EffectLds<E, KB>::BYTES;
+    static LdsLimitOnce limit, effect_limit;
+    const long long heads = (long long)a.B * a.Hv;
+    if (m.segments > 1) {
+        if (hipError_t e = allow_lds(effect_limit, effect_bytes, k_delta_effects<E, KB>); e != hipSuccess) return e;
+        const int segments = TAPE ? m.segments : m.segments - 1;       // the last one's effect is of use to the backward pass alone
+        const ScanShape sh = scan_shape(heads * segments, m.dvp / 16 + 2 * KB);
+        k_delta_effects<E, KB><<<(unsigned)(heads * segments * sh.blocks), 64 * sh.waves, effect_bytes, s>>>(a, m, sh.blocks, segments);
+        const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
+        k_delta_join<KB, false><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
+    }
+    if (hipError_t e = allow_lds(limit, bytes, k_delta_scan<E, KB, TAPE>); e != hipSuccess) return e;
+    const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
+    k_delta_scan<E, KB, TAPE><<<(unsigned)(heads * m.segments * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 template <class E, int KB>
-hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, const ScanShape &sh, hipStream_t s)
+hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
     constexpr int bytes = BackwardLds<E, KB>::BYTES;
     static LdsLimitOnce limit;
-    if (hipError_t e = limit.set({(const void *)k_delta_scan_back<E, KB>}, bytes); e != hipSuccess) return e;
-    k_delta_scan_back<E, KB><<<(unsigned)(a.B * a.Hv * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    if (hipError_t e = allow_lds(limit, bytes, k_delta_scan_back<E, KB, false>, k_delta_scan_back<E, KB, true>); e != hipSuccess) return e;
+    const long long heads = (long long)a.B * a.Hv;
+    if (m.segments > 1) {
+        const ScanShape sh = scan_shape(heads * (m.segments - 1), m.dvp / 16);
+        k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+        const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
+        k_delta_join<KB, true><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
+    }
+    const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
+    k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 
@@ -90,8 +134,7 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s)
     if (grid && tape) k_delta_prepare<E, KB, true><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const ScanShape sh = scan_shape(a, m.dvp);
-    return tape ? scan<E, KB, true>(a, m, sh, s) : scan<E, KB, false>(a, m, sh, s);
+    return tape ? scan<E, KB, true>(a, m, s) : scan<E, KB, false>(a, m, s);
 }
 
 template <class E, int KB>
@@ -103,8 +146,7 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s)
     backward_memory<E, KB>(a, a.workspace, &m);
     DeltaVec vec{};
     vec.d_o = rows_of_8(a.d_o, a.sdo, a.bf16), vec.dq = rows_of_8(a.dq, a.sdq, a.bf16), vec.dk = rows_of_8(a.dk, a.sdk, a.bf16);
-    const ScanShape sh = scan_shape(a, m.dvp);
-    if (hipError_t e = scan_back<E, KB>(a, m, sh, s); e != hipSuccess) return e;
+    if (hipError_t e = scan_back<E, KB>(a, m, s); e != hipSuccess) return e;
     if (m.chunks == 0) return hipSuccess;
     k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 64 * U::NT, 0, s>>>(a, m, vec);
     return hipGetLastError();

@@ -216,13 +216,19 @@ struct DeltaMemory {
     float *states, *errors;          // tape: S before each chunk [DKP][DVP], E [L][DVP]
     float *d_states, *d_values;      // backward: gradient of the state after each chunk, Y [L][DVP]
     int chunks, dvp, key_units, value_units;
+    // Where there are few heads, the chunks of a head are walked through in segments at once: a segment's effect on the state is S -> A S + B.
+    int segments, segment_chunks;
+    float *effects;                  // [b][hv][segment][DKP][DVP + DKP]: B and A (tape)
+    float *segment_states;           // [b][hv][segment][DKP][DVP]: the state before each
+    float *back_effects;             // backward: [b][hv][segment][DKP][DVP]: the gradient that a segment itself adds to that of the state before it
+    float *segment_d_states;         // backward: the gradient of the state after each segment
     bool vec_o;                      // rows of o take four elements at a time
 };
 
 __device__ __forceinline__ int sequence_length(const DeltaArgs &a, int b)
 {
     if (!a.lengths) return a.T;
-    const int n = a.lengths[b];
+    const int n = __builtin_amdgcn_readfirstlane(a.lengths[b]);
     return n < 0 ? 0 : n < a.T ? n : a.T;
 }
 
@@ -546,6 +552,13 @@ __device__ __forceinline__ void units_to_lds(const unsigned char *from, unsigned
     }
 }
 
+// An address that is the same for all lanes, in scalar registers.
+template <class T>
+__device__ __forceinline__ T *uniform(T *p)
+{
+    const uintptr_t u = (uintptr_t)p;
+    return (T *)((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
+}
 // The element `bytes` behind a uniform address: 32 bits a lane, so that the address stays scalar.
 template <class E>
 __device__ __forceinline__ const E *behind(const E *p, unsigned bytes) { return (const E *)((const char *)p + bytes); }
@@ -559,15 +572,12 @@ template <class E, int LB>
 __device__ __forceinline__ void load_columns(const E *p, long long token, unsigned at, int g, int count, E (&u)[LB][8])
 {
     if (count >= 32 * LB) {
-        asm("" : "+v"(at));
+        asm("" : "+v"(at));          // its extension to 64 bits belongs to the loads' addresses and not in front of the loop
+        const E *q = uniform(p);
 #pragma unroll
-        for (int s = 0; s < LB; ++s)
+        for (int s = 0; s < LB; ++s, q += 24 * token)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const E *q = p + (32 * s + e) * token;
-                asm("" : "+s"(q));
-                u[s][e] = *behind(q, at);
-            }
+            for (int e = 0; e < 8; ++e, q += token) u[s][e] = *behind(q, at);
     } else {
         p = behind(p, at) - 8 * g * token;
 #pragma unroll
@@ -659,16 +669,18 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);       // the blocks of a head, and heads that share keys, on one XCD
-    const int block = id % blocks_per_head, head = id / blocks_per_head;
+    const int block = id % blocks_per_head, at = id / blocks_per_head, segment = at % mem.segments, head = at / mem.segments;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
-    const int len = sequence_length(a, b), n = (len + L - 1) / L;
+    const int len = sequence_length(a, b), all = (len + L - 1) / L;
+    const int begin = segment * mem.segment_chunks, n = all < begin + mem.segment_chunks ? all : begin + mem.segment_chunks;   // chunks begin .. n - 1
     const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
     const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
     const int col0 = (block * waves + wave) * 16, col = col0 + m;
     const bool all_columns = a.Dv % 32 == 0;
 
     floatx4 S[DT];
-    load_state<DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
+    if (mem.segments > 1) load_state<DT>(mem.segment_states + (long long)at * U::DKP * mem.dvp, U::DKP, mem.dvp, col, g, S);
+    else load_state<DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
     E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
     const unsigned at_v = (8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0)) * sizeof(E);
@@ -686,10 +698,10 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     };
     E next[LB][8];
     auto load_v = [&](int chunk) { load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next); };
-    if (n > 0) {
-        load_first(0, 0);
-        if (Lds::DOUBLE) load_last(0, 0);
-        load_v(0);
+    if (n > begin) {
+        load_first(begin, begin & 1);
+        if (Lds::DOUBLE) load_last(begin, begin & 1);
+        load_v(begin);
     }
     Frag<PM> Sf[KB];            // the state as operand
     auto split_s = [&](int kb) {
@@ -701,7 +713,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) split_s(kb);
     __builtin_amdgcn_s_waitcnt(0);
-    for (int chunk = 0; chunk < n; ++chunk) {
+    for (int chunk = begin; chunk < n; ++chunk) {
         const int t0 = chunk * L, parity = chunk & 1;
         const unsigned char *ldsA = Lds::first(lds, parity), *ldsB = ldsA + A_UNITS * 1024, *ldsKT = Lds::last(lds, parity);
         const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
@@ -894,9 +906,205 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         }
     }
     // past the sequence's end
-    for (int t = n * L + g; t < a.T; t += 4)
+    const int last = segment + 1 < mem.segments ? (begin + mem.segment_chunks) * L : a.T;
+    for (int t = (n > begin ? n : begin) * L + g; t < last; t += 4)
         if (col < a.Dv) store_element(o + t * a.so.token + col, 0.0f);
-    if (a.final_state) store_state<DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
+    if (a.final_state && segment + 1 == mem.segments) store_state<DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
+}
+
+// LDS of the kernel below: K, gates, T | K'
+template <class E, int KB>
+struct EffectLds : ScanLds<DeltaUnits<E, KB>::Q + DeltaUnits<E, KB>::P, DeltaUnits<E, KB>::QT - DeltaUnits<E, KB>::KT> {};
+
+// The effect of each segment on the state, by the same walk without outputs: columns of B start from zeros, columns of A from the identity, without values.
+template <class E, int KB>
+__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_effects(DeltaArgs a, DeltaMemory mem, int blocks_per_segment,
+                                                                                                        int segments)
+{
+    typedef DeltaUnits<E, KB> U;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PM = DELTA_PM;
+    typedef EffectLds<E, KB> Lds;
+    constexpr int K_UNITS = U::Q, VALUE_UNITS = U::P;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int m = lane & 15, g = lane >> 4;
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int block = id % blocks_per_segment, at = id / blocks_per_segment, segment = at % segments, head = at / segments;
+    const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
+    const int len = sequence_length(a, b), all = (len + L - 1) / L;
+    const int begin = segment * mem.segment_chunks, n = all < begin + mem.segment_chunks ? all : begin + mem.segment_chunks;
+    const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
+    const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
+    const int width = mem.dvp + U::DKP, col0 = (block * waves + wave) * 16, col = col0 + m;
+    const bool of_values = col0 < mem.dvp;
+
+    floatx4 S[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][r] = tile_index(t, 4 * g + r) == col - mem.dvp ? 1.0f : 0.0f;
+    const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
+    const unsigned at_v = (8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0)) * sizeof(E);
+
+    auto load_first = [&](int chunk, int parity) {
+        unsigned char *to = Lds::first(lds, parity);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, wave, waves, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + K_UNITS * 1024, VALUE_UNITS, wave, waves, lane);
+    };
+    auto load_last = [&](int chunk, int parity) {
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, wave, waves, lane);
+    };
+    E next[LB][8] = {};
+    auto load_v = [&](int chunk) {
+        if (!of_values) return;
+        load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next);
+        mask_columns<E, LB>(next, false, col < a.Dv, g, len - chunk * L);
+    };
+    if (n > begin) {
+        load_first(begin, begin & 1);
+        if (Lds::DOUBLE) load_last(begin, begin & 1);
+        load_v(begin);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    for (int chunk = begin; chunk < n; ++chunk) {
+        const int parity = chunk & 1;
+        const unsigned char *ldsK = Lds::first(lds, parity), *ldsB = ldsK + K_UNITS * 1024, *ldsKT = Lds::last(lds, parity);
+        const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
+        __syncthreads();
+        const int after = chunk + 1 < n ? chunk + 1 : chunk;
+        if (!Lds::DOUBLE) load_last(chunk, parity);
+        if (chunk + 1 < n) {
+            load_first(after, parity ^ 1);
+            if (Lds::DOUBLE) load_last(after, parity ^ 1);
+        }
+        float x[LB][8];
+#pragma unroll
+        for (int s = 0; s < LB; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = to_float(next[s][e]);
+        load_v(after);
+        floatx4 KS[NT];
+        {
+            floatx4 *ks[NT];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) KS[i] = floatx4{0, 0, 0, 0}, ks[i] = &KS[i];
+            Frag<PI> kf[2][NT];
+            auto read = [&](int kb) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) kf[kb & 1][i] = load_frag<PI>(ldsK + (i * KB + kb) * PI * 1024, lane);
+            };
+            read(0);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                if (kb + 1 < KB) read(kb + 1);
+                Frag<PM> Sf;
+                set_four<PM>(Sf, 0, {S[2 * kb][0], S[2 * kb][1], S[2 * kb][2], S[2 * kb][3]});
+                set_four<PM>(Sf, 1, {S[2 * kb + 1][0], S[2 * kb + 1][1], S[2 * kb + 1][2], S[2 * kb + 1][3]});
+                mm_many<3, false>(kf[kb & 1], Sf, ks, NoWeave());
+            }
+        }
+        Frag<PM> W[LB];
+        {
+            Frag<PM> R[LB];
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                float decay[8], u[8];
+                load_gates(gates->decay + 32 * s + 8 * g, decay);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[2 * s + (e >> 2)][e & 3], x[s][e]);
+                R[s] = make_frag<PM>(u);
+            }
+#pragma unroll
+            for (int s = 0; s < LB; ++s) {
+                Frag<PM> tf[LB][2];
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) tf[kb][p] = load_frag<PM>(ldsB + (U::T + U::lower(2 * s + p, kb) * PM) * 1024, lane);
+                floatx4 Ee[2] = {floatx4{0, 0, 0, 0}, floatx4{0, 0, 0, 0}}, *to[2] = {&Ee[0], &Ee[1]};
+#pragma unroll
+                for (int kb = 0; kb <= s; ++kb) mm_many<3, false>(tf[kb], R[kb], to, NoWeave());
+                float be[8], left[8], u[8];
+                load_gates(gates->beta + 32 * s + 8 * g, be);
+                load_gates(gates->left + 32 * s + 8 * g, left);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = left[e] * (be[e] * Ee[e >> 2][e & 3]);
+                W[s] = make_frag<PM>(u);
+            }
+        }
+        const float whole = gates->whole;
+        if (!Lds::DOUBLE) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+        }
+        {
+            Frag<PI> kf[2][2];
+            auto read = [&](int update) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) kf[update & 1][p] = load_frag<PI>(ldsKT + ((2 * (update / LB) + p) * LB + update % LB) * PI * 1024, lane);
+            };
+            read(0);
+#pragma unroll
+            for (int update = 0; update < KB * LB; ++update) {
+                const int t = 2 * (update / LB), kb = update % LB;
+                if (update + 1 < KB * LB) read(update + 1);
+                if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
+                floatx4 *to[2] = {&S[t], &S[t + 1]};
+                mm_many<3, false>(kf[update & 1], W[kb], to, NoWeave());
+            }
+        }
+        if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
+    }
+    if (col0 < width) store_tiles<DT>(mem.effects + ((long long)head * mem.segments + segment) * U::DKP * width, width, (8 * g * (unsigned)width + col) * 4, S);
+}
+
+// The states before the segments, one after the other: S <- A S + B.  BACK: the gradients of the states after them, from the last one:
+// dS <- A' dS + b.  A workgroup takes up to eight tiles of columns of a head, and splits A for them in LDS.
+template <int KB, bool BACK>
+__global__ __launch_bounds__(SCAN_THREADS) void k_delta_join(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+{
+    constexpr int DT = 2 * KB, DKP = 32 * KB, PM = DELTA_PM;
+    __shared__ __attribute__((aligned(1024))) unsigned char As[DT * KB * PM * 1024];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int m = lane & 15, g = lane >> 4, block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int width = mem.dvp + DKP, col0 = (block * waves + wave) * 16, col = col0 + m;
+    const float *from = BACK ? a.d_final : a.initial;
+    floatx4 S[DT];
+    load_state<DT>(from ? from + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
+    for (int step = 0; step < mem.segments; ++step) {
+        const int segment = BACK ? mem.segments - 1 - step : step;
+        const long long at = (long long)head * mem.segments + segment;
+        if (col0 < mem.dvp)
+            store_tiles<DT>((BACK ? mem.segment_d_states : mem.segment_states) + at * DKP * mem.dvp, mem.dvp, (8 * g * (unsigned)mem.dvp + col) * 4, S);
+        if (step + 1 == mem.segments) break;
+        const float *A = mem.effects + at * DKP * width + mem.dvp;
+        floatx4 sum[DT];
+        const float *B = BACK ? mem.back_effects + at * DKP * mem.dvp : mem.effects + at * DKP * width;
+        load_state<DT>(B, DKP, BACK ? mem.dvp : width, col < mem.dvp ? col : 0, g, sum);
+        Frag<PM> Sf[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            set_four<PM>(Sf[kb], 0, {S[2 * kb][0], S[2 * kb][1], S[2 * kb][2], S[2 * kb][3]});
+            set_four<PM>(Sf[kb], 1, {S[2 * kb + 1][0], S[2 * kb + 1][1], S[2 * kb + 1][2], S[2 * kb + 1][3]});
+        }
+        __syncthreads();
+        for (int f = wave; f < DT * KB; f += waves) {
+            const int row = tile_index(f / KB, m), k = 32 * (f % KB) + 8 * g;
+            store_frag<PM>(As + f * PM * 1024, lane, BACK ? column_frag<PM>(A + k * width + row, width) : row_frag<PM>(A + row * width + k));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int t = 0; t < DT; t += 2) {
+                const Frag<PM> f[2] = {load_frag<PM>(As + (t * KB + kb) * PM * 1024, lane), load_frag<PM>(As + ((t + 1) * KB + kb) * PM * 1024, lane)};
+                floatx4 *to[2] = {&sum[t], &sum[t + 1]};
+                mm_many<3, false>(f, Sf[kb], to, NoWeave());
+            }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) S[t] = sum[t];
+    }
 }
 
 }  // namespace tfno
