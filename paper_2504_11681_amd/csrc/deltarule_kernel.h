@@ -538,20 +538,6 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------
-// Units of 1024 bytes from global memory to LDS, shared out over the waves of the workgroup; they are there after the wave's own
-// loads_done() and a barrier.
-__device__ __forceinline__ void units_to_lds(const unsigned char *from, unsigned char *to, int units, int wave, int waves, int lane)
-{
-    const unsigned at = lane * 16;          // a uniform address and 32 bits a lane: no vector instruction but the load
-    for (int u = wave; u < units; u += waves) {
-        const unsigned char *p = from + u * 1024;
-        unsigned off = at;
-        asm("" : "+s"(p), "+v"(off));
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned int *)(p + off),
-                                         (__attribute__((address_space(3))) unsigned int *)(to + u * 1024), 16, 0, 0);
-    }
-}
-
 // An address that is the same for all lanes, in scalar registers.
 template <class T>
 __device__ __forceinline__ T *uniform(T *p)
@@ -559,6 +545,19 @@ __device__ __forceinline__ T *uniform(T *p)
     const uintptr_t u = (uintptr_t)p;
     return (T *)((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
 }
+// Units of 1024 bytes from global memory to LDS, shared out over the waves of the workgroup; they are there after each wave's own wait for its
+// loads (s_waitcnt 0) and a barrier.  In assembly, because the compiler takes every later read of LDS for one that may need them and would wait
+// for the next chunk's blocks before the first product of this one (B 1, T 16384, 8 heads of 128: XXX us).  The instruction has no result register.
+__device__ __forceinline__ void units_to_lds(const unsigned char *from, const unsigned char *to, int units, int wave, int waves, int lane)
+{
+    const unsigned at = lane * 16;          // a uniform address and 32 bits a lane
+    from = uniform(from);
+    unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
+    lds += wave * 1024, from += wave * 1024;
+    for (int u = wave; u < units; u += waves, lds += waves * 1024, from += waves * 1024)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(at), "s"(from));
+}
+
 // The element `bytes` behind a uniform address: 32 bits a lane, so that the address stays scalar.
 template <class E>
 __device__ __forceinline__ const E *behind(const E *p, unsigned bytes) { return (const E *)((const char *)p + bytes); }
