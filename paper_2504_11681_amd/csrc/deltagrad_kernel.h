@@ -53,7 +53,9 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + h * a.sdo.head);
     E *dv = (E *)a.dv + (b * a.sdv.batch + h * a.sdv.head);
     const unsigned at_do = (8 * g * (unsigned)a.sdo.token + (col < a.Dv ? col : 0)) * sizeof(E);
-    const unsigned at_dv = (8 * g * (unsigned)a.sdv.token + col) * sizeof(E), at_tape = (8 * g * (unsigned)mem.dvp + col) * 4;
+    const unsigned at_tape = tiles_at(mem.dvp, col0, lane);
+    const int lane_token = 8 * g + (lane & 3), lane_col = col0 + (lane & 12);       // of the transposed tiles: four columns of a token
+    const unsigned at_dv = (lane_token * (unsigned)a.sdv.token + lane_col) * sizeof(E);
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             if (Lds::DOUBLE) load_last(before, parity ^ 1);
         }
         load_do(before);
-        if (!EFFECTS && col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        if (!EFFECTS && col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         // K dS' and P' dO, a pair of tiles of tokens at a time
         floatx4 KS[NT], PO_[NT];
         {
@@ -208,19 +210,26 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         }
         if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);      // what the next chunk needs is there; the stores have its time
         if (!EFFECTS && col0 < mem.dvp) {
-            store_tiles<NT>(mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Y);
-            const bool whole_chunk = t0 + L <= a.T;
+            store_tiles<NT>(mem.d_values + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, lane, Y);
+            const bool plain = mem.vec_dv && t0 + L <= a.T && (all_columns || col0 + 16 <= a.Dv);
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+            for (int i = 0; i < NT; ++i) {
+                const floatx4 y = quad_transpose(Y[i], lane);
+                const float u[4] = {y[0], y[1], y[2], y[3]};
+                const int row = t0 + 32 * (i >> 1) + 4 * (i & 1);
+                E *to = dv + row * a.sdv.token;
+                if (plain) {
+                    if (col0 < a.Dv) store4(behind(to, at_dv), u);
+                } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = t0 + 32 * (i >> 1) + 4 * (i & 1) + r;
-                    if (col < a.Dv && (whole_chunk || row + 8 * g < a.T)) store_element(behind(dv + row * a.sdv.token, at_dv), Y[i][r]);
+                    for (int r = 0; r < 4; ++r)
+                        if (row + lane_token < a.T && lane_col + r < a.Dv) store_element(behind(to, at_dv) + r, u[r]);
                 }
+            }
         }
     }
     if (EFFECTS) {
-        if (col0 < mem.dvp) store_tiles<DT>(mem.back_effects + at * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        if (col0 < mem.dvp) store_tiles<DT>(mem.back_effects + at * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         return;
     }
     const int last = segment + 1 < mem.segments ? (begin + mem.segment_chunks) * L : a.T;

@@ -7,7 +7,7 @@ namespace tfno {
 
 namespace {
 
-constexpr int SEGMENT_MAX_WAVES = 512, SEGMENT_WAVES = 2048, SEGMENT_MIN_CHUNKS = 8;
+constexpr int SEGMENT_MAX_WAVES = 256, SEGMENT_WAVES = 2048, SEGMENT_MIN_CHUNKS = 8;
 
 size_t pad(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -70,6 +70,12 @@ bool rows_of_8(const void *p, const Strides &s, bool bf16)
     return ((uintptr_t)p & 15) == 0 && s.batch % unit == 0 && s.token % unit == 0 && s.head % unit == 0;
 }
 
+// Rows that are written four elements at a time.
+bool rows_of_4(const void *p, const Strides &s, int columns, bool bf16)
+{
+    return columns % 4 == 0 && ((uintptr_t)p & (bf16 ? 7 : 15)) == 0 && s.batch % 4 == 0 && s.token % 4 == 0 && s.head % 4 == 0;
+}
+
 // Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few.
 struct ScanShape { int waves, blocks; };
 ScanShape scan_shape(long long walks, int tiles)
@@ -129,7 +135,7 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s)
     forward_memory<E, KB>(a, tape ? a.tape : a.workspace, tape, &m);
     DeltaVec vec{};
     vec.q = rows_of_8(a.q, a.sq, a.bf16), vec.k = rows_of_8(a.k, a.sk, a.bf16);
-    m.vec_o = a.Dv % 4 == 0 && ((uintptr_t)a.o & (a.bf16 ? 7 : 15)) == 0 && a.so.batch % 4 == 0 && a.so.token % 4 == 0 && a.so.head % 4 == 0;
+    m.vec_o = rows_of_4(a.o, a.so, a.Dv, a.bf16);
     const unsigned grid = (unsigned)(a.B * a.Hv * m.chunks);
     if (grid && tape) k_delta_prepare<E, KB, true><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
@@ -146,6 +152,7 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s)
     backward_memory<E, KB>(a, a.workspace, &m);
     DeltaVec vec{};
     vec.d_o = rows_of_8(a.d_o, a.sdo, a.bf16), vec.dq = rows_of_8(a.dq, a.sdq, a.bf16), vec.dk = rows_of_8(a.dk, a.sdk, a.bf16);
+    m.vec_dv = rows_of_4(a.dv, a.sdv, a.Dv, a.bf16);
     if (hipError_t e = scan_back<E, KB>(a, m, s); e != hipSuccess) return e;
     if (m.chunks == 0) return hipSuccess;
     k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 64 * U::NT, 0, s>>>(a, m, vec);

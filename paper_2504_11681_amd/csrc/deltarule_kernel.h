@@ -222,7 +222,7 @@ struct DeltaMemory {
     float *segment_states;           // [b][hv][segment][DKP][DVP]: the state before each
     float *back_effects;             // backward: [b][hv][segment][DKP][DVP]: the gradient that a segment itself adds to that of the state before it
     float *segment_d_states;         // backward: the gradient of the state after each segment
-    bool vec_o;                      // rows of o take four elements at a time
+    bool vec_o, vec_dv;              // rows of o and of the gradient of v take four elements at a time
 };
 
 __device__ __forceinline__ int sequence_length(const DeltaArgs &a, int b)
@@ -627,14 +627,34 @@ __device__ __forceinline__ void store_state(float *p, int Dk, int Dv, int col, i
             if (d < Dk && col < Dv) p[d * Dv + col] = S[t][r];
         }
 }
-// Tiles of rows tile_index(t, 4 g + r) of a matrix of `stride` columns in the memory between the kernels; `at` = 8 g rows and the column, in bytes.
+// A 4 x 4 transposition in each group of four lanes: element r of lane j becomes element j of lane r.
+template <int CONTROL>
+__device__ __forceinline__ float quad_move(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ floatx4 quad_transpose(const floatx4 &x, int lane)
+{
+    const bool odd = lane & 1, high = lane & 2;
+    const float s0 = quad_move<0xB1>(odd ? x[0] : x[1]), s1 = quad_move<0xB1>(odd ? x[2] : x[3]);      // from the lane next to it
+    const float a0 = odd ? s0 : x[0], a1 = odd ? x[1] : s0, a2 = odd ? s1 : x[2], a3 = odd ? x[3] : s1;
+    const float u0 = quad_move<0x4E>(high ? a0 : a2), u1 = quad_move<0x4E>(high ? a1 : a3);            // from the other pair
+    return floatx4{high ? u0 : a0, high ? u1 : a1, high ? a2 : u0, high ? a3 : u1};
+}
+
+// Tiles of rows tile_index(t, 4 g + r) and columns m of a matrix of `stride` columns in the memory between the kernels, 16 bytes a lane: after the
+// transposition a lane has four columns of row j = lane % 4.  `at` = 8 g + j rows and the first of those columns, in bytes.  (One dword a row and
+// lane took four times the instructions: a chunk's states and errors were 8000 of the 23000 cycles of a training scan.)
 template <int N>
-__device__ __forceinline__ void store_tiles(float *p, int stride, unsigned at, const floatx4 (&x)[N])
+__device__ __forceinline__ void store_tiles(float *p, int stride, unsigned at, int lane, const floatx4 (&x)[N])
 {
 #pragma unroll
-    for (int t = 0; t < N; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) *behind(p + (32 * (t >> 1) + 4 * (t & 1) + r) * stride, at) = x[t][r];
+    for (int t = 0; t < N; ++t) *behind((floatx4 *)(p + (32 * (t >> 1) + 4 * (t & 1)) * stride), at) = quad_transpose(x[t], lane);
+}
+// The lane's offset for store_tiles.
+__device__ __forceinline__ unsigned tiles_at(int stride, int col0, int lane)
+{
+    return ((8 * (lane >> 4) + (lane & 3)) * stride + col0 + (lane & 12)) * 4;
 }
 
 // LDS of a scan, in units: what a chunk needs first (FIRST) for two chunks, what its last products need (LAST) for two where that fits into 160,
@@ -683,7 +703,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
     E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
     const unsigned at_v = (8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0)) * sizeof(E);
-    const unsigned at_tape = (8 * g * (unsigned)mem.dvp + col) * 4;
+    const unsigned at_tape = tiles_at(mem.dvp, col0, lane);
     const int lane_token = 8 * (m >> 2) + (m & 3);              // where tokens are columns: token lane_token of a tile, columns col0 + 4 g ..
     const unsigned at_o = (lane_token * (unsigned)a.so.token + 4 * g) * sizeof(E);
 
@@ -724,7 +744,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             load_first(after, parity ^ 1);
             if (Lds::DOUBLE) load_last(after, parity ^ 1);
         }
-        if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, S);
+        if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         region_end();
 
         // K S, tokens in rows; then (Q S)', tokens in columns, and meanwhile R = V - e^G K S as operand
@@ -829,7 +849,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int e = 0; e < 2; ++e) split_u(0, e);
         }
-        if (TAPE && col0 < mem.dvp) store_tiles<NT>(mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, Ee);
+        if (TAPE && col0 < mem.dvp) store_tiles<NT>(mem.errors + ((long long)head * mem.chunks + chunk) * L * mem.dvp, mem.dvp, at_tape, lane, Ee);
         if (!Lds::DOUBLE) {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
@@ -1055,7 +1075,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         }
         if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
     }
-    if (col0 < width) store_tiles<DT>(mem.effects + ((long long)head * mem.segments + segment) * U::DKP * width, width, (8 * g * (unsigned)width + col) * 4, S);
+    if (col0 < width) store_tiles<DT>(mem.effects + ((long long)head * mem.segments + segment) * U::DKP * width, width, tiles_at(width, col0, lane), lane, S);
 }
 
 // The states before the segments, one after the other: S <- A S + B.  BACK: the gradients of the states after them, from the last one:
@@ -1075,7 +1095,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void k_delta_join(DeltaArgs a, DeltaM
         const int segment = BACK ? mem.segments - 1 - step : step;
         const long long at = (long long)head * mem.segments + segment;
         if (col0 < mem.dvp)
-            store_tiles<DT>((BACK ? mem.segment_d_states : mem.segment_states) + at * DKP * mem.dvp, mem.dvp, (8 * g * (unsigned)mem.dvp + col) * 4, S);
+            store_tiles<DT>((BACK ? mem.segment_d_states : mem.segment_states) + at * DKP * mem.dvp, mem.dvp, tiles_at(mem.dvp, col0, lane), lane, S);
         if (step + 1 == mem.segments) break;
         const float *A = mem.effects + at * DKP * width + mem.dvp;
         floatx4 sum[DT];
