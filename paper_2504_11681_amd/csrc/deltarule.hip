@@ -77,7 +77,10 @@ bool rows_of_4(const void *p, const Strides &s, int columns, bool bf16)
 }
 
 // Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few.
-struct ScanShape { int waves, blocks; };
+struct ScanShape {
+    int waves, blocks;
+    int threads() const { return 64 * (waves < SCAN_THREADS / 64 ? waves + 1 : waves); }      // one more that loads
+};
 ScanShape scan_shape(long long walks, int tiles)
 {
     ScanShape s{SCAN_THREADS / 64, 0};
@@ -99,13 +102,13 @@ hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
         if (hipError_t e = allow_lds(effect_limit, effect_bytes, k_delta_effects<E, KB>); e != hipSuccess) return e;
         const int segments = TAPE ? m.segments : m.segments - 1;       // the last one's effect is of use to the backward pass alone
         const ScanShape sh = scan_shape(heads * segments, m.dvp / 16 + 2 * KB);
-        k_delta_effects<E, KB><<<(unsigned)(heads * segments * sh.blocks), 64 * sh.waves, effect_bytes, s>>>(a, m, sh.blocks, segments);
+        k_delta_effects<E, KB><<<(unsigned)(heads * segments * sh.blocks), sh.threads(), effect_bytes, s>>>(a, m, sh.blocks, segments);
         const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
         k_delta_join<KB, false><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
     }
     if (hipError_t e = allow_lds(limit, bytes, k_delta_scan<E, KB, TAPE>); e != hipSuccess) return e;
     const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
-    k_delta_scan<E, KB, TAPE><<<(unsigned)(heads * m.segments * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    k_delta_scan<E, KB, TAPE><<<(unsigned)(heads * m.segments * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 template <class E, int KB>
@@ -117,12 +120,12 @@ hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
     const long long heads = (long long)a.B * a.Hv;
     if (m.segments > 1) {
         const ScanShape sh = scan_shape(heads * (m.segments - 1), m.dvp / 16);
-        k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+        k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
         const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
         k_delta_join<KB, true><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
     }
     const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
-    k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), 64 * sh.waves, bytes, s>>>(a, m, sh.blocks);
+    k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 

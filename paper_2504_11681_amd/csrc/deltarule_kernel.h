@@ -672,6 +672,9 @@ struct ForwardLds : ScanLds<DeltaUnits<E, KB>::KT + DeltaUnits<E, KB>::VALUE_FOR
 
 constexpr int SCAN_THREADS = 512;
 
+// A workgroup of fewer than eight waves has one more, which does nothing but these loads: 75 cycles each of a wave that issues them, 40 for each of two waves
+// and a chunk of heads of 128.  (Eight waves, two a SIMD, share them out: there the one multiplies while the other issues.)
+//
 // A workgroup walks through the chunks of one head with 16 columns of its state a wave, which stay in the wave's registers.  A chunk's blocks come
 // to LDS while the chunk before it is computed with; K', where two do not fit, while the chunk's first products are.  Blocks are read from
 // LDS one group ahead of their products, and a group has several accumulators, so that products follow at the rate of the matrix pipe.  Two waves
@@ -685,7 +688,9 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int A_UNITS = U::KT;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), total = blockDim.x >> 6;
+    const int waves = total < SCAN_THREADS / 64 ? total - 1 : total;       // those that compute; the one beyond them loads
+    const bool loader = wave == waves, shared_out = waves == total;
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);       // the blocks of a head, and heads that share keys, on one XCD
     const int block = id % blocks_per_head, at = id / blocks_per_head, segment = at % mem.segments, head = at / mem.segments;
@@ -709,19 +714,38 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, wave, waves, lane);
-        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, U::VALUE_FORWARD, wave, waves, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, U::VALUE_FORWARD, loader ? 0 : wave, shared_out ? waves : 1, lane);
     };
     auto load_last = [&](int chunk, int parity) {
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, wave, waves, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, loader ? 0 : wave, shared_out ? waves : 1, lane);
     };
     E next[LB][8];
     auto load_v = [&](int chunk) { load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next); };
-    if (n > begin) {
+    auto load_next = [&](int chunk) {
+        if (!Lds::DOUBLE) load_last(chunk, chunk & 1);
+        if (chunk + 1 < n) {
+            load_first(chunk + 1, (chunk + 1) & 1);
+            if (Lds::DOUBLE) load_last(chunk + 1, (chunk + 1) & 1);
+        }
+    };
+    if (n > begin && (loader || shared_out)) {
         load_first(begin, begin & 1);
         if (Lds::DOUBLE) load_last(begin, begin & 1);
-        load_v(begin);
     }
+    if (loader) {
+        for (int chunk = begin; chunk < n; ++chunk) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            load_next(chunk);
+            if (!Lds::DOUBLE) {
+                __builtin_amdgcn_s_waitcnt(0);
+                __syncthreads();
+            }
+        }
+        return;
+    }
+    if (n > begin) load_v(begin);
     Frag<PM> Sf[KB];            // the state as operand
     auto split_s = [&](int kb) {
         float u[8];
@@ -739,11 +763,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         __syncthreads();
         mask_columns<E, LB>(next, all_columns, col < a.Dv, g, len - t0);
         const int after = chunk + 1 < n ? chunk + 1 : chunk;
-        if (!Lds::DOUBLE) load_last(chunk, parity);
-        if (chunk + 1 < n) {
-            load_first(after, parity ^ 1);
-            if (Lds::DOUBLE) load_last(after, parity ^ 1);
-        }
+        if (shared_out) load_next(chunk);
         if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         region_end();
 
@@ -946,7 +966,9 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int K_UNITS = U::Q, VALUE_UNITS = U::P;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), total = blockDim.x >> 6;
+    const int waves = total < SCAN_THREADS / 64 ? total - 1 : total;       // those that compute; the one beyond them loads
+    const bool loader = wave == waves, shared_out = waves == total;
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int block = id % blocks_per_segment, at = id / blocks_per_segment, segment = at % segments, head = at / segments;
@@ -968,11 +990,11 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, wave, waves, lane);
-        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + K_UNITS * 1024, VALUE_UNITS, wave, waves, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + K_UNITS * 1024, VALUE_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
     };
     auto load_last = [&](int chunk, int parity) {
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, wave, waves, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, loader ? 0 : wave, shared_out ? waves : 1, lane);
     };
     E next[LB][8] = {};
     auto load_v = [&](int chunk) {
@@ -980,11 +1002,30 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next);
         mask_columns<E, LB>(next, false, col < a.Dv, g, len - chunk * L);
     };
-    if (n > begin) {
+    auto load_next = [&](int chunk) {
+        if (!Lds::DOUBLE) load_last(chunk, chunk & 1);
+        if (chunk + 1 < n) {
+            load_first(chunk + 1, (chunk + 1) & 1);
+            if (Lds::DOUBLE) load_last(chunk + 1, (chunk + 1) & 1);
+        }
+    };
+    if (n > begin && (loader || shared_out)) {
         load_first(begin, begin & 1);
         if (Lds::DOUBLE) load_last(begin, begin & 1);
-        load_v(begin);
     }
+    if (loader) {
+        for (int chunk = begin; chunk < n; ++chunk) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            load_next(chunk);
+            if (!Lds::DOUBLE) {
+                __builtin_amdgcn_s_waitcnt(0);
+                __syncthreads();
+            }
+        }
+        return;
+    }
+    if (n > begin) load_v(begin);
     __builtin_amdgcn_s_waitcnt(0);
     for (int chunk = begin; chunk < n; ++chunk) {
         const int parity = chunk & 1;
@@ -992,11 +1033,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
         __syncthreads();
         const int after = chunk + 1 < n ? chunk + 1 : chunk;
-        if (!Lds::DOUBLE) load_last(chunk, parity);
-        if (chunk + 1 < n) {
-            load_first(after, parity ^ 1);
-            if (Lds::DOUBLE) load_last(after, parity ^ 1);
-        }
+        if (shared_out) load_next(chunk);
         float x[LB][8];
 #pragma unroll
         for (int s = 0; s < LB; ++s)
