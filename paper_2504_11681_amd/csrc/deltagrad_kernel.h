@@ -255,35 +255,48 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     if (a.d_initial && segment == 0) store_state<DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
 }
 
-// One workgroup for a chunk of a key head, a wave for each 16 tokens of it.
+// LDS of the gradients, 32 columns of the states at a time: operand blocks of S and dS' (rows: Dk), of E and Y (rows: tokens), for two rounds.
 template <class E, int KB>
-__global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
+struct GradientLds {
+    typedef DeltaUnits<E, KB> U;
+    static constexpr int S = 0, D = U::DT * DELTA_PM, ERR = 2 * U::DT * DELTA_PM, Y = ERR + U::NT * DELTA_PM, UNITS = Y + U::NT * DELTA_PM;
+    static constexpr int COL = U::L + 4, MATRICES = 2 * U::L * COL * 4;
+    static constexpr int BYTES = 2 * UNITS * 1024 > MATRICES ? 2 * UNITS * 1024 : MATRICES;
+};
+
+// One workgroup for a chunk of a key head.  L / 16 waves take the products of pairs of tokens, as many the products with the states, each for 16
+// tokens; the latter bring the states and errors in, split them once for all and leave them in LDS, a round ahead of the products.  (All of it
+// in every wave took 512 registers, so one wave a SIMD, and waited for memory in every round: B 4, T 2048, 16 heads of 128: 338 us.)
+template <class E, int KB>
+__global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_gradients(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
 {
     typedef DeltaUnits<E, KB> U;
-    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PM = DELTA_PM, COL = L + 4;
-    constexpr int PANEL = DT * PM * 1024 * 2, MATRICES = 2 * L * COL * 4;
-    __shared__ __attribute__((aligned(1024))) unsigned char shared[PANEL > MATRICES ? PANEL : MATRICES];
-    unsigned char *panelS = shared, *panelD = shared + PANEL / 2;    // 32 columns of S and dS' as operand blocks
-    float *Mq = (float *)shared, *Mk = Mq + L * COL;                 // after the last of them
-    __shared__ float hi[L], lo[L], beta[L], left[L], column_sums[NT][L], row_sums[L], token_g[L], token_beta[L], inner[NT];
+    typedef GradientLds<E, KB> Lds;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PM = DELTA_PM, COL = Lds::COL;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    float *Mq = (float *)lds, *Mk = Mq + L * COL;                    // once the states are done with
+    __shared__ float hi[L], lo[L], beta[L], column_sums[NT][L], row_sums[L], token_g[L], token_beta[L], inner[NT];
+    __shared__ float whole;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
-    const int chunk = blockIdx.x % mem.chunks, kh = blockIdx.x / mem.chunks;
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int chunk = id % mem.chunks, kh = id / mem.chunks;
     const int b = kh / a.Hk, hk = kh - b * a.Hk, group = a.Hv / a.Hk;
     const int len = sequence_length(a, b), t0 = chunk * L;
-    const int i = wave, token = t0 + tile_index(i, m);               // the lane's token where tokens are columns
+    const bool pairs = wave < NT;
+    const int i = pairs ? wave : wave - NT, token = t0 + tile_index(i, m);          // the lane's token where tokens are columns
     E *dq = (E *)a.dq + (b * a.sdq.batch + (long long)token * a.sdq.token + hk * a.sdq.head);
     E *dk = (E *)a.dk + (b * a.sdk.batch + (long long)token * a.sdk.token + hk * a.sdk.head);
 
     if (t0 >= len) {                     // past the sequence's end
         const float zero[8] = {};
-        if (token < a.T)
+        if (token < a.T && !pairs)
 #pragma unroll
             for (int s = 0; s < KB; ++s) {
                 store8(dq + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dq, zero);
                 store8(dk + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dk, zero);
             }
-        for (int x = tid; x < L * group; x += 64 * NT) {
+        for (int x = tid; x < L * group; x += 128 * NT) {
             const int t = t0 + x % L, h = hk * group + x / L;
             if (t < a.T) {
                 if (a.dg) a.dg[b * a.sdg.batch + (long long)t * a.sdg.token + h * a.sdg.head] = 0.0f;
@@ -294,85 +307,63 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
     }
 
     const unsigned char *key = mem.key + ((long long)kh * mem.chunks + chunk) * mem.key_units * 1024;
-    Frag<PI> kf[KB], qf[KB];
-    floatx4 kk[NT], qk[NT], mq[NT], mk[NT], accq[DT], acck[DT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) kk[j] = qk[j] = mq[j] = mk[j] = floatx4{0, 0, 0, 0};
-#pragma unroll
-    for (int t = 0; t < DT; ++t) accq[t] = acck[t] = floatx4{0, 0, 0, 0};
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        kf[kb] = load_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane);
-        qf[kb] = load_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {            // all tiles, the unused ones too: no branches between the products
-            const Frag<PI> other = load_frag<PI>(key + (U::K + (j * KB + kb) * PI) * 1024, lane);
-            kk[j] = mm<3>(kf[kb], other, kk[j]);
-            qk[j] = mm<3>(qf[kb], other, qk[j]);
-        }
-    }
+    const int rounds = mem.dvp / 32;
+    auto part = [&](int member) { return ((long long)(b * a.Hv + hk * group + member)) * mem.chunks + chunk; };
+    // dO of the lane's token in a round: 8 columns
+    const unsigned at_do = ((8 * (m >> 2) + (m & 3)) * (unsigned)a.sdo.token + 8 * g) * sizeof(E);
+    auto load_do = [&](int member, int kb, float (&u)[8]) {
+        const E *p = uniform((const E *)a.d_o + (b * a.sdo.batch + (t0 + tile_index(i, 0)) * a.sdo.token + (hk * group + member) * a.sdo.head + 32 * kb));
+        unsigned off = at_do;
+        asm("" : "+v"(off));
+        load8(behind(p, off), token < len ? a.Dv - 32 * kb - 8 * g : 0, vec.d_o, u);
+    };
 
-    for (int member = 0; member < group; ++member) {
-        const int h = hk * group + member;
-        const long long at = ((long long)(b * a.Hv + h)) * mem.chunks + chunk;
-        const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
-        const float *states = mem.states + at * DKP * mem.dvp, *d_states = mem.d_states + at * DKP * mem.dvp;
-        const float *errors = mem.errors + at * L * mem.dvp, *d_values = mem.d_values + at * L * mem.dvp;
-        const E *d_o = (const E *)a.d_o + (b * a.sdo.batch + (long long)token * a.sdo.token + h * a.sdo.head);
-        __syncthreads();
-        if (tid < L) hi[tid] = mem.logs[at * 2 * L + tid], lo[tid] = mem.logs[at * 2 * L + L + tid], beta[tid] = gates->beta[tid], left[tid] = gates->left[tid];
-
-        floatx4 D[NT], C[NT], hq[DT], hy[DT], he[DT];
+    if (pairs) {
+        floatx4 kk[NT], qk[NT], mq[NT], mk[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) D[j] = C[j] = floatx4{0, 0, 0, 0};
+        for (int j = 0; j < NT; ++j) kk[j] = qk[j] = mq[j] = mk[j] = floatx4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < DT; ++t) hq[t] = hy[t] = he[t] = floatx4{0, 0, 0, 0};
-        float dot = 0.0f;
-        for (int kb = 0; kb < mem.dvp / 32; ++kb) {
-            const int c0 = 32 * kb + 8 * g;
-            __syncthreads();
-            for (int t = wave; t < DT; t += NT) {
-                const long long row = (long long)tile_index(t, m) * mem.dvp + c0;
-                float u[8], w[8];
-                load8(states + row, 8, true, u);
-                load8(d_states + row, 8, true, w);
+        for (int kb = 0; kb < KB; ++kb) {
+            const Frag<PI> kf = load_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane), qf = load_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot = fmaf(u[e], w[e], dot);
-                store_frag<PM>(panelS + t * PM * 1024, lane, make_frag<PM>(u));
-                store_frag<PM>(panelD + t * PM * 1024, lane, make_frag<PM>(w));
+            for (int j = 0; j < NT; ++j) {            // all tiles, the unused ones too: no branches between the products
+                const Frag<PI> other = load_frag<PI>(key + (U::K + (j * KB + kb) * PI) * 1024, lane);
+                kk[j] = mm<3>(kf, other, kk[j]);
+                qk[j] = mm<3>(qf, other, qk[j]);
             }
-            float u[8];
-            load8(d_o + c0, token < len ? a.Dv - c0 : 0, vec.d_o, u);
-            const Frag<PI> of = make_frag<PI>(u);
-            load8(d_values + tile_index(i, m) * mem.dvp + c0, 8, true, u);
-            const Frag<PM> yf = make_frag<PM>(u);
-            Frag<PM> ef{};
+        }
+        float next[8];
+        load_do(0, 0, next);
+        for (int member = 0; member < group; ++member) {
+            const long long at = part(member);
+            const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
+            if (tid < L) {
+                hi[tid] = mem.logs[at * 2 * L + tid], lo[tid] = mem.logs[at * 2 * L + L + tid];
+                beta[tid] = gates->beta[tid];
+                if (tid == 0) whole = gates->whole;
+            }
+            floatx4 D[NT], C[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) D[j] = C[j] = floatx4{0, 0, 0, 0};
+            for (int kb = 0; kb < rounds; ++kb) {
+                const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
+                const Frag<PI> of = make_frag<PI>(next);
+                if (kb + 1 < rounds) load_do(member, kb + 1, next);
+                else if (member + 1 < group) load_do(member + 1, 0, next);
+                __syncthreads();
+                const Frag<PM> yf = load_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const Frag<PM> f = load_frag<PM>(panel + (Lds::ERR + j * PM) * 1024, lane);
+                    D[j] = mm<3>(of, f, D[j]);
+                    C[j] = mm<3>(yf, f, C[j]);
+                }
+            }
+            // matrices of token pairs: rows tile_index(i, 4 g + r), column tile_index(j, m)
+            float rows[4] = {};
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                load8(errors + tile_index(j, m) * mem.dvp + c0, 8, true, u);
-                const Frag<PM> f = make_frag<PM>(u);
-                D[j] = mm<3>(of, f, D[j]);
-                C[j] = mm<3>(yf, f, C[j]);
-                if (j == i) ef = f;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                const Frag<PM> sf = load_frag<PM>(panelS + t * PM * 1024, lane), df = load_frag<PM>(panelD + t * PM * 1024, lane);
-                hq[t] = mm<3>(sf, of, hq[t]);
-                hy[t] = mm<3>(sf, yf, hy[t]);
-                he[t] = mm<3>(df, ef, he[t]);
-            }
-        }
-        dot = group_sum(dot, 64);
-        if (lane == 0) inner[wave] = dot;
-
-        // matrices of token pairs: rows tile_index(i, 4 g + r), column tile_index(j, m)
-        float rows[4] = {};
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float column = 0.0f;
-            if (j <= (i | 1)) {
+                float column = 0.0f;
                 const int col = tile_index(j, m);
                 const float be = beta[col];
 #pragma unroll
@@ -386,71 +377,154 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_gradients(Delta
                     mq[j][r] = fmaf(Dm, be, mq[j][r]);
                     mk[j][r] = fmaf(-Cm, be, mk[j][r]);
                 }
+                column += __shfl_xor(column, 16, 64);
+                column += __shfl_xor(column, 32, 64);
+                if (g == 0) column_sums[i][col] = column;
             }
-            column += __shfl_xor(column, 16, 64);
-            column += __shfl_xor(column, 32, 64);
-            if (g == 0) column_sums[wave][tile_index(j, m)] = column;
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            rows[r] = group_sum(rows[r], 16);
-            if (m == 0) row_sums[tile_index(i, 4 * g + r)] = rows[r];
-        }
-        // terms with the states: token in columns
-        {
-            const int tok = tile_index(i, m);
-            const float decay = gates->decay[tok], fq = a.scale * decay, fe = left[tok], be = beta[tok];
-            float tg = 0.0f, tb = 0.0f;
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int e = 4 * (t & 1) + r;
-                    const float q = frag_value<PI>(qf[t >> 1], e), k = frag_value<PI>(kf[t >> 1], e);
-                    const float vq = fq * hq[t][r], vy = decay * hy[t][r], ve = fe * he[t][r];
-                    tg = fmaf(q, vq, fmaf(-k, vy, tg));
-                    tb = fmaf(k, ve, tb);
-                    accq[t][r] += vq;
-                    acck[t][r] += fmaf(be, ve, -vy);
-                }
-            tg += __shfl_xor(tg, 16, 64), tg += __shfl_xor(tg, 32, 64);
-            tb += __shfl_xor(tb, 16, 64), tb += __shfl_xor(tb, 32, 64);
-            if (g == 0) token_g[tok] = tg, token_beta[tok] = tb;
-        }
-        __syncthreads();
-        if (wave == 0) {
-            const int tok = lane < L ? lane : 0;
-            float column = 0.0f, whole = 0.0f;
-#pragma unroll
-            for (int w = 0; w < NT; ++w) column += column_sums[w][tok], whole += inner[w];
-            const float c = lane < L ? beta[tok] * token_beta[tok] : 0.0f;
-            float dG = lane < L ? row_sums[tok] - beta[tok] * column + token_g[tok] - c : 0.0f;
-            const float all = group_sum(c, 64);
-            if (lane == L - 1) dG += all + gates->whole * whole;
-            for (int step = 1; step < 64; step <<= 1) {
-                const float u = __shfl_down(dG, step, 64);
-                if (lane + step < 64) dG += u;
-            }
-            const int t = t0 + lane;
-            if (lane < L && t < a.T) {
-                const bool live = t < len;
-                if (a.dg) a.dg[b * a.sdg.batch + (long long)t * a.sdg.token + h * a.sdg.head] = live ? dG : 0.0f;
-                a.dbeta[b * a.sdbeta.batch + (long long)t * a.sdbeta.token + h * a.sdbeta.head] = live ? column + token_beta[tok] : 0.0f;
-            }
-        }
-    }
-    __syncthreads();
-
-    // products of token pairs with K and Q, once for the group
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-        if (j <= (i | 1))
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int at = tile_index(i, 4 * g + r) * COL + tile_index(j, m);
-                Mq[at] = mq[j][r], Mk[at] = mk[j][r];
+                rows[r] = group_sum(rows[r], 16);
+                if (m == 0) row_sums[tile_index(i, 4 * g + r)] = rows[r];
             }
-    __syncthreads();
+            __syncthreads();
+            if (wave == 0) {
+                const int tok = lane < L ? lane : 0, h = hk * group + member;
+                float column = 0.0f, all = 0.0f;
+#pragma unroll
+                for (int w = 0; w < NT; ++w) column += column_sums[w][tok], all += inner[w];
+                const float c = lane < L ? beta[tok] * token_beta[tok] : 0.0f;
+                float dG = lane < L ? row_sums[tok] - beta[tok] * column + token_g[tok] - c : 0.0f;
+                const float sum = group_sum(c, 64);
+                if (lane == L - 1) dG += sum + whole * all;
+                for (int step = 1; step < 64; step <<= 1) {
+                    const float u = __shfl_down(dG, step, 64);
+                    if (lane + step < 64) dG += u;
+                }
+                const int t = t0 + lane;
+                if (lane < L && t < a.T) {
+                    const bool live = t < len;
+                    if (a.dg) a.dg[b * a.sdg.batch + (long long)t * a.sdg.token + h * a.sdg.head] = live ? dG : 0.0f;
+                    a.dbeta[b * a.sdbeta.batch + (long long)t * a.sdbeta.token + h * a.sdbeta.head] = live ? column + token_beta[tok] : 0.0f;
+                }
+            }
+            __syncthreads();
+        }
+        // products of token pairs with K and Q, once for the group: the other waves take them
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            if (j <= (i | 1))
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = tile_index(i, 4 * g + r) * COL + tile_index(j, m);
+                    Mq[at] = mq[j][r], Mk[at] = mk[j][r];
+                }
+        __syncthreads();
+        return;
+    }
+
+    // the waves of the states.  Factors of a token go into its operand, so that dq and dk add up without a second set of accumulators; what a member adds
+    // to q.dq and k.dk is then the difference of the sums behind and before it
+    constexpr int TILES = DT > NT ? DT / NT : 1;
+    floatx4 accq[DT], acck[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) accq[t] = acck[t] = floatx4{0, 0, 0, 0};
+    struct Round { float s[TILES][8], d[TILES][8], e[8], y[8], o[8]; } next;
+    // rows of 32 columns between the kernels: a uniform address, and the lane's row of a tile and its eight columns
+    const unsigned at_row = ((8 * (m >> 2) + (m & 3)) * mem.dvp + 8 * g) * 4;
+    auto load_row = [&](const float *p, int tile, float (&x)[8]) {
+        unsigned off = at_row;
+        asm("" : "+v"(off));
+        load8(behind(uniform(p + tile_index(tile, 0) * mem.dvp), off), 8, true, x);
+    };
+    auto load_round = [&](int member, int kb, Round &x) {
+        const long long at = part(member);
+#pragma unroll
+        for (int p = 0; p < TILES; ++p) {
+            const int t = i + p * NT;
+            if (t < DT) {
+                load_row(mem.states + at * DKP * mem.dvp + 32 * kb, t, x.s[p]);
+                load_row(mem.d_states + at * DKP * mem.dvp + 32 * kb, t, x.d[p]);
+            }
+        }
+        load_row(mem.errors + at * L * mem.dvp + 32 * kb, i, x.e);
+        load_row(mem.d_values + at * L * mem.dvp + 32 * kb, i, x.y);
+        load_do(member, kb, x.o);
+    };
+    const int tok = tile_index(i, m);
+    // sums over the state's rows of q times accq and k times x
+    auto dots = [&](const floatx4 (&x)[DT], float &q_sum, float &k_sum) {
+        q_sum = k_sum = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const Frag<PI> kf = load_frag<PI>(key + (U::K + (i * KB + kb) * PI) * 1024, lane), qf = load_frag<PI>(key + (U::Q + (i * KB + kb) * PI) * 1024, lane);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int t = 2 * kb + (e >> 2), r = e & 3;
+                q_sum = fmaf(frag_value<PI>(qf, e), accq[t][r], q_sum);
+                k_sum = fmaf(frag_value<PI>(kf, e), x[t][r], k_sum);
+            }
+        }
+        q_sum += __shfl_xor(q_sum, 16, 64), q_sum += __shfl_xor(q_sum, 32, 64);
+        k_sum += __shfl_xor(k_sum, 16, 64), k_sum += __shfl_xor(k_sum, 32, 64);
+    };
+    load_round(0, 0, next);
+    for (int member = 0; member < group; ++member) {
+        const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + part(member) * mem.value_units * 1024);
+        const float decay = gates->decay[tok], fe = gates->left[tok], be = gates->beta[tok];
+        floatx4 he[DT];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) he[t] = floatx4{0, 0, 0, 0};
+        float dot = 0.0f, q_before = 0.0f, k_before = 0.0f, q_sum, k_sum, e_sum, unused;
+        if (member > 0) dots(acck, q_before, k_before);
+        for (int kb = 0; kb < rounds; ++kb) {
+            unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
+#pragma unroll
+            for (int p = 0; p < TILES; ++p) {
+                const int t = i + p * NT;
+                if (t < DT) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dot = fmaf(next.s[p][e], next.d[p][e], dot);
+                    store_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane, make_frag<PM>(next.s[p]));
+                    store_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane, make_frag<PM>(next.d[p]));
+                }
+            }
+            const Frag<PM> ef = make_frag<PM>(next.e);
+            store_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane, ef);
+            store_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane, make_frag<PM>(next.y));
+            float u[8], w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = a.scale * decay * next.o[e], w[e] = -decay * next.y[e];
+            const Frag<PM> of = make_frag<PM>(u), yf = make_frag<PM>(w);
+            if (kb + 1 < rounds) load_round(member, kb + 1, next);
+            else if (member + 1 < group) load_round(member + 1, 0, next);
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                const Frag<PM> sf = load_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane), df = load_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane);
+#pragma unroll
+                for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+                    for (int p = 0; p <= sum; ++p) {
+                        accq[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf.part(p), of.part(sum - p), accq[t], 0, 0, 0);
+                        acck[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sf.part(p), yf.part(sum - p), acck[t], 0, 0, 0);
+                        he[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df.part(p), ef.part(sum - p), he[t], 0, 0, 0);
+                    }
+            }
+        }
+        dot = group_sum(dot, 64);
+        if (lane == 0) inner[i] = dot;
+        dots(acck, q_sum, k_sum);
+        dots(he, unused, e_sum);
+        const float tb = fe * e_sum;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acck[t][r] = fmaf(be * fe, he[t][r], acck[t][r]);
+        if (g == 0) token_g[tok] = (q_sum - q_before) + (k_sum - k_before), token_beta[tok] = tb;
+        __syncthreads();
+        __syncthreads();
+    }
+    __syncthreads();             // the matrices of token pairs are there
     const int row = tile_index(i, m);
 #pragma unroll
     for (int kb = 0; kb < LB; ++kb) {

@@ -158,7 +158,10 @@ hipError_t backward(const DeltaArgs &a, hipStream_t s)
     m.vec_dv = rows_of_4(a.dv, a.sdv, a.Dv, a.bf16);
     if (hipError_t e = scan_back<E, KB>(a, m, s); e != hipSuccess) return e;
     if (m.chunks == 0) return hipSuccess;
-    k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 64 * U::NT, 0, s>>>(a, m, vec);
+    constexpr int bytes = GradientLds<E, KB>::BYTES;
+    static LdsLimitOnce limit;
+    if (hipError_t e = allow_lds(limit, bytes, k_delta_gradients<E, KB>); e != hipSuccess) return e;
+    k_delta_gradients<E, KB><<<(unsigned)(a.B * a.Hk * m.chunks), 128 * U::NT, bytes, s>>>(a, m, vec);
     return hipGetLastError();
 }
 
