@@ -249,7 +249,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         if (col0 < mem.dvp) store_tiles<DT>(mem.back_effects + at * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         return;
     }
-    const int last = segment + 1 < mem.segments ? (begin + mem.segment_chunks) * L : a.T;
+    const int last = min((begin + mem.segment_chunks) * L, a.T);
     for (int t = (n > begin ? n : begin) * L + g; t < last; t += 4)
         if (col < a.Dv) store_element(dv + t * a.sdv.token + col, 0.0f);
     if (a.d_initial && segment == 0) store_state<DT>(a.d_initial + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);

@@ -7,7 +7,7 @@ namespace tfno {
 
 namespace {
 
-constexpr int SEGMENT_MAX_WAVES = 256, SEGMENT_WAVES = 2048, SEGMENT_MIN_CHUNKS = 8;
+constexpr int SEGMENT_MAX_WAVES = 256, SEGMENT_WAVES = 1024, SEGMENT_MIN_CHUNKS = 4;
 
 size_t pad(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -18,7 +18,9 @@ int segments_of(const DeltaArgs &a, int chunks)
     const long long waves = (long long)a.B * a.Hv * ((a.Dv + 31) / 32 * 2);
     if (waves == 0 || waves > SEGMENT_MAX_WAVES) return 1;
     const long long n = std::min<long long>(SEGMENT_WAVES / waves, chunks / SEGMENT_MIN_CHUNKS);
-    return n < 2 ? 1 : (int)n;
+    if (n < 2) return 1;
+    const int each = (int)((chunks + n - 1) / n);
+    return (chunks + each - 1) / each;           // none without chunks
 }
 
 // Layout of the tape, or of the workspace of a forward pass without one; `base` may be NULL for its size alone.
@@ -96,15 +98,16 @@ template <class E, int KB, bool TAPE>
 hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
     constexpr int bytes = ForwardLds<E, KB>::BYTES, effect_bytes = EffectLds<E, KB>::BYTES;
-    static LdsLimitOnce limit, effect_limit;
+    static LdsLimitOnce limit, effect_limit, join_limit;
     const long long heads = (long long)a.B * a.Hv;
     if (m.segments > 1) {
         if (hipError_t e = allow_lds(effect_limit, effect_bytes, k_delta_effects<E, KB>); e != hipSuccess) return e;
         const int segments = TAPE ? m.segments : m.segments - 1;       // the last one's effect is of use to the backward pass alone
         const ScanShape sh = scan_shape(heads * segments, m.dvp / 16 + 2 * KB);
         k_delta_effects<E, KB><<<(unsigned)(heads * segments * sh.blocks), sh.threads(), effect_bytes, s>>>(a, m, sh.blocks, segments);
-        const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
-        k_delta_join<KB, false><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
+        const int blocks = (m.dvp / 16 + JOIN_TILES - 1) / JOIN_TILES;
+        if (hipError_t e = allow_lds(join_limit, JoinLds<KB>::BYTES, k_delta_join<KB, false>); e != hipSuccess) return e;
+        k_delta_join<KB, false><<<(unsigned)(heads * blocks), SCAN_THREADS, JoinLds<KB>::BYTES, s>>>(a, m, blocks);
     }
     if (hipError_t e = allow_lds(limit, bytes, k_delta_scan<E, KB, TAPE>); e != hipSuccess) return e;
     const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
@@ -115,14 +118,15 @@ template <class E, int KB>
 hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
     constexpr int bytes = BackwardLds<E, KB>::BYTES;
-    static LdsLimitOnce limit;
+    static LdsLimitOnce limit, join_limit;
     if (hipError_t e = allow_lds(limit, bytes, k_delta_scan_back<E, KB, false>, k_delta_scan_back<E, KB, true>); e != hipSuccess) return e;
     const long long heads = (long long)a.B * a.Hv;
     if (m.segments > 1) {
         const ScanShape sh = scan_shape(heads * (m.segments - 1), m.dvp / 16);
         k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
-        const int waves = std::min(m.dvp / 16, SCAN_THREADS / 64), blocks = (m.dvp / 16 + waves - 1) / waves;
-        k_delta_join<KB, true><<<(unsigned)(heads * blocks), 64 * waves, 0, s>>>(a, m, blocks);
+        const int blocks = (m.dvp / 16 + JOIN_TILES - 1) / JOIN_TILES;
+        if (hipError_t e = allow_lds(join_limit, JoinLds<KB>::BYTES, k_delta_join<KB, true>); e != hipSuccess) return e;
+        k_delta_join<KB, true><<<(unsigned)(heads * blocks), SCAN_THREADS, JoinLds<KB>::BYTES, s>>>(a, m, blocks);
     }
     const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
     k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);

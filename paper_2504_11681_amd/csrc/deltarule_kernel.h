@@ -945,7 +945,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         }
     }
     // past the sequence's end
-    const int last = segment + 1 < mem.segments ? (begin + mem.segment_chunks) * L : a.T;
+    const int last = min((begin + mem.segment_chunks) * L, a.T);
     for (int t = (n > begin ? n : begin) * L + g; t < last; t += 4)
         if (col < a.Dv) store_element(o + t * a.so.token + col, 0.0f);
     if (a.final_state && segment + 1 == mem.segments) store_state<DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
@@ -1116,50 +1116,103 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 }
 
 // The states before the segments, one after the other: S <- A S + B.  BACK: the gradients of the states after them, from the last one:
-// dS <- A' dS + b.  A workgroup takes up to eight tiles of columns of a head, and splits A for them in LDS.
+// dS <- A' dS + b.  A workgroup takes four tiles of columns of a head, two waves a tile, each with half of the state's rows: the waves split A
+// and their part of the state for all of them in LDS, and fetch the next segment's A and B meanwhile.
+constexpr int JOIN_TILES = 4;
+template <int KB>
+struct JoinLds { static constexpr int DT = 2 * KB, A = DT * KB * DELTA_PM, BYTES = (A + JOIN_TILES * KB * DELTA_PM) * 1024; };
+
 template <int KB, bool BACK>
 __global__ __launch_bounds__(SCAN_THREADS) void k_delta_join(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
-    constexpr int DT = 2 * KB, DKP = 32 * KB, PM = DELTA_PM;
-    __shared__ __attribute__((aligned(1024))) unsigned char As[DT * KB * PM * 1024];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    constexpr int DT = 2 * KB, DKP = 32 * KB, PM = DELTA_PM, WAVES = SCAN_THREADS / 64, OWN = KB, FRAGS = (DT * KB + WAVES - 1) / WAVES;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+    unsigned char *As = lds, *Ss = lds + JoinLds<KB>::A * 1024;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, g = lane >> 4, block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
-    const int width = mem.dvp + DKP, col0 = (block * waves + wave) * 16, col = col0 + m;
+    const int tile = wave >> 1, half = wave & 1;                   // row tiles half * KB .. + KB - 1 of the state: pairs where KB is even
+    const int width = mem.dvp + DKP, col0 = (block * JOIN_TILES + tile) * 16, col = col0 + m;
+    const bool live = col0 < mem.dvp;
     const float *from = BACK ? a.d_final : a.initial;
-    floatx4 S[DT];
-    load_state<DT>(from ? from + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
+    floatx4 S[OWN], next_b[OWN];
+    float next_a[FRAGS][8];
+    // an element of the wave's rows
+    auto at_row = [&](int t, int r) { return tile_index(half * KB + t, 4 * g + r); };
+    auto load_own = [&](const float *p, int rows, int columns, int stride, floatx4 (&x)[OWN]) {
+#pragma unroll
+        for (int t = 0; t < OWN; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[t][r] = p[at_row(t, r) < rows && col < columns ? at_row(t, r) * stride + col : 0];
+#pragma unroll
+        for (int t = 0; t < OWN; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (at_row(t, r) >= rows || col >= columns) x[t][r] = 0.0f;
+    };
+    auto load_next = [&](int segment) {
+        const long long at = (long long)head * mem.segments + segment;
+        const float *A = mem.effects + at * DKP * width + mem.dvp;
+        load_own(BACK ? mem.back_effects + at * DKP * mem.dvp : mem.effects + at * DKP * width, DKP, mem.dvp, BACK ? mem.dvp : width, next_b);
+#pragma unroll
+        for (int x = 0; x < FRAGS; ++x) {
+            const int f = wave + x * WAVES;
+            if (f < DT * KB) {
+                const int row = tile_index(f / KB, m), k = 32 * (f % KB) + 8 * g;
+                if (BACK) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) next_a[x][e] = A[(k + e) * width + row];
+                } else {
+                    load8(A + row * width + k, 8, true, next_a[x]);
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int t = 0; t < OWN; ++t) S[t] = floatx4{0, 0, 0, 0};
+    if (from) load_own(from + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, a.Dv, S);
+    load_next(BACK ? mem.segments - 1 : 0);
     for (int step = 0; step < mem.segments; ++step) {
         const int segment = BACK ? mem.segments - 1 - step : step;
         const long long at = (long long)head * mem.segments + segment;
-        if (col0 < mem.dvp)
-            store_tiles<DT>((BACK ? mem.segment_d_states : mem.segment_states) + at * DKP * mem.dvp, mem.dvp, tiles_at(mem.dvp, col0, lane), lane, S);
+        if (live) {
+            float *to = (BACK ? mem.segment_d_states : mem.segment_states) + at * DKP * mem.dvp;
+#pragma unroll
+            for (int t = 0; t < OWN; ++t) {
+                const int tt = half * KB + t;
+                *behind((floatx4 *)(to + (32 * (tt >> 1) + 4 * (tt & 1)) * mem.dvp), tiles_at(mem.dvp, col0, lane)) = quad_transpose(S[t], lane);
+            }
+        }
         if (step + 1 == mem.segments) break;
-        const float *A = mem.effects + at * DKP * width + mem.dvp;
-        floatx4 sum[DT];
-        const float *B = BACK ? mem.back_effects + at * DKP * mem.dvp : mem.effects + at * DKP * width;
-        load_state<DT>(B, DKP, BACK ? mem.dvp : width, col < mem.dvp ? col : 0, g, sum);
-        Frag<PM> Sf[KB];
+#pragma unroll
+        for (int x = 0; x < FRAGS; ++x)
+            if (wave + x * WAVES < DT * KB) store_frag<PM>(As + (wave + x * WAVES) * PM * 1024, lane, make_frag<PM>(next_a[x]));
+        // the state as operand blocks: four of a lane's eight values are a tile's
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) {
+            const int tt = half * KB + t;
+            Frag<PM> f{};
+            set_four<PM>(f, 0, {S[t][0], S[t][1], S[t][2], S[t][3]});
+#pragma unroll
+            for (int p = 0; p < PM; ++p)
+                *reinterpret_cast<uint2 *>(Ss + ((tile * KB + (tt >> 1)) * PM + p) * 1024 + lane * 16 + (tt & 1) * 8) = make_uint2(f.w[p][0], f.w[p][1]);
+        }
+        floatx4 sum[OWN];
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) sum[t] = next_b[t];
+        if (step + 2 < mem.segments) load_next(BACK ? segment - 1 : segment + 1);
+        __syncthreads();
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            set_four<PM>(Sf[kb], 0, {S[2 * kb][0], S[2 * kb][1], S[2 * kb][2], S[2 * kb][3]});
-            set_four<PM>(Sf[kb], 1, {S[2 * kb + 1][0], S[2 * kb + 1][1], S[2 * kb + 1][2], S[2 * kb + 1][3]});
+            const Frag<PM> sf = load_frag<PM>(Ss + (tile * KB + kb) * PM * 1024, lane);
+            Frag<PM> f[OWN];
+            floatx4 *to[OWN];
+#pragma unroll
+            for (int t = 0; t < OWN; ++t) f[t] = load_frag<PM>(As + ((half * KB + t) * KB + kb) * PM * 1024, lane), to[t] = &sum[t];
+            mm_many<3, false>(f, sf, to, NoWeave());
         }
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) S[t] = sum[t];
         __syncthreads();
-        for (int f = wave; f < DT * KB; f += waves) {
-            const int row = tile_index(f / KB, m), k = 32 * (f % KB) + 8 * g;
-            store_frag<PM>(As + f * PM * 1024, lane, BACK ? column_frag<PM>(A + k * width + row, width) : row_frag<PM>(A + row * width + k));
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int t = 0; t < DT; t += 2) {
-                const Frag<PM> f[2] = {load_frag<PM>(As + (t * KB + kb) * PM * 1024, lane), load_frag<PM>(As + ((t + 1) * KB + kb) * PM * 1024, lane)};
-                floatx4 *to[2] = {&sum[t], &sum[t + 1]};
-                mm_many<3, false>(f, Sf[kb], to, NoWeave());
-            }
-#pragma unroll
-        for (int t = 0; t < DT; ++t) S[t] = sum[t];
     }
 }
 
