@@ -32,9 +32,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     constexpr int K_UNITS = U::Q, TRI_UNITS = U::TRI * PM;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), total = blockDim.x >> 6;
-    const int waves = total < SCAN_THREADS / 64 ? total - 1 : total;       // those that compute; the one beyond them loads
-    const bool loader = wave == waves, shared_out = waves == total;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (blockDim.x >> 6) - 1;      // and one that loads
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int some = EFFECTS ? mem.segments - 1 : mem.segments;
@@ -62,13 +60,13 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
         const unsigned char *v = value + (long long)chunk * mem.value_units * 1024;
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
-        units_to_lds(v + U::GATES * 1024, to + K_UNITS * 1024, 1, loader ? 0 : wave, shared_out ? waves : 1, lane);
-        units_to_lds(v + U::PT * 1024, to + (K_UNITS + 1) * 1024, TRI_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
-        units_to_lds(v + U::TT * 1024, to + (K_UNITS + 1 + TRI_UNITS) * 1024, TRI_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, lane);
+        units_to_lds(v + U::GATES * 1024, to + K_UNITS * 1024, 1, lane);
+        units_to_lds(v + U::PT * 1024, to + (K_UNITS + 1) * 1024, TRI_UNITS, lane);
+        units_to_lds(v + U::TT * 1024, to + (K_UNITS + 1 + TRI_UNITS) * 1024, TRI_UNITS, lane);
     };
     auto load_last = [&](int chunk, int parity) {
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, lane);
     };
     E next[LB][8];
     auto load_do = [&](int chunk) { load_columns<E, LB>(d_o + (long long)chunk * L * a.sdo.token, a.sdo.token, at_do, g, len - chunk * L, next); };
@@ -79,11 +77,11 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             if (Lds::DOUBLE) load_last(chunk - 1, (chunk - 1) & 1);
         }
     };
-    if (n > begin && (loader || shared_out)) {
-        load_first(n - 1, (n - 1) & 1);
-        if (Lds::DOUBLE) load_last(n - 1, (n - 1) & 1);
-    }
-    if (loader) {
+    if (wave == waves) {
+        if (n > begin) {
+            load_first(n - 1, (n - 1) & 1);
+            if (Lds::DOUBLE) load_last(n - 1, (n - 1) & 1);
+        }
         for (int chunk = n - 1; chunk >= begin; --chunk) {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
@@ -110,7 +108,6 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[s][e] = to_float(next[s][e]);
         const int before = chunk > begin ? chunk - 1 : begin;
-        if (shared_out) load_next(chunk);
         load_do(before);
         if (!EFFECTS && col0 < mem.dvp) store_tiles<DT>(mem.d_states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         // K dS' and P' dO, a pair of tiles of tokens at a time

@@ -78,14 +78,11 @@ bool rows_of_4(const void *p, const Strides &s, int columns, bool bf16)
     return columns % 4 == 0 && ((uintptr_t)p & (bf16 ? 7 : 15)) == 0 && s.batch % 4 == 0 && s.token % 4 == 0 && s.head % 4 == 0;
 }
 
-// Waves of a scan's workgroup, one for 16 columns: as many as share a chunk's blocks, down to two where there are few.
-struct ScanShape {
-    int waves, blocks;
-    int threads() const { return 64 * (waves < SCAN_THREADS / 64 ? waves + 1 : waves); }      // one more that loads
-};
+// Waves of a scan's workgroup that compute, one for 16 columns: as many as share a chunk's blocks, down to two where there are few.
+struct ScanShape { int waves, blocks; };
 ScanShape scan_shape(long long walks, int tiles)
 {
-    ScanShape s{SCAN_THREADS / 64, 0};
+    ScanShape s{SCAN_WAVES, 0};
     while (s.waves > 2 && (walks * tiles < 256LL * s.waves || s.waves > tiles)) s.waves >>= 1;
     s.blocks = (tiles + s.waves - 1) / s.waves;
     return s;
@@ -94,42 +91,50 @@ ScanShape scan_shape(long long walks, int tiles)
 template <class... Kernels>
 hipError_t allow_lds(LdsLimitOnce &limit, int bytes, Kernels... k) { return limit.set({(const void *)k...}, bytes); }
 
+template <class E, int KB, int MODE>
+hipError_t scan_one(const DeltaArgs &a, const DeltaMemory &m, int segments, int tiles, hipStream_t s)
+{
+    constexpr int bytes = ForwardLds<E, KB, MODE>::BYTES;
+    static LdsLimitOnce limit;
+    if (hipError_t e = allow_lds(limit, bytes, k_delta_scan<E, KB, MODE>); e != hipSuccess) return e;
+    const long long walks = (long long)a.B * a.Hv * segments;
+    const ScanShape sh = scan_shape(walks, tiles);
+    k_delta_scan<E, KB, MODE><<<(unsigned)(walks * sh.blocks), 64 * (sh.waves + 1), bytes, s>>>(a, m, sh.blocks, segments);
+    return hipGetLastError();
+}
+template <int KB, bool BACK>
+hipError_t join(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
+{
+    static LdsLimitOnce limit;
+    if (hipError_t e = allow_lds(limit, JoinLds<KB>::BYTES, k_delta_join<KB, BACK>); e != hipSuccess) return e;
+    const int blocks = (m.dvp / 16 + JOIN_TILES - 1) / JOIN_TILES;
+    k_delta_join<KB, BACK><<<(unsigned)(a.B * a.Hv * blocks), JOIN_THREADS, JoinLds<KB>::BYTES, s>>>(a, m, blocks);
+    return hipGetLastError();
+}
 template <class E, int KB, bool TAPE>
 hipError_t scan(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
-    constexpr int bytes = ForwardLds<E, KB>::BYTES, effect_bytes = EffectLds<E, KB>::BYTES;
-    static LdsLimitOnce limit, effect_limit, join_limit;
-    const long long heads = (long long)a.B * a.Hv;
     if (m.segments > 1) {
-        if (hipError_t e = allow_lds(effect_limit, effect_bytes, k_delta_effects<E, KB>); e != hipSuccess) return e;
-        const int segments = TAPE ? m.segments : m.segments - 1;       // the last one's effect is of use to the backward pass alone
-        const ScanShape sh = scan_shape(heads * segments, m.dvp / 16 + 2 * KB);
-        k_delta_effects<E, KB><<<(unsigned)(heads * segments * sh.blocks), sh.threads(), effect_bytes, s>>>(a, m, sh.blocks, segments);
-        const int blocks = (m.dvp / 16 + JOIN_TILES - 1) / JOIN_TILES;
-        if (hipError_t e = allow_lds(join_limit, JoinLds<KB>::BYTES, k_delta_join<KB, false>); e != hipSuccess) return e;
-        k_delta_join<KB, false><<<(unsigned)(heads * blocks), SCAN_THREADS, JoinLds<KB>::BYTES, s>>>(a, m, blocks);
+        // the last segment's effect is of use to the backward pass alone
+        if (hipError_t e = scan_one<E, KB, SCAN_EFFECTS>(a, m, TAPE ? m.segments : m.segments - 1, m.dvp / 16 + 2 * KB, s); e != hipSuccess) return e;
+        if (hipError_t e = join<KB, false>(a, m, s); e != hipSuccess) return e;
     }
-    if (hipError_t e = allow_lds(limit, bytes, k_delta_scan<E, KB, TAPE>); e != hipSuccess) return e;
-    const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
-    k_delta_scan<E, KB, TAPE><<<(unsigned)(heads * m.segments * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
-    return hipGetLastError();
+    return scan_one<E, KB, TAPE ? SCAN_TAPE : SCAN_OUTPUTS>(a, m, m.segments, m.dvp / 16, s);
 }
 template <class E, int KB>
 hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
 {
     constexpr int bytes = BackwardLds<E, KB>::BYTES;
-    static LdsLimitOnce limit, join_limit;
+    static LdsLimitOnce limit;
     if (hipError_t e = allow_lds(limit, bytes, k_delta_scan_back<E, KB, false>, k_delta_scan_back<E, KB, true>); e != hipSuccess) return e;
     const long long heads = (long long)a.B * a.Hv;
     if (m.segments > 1) {
         const ScanShape sh = scan_shape(heads * (m.segments - 1), m.dvp / 16);
-        k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
-        const int blocks = (m.dvp / 16 + JOIN_TILES - 1) / JOIN_TILES;
-        if (hipError_t e = allow_lds(join_limit, JoinLds<KB>::BYTES, k_delta_join<KB, true>); e != hipSuccess) return e;
-        k_delta_join<KB, true><<<(unsigned)(heads * blocks), SCAN_THREADS, JoinLds<KB>::BYTES, s>>>(a, m, blocks);
+        k_delta_scan_back<E, KB, true><<<(unsigned)(heads * (m.segments - 1) * sh.blocks), 64 * (sh.waves + 1), bytes, s>>>(a, m, sh.blocks);
+        if (hipError_t e = join<KB, true>(a, m, s); e != hipSuccess) return e;
     }
     const ScanShape sh = scan_shape(heads * m.segments, m.dvp / 16);
-    k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), sh.threads(), bytes, s>>>(a, m, sh.blocks);
+    k_delta_scan_back<E, KB, false><<<(unsigned)(heads * m.segments * sh.blocks), 64 * (sh.waves + 1), bytes, s>>>(a, m, sh.blocks);
     return hipGetLastError();
 }
 

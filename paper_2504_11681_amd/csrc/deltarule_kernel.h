@@ -545,16 +545,15 @@ __device__ __forceinline__ T *uniform(T *p)
     const uintptr_t u = (uintptr_t)p;
     return (T *)((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
 }
-// Units of 1024 bytes from global memory to LDS, shared out over the waves of the workgroup; they are there after each wave's own wait for its
-// loads (s_waitcnt 0) and a barrier.  In assembly, because the compiler takes every later read of LDS for one that may need them and would wait
-// for the next chunk's blocks before the first product of this one (B 1, T 16384, 8 heads of 128: XXX us).  The instruction has no result register.
-__device__ __forceinline__ void units_to_lds(const unsigned char *from, const unsigned char *to, int units, int wave, int waves, int lane)
+// Units of 1024 bytes from global memory to LDS by one wave; they are there for the others after its wait for its loads (s_waitcnt 0) and a barrier.
+// In assembly, because the compiler takes every later read of LDS for one that may need them and would wait for the next chunk's blocks
+// before the first product of this one.  The instruction has no result register.
+__device__ __forceinline__ void units_to_lds(const unsigned char *from, const unsigned char *to, int units, int lane)
 {
     const unsigned at = lane * 16;          // a uniform address and 32 bits a lane
     from = uniform(from);
     unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
-    lds += wave * 1024, from += wave * 1024;
-    for (int u = wave; u < units; u += waves, lds += waves * 1024, from += waves * 1024)
+    for (int u = 0; u < units; ++u, lds += 1024, from += 1024)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(at), "s"(from));
 }
 
@@ -667,33 +666,37 @@ struct ScanLds {
     static __device__ __forceinline__ unsigned char *first(unsigned char *lds, int parity) { return lds + parity * FIRST * 1024; }
     static __device__ __forceinline__ unsigned char *last(unsigned char *lds, int parity) { return lds + (2 * FIRST + (DOUBLE ? parity * LAST : 0)) * 1024; }
 };
-template <class E, int KB>
-struct ForwardLds : ScanLds<DeltaUnits<E, KB>::KT + DeltaUnits<E, KB>::VALUE_FORWARD, DeltaUnits<E, KB>::QT - DeltaUnits<E, KB>::KT> {};
 
-constexpr int SCAN_THREADS = 512;
+// What a walk is for: outputs; outputs and a tape; the effect of each segment on the state alone.
+enum { SCAN_OUTPUTS, SCAN_TAPE, SCAN_EFFECTS };
+// K, Q, gates, T, P | K'; for effects without Q and P
+template <class E, int KB, int MODE>
+struct ForwardLds : ScanLds<(MODE == SCAN_EFFECTS ? DeltaUnits<E, KB>::Q + DeltaUnits<E, KB>::P : DeltaUnits<E, KB>::KT + DeltaUnits<E, KB>::VALUE_FORWARD),
+                            DeltaUnits<E, KB>::QT - DeltaUnits<E, KB>::KT> {};
 
-// A workgroup of fewer than eight waves has one more, which does nothing but these loads: 75 cycles each of a wave that issues them, 40 for each of two waves
-// and a chunk of heads of 128.  (Eight waves, two a SIMD, share them out: there the one multiplies while the other issues.)
-//
-// A workgroup walks through the chunks of one head with 16 columns of its state a wave, which stay in the wave's registers.  A chunk's blocks come
-// to LDS while the chunk before it is computed with; K', where two do not fit, while the chunk's first products are.  Blocks are read from
-// LDS one group ahead of their products, and a group has several accumulators, so that products follow at the rate of the matrix pipe.  Two waves
-// a SIMD (256 registers each, none of them accumulation registers, whose copies would cost as much as the splits): one splits while the other multiplies.
-template <class E, int KB, bool TAPE>
-__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+constexpr int SCAN_WAVES = 4, SCAN_THREADS = 64 * (SCAN_WAVES + 1);       // waves that compute, at most, and one that loads
+
+// A workgroup walks through the chunks of one head, or of one segment of it, with 16 columns of its state a wave, which stay in the wave's registers.
+// One more wave does nothing but bring the next chunk's blocks to LDS (75 cycles of issue each, 79 of them for heads of 128: a wave that
+// computes would lose 3000 cycles to a half of them); K', where two chunks' do not fit, comes while the chunk's first products run.  Blocks are read from LDS
+// one group ahead of their products, a group has several accumulators, and the splits stand between the products: 182 of them are 2900 cycles,
+// a chunk takes 7700 (B 1, T 16384, 8 heads of 128 in 16 segments).  256 registers a wave, none of them accumulation registers, whose copies would cost as
+// much as the splits.  Effects: columns of B start from zeros, columns of A from the identity, without values.
+template <class E, int KB, int MODE>
+__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head, int segments)
 {
     typedef DeltaUnits<E, KB> U;
     constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PO = U::PO, PM = DELTA_PM;
-    typedef ForwardLds<E, KB> Lds;               // K, Q, gates, T, P | K'
-    constexpr int A_UNITS = U::KT;
+    constexpr bool TAPE = MODE == SCAN_TAPE, EFFECTS = MODE == SCAN_EFFECTS;
+    typedef ForwardLds<E, KB, MODE> Lds;
+    constexpr int A_UNITS = EFFECTS ? U::Q : U::KT, VALUE_UNITS = EFFECTS ? U::P : U::VALUE_FORWARD;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), total = blockDim.x >> 6;
-    const int waves = total < SCAN_THREADS / 64 ? total - 1 : total;       // those that compute; the one beyond them loads
-    const bool loader = wave == waves, shared_out = waves == total;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = (blockDim.x >> 6) - 1;      // and one that loads
     const int m = lane & 15, g = lane >> 4;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);       // the blocks of a head, and heads that share keys, on one XCD
-    const int block = id % blocks_per_head, at = id / blocks_per_head, segment = at % mem.segments, head = at / mem.segments;
+    const int block = id % blocks_per_head, part = id / blocks_per_head, segment = part % segments, head = part / segments;
+    const long long at = (long long)head * mem.segments + segment;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
     const int len = sequence_length(a, b), all = (len + L - 1) / L;
     const int begin = segment * mem.segment_chunks, n = all < begin + mem.segment_chunks ? all : begin + mem.segment_chunks;   // chunks begin .. n - 1
@@ -703,7 +706,12 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const bool all_columns = a.Dv % 32 == 0;
 
     floatx4 S[DT];
-    if (mem.segments > 1) load_state<DT>(mem.segment_states + (long long)at * U::DKP * mem.dvp, U::DKP, mem.dvp, col, g, S);
+    if constexpr (EFFECTS) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][r] = tile_index(t, 4 * g + r) == col - mem.dvp ? 1.0f : 0.0f;
+    } else if (mem.segments > 1) load_state<DT>(mem.segment_states + at * U::DKP * mem.dvp, U::DKP, mem.dvp, col, g, S);
     else load_state<DT>(a.initial ? a.initial + (long long)head * a.Dk * a.Dv : nullptr, a.Dk, a.Dv, col, g, S);
     const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
     E *o = (E *)a.o + (b * a.so.batch + h * a.so.head);
@@ -714,14 +722,17 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
-        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, U::VALUE_FORWARD, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, lane);
+        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, VALUE_UNITS, lane);
     };
     auto load_last = [&](int chunk, int parity) {
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, loader ? 0 : wave, shared_out ? waves : 1, lane);
+        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, lane);
     };
-    E next[LB][8];
-    auto load_v = [&](int chunk) { load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next); };
+    E next[LB][8] = {};
+    auto load_v = [&](int chunk) {
+        if (EFFECTS && col0 >= mem.dvp) return;
+        load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next);
+    };
     auto load_next = [&](int chunk) {
         if (!Lds::DOUBLE) load_last(chunk, chunk & 1);
         if (chunk + 1 < n) {
@@ -729,11 +740,11 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             if (Lds::DOUBLE) load_last(chunk + 1, (chunk + 1) & 1);
         }
     };
-    if (n > begin && (loader || shared_out)) {
-        load_first(begin, begin & 1);
-        if (Lds::DOUBLE) load_last(begin, begin & 1);
-    }
-    if (loader) {
+    if (wave == waves) {
+        if (n > begin) {
+            load_first(begin, begin & 1);
+            if (Lds::DOUBLE) load_last(begin, begin & 1);
+        }
         for (int chunk = begin; chunk < n; ++chunk) {
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
@@ -763,11 +774,10 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         __syncthreads();
         mask_columns<E, LB>(next, all_columns, col < a.Dv, g, len - t0);
         const int after = chunk + 1 < n ? chunk + 1 : chunk;
-        if (shared_out) load_next(chunk);
         if (TAPE && col0 < mem.dvp) store_tiles<DT>(mem.states + ((long long)head * mem.chunks + chunk) * U::DKP * mem.dvp, mem.dvp, at_tape, lane, S);
         region_end();
 
-        // K S, tokens in rows; then (Q S)', tokens in columns, and meanwhile R = V - e^G K S as operand
+        // K S, tokens in rows; then (Q S)', tokens in columns, and meanwhile R = V - e^G K S as operand (effects: R alone)
         floatx4 KS[NT], QS[NT];
         Frag<PM> R[LB];
         {
@@ -786,7 +796,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 if (kb + 1 < KB) read(U::K, kb + 1, (kb + 1) & 1);
-                else read(U::Q, 0, (kb + 1) & 1);
+                else if (!EFFECTS) read(U::Q, 0, (kb + 1) & 1);
                 region_end();
                 mm_many<3, false>(kf[kb & 1], Sf[kb], ks, NoWeave());
                 region_end();
@@ -799,13 +809,14 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 for (int r = 0; r < 4; ++r) u[r] = fmaf(-decay[s][4 * e + r], KS[2 * s + e][r], to_float(next[s][4 * e + r]));
                 set_four<PM>(R[s], e, u);
             });
+            if constexpr (!EFFECTS)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                if (kb + 1 < KB) read(U::Q, kb + 1, (KB + kb + 1) & 1);
-                region_end();
-                mm_many<PO, true>(kf[(KB + kb) & 1], Sf[kb], qs, pieces);
-                region_end();
-            }
+                for (int kb = 0; kb < KB; ++kb) {
+                    if (kb + 1 < KB) read(U::Q, kb + 1, (KB + kb + 1) & 1);
+                    region_end();
+                    mm_many<PO, true>(kf[(KB + kb) & 1], Sf[kb], qs, pieces);
+                    region_end();
+                }
             pieces.rest();
 #pragma unroll
             for (int s = 0; s < LB; ++s) hold(R[s]);
@@ -825,7 +836,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         };
         read_t(0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) decay_o[i] = gates->decay[tile_index(i, m)], Ee[i] = floatx4{0, 0, 0, 0};
+        for (int i = 0; i < NT; ++i) decay_o[i] = EFFECTS ? 0.0f : gates->decay[tile_index(i, m)], Ee[i] = floatx4{0, 0, 0, 0};
         const float whole = gates->whole;
         auto split_u = [&](int s, int e) {
             float u[4], w[4];
@@ -834,7 +845,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 u[r] = be[s][4 * e + r] * Ee[2 * s + e][r];
                 w[r] = left[s][4 * e + r] * u[r];
             }
-            set_four<PO>(Uf[s], e, u);
+            if (!EFFECTS) set_four<PO>(Uf[s], e, u);
             set_four<PM>(W[s], e, w);
         };
         Frag<PO> pf[2][2];
@@ -849,12 +860,12 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             load_gates(gates->left + 8 * g, left[0]);
             region_end();
             auto pieces = weave<1, NT + DT>([&](int k) {
-                if (k < NT) QS[k] *= decay_o[k];
-                else S[k - NT] *= whole;
+                if (k >= DT) QS[k - DT] *= decay_o[k - DT];
+                else S[k] *= whole;
             });
             mm_many<3, false>(tf[0], R[0], to, pieces);
             if (LB > 1) read_t(1, 1, 0);
-            read_p(0, 0, 0);
+            if (!EFFECTS) read_p(0, 0, 0);
             pieces.rest();
         }
         if constexpr (LB > 1) {
@@ -885,15 +896,17 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         read_k(0);
         read_k(1);
         if constexpr (LB > 1) {
-            constexpr int MFMA = 4 * products(PO, PO, PO) + KB * 2 * products(PI, PM, 3);
+            constexpr int MFMA = (EFFECTS ? 0 : 4 * products(PO, PO, PO)) + KB * 2 * products(PI, PM, 3);
             floatx4 *o1[2] = {&QS[2], &QS[3]};
             auto pieces = weave<MFMA / 3, 2>([&](int e) { split_u(1, e); });
-            read_p(1, 0, 1);
-            region_end();
-            mm_many<PO, true>(pf[0], Uf[0], o0, pieces);
-            read_p(1, 1, 0);
-            region_end();
-            mm_many<PO, true>(pf[1], Uf[0], o1, pieces);
+            if constexpr (!EFFECTS) {
+                read_p(1, 0, 1);
+                region_end();
+                mm_many<PO, true>(pf[0], Uf[0], o0, pieces);
+                read_p(1, 1, 0);
+                region_end();
+                mm_many<PO, true>(pf[1], Uf[0], o1, pieces);
+            }
 #pragma unroll
             for (int pair = 0; pair < KB; ++pair) {
                 floatx4 *to[2] = {&S[2 * pair], &S[2 * pair + 1]};
@@ -922,13 +935,15 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             }
             auto pieces = weave<2, 2>([&](int e) { split_s(KB - 1, e); });
             floatx4 *to[2] = {&QS[NT - 2], &QS[NT - 1]};
-            mm_many<PO, true>(pf[0], Uf[LB - 1], to, pieces);
+            if constexpr (!EFFECTS) mm_many<PO, true>(pf[0], Uf[LB - 1], to, pieces);
+            pieces.rest();
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) hold(Sf[kb]);
             region_end();
         }
         // what the next chunk needs is there; the outputs are stored behind that wait and have the next chunk's time
         if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
+        if (EFFECTS) continue;
         const bool plain = mem.vec_o && t0 + L <= a.T && (all_columns || col0 + 16 <= a.Dv);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -944,6 +959,11 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             }
         }
     }
+    if (EFFECTS) {
+        const int width = mem.dvp + U::DKP;
+        if (col0 < width) store_tiles<DT>(mem.effects + at * U::DKP * width, width, tiles_at(width, col0, lane), lane, S);
+        return;
+    }
     // past the sequence's end
     const int last = min((begin + mem.segment_chunks) * L, a.T);
     for (int t = (n > begin ? n : begin) * L + g; t < last; t += 4)
@@ -951,181 +971,17 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     if (a.final_state && segment + 1 == mem.segments) store_state<DT>(a.final_state + (long long)head * a.Dk * a.Dv, a.Dk, a.Dv, col, g, S);
 }
 
-// LDS of the kernel below: K, gates, T | K'
-template <class E, int KB>
-struct EffectLds : ScanLds<DeltaUnits<E, KB>::Q + DeltaUnits<E, KB>::P, DeltaUnits<E, KB>::QT - DeltaUnits<E, KB>::KT> {};
-
-// The effect of each segment on the state, by the same walk without outputs: columns of B start from zeros, columns of A from the identity, without values.
-template <class E, int KB>
-__global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_effects(DeltaArgs a, DeltaMemory mem, int blocks_per_segment,
-                                                                                                        int segments)
-{
-    typedef DeltaUnits<E, KB> U;
-    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PM = DELTA_PM;
-    typedef EffectLds<E, KB> Lds;
-    constexpr int K_UNITS = U::Q, VALUE_UNITS = U::P;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), total = blockDim.x >> 6;
-    const int waves = total < SCAN_THREADS / 64 ? total - 1 : total;       // those that compute; the one beyond them loads
-    const bool loader = wave == waves, shared_out = waves == total;
-    const int m = lane & 15, g = lane >> 4;
-    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int block = id % blocks_per_segment, at = id / blocks_per_segment, segment = at % segments, head = at / segments;
-    const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
-    const int len = sequence_length(a, b), all = (len + L - 1) / L;
-    const int begin = segment * mem.segment_chunks, n = all < begin + mem.segment_chunks ? all : begin + mem.segment_chunks;
-    const unsigned char *key = mem.key + (long long)(b * a.Hk + hk) * mem.chunks * mem.key_units * 1024;
-    const unsigned char *value = mem.value + (long long)head * mem.chunks * mem.value_units * 1024;
-    const int width = mem.dvp + U::DKP, col0 = (block * waves + wave) * 16, col = col0 + m;
-    const bool of_values = col0 < mem.dvp;
-
-    floatx4 S[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = tile_index(t, 4 * g + r) == col - mem.dvp ? 1.0f : 0.0f;
-    const E *v = (const E *)a.v + (b * a.sv.batch + h * a.sv.head);
-    const unsigned at_v = (8 * g * (unsigned)a.sv.token + (col < a.Dv ? col : 0)) * sizeof(E);
-
-    auto load_first = [&](int chunk, int parity) {
-        unsigned char *to = Lds::first(lds, parity);
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, K_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
-        units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + K_UNITS * 1024, VALUE_UNITS, loader ? 0 : wave, shared_out ? waves : 1, lane);
-    };
-    auto load_last = [&](int chunk, int parity) {
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::KT) * 1024, Lds::last(lds, parity), Lds::LAST, loader ? 0 : wave, shared_out ? waves : 1, lane);
-    };
-    E next[LB][8] = {};
-    auto load_v = [&](int chunk) {
-        if (!of_values) return;
-        load_columns<E, LB>(v + (long long)chunk * L * a.sv.token, a.sv.token, at_v, g, len - chunk * L, next);
-        mask_columns<E, LB>(next, false, col < a.Dv, g, len - chunk * L);
-    };
-    auto load_next = [&](int chunk) {
-        if (!Lds::DOUBLE) load_last(chunk, chunk & 1);
-        if (chunk + 1 < n) {
-            load_first(chunk + 1, (chunk + 1) & 1);
-            if (Lds::DOUBLE) load_last(chunk + 1, (chunk + 1) & 1);
-        }
-    };
-    if (n > begin && (loader || shared_out)) {
-        load_first(begin, begin & 1);
-        if (Lds::DOUBLE) load_last(begin, begin & 1);
-    }
-    if (loader) {
-        for (int chunk = begin; chunk < n; ++chunk) {
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-            load_next(chunk);
-            if (!Lds::DOUBLE) {
-                __builtin_amdgcn_s_waitcnt(0);
-                __syncthreads();
-            }
-        }
-        return;
-    }
-    if (n > begin) load_v(begin);
-    __builtin_amdgcn_s_waitcnt(0);
-    for (int chunk = begin; chunk < n; ++chunk) {
-        const int parity = chunk & 1;
-        const unsigned char *ldsK = Lds::first(lds, parity), *ldsB = ldsK + K_UNITS * 1024, *ldsKT = Lds::last(lds, parity);
-        const DeltaGates<L> *gates = (const DeltaGates<L> *)ldsB;
-        __syncthreads();
-        const int after = chunk + 1 < n ? chunk + 1 : chunk;
-        if (shared_out) load_next(chunk);
-        float x[LB][8];
-#pragma unroll
-        for (int s = 0; s < LB; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[s][e] = to_float(next[s][e]);
-        load_v(after);
-        floatx4 KS[NT];
-        {
-            floatx4 *ks[NT];
-#pragma unroll
-            for (int i = 0; i < NT; ++i) KS[i] = floatx4{0, 0, 0, 0}, ks[i] = &KS[i];
-            Frag<PI> kf[2][NT];
-            auto read = [&](int kb) {
-#pragma unroll
-                for (int i = 0; i < NT; ++i) kf[kb & 1][i] = load_frag<PI>(ldsK + (i * KB + kb) * PI * 1024, lane);
-            };
-            read(0);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                if (kb + 1 < KB) read(kb + 1);
-                Frag<PM> Sf;
-                set_four<PM>(Sf, 0, {S[2 * kb][0], S[2 * kb][1], S[2 * kb][2], S[2 * kb][3]});
-                set_four<PM>(Sf, 1, {S[2 * kb + 1][0], S[2 * kb + 1][1], S[2 * kb + 1][2], S[2 * kb + 1][3]});
-                mm_many<3, false>(kf[kb & 1], Sf, ks, NoWeave());
-            }
-        }
-        Frag<PM> W[LB];
-        {
-            Frag<PM> R[LB];
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                float decay[8], u[8];
-                load_gates(gates->decay + 32 * s + 8 * g, decay);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = fmaf(-decay[e], KS[2 * s + (e >> 2)][e & 3], x[s][e]);
-                R[s] = make_frag<PM>(u);
-            }
-#pragma unroll
-            for (int s = 0; s < LB; ++s) {
-                Frag<PM> tf[LB][2];
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb)
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) tf[kb][p] = load_frag<PM>(ldsB + (U::T + U::lower(2 * s + p, kb) * PM) * 1024, lane);
-                floatx4 Ee[2] = {floatx4{0, 0, 0, 0}, floatx4{0, 0, 0, 0}}, *to[2] = {&Ee[0], &Ee[1]};
-#pragma unroll
-                for (int kb = 0; kb <= s; ++kb) mm_many<3, false>(tf[kb], R[kb], to, NoWeave());
-                float be[8], left[8], u[8];
-                load_gates(gates->beta + 32 * s + 8 * g, be);
-                load_gates(gates->left + 32 * s + 8 * g, left);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = left[e] * (be[e] * Ee[e >> 2][e & 3]);
-                W[s] = make_frag<PM>(u);
-            }
-        }
-        const float whole = gates->whole;
-        if (!Lds::DOUBLE) {
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-        }
-        {
-            Frag<PI> kf[2][2];
-            auto read = [&](int update) {
-#pragma unroll
-                for (int p = 0; p < 2; ++p) kf[update & 1][p] = load_frag<PI>(ldsKT + ((2 * (update / LB) + p) * LB + update % LB) * PI * 1024, lane);
-            };
-            read(0);
-#pragma unroll
-            for (int update = 0; update < KB * LB; ++update) {
-                const int t = 2 * (update / LB), kb = update % LB;
-                if (update + 1 < KB * LB) read(update + 1);
-                if (kb == 0) S[t] *= whole, S[t + 1] *= whole;
-                floatx4 *to[2] = {&S[t], &S[t + 1]};
-                mm_many<3, false>(kf[update & 1], W[kb], to, NoWeave());
-            }
-        }
-        if (Lds::DOUBLE) __builtin_amdgcn_s_waitcnt(0);
-    }
-    if (col0 < width) store_tiles<DT>(mem.effects + ((long long)head * mem.segments + segment) * U::DKP * width, width, tiles_at(width, col0, lane), lane, S);
-}
-
 // The states before the segments, one after the other: S <- A S + B.  BACK: the gradients of the states after them, from the last one:
 // dS <- A' dS + b.  A workgroup takes four tiles of columns of a head, two waves a tile, each with half of the state's rows: the waves split A
 // and their part of the state for all of them in LDS, and fetch the next segment's A and B meanwhile.
-constexpr int JOIN_TILES = 4;
+constexpr int JOIN_TILES = 4, JOIN_THREADS = 512;
 template <int KB>
 struct JoinLds { static constexpr int DT = 2 * KB, A = DT * KB * DELTA_PM, BYTES = (A + JOIN_TILES * KB * DELTA_PM) * 1024; };
 
 template <int KB, bool BACK>
-__global__ __launch_bounds__(SCAN_THREADS) void k_delta_join(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
+__global__ __launch_bounds__(JOIN_THREADS) void k_delta_join(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
-    constexpr int DT = 2 * KB, DKP = 32 * KB, PM = DELTA_PM, WAVES = SCAN_THREADS / 64, OWN = KB, FRAGS = (DT * KB + WAVES - 1) / WAVES;
+    constexpr int DT = 2 * KB, DKP = 32 * KB, PM = DELTA_PM, WAVES = JOIN_THREADS / 64, OWN = KB, FRAGS = (DT * KB + WAVES - 1) / WAVES;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     unsigned char *As = lds, *Ss = lds + JoinLds<KB>::A * 1024;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
