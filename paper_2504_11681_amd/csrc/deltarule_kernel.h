@@ -990,7 +990,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_delta_join(DeltaArgs a, DeltaM
     const int width = mem.dvp + DKP, col0 = (block * JOIN_TILES + tile) * 16, col = col0 + m;
     const bool live = col0 < mem.dvp;
     const float *from = BACK ? a.d_final : a.initial;
-    floatx4 S[OWN], next_b[OWN];
+    floatx4 S[OWN], next_b[OWN] = {};
     float next_a[FRAGS][8];
     // an element of the wave's rows
     auto at_row = [&](int t, int r) { return tile_index(half * KB + t, 4 * g + r); };
@@ -1008,17 +1008,30 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_delta_join(DeltaArgs a, DeltaM
     auto load_next = [&](int segment) {
         const long long at = (long long)head * mem.segments + segment;
         const float *A = mem.effects + at * DKP * width + mem.dvp;
-        load_own(BACK ? mem.back_effects + at * DKP * mem.dvp : mem.effects + at * DKP * width, DKP, mem.dvp, BACK ? mem.dvp : width, next_b);
+        const int stride = BACK ? mem.dvp : width;
+        if (live) {
+            const float *b = uniform((BACK ? mem.back_effects : mem.effects) + at * DKP * stride);
+            unsigned off = (8 * g * stride + col) * 4;
+            asm("" : "+v"(off));
+#pragma unroll
+            for (int t = 0; t < OWN; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) next_b[t][r] = *behind(b + (tile_index(half * KB + t, 0) + r) * stride, off);
+        }
 #pragma unroll
         for (int x = 0; x < FRAGS; ++x) {
             const int f = wave + x * WAVES;
             if (f < DT * KB) {
-                const int row = tile_index(f / KB, m), k = 32 * (f % KB) + 8 * g;
+                // row tile_index(f / KB, m), columns 32 (f % KB) + 8 g ..; of A' if BACK
+                const int row = tile_index(f / KB, 0), k = 32 * (f % KB), lane_row = 8 * (m >> 2) + (m & 3);
+                const float *p = uniform(BACK ? A + k * width + row : A + row * width + k);
+                unsigned off = (BACK ? 8 * g * width + lane_row : lane_row * width + 8 * g) * 4;
+                asm("" : "+v"(off));
                 if (BACK) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) next_a[x][e] = A[(k + e) * width + row];
+                    for (int e = 0; e < 8; ++e) next_a[x][e] = *behind(p + e * width, off);
                 } else {
-                    load8(A + row * width + k, 8, true, next_a[x]);
+                    load8(behind(p, off), 8, true, next_a[x]);
                 }
             }
         }
