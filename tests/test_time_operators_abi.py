@@ -259,3 +259,12 @@ def test_binding_refuses_shapes_of_the_norm_and_the_step_that_do_not_fit():
             step(*bad)
     with pytest.raises(TypeError):
         step(s, torch.zeros(2))
+
+
+def test_rule_says_which_distances_it_does_not_support(L):
+    """Tokens of v, o and their gradients are walked with 32-bit offsets inside a chunk: their distance is below 2^24 elements."""
+    far = tfno._Strides(1 << 30, 1 << 24, 64)
+    for n in ("v", "o"):
+        assert call(L.tfno_gated_delta_rule, rule_desc(**{n: far}), RULE) == tfno.ERR_UNSUPPORTED, n
+    for n in ("o", "dv"):            # the gradient is taken from the tape, which holds what it needs of v
+        assert call(L.tfno_gated_delta_rule_backward, rule_desc(**{n: far}), RULE_BACK) == tfno.ERR_UNSUPPORTED, n

@@ -170,6 +170,38 @@ def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
     check_forward(tfno, x, "without tape")
 
 
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(1, 1100, 1, 1, 128, 128), (1, 1217, 2, 2, 64, 100), (3, 640, 1, 2, 33, 40), (2, 961, 1, 1, 100, 256), (4, 383, 1, 1, 16, 16)])
+def test_few_heads_of_long_sequences(tfno, dtype, size):
+    """So few heads that a sequence is cut into segments of chunks; ends inside a chunk, chunks that no segment is full of."""
+    check_both(tfno, inputs(dtype, *size, seed=10), f"[case] segments {dtype} {size}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("T", (700, 1089))
+def test_lengths_of_few_heads(tfno, dtype, T):
+    """Sequences that end in the first segment, in the middle, at a segment's edge and past all of them, with NaN behind their ends."""
+    x = inputs(dtype, 7, T, 1, 2, 48, 40, seed=11)
+    x["lengths"] = torch.tensor([T, 0, 1, T // 2, 256, T + 50, 513], dtype=torch.int32, device="cuda")
+    live = oracle.tokens_of(x["lengths"], 7, T, "cuda")
+    for n in ("q", "k", "v", "g", "beta", "d_o"):
+        x[n][~live] = float("nan")
+    o, final, d = check_both(tfno, x, f"[case] lengths of segments {dtype} {T}")
+    for t in (o, d["q"], d["k"], d["v"], d["g"], d["beta"]):
+        assert (t[~live] == 0).all()
+    assert torch.equal(final[1], x["initial"][1]) and torch.equal(d["initial"][1], x["d_final"][1])
+    check_forward(tfno, x, "without tape")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_segments_that_forget_all_or_nothing(tfno, dtype):
+    x = inputs(dtype, 2, 900, 1, 1, 64, 64, seed=12)
+    x["g"][0] = 0.0
+    x["g"][1, ::100] = float("-inf")
+    x["beta"][1, 300:700] = 0.0
+    check_both(tfno, x, f"[case] segments at the gates' ends {dtype}")
+
+
 def test_no_tokens_at_all(tfno):
     x = inputs(F32, 3, 0, 2, 2, 16, 16, seed=7)
     tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
