@@ -407,9 +407,26 @@ def fno1d_real(x, W, y, stream=None):
 # ---------------------------------------------------------------- operators along time
 #
 # A call's descriptor and all checks of its arguments depend on types, devices, shapes and strides alone.  They are made once for each such
-# combination (_plan) and looked up afterwards: what a call costs on the host is its rate for one token.
+# combination (_plan) and looked up afterwards: what a call costs on the host is its rate for one token.  The combination's key and the call
+# itself are made in C++ (csrc/marshal.cpp).
 
 _plans = {}
+_marshal = None
+
+
+def _load_marshal():
+    global _marshal
+    lib()
+    if _torch is None:
+        _load_torch()
+    try:
+        from . import _marshal as m
+    except ImportError as e:
+        raise RuntimeError("_marshal.so is missing or of another torch: build it with `python -m paper_2504_11681_amd.build` "
+                           "(there is no fallback path)") from e
+    m.open(LIB_PATH)
+    _marshal = m
+    return m
 
 
 def _of(t):
@@ -417,10 +434,10 @@ def _of(t):
     return None if t is None else (t.dtype, t.get_device(), t.shape, t.stride())
 
 
-def _plan(key, make, *args):
+def _plan(key, make, tensors, *args):
     if len(_plans) >= 4096:
         _plans.clear()
-    plan = _plans[key] = make(*args)
+    plan = _plans[key] = make(*map(_of, tensors), *args)
     return plan
 
 
@@ -469,10 +486,6 @@ def _check_contiguous(shape, *tensors):
             step *= size
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
 def _head_norm_plan(q, k, q_out, k_out, dq, dk, positions, wq, wk, dwq, dwk, cos, sin, eps, interleaved):
     names = (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("dq", dq), ("dk", dk))
     _check_types(q, names, f32=(("wq", wq), ("wk", wk), ("dwq", dwq), ("dwk", dwk), ("cos", cos), ("sin", sin)), i32=(("positions", positions),))
@@ -493,17 +506,18 @@ def _head_norm_plan(q, k, q_out, k_out, dq, dk, positions, wq, wk, dwq, dwk, cos
     for (name, t), H in zip(names, (Hq, Hk) * 3):
         if t is not None:
             setattr(d, name, _strides4(name, t, (B, T, H, D)))
-    return ctypes.addressof(d), _entry("tfno_head_norm_rope_workspace_bytes")(D), d
+    return ctypes.addressof(d), _entry("tfno_head_norm_rope_workspace_bytes")(D), q[1], d
 
 
 def head_norm_rope(q, k, wq, wk, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6, interleaved: bool = False, stream=None):
     """Norm of queries and keys for each head with the rotation by position: q [B, T, Hq, D] and k [B, T, Hk, D] (float32 or bfloat16, any
     strides with the last axis contiguous) into q_out and k_out, which may be q and k themselves.  wq, wk: float32 [D] or None (ones);
     cos, sin: float32 [P, R / 2] or None (no rotation); positions: int32 [B, T] or None (0 .. T - 1)."""
-    key = (_of(q), _of(k), _of(q_out), _of(k_out), None, None, _of(positions), _of(wq), _of(wk), None, None, _of(cos), _of(sin), eps, interleaved)
-    plan = _plans.get(key) or _plan(key, _head_norm_plan, *key)
-    st = _entry("tfno_head_norm_rope")(plan[0], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
-                                       q_out.data_ptr(), k_out.data_ptr(), _raw_stream(key[0][1]) if stream is None else stream)
+    m = _marshal or _load_marshal()
+    tensors = (q, k, q_out, k_out, None, None, positions, wq, wk, None, None, cos, sin)
+    key = (m.key(*tensors), eps := float(eps), interleaved := bool(interleaved))
+    plan = _plans.get(key) or _plan(key, _head_norm_plan, tensors, eps, interleaved)
+    st = m.tfno_head_norm_rope(plan[0], q, k, wq, wk, cos, sin, positions, q_out, k_out, _raw_stream(plan[2]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_head_norm_rope")
     return q_out, k_out
@@ -512,13 +526,13 @@ def head_norm_rope(q, k, wq, wk, cos, sin, q_out, k_out, positions=None, eps: fl
 def head_norm_rope_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq, dk, dwq=None, dwk=None, positions=None, eps: float = 1e-6,
                             interleaved: bool = False, stream=None):
     """Gradients dq, dk and, where given, dwq, dwk (float32 [D]) of head_norm_rope from those of its results, dq_out and dk_out."""
-    key = (_of(q), _of(k), _of(dq_out), _of(dk_out), _of(dq), _of(dk), _of(positions), _of(wq), _of(wk), _of(dwq), _of(dwk), _of(cos), _of(sin), eps,
-           interleaved)
-    plan = _plans.get(key) or _plan(key, _head_norm_plan, *key)
+    m = _marshal or _load_marshal()
+    tensors = (q, k, dq_out, dk_out, dq, dk, positions, wq, wk, dwq, dwk, cos, sin)
+    key = (m.key(*tensors), eps := float(eps), interleaved := bool(interleaved))
+    plan = _plans.get(key) or _plan(key, _head_norm_plan, tensors, eps, interleaved)
     ensure_workspace(plan[1], q.device)
-    st = _entry("tfno_head_norm_rope_backward")(plan[0], q.data_ptr(), k.data_ptr(), _ptr(wq), _ptr(wk), _ptr(cos), _ptr(sin), _ptr(positions),
-                                                dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(dwq), _ptr(dwk),
-                                                _raw_stream(key[0][1]) if stream is None else stream)
+    st = m.tfno_head_norm_rope_backward(plan[0], q, k, wq, wk, cos, sin, positions, dq_out, dk_out, dq, dk, dwq, dwk,
+                                        _raw_stream(plan[2]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_head_norm_rope_backward")
     return dq, dk
@@ -549,14 +563,15 @@ def _rule_plan(q, k, v, o, g, beta, dq, dk, dv, dg, dbeta, lengths, tape, initia
     if tape is not None and (len(tape[2]) != 1 or tape[3][0] != 1 or tape[2][0] < need):
         raise ValueError(f"the tape must be contiguous and hold {need} bytes")
     ask = _entry("tfno_gated_delta_rule_workspace_bytes")
-    return at, need, ask(at, 0), ask(at, 1), d
+    return at, need, ask(at, 0), ask(at, 1), q[1], d
 
 
 def gated_delta_rule_tape(q, v):
     """A tape for gated_delta_rule and gated_delta_rule_backward on tensors of the sizes of q [B, T, Hk, Dk] and v [B, T, Hv, Dv]."""
     torch = _torch or _load_torch()
-    key = ("tape", _of(q), _of(v))
-    plan = _plans.get(key) or _plan(key, lambda: _rule_plan(key[1], key[1], key[2], *(None,) * 14))
+    m = _marshal or _load_marshal()
+    key = ("tape", m.key(q, v))
+    plan = _plans.get(key) or _plan(key, _rule_plan, (q, q, v, *(None,) * 13), None)
     return torch.empty(plan[1], dtype=torch.uint8, device=q.device)
 
 
@@ -564,13 +579,14 @@ def gated_delta_rule(q, k, v, g, beta, o, scale=None, initial_state=None, final_
     """The gated delta rule over whole sequences: q, k [B, T, Hk, Dk], v, o [B, T, Hv, Dv] (float32 or bfloat16, any strides with the last axis
     contiguous), g (log decay, or None) and beta float32 [B, T, Hv], states float32 [B, Hv, Dk, Dv], lengths int32 [B].  scale is Dk ** -0.5
     where it is not given.  With a tape (gated_delta_rule_tape) the gradient can be taken afterwards."""
-    key = (_of(q), _of(k), _of(v), _of(o), _of(g), _of(beta), None, None, None, None, None, _of(lengths), _of(tape), _of(initial_state),
-           _of(final_state), None, scale)
-    plan = _plans.get(key) or _plan(key, _rule_plan, *key)
+    m = _marshal or _load_marshal()
+    tensors = (q, k, v, o, g, beta, None, None, None, None, None, lengths, tape, initial_state, final_state, None)
+    key = ("rule", m.key(*tensors), scale := None if scale is None else float(scale))
+    plan = _plans.get(key) or _plan(key, _rule_plan, tensors, scale)
     if tape is None:
         ensure_workspace(plan[2], q.device)
-    st = _entry("tfno_gated_delta_rule")(plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state),
-                                         o.data_ptr(), _ptr(final_state), _ptr(tape), _raw_stream(key[0][1]) if stream is None else stream)
+    st = m.tfno_gated_delta_rule(plan[0], q, k, v, g, beta, lengths, initial_state, o, final_state, tape,
+                                 _raw_stream(plan[4]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule")
     return o
@@ -580,14 +596,13 @@ def gated_delta_rule_backward(q, k, v, g, beta, d_o, dq, dk, dv, dg, dbeta, tape
                               d_initial_state=None, lengths=None, stream=None):
     """Gradients of gated_delta_rule with the same inputs, from its tape and the gradients d_o of o and d_final_state of the final state
     (None: zeros).  dg and d_initial_state may be None."""
-    key = (_of(q), _of(k), _of(v), _of(d_o), _of(g), _of(beta), _of(dq), _of(dk), _of(dv), _of(dg), _of(dbeta), _of(lengths), _of(tape),
-           _of(initial_state), _of(d_final_state), _of(d_initial_state), scale)
-    plan = _plans.get(key) or _plan(key, _rule_plan, *key)
+    m = _marshal or _load_marshal()
+    tensors = (q, k, v, d_o, g, beta, dq, dk, dv, dg, dbeta, lengths, tape, initial_state, d_final_state, d_initial_state)
+    key = ("rule", m.key(*tensors), scale := None if scale is None else float(scale))
+    plan = _plans.get(key) or _plan(key, _rule_plan, tensors, scale)
     ensure_workspace(plan[3], q.device)
-    st = _entry("tfno_gated_delta_rule_backward")(
-        plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), _ptr(lengths), _ptr(initial_state), tape.data_ptr(), d_o.data_ptr(),
-        _ptr(d_final_state), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dg), dbeta.data_ptr(), _ptr(d_initial_state),
-        _raw_stream(key[0][1]) if stream is None else stream)
+    st = m.tfno_gated_delta_rule_backward(plan[0], q, k, v, g, beta, lengths, initial_state, tape, d_o, d_final_state, dq, dk, dv, dg, dbeta,
+                                          d_initial_state, _raw_stream(plan[4]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule_backward")
     return dq, dk, dv, dg, dbeta
@@ -614,16 +629,17 @@ def _step_plan(q, k, v, o, g, beta, states, slots, scale):
             if tuple(t[2]) != (B, Hv):
                 raise ValueError(f"{name} must be [B, Hv]")
             setattr(d, name, _Strides(t[3][0], 0, t[3][1]))
-    return ctypes.addressof(d), d
+    return ctypes.addressof(d), q[1], d
 
 
 def gated_delta_rule_step(q, k, v, g, beta, states, o, slots=None, scale=None, stream=None):
     """One token of the gated delta rule: q, k [B, Hk, Dk], v, o [B, Hv, Dv], g (or None) and beta float32 [B, Hv]; the states float32
     [pool, Hv, Dk, Dv] of the slots int32 [B] (None: 0 .. B - 1; negative: no sequence) are advanced in place."""
-    key = (_of(q), _of(k), _of(v), _of(o), _of(g), _of(beta), _of(states), _of(slots), scale)
-    plan = _plans.get(key) or _plan(key, _step_plan, *key)
-    st = _entry("tfno_gated_delta_rule_step")(plan[0], q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(g), beta.data_ptr(), states.data_ptr(), _ptr(slots),
-                                              key[6][2][0], o.data_ptr(), _raw_stream(key[0][1]) if stream is None else stream)
+    m = _marshal or _load_marshal()
+    tensors = (q, k, v, o, g, beta, states, slots)
+    key = ("step", m.key(*tensors), scale := None if scale is None else float(scale))
+    plan = _plans.get(key) or _plan(key, _step_plan, tensors, scale)
+    st = m.tfno_gated_delta_rule_step(plan[0], q, k, v, g, beta, states, slots, states.size(0), o, _raw_stream(plan[1]) if stream is None else stream)
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule_step")
     return o

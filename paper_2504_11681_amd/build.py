@@ -1,4 +1,4 @@
-"""Builds libtfno.so (the HIP library) in-tree with hipcc for gfx950.
+"""Builds libtfno.so (the HIP library) in-tree with hipcc for gfx950, and _marshal.so (calls from Python) with the host's compiler.
 
 Usage: ``python -m paper_2504_11681_amd.build``  (no GPU needed: hipcc cross-compiles).
 """
@@ -9,11 +9,13 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtfno.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 
 # packed FP32 instructions are switched off for all device code in this library
 HIPCC_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
@@ -30,17 +32,31 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _run(cmd, what: str) -> None:
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
+
+
+def _build_marshal() -> None:
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
+    _run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+          os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-ldl"], "marshal.cpp")
+
+
 def build(verbose: bool = True, jobs: int = 8) -> str:
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:
+        marshal = ex.submit(_build_marshal)
         objs = list(ex.map(_compile, srcs))
-    cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+        marshal.result()
+    _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], "link")
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources", file=sys.stderr)
+        print(f"built {LIB} from {len(srcs)} sources, and {MARSHAL}", file=sys.stderr)
     return LIB
 
 

@@ -268,3 +268,29 @@ def test_rule_says_which_distances_it_does_not_support(L):
         assert call(L.tfno_gated_delta_rule, rule_desc(**{n: far}), RULE) == tfno.ERR_UNSUPPORTED, n
     for n in ("o", "dv"):            # the gradient is taken from the tape, which holds what it needs of v
         assert call(L.tfno_gated_delta_rule_backward, rule_desc(**{n: far}), RULE_BACK) == tfno.ERR_UNSUPPORTED, n
+
+
+def test_key_holds_all_that_a_plan_depends_on(L):
+    m = tfno._load_marshal()
+    x = torch.zeros(2, 3, 4)
+    keys = [m.key(t) for t in (x, x.bfloat16(), x.int(), x.byte(), x[:1], x[:, :0], x.transpose(0, 1), x.expand(2, 3, 4).as_strided((2, 3, 4), (0, 4, 1)),
+                               x.as_strided((1, 3, 4), (1 << 40, 4, 1)), x[0], x[0, 0], x[0, 0, 0], None)]
+    keys += [m.key(), m.key(x, None), m.key(None, x), m.key(x, x), m.key(None, None)]
+    assert len(set(keys)) == len(keys)
+    assert m.key(x, None) == m.key(torch.ones(2, 3, 4), None)
+
+
+def test_what_is_no_tensor_or_has_no_memory_of_its_own_values_is_refused(L):
+    m = tfno._load_marshal()
+    x = torch.zeros(2, 8, 2, 64, dtype=torch.complex64)
+    for bad, error in ((1.0, TypeError), ("x", TypeError), (x.conj(), ValueError), (x.conj().imag, ValueError), (x.real.to_sparse(), ValueError),
+                       (torch.zeros((1,) * 9), ValueError)):
+        with pytest.raises(error):
+            m.key(bad)
+    with pytest.raises(TypeError):
+        m.tfno_gated_delta_rule_step(None)
+    q = torch.zeros(2, 8, 2, 64)
+    with pytest.raises(TypeError):                       # not on a GPU
+        tfno.head_norm_rope(q, q, None, None, None, None, q, q)
+    with pytest.raises((TypeError, AttributeError)):
+        tfno.gated_delta_rule(None, None, None, None, None, None)
