@@ -44,6 +44,25 @@ __device__ __forceinline__ void load4(const bf16 *p, float (&v)[4])
     v[0] = __uint_as_float(t.x << 16), v[1] = __uint_as_float(t.x & 0xffff0000u);
     v[2] = __uint_as_float(t.y << 16), v[3] = __uint_as_float(t.y & 0xffff0000u);
 }
+// The same as they stand in memory, for values that wait in registers.
+template <class E>
+struct Quad;
+template <>
+struct Quad<float> {
+    float4 at;
+    __device__ __forceinline__ void load(const float *p) { at = *reinterpret_cast<const float4 *>(p); }
+    __device__ __forceinline__ void values(float (&v)[4]) const { v[0] = at.x, v[1] = at.y, v[2] = at.z, v[3] = at.w; }
+};
+template <>
+struct Quad<bf16> {
+    uint2 at;
+    __device__ __forceinline__ void load(const bf16 *p) { at = *reinterpret_cast<const uint2 *>(p); }
+    __device__ __forceinline__ void values(float (&v)[4]) const
+    {
+        v[0] = __uint_as_float(at.x << 16), v[1] = __uint_as_float(at.x & 0xffff0000u);
+        v[2] = __uint_as_float(at.y << 16), v[3] = __uint_as_float(at.y & 0xffff0000u);
+    }
+};
 __device__ __forceinline__ void store4(float *p, const float (&v)[4]) { *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 __device__ __forceinline__ void store4(bf16 *p, const float (&v)[4])
 {

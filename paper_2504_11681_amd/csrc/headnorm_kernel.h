@@ -6,13 +6,19 @@
 // holds pairs of values, the two that one rotation turns into each other, so the rotation needs no exchange between lanes and the
 // norm one sum over the group.  The values past the first R go through as pairs that are not turned.  A group takes NH heads
 // of one token, whose angles it loads once.  A workgroup takes heads of queries or heads of keys, never both: one set of weights.
+//
+// What is loaded waits in registers as it stands in memory, so that four waves of a SIMD fit beside all loads of four heads: with its values as
+// float32 three did, and the gradient of 16 x 1024 tokens of 16 + 8 heads of 128 in BF16 took 98 us; it takes 60 (302 MB, 5.0 TB/s, what a copy
+// reaches), the forward pass 43 (201 MB, 4.6 TB/s).
 #pragma once
 #include "headnorm.h"
 
 namespace tfno {
 
 constexpr int HEAD_NORM_THREADS = 256;
-constexpr int HEAD_NORM_BLOCKS = 2048;     // of the backward kernel, at most: each leaves one partial sum of the weights' gradient
+// Workgroups of the backward kernel, at most: as many as the chip holds at four waves a SIMD, each with one partial sum of the weights' gradient (both
+// directions of the batch above: 104 us; with 768 111, with 512 128, with 2048 107).
+constexpr int HEAD_NORM_BLOCKS = 1024;
 
 struct HeadNormShape {
     int lpr;                        // lanes of a head
@@ -20,23 +26,34 @@ struct HeadNormShape {
     unsigned chunks[2], items[2];   // groups of NH heads of a token, and of all tokens: queries, keys
 };
 
-// The two halves of VEC pairs: values first[] and second[] of the head at `p`.
+// VEC pairs of the head at `p` as they stand in memory (in BF16 half the registers of their values), until they are used.
 template <class E, int VEC, bool INTER>
-__device__ __forceinline__ void load_pairs(const E *p, int first, int second, bool has_second, float (&x)[VEC], float (&y)[VEC])
-{
-    if constexpr (VEC == 4 && INTER) {
-        float u[4], v[4];
-        load4(p + first, u);
-        load4(p + first + 4, v);
-        x[0] = u[0], y[0] = u[1], x[1] = u[2], y[1] = u[3], x[2] = v[0], y[2] = v[1], x[3] = v[2], y[3] = v[3];
-    } else if constexpr (VEC == 4) {
-        load4(p + first, x);
-        load4(p + second, y);
-    } else {
-        x[0] = to_float(p[first]);
-        y[0] = has_second ? to_float(p[second]) : 0.0f;
+struct Pairs {
+    Quad<E> u, v;
+    __device__ __forceinline__ void clear() { u = v = {}; }
+    __device__ __forceinline__ void load(const E *p, int first, int second, bool) { u.load(p + first), v.load(p + (INTER ? first + 4 : second)); }
+    __device__ __forceinline__ void values(float (&x)[VEC], float (&y)[VEC]) const
+    {
+        if constexpr (INTER) {
+            float a[4], b[4];
+            u.values(a), v.values(b);
+            x[0] = a[0], y[0] = a[1], x[1] = a[2], y[1] = a[3], x[2] = b[0], y[2] = b[1], x[3] = b[2], y[3] = b[3];
+        } else {
+            u.values(x), v.values(y);
+        }
     }
-}
+};
+template <class E, bool INTER>
+struct Pairs<E, 1, INTER> {
+    E u, v;
+    __device__ __forceinline__ void clear() { u = v = {}; }
+    __device__ __forceinline__ void load(const E *p, int first, int second, bool has_second)
+    {
+        u = p[first];
+        if (has_second) v = p[second];
+    }
+    __device__ __forceinline__ void values(float (&x)[1], float (&y)[1]) const { x[0] = to_float(u), y[0] = to_float(v); }
+};
 template <class E, int VEC, bool INTER>
 __device__ __forceinline__ void store_pairs(E *p, int first, int second, bool has_second, const float (&x)[VEC], const float (&y)[VEC])
 {
@@ -54,7 +71,7 @@ __device__ __forceinline__ void store_pairs(E *p, int first, int second, bool ha
 }
 
 template <class E, int VEC, int ITER, int NH, bool INTER, bool BACKWARD>
-__global__ __launch_bounds__(HEAD_NORM_THREADS) void k_head_norm(HeadNormArgs a, HeadNormShape s)
+__global__ __launch_bounds__(HEAD_NORM_THREADS) __attribute__((amdgpu_waves_per_eu(4))) void k_head_norm(HeadNormArgs a, HeadNormShape s)
 {
     const int lane = threadIdx.x & (s.lpr - 1), group = threadIdx.x / s.lpr, groups = HEAD_NORM_THREADS / s.lpr;
     const int turned = a.R >> 1, rest = (a.D - a.R + 1) >> 1;
@@ -89,18 +106,18 @@ __global__ __launch_bounds__(HEAD_NORM_THREADS) void k_head_norm(HeadNormArgs a,
     for (unsigned item = block * groups + group; item < items; item += blocks * groups) {
         const unsigned token = item / chunks, chunk = item - token * chunks;
         const unsigned b = token / (unsigned)a.T, t = token - b * (unsigned)a.T;
-        float x[2][NH][ITER][VEC], d[2][NH][ITER][VEC];
+        Pairs<E, VEC, INTER> in_x[NH][ITER], in_d[BACKWARD ? NH : 1][ITER];
         const E *p = in + (b * si.batch + t * si.token), *o = grad + (b * sg.batch + t * sg.token);
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
             const int h = chunk * NH + n;
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) x[0][n][i][e] = x[1][n][i][e] = d[0][n][i][e] = d[1][n][i][e] = 0.0f;
+                in_x[n][i].clear();
+                if constexpr (BACKWARD) in_d[n][i].clear();
                 if (!has[i] || h >= H) continue;
-                load_pairs<E, VEC, INTER>(p + h * si.head, first[i], second[i], has_second[i], x[0][n][i], x[1][n][i]);
-                if constexpr (BACKWARD) load_pairs<E, VEC, INTER>(o + h * sg.head, first[i], second[i], has_second[i], d[0][n][i], d[1][n][i]);
+                in_x[n][i].load(p + h * si.head, first[i], second[i], has_second[i]);
+                if constexpr (BACKWARD) in_d[n][i].load(o + h * sg.head, first[i], second[i], has_second[i]);
             }
         }
         // the token's angles; a position that the tables do not hold gives NaN, and nothing is read for it
@@ -130,20 +147,23 @@ __global__ __launch_bounds__(HEAD_NORM_THREADS) void k_head_norm(HeadNormArgs a,
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
             const int h = chunk * NH + n;
-            float squares = 0.0f, dot = 0.0f;
+            float squares = 0.0f, dot = 0.0f, x[2][ITER][VEC], d[2][ITER][VEC];
 #pragma unroll
-            for (int i = 0; i < ITER; ++i)
+            for (int i = 0; i < ITER; ++i) {
+                in_x[n][i].values(x[0][i], x[1][i]);
+                if constexpr (BACKWARD) in_d[n][i].values(d[0][i], d[1][i]);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    squares = fmaf(x[0][n][i][e], x[0][n][i][e], fmaf(x[1][n][i][e], x[1][n][i][e], squares));
+                    squares = fmaf(x[0][i][e], x[0][i][e], fmaf(x[1][i][e], x[1][i][e], squares));
                     if constexpr (BACKWARD) {
-                        const float u = d[0][n][i][e], v = d[1][n][i][e];
-                        d[0][n][i][e] = fmaf(u, c[i][e], v * r[i][e]);
-                        d[1][n][i][e] = fmaf(v, c[i][e], -(u * r[i][e]));
-                        dot = fmaf(d[0][n][i][e] * w[0][i][e], x[0][n][i][e], dot);
-                        dot = fmaf(d[1][n][i][e] * w[1][i][e], x[1][n][i][e], dot);
+                        const float u = d[0][i][e], v = d[1][i][e];
+                        d[0][i][e] = fmaf(u, c[i][e], v * r[i][e]);
+                        d[1][i][e] = fmaf(v, c[i][e], -(u * r[i][e]));
+                        dot = fmaf(d[0][i][e] * w[0][i][e], x[0][i][e], dot);
+                        dot = fmaf(d[1][i][e] * w[1][i][e], x[1][i][e], dot);
                     }
                 }
+            }
             squares = group_sum(squares, s.lpr);
             const float norm = 1.0f / sqrtf(fmaf(squares, over_D, a.eps));
             float mean = 0.0f;
@@ -155,12 +175,12 @@ __global__ __launch_bounds__(HEAD_NORM_THREADS) void k_head_norm(HeadNormArgs a,
                 for (int e = 0; e < VEC; ++e) {
                     if constexpr (BACKWARD) {
                         // a head past the last one has zeros in d
-                        dw[0][i][e] = fmaf(d[0][n][i][e], x[0][n][i][e] * norm, dw[0][i][e]);
-                        dw[1][i][e] = fmaf(d[1][n][i][e], x[1][n][i][e] * norm, dw[1][i][e]);
-                        y[0][e] = norm * fmaf(d[0][n][i][e], w[0][i][e], -(x[0][n][i][e] * mean));
-                        y[1][e] = norm * fmaf(d[1][n][i][e], w[1][i][e], -(x[1][n][i][e] * mean));
+                        dw[0][i][e] = fmaf(d[0][i][e], x[0][i][e] * norm, dw[0][i][e]);
+                        dw[1][i][e] = fmaf(d[1][i][e], x[1][i][e] * norm, dw[1][i][e]);
+                        y[0][e] = norm * fmaf(d[0][i][e], w[0][i][e], -(x[0][i][e] * mean));
+                        y[1][e] = norm * fmaf(d[1][i][e], w[1][i][e], -(x[1][i][e] * mean));
                     } else {
-                        const float n0 = x[0][n][i][e] * norm * w[0][i][e], n1 = x[1][n][i][e] * norm * w[1][i][e];
+                        const float n0 = x[0][i][e] * norm * w[0][i][e], n1 = x[1][i][e] * norm * w[1][i][e];
                         y[0][e] = fmaf(n0, c[i][e], -(n1 * r[i][e]));
                         y[1][e] = fmaf(n0, r[i][e], n1 * c[i][e]);
                     }
