@@ -315,7 +315,52 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         load8(behind(p, off), token < len ? a.Dv - 32 * kb - 8 * g : 0, vec.d_o, u);
     };
 
+    // rows of 32 columns between the kernels: a uniform address, and the lane's row of a tile and its eight columns
+    const unsigned at_row = ((8 * (m >> 2) + (m & 3)) * mem.dvp + 8 * g) * 4;
+    auto load_row = [&](const float *p, int tile, float (&x)[8]) {
+        unsigned off = at_row;
+        asm("" : "+v"(off));
+        load8(behind(uniform(p + tile_index(tile, 0) * mem.dvp), off), 8, true, x);
+    };
+
     if (pairs) {
+        constexpr int TILES = DT > NT ? DT / NT : 1;
+        struct Round { float s[TILES][8], d[TILES][8], e[8], y[8]; } next;
+        float next_o[8], dot = 0.0f;
+        // Splits what waits in `next` as round `split` (-1: nothing does) and loads round `load` (from `count` on: none), a row of tiles after the other: all loads
+        // at once fill the queues, and the wave stands still until they have room.
+        const int count = group * rounds;
+        auto turn = [&](int split, int load) {
+            unsigned char *panel = lds + (split & 1) * Lds::UNITS * 1024;
+            const int member = load / rounds, kb = load - member * rounds;
+            const long long at = part(member);
+#pragma unroll
+            for (int p = 0; p < TILES; ++p) {
+                const int t = i + p * NT;
+                if (t < DT) {
+                    if (split >= 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) dot = fmaf(next.s[p][e], next.d[p][e], dot);
+                        store_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane, make_frag<PM>(next.s[p]));
+                        store_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane, make_frag<PM>(next.d[p]));
+                    }
+                    if (load < count) {
+                        load_row(mem.states + at * DKP * mem.dvp + 32 * kb, t, next.s[p]);
+                        load_row(mem.d_states + at * DKP * mem.dvp + 32 * kb, t, next.d[p]);
+                    }
+                }
+            }
+            if (split >= 0) {
+                store_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane, make_frag<PM>(next.e));
+                store_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane, make_frag<PM>(next.y));
+            }
+            if (load < count) {
+                load_row(mem.errors + at * L * mem.dvp + 32 * kb, i, next.e);
+                load_row(mem.d_values + at * L * mem.dvp + 32 * kb, i, next.y);
+            }
+        };
+        turn(-1, 0);
+        load_do(0, 0, next_o);
         floatx4 kk[NT], qk[NT], mq[NT], mk[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) kk[j] = qk[j] = mq[j] = mk[j] = floatx4{0, 0, 0, 0};
@@ -329,8 +374,7 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
                 qk[j] = mm<3>(qf, other, qk[j]);
             }
         }
-        float next[8];
-        load_do(0, 0, next);
+        turn(0, 1);
         for (int member = 0; member < group; ++member) {
             const long long at = part(member);
             const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
@@ -343,11 +387,18 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
 #pragma unroll
             for (int j = 0; j < NT; ++j) D[j] = C[j] = floatx4{0, 0, 0, 0};
             for (int kb = 0; kb < rounds; ++kb) {
-                const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
-                const Frag<PI> of = make_frag<PI>(next);
-                if (kb + 1 < rounds) load_do(member, kb + 1, next);
-                else if (member + 1 < group) load_do(member + 1, 0, next);
+                const int round = member * rounds + kb;
+                const unsigned char *panel = lds + (round & 1) * Lds::UNITS * 1024;
+                const Frag<PI> of = make_frag<PI>(next_o);
                 __syncthreads();
+                if (kb + 1 < rounds) load_do(member, kb + 1, next_o);
+                else {
+                    if (member + 1 < group) load_do(member + 1, 0, next_o);
+                    dot = group_sum(dot, 64);                  // the member's states have all been through
+                    if (lane == 0) inner[i] = dot;
+                    dot = 0.0f;
+                }
+                if (round + 1 < count) turn(round + 1, round + 2);
                 const Frag<PM> yf = load_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
@@ -421,32 +472,9 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
 
     // the waves of the states.  Factors of a token go into its operand, so that dq and dk add up without a second set of accumulators; what a member adds
     // to q.dq and k.dk is then the difference of the sums behind and before it
-    constexpr int TILES = DT > NT ? DT / NT : 1;
     floatx4 accq[DT], acck[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) accq[t] = acck[t] = floatx4{0, 0, 0, 0};
-    struct Round { float s[TILES][8], d[TILES][8], e[8], y[8], o[8]; } next;
-    // rows of 32 columns between the kernels: a uniform address, and the lane's row of a tile and its eight columns
-    const unsigned at_row = ((8 * (m >> 2) + (m & 3)) * mem.dvp + 8 * g) * 4;
-    auto load_row = [&](const float *p, int tile, float (&x)[8]) {
-        unsigned off = at_row;
-        asm("" : "+v"(off));
-        load8(behind(uniform(p + tile_index(tile, 0) * mem.dvp), off), 8, true, x);
-    };
-    auto load_round = [&](int member, int kb, Round &x) {
-        const long long at = part(member);
-#pragma unroll
-        for (int p = 0; p < TILES; ++p) {
-            const int t = i + p * NT;
-            if (t < DT) {
-                load_row(mem.states + at * DKP * mem.dvp + 32 * kb, t, x.s[p]);
-                load_row(mem.d_states + at * DKP * mem.dvp + 32 * kb, t, x.d[p]);
-            }
-        }
-        load_row(mem.errors + at * L * mem.dvp + 32 * kb, i, x.e);
-        load_row(mem.d_values + at * L * mem.dvp + 32 * kb, i, x.y);
-        load_do(member, kb, x.o);
-    };
     const int tok = tile_index(i, m);
     // sums over the state's rows of q times accq and k times x
     auto dots = [&](const floatx4 (&x)[DT], float &q_sum, float &k_sum) {
@@ -464,37 +492,30 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         q_sum += __shfl_xor(q_sum, 16, 64), q_sum += __shfl_xor(q_sum, 32, 64);
         k_sum += __shfl_xor(k_sum, 16, 64), k_sum += __shfl_xor(k_sum, 32, 64);
     };
-    load_round(0, 0, next);
+    struct { float y[8], o[8]; } next;
+    auto load_round = [&](int member, int kb) {
+        load_row(mem.d_values + part(member) * L * mem.dvp + 32 * kb, i, next.y);
+        load_do(member, kb, next.o);
+    };
+    load_round(0, 0);
     for (int member = 0; member < group; ++member) {
         const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + part(member) * mem.value_units * 1024);
         const float decay = gates->decay[tok], fe = gates->left[tok], be = gates->beta[tok];
         floatx4 he[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t) he[t] = floatx4{0, 0, 0, 0};
-        float dot = 0.0f, q_before = 0.0f, k_before = 0.0f, q_sum, k_sum, e_sum, unused;
+        float q_before = 0.0f, k_before = 0.0f, q_sum, k_sum, e_sum, unused;
         if (member > 0) dots(acck, q_before, k_before);
         for (int kb = 0; kb < rounds; ++kb) {
-            unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
-#pragma unroll
-            for (int p = 0; p < TILES; ++p) {
-                const int t = i + p * NT;
-                if (t < DT) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dot = fmaf(next.s[p][e], next.d[p][e], dot);
-                    store_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane, make_frag<PM>(next.s[p]));
-                    store_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane, make_frag<PM>(next.d[p]));
-                }
-            }
-            const Frag<PM> ef = make_frag<PM>(next.e);
-            store_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane, ef);
-            store_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane, make_frag<PM>(next.y));
+            const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
             float u[8], w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] = a.scale * decay * next.o[e], w[e] = -decay * next.y[e];
             const Frag<PM> of = make_frag<PM>(u), yf = make_frag<PM>(w);
-            if (kb + 1 < rounds) load_round(member, kb + 1, next);
-            else if (member + 1 < group) load_round(member + 1, 0, next);
+            if (kb + 1 < rounds) load_round(member, kb + 1);
+            else if (member + 1 < group) load_round(member + 1, 0);
             __syncthreads();
+            const Frag<PM> ef = load_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane);
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 const Frag<PM> sf = load_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane), df = load_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane);
@@ -508,8 +529,6 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
                     }
             }
         }
-        dot = group_sum(dot, 64);
-        if (lane == 0) inner[i] = dot;
         dots(acck, q_sum, k_sum);
         dots(he, unused, e_sum);
         const float tb = fe * e_sum;
