@@ -325,7 +325,7 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
 
     if (pairs) {
         constexpr int TILES = DT > NT ? DT / NT : 1;
-        struct Round { float s[TILES][8], d[TILES][8], e[8], y[8]; } next;
+        struct Round { float s[TILES][8], d[TILES][8]; } next;
         float next_o[8], dot = 0.0f;
         // Splits what waits in `next` as round `split` (-1: nothing does) and loads round `load` (from `count` on: none), a row of tiles after the other: all loads
         // at once fill the queues, and the wave stands still until they have room.
@@ -349,14 +349,6 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
                         load_row(mem.d_states + at * DKP * mem.dvp + 32 * kb, t, next.d[p]);
                     }
                 }
-            }
-            if (split >= 0) {
-                store_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane, make_frag<PM>(next.e));
-                store_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane, make_frag<PM>(next.y));
-            }
-            if (load < count) {
-                load_row(mem.errors + at * L * mem.dvp + 32 * kb, i, next.e);
-                load_row(mem.d_values + at * L * mem.dvp + 32 * kb, i, next.y);
             }
         };
         turn(-1, 0);
@@ -492,15 +484,33 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         q_sum += __shfl_xor(q_sum, 16, 64), q_sum += __shfl_xor(q_sum, 32, 64);
         k_sum += __shfl_xor(k_sum, 16, 64), k_sum += __shfl_xor(k_sum, 32, 64);
     };
-    struct { float y[8], o[8]; } next;
-    auto load_round = [&](int member, int kb) {
+    const int count = group * rounds;
+    struct { float e[8], y[8], o[8]; } next;
+    Frag<PM> ef, of, yf;
+    auto load_round = [&](int round) {
+        const int member = round / rounds, kb = round - member * rounds;
+        load_row(mem.errors + part(member) * L * mem.dvp + 32 * kb, i, next.e);
         load_row(mem.d_values + part(member) * L * mem.dvp + 32 * kb, i, next.y);
         load_do(member, kb, next.o);
     };
-    load_round(0, 0);
+    // Splits the errors and gradients of a round: for the waves of token pairs, and with the token's factor for this one.
+    auto split_round = [&](int round, float decay) {
+        unsigned char *panel = lds + (round & 1) * Lds::UNITS * 1024;
+        ef = make_frag<PM>(next.e);
+        store_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane, ef);
+        store_frag<PM>(panel + (Lds::Y + i * PM) * 1024, lane, make_frag<PM>(next.y));
+        float u[8], w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = a.scale * decay * next.o[e], w[e] = -decay * next.y[e];
+        of = make_frag<PM>(u), yf = make_frag<PM>(w);
+    };
+    auto gates_of = [&](int member) { return (const DeltaGates<L> *)(mem.value + part(member) * mem.value_units * 1024); };
+    load_round(0);
+    split_round(0, gates_of(0)->decay[tok]);
+    if (count > 1) load_round(1);
     for (int member = 0; member < group; ++member) {
-        const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + part(member) * mem.value_units * 1024);
-        const float decay = gates->decay[tok], fe = gates->left[tok], be = gates->beta[tok];
+        const DeltaGates<L> *gates = gates_of(member);
+        const float fe = gates->left[tok], be = gates->beta[tok], decay = gates->decay[tok], next_decay = gates_of(min(member + 1, group - 1))->decay[tok];
         floatx4 he[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t) he[t] = floatx4{0, 0, 0, 0};
@@ -508,14 +518,7 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         if (member > 0) dots(acck, q_before, k_before);
         for (int kb = 0; kb < rounds; ++kb) {
             const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
-            float u[8], w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = a.scale * decay * next.o[e], w[e] = -decay * next.y[e];
-            const Frag<PM> of = make_frag<PM>(u), yf = make_frag<PM>(w);
-            if (kb + 1 < rounds) load_round(member, kb + 1);
-            else if (member + 1 < group) load_round(member + 1, 0);
             __syncthreads();
-            const Frag<PM> ef = load_frag<PM>(panel + (Lds::ERR + i * PM) * 1024, lane);
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 const Frag<PM> sf = load_frag<PM>(panel + (Lds::S + t * PM) * 1024, lane), df = load_frag<PM>(panel + (Lds::D + t * PM) * 1024, lane);
@@ -528,6 +531,9 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
                         he[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df.part(p), ef.part(sum - p), he[t], 0, 0, 0);
                     }
             }
+            const int round = member * rounds + kb + 1;
+            if (round < count) split_round(round, kb + 1 < rounds ? decay : next_decay);
+            if (round + 1 < count) load_round(round + 1);
         }
         dots(acck, q_sum, k_sum);
         dots(he, unused, e_sum);
