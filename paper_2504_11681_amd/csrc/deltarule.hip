@@ -148,6 +148,8 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s)
     DeltaVec vec{};
     vec.q = rows_of_8(a.q, a.sq, a.bf16), vec.k = rows_of_8(a.k, a.sk, a.bf16);
     m.vec_o = rows_of_4(a.o, a.so, a.Dv, a.bf16);
+    // Without a tape nothing else needs blocks of K and Q, and in BF16 they are the rows that the caller has.
+    m.rows = !tape && a.bf16 && vec.q && vec.k && a.Dk % 8 == 0;
     const unsigned grid = (unsigned)(a.B * a.Hv * m.chunks);
     if (grid && tape) k_delta_prepare<E, KB, true><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);

@@ -208,6 +208,8 @@ struct DeltaGates {
     float left[L];         // exp(GL - G)
     float whole;           // exp(GL)
 };
+constexpr int DELTA_ZEROS = 1024 - 16;      // behind them in that unit: 16 bytes of zeros, where `rows` is set
+
 
 // Where the parts of a call's memory lie.
 struct DeltaMemory {
@@ -222,6 +224,7 @@ struct DeltaMemory {
     float *segment_states;           // [b][hv][segment][DKP][DVP]: the state before each
     float *back_effects;             // backward: [b][hv][segment][DKP][DVP]: the gradient that a segment itself adds to that of the state before it
     float *segment_d_states;         // backward: the gradient of the state after each segment
+    bool rows;                       // the scans take K and Q from the caller's tensors: no blocks of them
     bool vec_o, vec_dv;              // rows of o and of the gradient of v take four elements at a time
 };
 
@@ -434,6 +437,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
             gates->beta[lane] = be;
             gates->left[lane] = __builtin_amdgcn_exp2f((float)(all - s));
             if (lane == 0) gates->whole = __builtin_amdgcn_exp2f((float)all);
+            if (lane == 0 && !TAPE) *(uint4 *)(value + DELTA_ZEROS) = uint4{0, 0, 0, 0};
             if (TAPE) {
                 float *logs = mem.logs + (head * mem.chunks + chunk) * 2 * L;
                 logs[lane] = h0, logs[L + lane] = l0;
@@ -450,7 +454,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const Frag<PI> kf = row_frag<PI>(Ks + own * ROW + 32 * kb + 8 * g), qf = row_frag<PI>(Qs + own * ROW + 32 * kb + 8 * g);
-            if (first) {
+            if (first && (TAPE || !mem.rows)) {
                 store_frag<PI>(key + (U::K + (w * KB + kb) * PI) * 1024, lane, kf);
                 store_frag<PI>(key + (U::Q + (w * KB + kb) * PI) * 1024, lane, qf);
             }
@@ -576,6 +580,13 @@ __device__ __forceinline__ void units_to_lds(const unsigned char *from, const un
     unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
     for (int u = 0; u < units; ++u, lds += 1024, from += 1024)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(at), "s"(from));
+}
+
+// The same from 16 bytes of each lane's own.
+__device__ __forceinline__ void lanes_to_lds(const void *from, const unsigned char *to)
+{
+    const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from));
 }
 
 // The element `bytes` behind a uniform address: 32 bits a lane, so that the address stays scalar.
@@ -741,9 +752,26 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
     const int lane_token = 8 * (m >> 2) + (m & 3);              // where tokens are columns: token lane_token of a tile, columns col0 + 4 g ..
     const unsigned at_o = (lane_token * (unsigned)a.so.token + 4 * g) * sizeof(E);
 
+    // Blocks of a tensor of BF16 are its rows as they are, 16 bytes a lane; lanes past its end read zeros.
+    auto rows_to_lds = [&](const void *x, const Strides &s, int chunk, unsigned char *to) {
+        const E *p = (const E *)x + (b * s.batch + hk * s.head + (long long)(chunk * L + 8 * (m >> 2) + (m & 3)) * s.token + 8 * g);
+        const void *zeros = value + (long long)chunk * mem.value_units * 1024 + DELTA_ZEROS;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const E *row = p + tile_index(i, 0) * s.token;
+            const bool there = chunk * L + tile_index(i, m) < len;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb, to += 1024) lanes_to_lds(there && 32 * kb + 8 * g < a.Dk ? (const void *)(row + 32 * kb) : zeros, to);
+        }
+    };
     auto load_first = [&](int chunk, int parity) {
         unsigned char *to = Lds::first(lds, parity);
-        units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, lane);
+        if (PI == 1 && !TAPE && mem.rows) {
+            rows_to_lds(a.k, a.sk, chunk, to);
+            if (!EFFECTS) rows_to_lds(a.q, a.sq, chunk, to + U::Q * 1024);
+        } else {
+            units_to_lds(key + ((long long)chunk * mem.key_units + U::K) * 1024, to, A_UNITS, lane);
+        }
         units_to_lds(value + (long long)chunk * mem.value_units * 1024, to + A_UNITS * 1024, VALUE_UNITS, lane);
     };
     auto load_last = [&](int chunk, int parity) {
