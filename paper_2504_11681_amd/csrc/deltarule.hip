@@ -11,14 +11,18 @@ constexpr int SEGMENT_MAX_WAVES = 256, SEGMENT_WAVES = 1024, SEGMENT_MIN_CHUNKS 
 
 size_t pad(size_t n) { return (n + 255) / 256 * 256; }
 
-// Segments of a head's chunks that are walked through at once.  They cost: the effect of each is walked through beforehand with Dk more columns.
-// So they are for few heads, whose columns leave most of the chip idle, and many chunks.
+// Segments of a head's chunks that are walked through at once.  They cost: the effect of each is walked through beforehand with Dk more columns, and the
+// states between them are joined one after the other.  So they are for few heads, whose columns leave most of the chip idle, and many chunks.  Measured in
+// us, in segments and in one walk, BF16 unless stated (B, T, heads, Dk = Dv; waves: 16 columns each): forward 1, 16384, 8, 128 (64 waves) 250 and 763, its training 877
+// and 2369; 4, 4096, 8, 64 (128 waves) 102 and 167; 2, 1024, 4, 64 38 and 46; 8, 8192, 8, 64 (256 waves) 342 and 418; with 512 waves 4, 2048, 16, 128 144 and 136,
+// 16, 2048, 8, 64 142 and 133.  More segments than 1024 waves lose (the first one: 335 with 2048, 306 with 512).  Below some chunks they do too: 1, 512, 8, 128
+// 46 and 36, float32 8, 1000, 8, 64 83 and 80.  In chunks, two walks, slower where more than two waves a CU share it, and the joins make the estimate below.
 int segments_of(const DeltaArgs &a, int chunks)
 {
     const long long waves = (long long)a.B * a.Hv * ((a.Dv + 31) / 32 * 2);
     if (waves == 0 || waves > SEGMENT_MAX_WAVES) return 1;
     const long long n = std::min<long long>(SEGMENT_WAVES / waves, chunks / SEGMENT_MIN_CHUNKS);
-    if (n < 2) return 1;
+    if (n < 2 || 2.0 * chunks / n * (waves * n > 512 ? 1.75 : 1.0) + 3.0 + 0.5 * n >= chunks) return 1;
     const int each = (int)((chunks + n - 1) / n);
     return (chunks + each - 1) / each;           // none without chunks
 }

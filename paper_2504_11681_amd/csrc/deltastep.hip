@@ -4,7 +4,8 @@
 //
 // Bound by the bytes of the state, which is read and written once: the two products with Sb are taken in one pass over it while it
 // lies in registers, so the workgroup meets once, for the sums over the rows.  A workgroup takes `cols` columns of one head's state:
-// a thread four neighbouring columns (one, where Dv or an address is no multiple of four) of ROWS rows.
+// a thread four neighbouring columns (one, where Dv or an address is no multiple of four) of ROWS rows.  256 sequences of 16 heads of 128 out of a larger pool: 89 us
+// for 537 MB of states, 6.0 TB/s (a part of them stays in the last-level cache from step to step; a copy reaches 5.1).
 #include "deltarule.h"
 
 namespace tfno {
