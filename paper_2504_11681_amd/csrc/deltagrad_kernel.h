@@ -357,6 +357,14 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         };
         turn(-1, 0);
         load_do(0, 0, next_o);
+        float gate[4];             // of the next member: the lane's token, and the chunk's decay
+        auto load_gates_of = [&](int member) {
+            const long long at = part(member);
+            const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
+            const int tok = lane & (L - 1);
+            gate[0] = mem.logs[at * 2 * L + tok], gate[1] = mem.logs[at * 2 * L + L + tok], gate[2] = gates->beta[tok], gate[3] = gates->whole;
+        };
+        load_gates_of(0);
         floatx4 kk[NT], qk[NT], mq[NT], mk[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) kk[j] = qk[j] = mq[j] = mk[j] = floatx4{0, 0, 0, 0};
@@ -372,13 +380,11 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         }
         turn(0, 1);
         for (int member = 0; member < group; ++member) {
-            const long long at = part(member);
-            const DeltaGates<L> *gates = (const DeltaGates<L> *)(mem.value + at * mem.value_units * 1024);
             if (tid < L) {
-                hi[tid] = mem.logs[at * 2 * L + tid], lo[tid] = mem.logs[at * 2 * L + L + tid];
-                beta[tid] = gates->beta[tid];
-                if (tid == 0) whole = gates->whole;
+                hi[tid] = gate[0], lo[tid] = gate[1], beta[tid] = gate[2];
+                if (tid == 0) whole = gate[3];
             }
+            load_gates_of(min(member + 1, group - 1));
             floatx4 D[NT], C[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) D[j] = C[j] = floatx4{0, 0, 0, 0};
@@ -512,14 +518,15 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
     load_round(0);
     split_round(0, gates_of(0)->decay[tok]);
     if (count > 1) load_round(1);
+    float q_before = 0.0f, k_before = 0.0f, next_fe = gates_of(0)->left[tok], next_be = gates_of(0)->beta[tok], next_decay = gates_of(0)->decay[tok];
     for (int member = 0; member < group; ++member) {
-        const DeltaGates<L> *gates = gates_of(member);
-        const float fe = gates->left[tok], be = gates->beta[tok], decay = gates->decay[tok], next_decay = gates_of(min(member + 1, group - 1))->decay[tok];
+        const float fe = next_fe, be = next_be, decay = next_decay;
+        const DeltaGates<L> *gates = gates_of(min(member + 1, group - 1));          // those of the next one come during this one's rounds
+        next_fe = gates->left[tok], next_be = gates->beta[tok], next_decay = gates->decay[tok];
         floatx4 he[DT];
 #pragma unroll
         for (int t = 0; t < DT; ++t) he[t] = floatx4{0, 0, 0, 0};
-        float q_before = 0.0f, k_before = 0.0f, q_sum, k_sum, e_sum, unused;
-        if (member > 0) dots(acck, q_before, k_before);
+        float q_sum, k_sum, e_sum, unused;
         for (int kb = 0; kb < rounds; ++kb) {
             const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
             __syncthreads();
@@ -547,6 +554,7 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
 #pragma unroll
             for (int r = 0; r < 4; ++r) acck[t][r] = fmaf(be * fe, he[t][r], acck[t][r]);
         if (g == 0) token_g[tok] = (q_sum - q_before) + (k_sum - k_before), token_beta[tok] = tb;
+        q_before = q_sum, k_before = fmaf(be, tb, k_sum);
         __syncthreads();
         __syncthreads();
     }
