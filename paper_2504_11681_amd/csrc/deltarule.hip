@@ -142,8 +142,29 @@ hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
     return hipGetLastError();
 }
 
+// Sequences of a batch that go through preparation and walk before the next ones do, without a tape: what the one leaves for the other then stays in the
+// last-level cache (256 MB), in memory that the next ones use again, instead of passing through HBM.  Whole rounds of workgroups, one a CU, of up to 192 MB; not where
+// one round is more than the cache.  In us, in one piece and in such ones (B, T, heads, Dk = Dv): BF16 256, 1024, 2, 64 243 and 203, 512, 512, 4, 32 383 and 340, float32
+// 64, 512, 8, 64 236 and 196; rounds over 256 MB lose, float32 100, 777, 6, 48 405 and 439, BF16 32, 2048, 16, 64 463 and 473.  Heads over 64 are bound by the walk's
+// instructions and gain nothing: BF16 64, 512, 16, 128 398 and 393, 48, 512, 16, 128 288 and 297.
 template <class E, int KB>
-hipError_t forward(const DeltaArgs &a, hipStream_t s)
+int batch_piece(const DeltaArgs &a)
+{
+    typedef DeltaUnits<E, KB> U;
+    const int chunks = (a.T + U::L - 1) / U::L;
+    if (KB > 2 || a.B < 2 || chunks == 0 || segments_of(a, chunks) > 1) return a.B;
+    const long long key_units = U::PI == 1 ? U::QT - U::KT : U::KEY_FORWARD;
+    const long long bytes = chunks * (a.Hk * key_units + a.Hv * (long long)U::VALUE_FORWARD) * 1024;
+    const long long workgroups = a.Hv * (((a.Dv + 31) / 32 * 2 + SCAN_WAVES - 1) / SCAN_WAVES);
+    const long long round = std::max<long long>(1, 256 / workgroups), fit = (192LL << 20) / bytes;
+    if (round * bytes > 256LL << 20) return a.B;
+    return (int)std::min<long long>(a.B, std::max(round, fit / round * round));
+}
+// How many of `left` sequences are next: what is less than half a piece goes with the last whole one.
+int next_piece(int left, int piece) { return left < piece + (piece + 1) / 2 ? left : piece; }
+
+template <class E, int KB>
+hipError_t forward_piece(const DeltaArgs &a, hipStream_t s)
 {
     typedef DeltaUnits<E, KB> U;
     DeltaMemory m{};
@@ -159,6 +180,26 @@ hipError_t forward(const DeltaArgs &a, hipStream_t s)
     else if (grid) k_delta_prepare<E, KB, false><<<grid, 64 * U::NT, 0, s>>>(a, m, vec);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return tape ? scan<E, KB, true>(a, m, s) : scan<E, KB, false>(a, m, s);
+}
+template <class E, int KB>
+hipError_t forward(const DeltaArgs &a, hipStream_t s)
+{
+    if (a.tape) return forward_piece<E, KB>(a, s);
+    const int piece = batch_piece<E, KB>(a);
+    const long long states = (long long)a.Hv * a.Dk * a.Dv;
+    for (int b = 0; b < a.B;) {
+        DeltaArgs p = a;
+        p.B = next_piece(a.B - b, piece);
+        p.q = (const E *)a.q + b * a.sq.batch, p.k = (const E *)a.k + b * a.sk.batch, p.v = (const E *)a.v + b * a.sv.batch;
+        p.o = (E *)a.o + b * a.so.batch, p.beta = a.beta + b * a.sbeta.batch;
+        if (a.g) p.g = a.g + b * a.sg.batch;
+        if (a.lengths) p.lengths = a.lengths + b;
+        if (a.initial) p.initial = a.initial + b * states;
+        if (a.final_state) p.final_state = a.final_state + b * states;
+        if (hipError_t e = forward_piece<E, KB>(p, s); e != hipSuccess) return e;
+        b += p.B;
+    }
+    return hipSuccess;
 }
 
 template <class E, int KB>
@@ -189,7 +230,19 @@ struct Forward { const DeltaArgs &a; hipStream_t s; template <class E, int KB> h
 struct Backward { const DeltaArgs &a; hipStream_t s; template <class E, int KB> hipError_t operator()() const { return backward<E, KB>(a, s); } };
 struct ForwardBytes {
     const DeltaArgs &a; bool tape;
-    template <class E, int KB> size_t operator()() const { DeltaMemory m{}; return forward_memory<E, KB>(a, nullptr, tape, &m); }
+    template <class E, int KB> size_t operator()() const
+    {
+        DeltaMemory m{};
+        if (tape) return forward_memory<E, KB>(a, nullptr, true, &m);
+        const int piece = batch_piece<E, KB>(a);
+        size_t most = 0;
+        DeltaArgs p = a;
+        for (int b = 0; b < a.B; b += p.B) {
+            p.B = next_piece(a.B - b, piece);
+            most = std::max(most, forward_memory<E, KB>(p, nullptr, false, &m));
+        }
+        return most;
+    }
 };
 struct BackwardBytes {
     const DeltaArgs &a;

@@ -120,6 +120,21 @@ def test_rule_of_many_heads_and_of_long_sequences(tfno, dtype, size):
     check_both(tfno, inputs(dtype, *size, seed=2), f"[case] large {dtype} {size}")
 
 
+@pytest.mark.parametrize("dtype, size", [(BF16, (300, 520, 2, 4, 64, 64)), (F32, (101, 260, 4, 8, 40, 60))])
+def test_batches_in_pieces(tfno, dtype, size):
+    """So large a batch that it goes through the two kernels piece by piece: every sequence with its own lengths, first and last state."""
+    x = inputs(dtype, *size, seed=13)
+    B, T = size[:2]
+    x["lengths"] = torch.randint(0, T + 1, (B,), generator=torch.Generator().manual_seed(5)).to(torch.int32).cuda()
+    o, final = check_forward(tfno, x, f"[case] pieces {dtype} {size}")
+    last = dict(x, lengths=x["lengths"][-3:].contiguous(), initial=x["initial"][-3:].contiguous())
+    for n in ("q", "k", "v", "g", "beta"):
+        last[n] = x[n][-3:]
+    o2, final2 = forward(tfno, last)
+    near("o of the last ones by themselves", o2, o[-3:].double(), oracle.REL[dtype])
+    near("their states", final2, final[-3:].double(), oracle.REL[F32])
+
+
 @pytest.mark.parametrize("dtype", (F32, BF16))
 def test_gates_at_their_ends(tfno, dtype):
     x = inputs(dtype, 2, 150, 2, 2, 64, 48, seed=3)
