@@ -264,8 +264,8 @@ struct GradientLds {
 
 // One workgroup for a chunk of a key head.  L / 16 waves take the products of pairs of tokens and bring the states in, as many the products with the states,
 // each for 16 tokens, whose errors and values' gradients they bring in.  What comes is split once for all and left in LDS, a round of 32 columns ahead of its
-// products.  B 4, T 2048, 8 key heads and 16 value heads of 128 in BF16: 215 us for 450 MB, a round 8000 cycles, the products of a SIMD's two waves 3000 of them; the rest is the
-// splits and the loads' issue, which stands still while their queues are full, and 25000 cycles a workgroup before the first round and after the last, alone on its CU.
+// products.  B 4, T 2048, 8 key heads and 16 value heads of 128 in BF16: 212 us for 450 MB, a round 8000 cycles, the products of a SIMD's two waves 3000 of them; the rest is the
+// splits and the loads' issue, which stands still while their queues are full, and some 20000 cycles a workgroup before the first round and after the last, alone on its CU.
 // (All of it in every wave took 512 registers, so one wave a SIMD, and waited for memory in every round: 338 us; all loads and splits in the waves of the
 // states 266; loads one after the other behind all splits 256.)
 template <class E, int KB>
