@@ -13,8 +13,8 @@ MB = 1 << 20
 
 @pytest.fixture(scope="module")
 def L():
-    if not os.path.exists(tfno.LIB_PATH):
-        from paper_2504_11681_amd import build
+    from paper_2504_11681_amd import build
+    if not os.path.exists(tfno.LIB_PATH) or not os.path.exists(build.MARSHAL):
         build.build(verbose=False)
     return tfno.lib()
 
@@ -294,3 +294,15 @@ def test_what_is_no_tensor_or_has_no_memory_of_its_own_values_is_refused(L):
         tfno.head_norm_rope(q, q, None, None, None, None, q, q)
     with pytest.raises((TypeError, AttributeError)):
         tfno.gated_delta_rule(None, None, None, None, None, None)
+
+
+def test_workspace_of_large_batches_is_that_of_a_piece(L):
+    """Without a tape a large batch goes through in pieces that share one workspace; its size does not grow with the batch, nor does a call ask for less than a piece."""
+    def need(**kw):
+        d = rule_desc(Hk=2, Hv=2, T=1024, **kw)
+        return L.tfno_gated_delta_rule_workspace_bytes(ctypes.addressof(d), 0)
+
+    sizes = [need(B=B) for B in (1, 64, 128, 256, 1024, 4096)]
+    assert all(x > 0 for x in sizes) and sizes[1] < sizes[2] and sizes[3] < 2 * sizes[2] and sizes[5] == sizes[4] == sizes[3]
+    assert need(B=150) > sizes[2] and need(B=257) >= sizes[2]
+    assert need(B=1, Dk=128) > 0 and need(B=0) == 0
