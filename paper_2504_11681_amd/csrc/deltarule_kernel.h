@@ -20,9 +20,10 @@
 // so that the two results of a pair hold in each lane just the eight consecutive indexes that an operand block needs: a result becomes
 // an operand without leaving its registers.
 //
-// Float32 values (the state, E, T, P, and float32 inputs) are operands as three BF16 parts that add up to them, and products of parts
-// below 2^-24 are left out, so sums have float32's accuracy.  BF16 inputs are one part.  What goes into a BF16 output alone (P, and S as
-// the outputs read it) is taken in two parts, 2^-16 off, which the output's own 2^-9 hides.
+// Float32 values (the state, E, U, T, P, and float32 inputs) are operands as three BF16 parts that add up to them, and products of parts
+// below 2^-24 are left out, so sums have float32's accuracy.  BF16 inputs are one part.  What goes into a BF16 output alone (P, U, and S as the
+// outputs read it) has three parts too: where a key is written over, Q S and P U are large and cancel, and with two parts, 2^-15 off, outputs a
+// thousandth of the old value were 2e-2 off.  That is a tenth of the time (256 x 1024 tokens, 2 heads of 64: 205 -> 224 us).
 #pragma once
 #include "bf16x3.h"
 #include "deltarule.h"
@@ -179,22 +180,22 @@ __device__ __forceinline__ int tile_index(int i, int r) { return 32 * (i >> 1) +
 // What the kernels are built for.  BF16: chunks of 64, one part an input; float32: chunks of 32 (its operands are three times as large),
 // three parts.
 template <class E> struct DeltaKind;
-template <> struct DeltaKind<bf16> { static constexpr int L = 64, PI = 1, PO = 2; };
-template <> struct DeltaKind<float> { static constexpr int L = 32, PI = 3, PO = 3; };
+template <> struct DeltaKind<bf16> { static constexpr int L = 64, PI = 1; };
+template <> struct DeltaKind<float> { static constexpr int L = 32, PI = 3; };
 
 constexpr int DELTA_PM = 3;      // parts of float32 operands
 
 // Memory of a chunk, in units of 1024 bytes (one part of an operand block).  KB = ceil(Dk / 32).
 template <class E, int KB>
 struct DeltaUnits {
-    static constexpr int L = DeltaKind<E>::L, PI = DeltaKind<E>::PI, PO = DeltaKind<E>::PO;
+    static constexpr int L = DeltaKind<E>::L, PI = DeltaKind<E>::PI;
     static constexpr int NT = L / 16, LB = L / 32, DT = 2 * KB, DKP = 32 * KB;
     static constexpr int TRI = NT == 2 ? 2 : 6;                    // blocks on and below the diagonal
     // of a key head: K, Q [NT][KB], K', Q' [DT][LB]
     static constexpr int K = 0, Q = NT * KB * PI, KT = 2 * NT * KB * PI, QT = KT + DT * LB * PI;
     static constexpr int KEY_FORWARD = QT, KEY_TAPE = QT + DT * LB * PI;
     // of a value head: gates, T, P; with a tape T', P'
-    static constexpr int GATES = 0, T = 1, P = T + TRI * DELTA_PM, VALUE_FORWARD = P + TRI * PO;
+    static constexpr int GATES = 0, T = 1, P = T + TRI * DELTA_PM, VALUE_FORWARD = P + TRI * DELTA_PM;
     static constexpr int TT = VALUE_FORWARD, PT = TT + TRI * DELTA_PM, VALUE_TAPE = PT + TRI * DELTA_PM;
     static constexpr int lower(int i, int kb) { return NT == 2 ? i : i < 2 ? i : 2 + 2 * (i - 2) + kb; }   // kb <= i / 2
     static constexpr int upper(int i, int kb) { return NT == 2 ? i : i < 2 ? 2 * i + kb : 4 + (i - 2); }   // kb >= i / 2
@@ -361,7 +362,7 @@ template <class E, int KB, bool TAPE>
 __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaArgs a, DeltaMemory mem, DeltaVec vec)
 {
     typedef DeltaUnits<E, KB> U;
-    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PO = U::PO, PM = DELTA_PM;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, DKP = U::DKP, PI = U::PI, PM = DELTA_PM;
     constexpr int ROW = DKP + 16 / sizeof(E), COL = L + 4;
     constexpr int ROWS_BYTES = 2 * L * ROW * sizeof(E), MATRIX_BYTES = L * COL * 4;
     __shared__ __attribute__((aligned(16))) unsigned char shared[ROWS_BYTES > MATRIX_BYTES ? ROWS_BYTES : MATRIX_BYTES];
@@ -489,7 +490,7 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     u[e] = 32 * s + 8 * g + e <= own ? decay_between(hi_own, lo_own, h8[e], l8[e]) * kq[2 * s + (e >> 2)][e & 3] : 0.0f;
-                store_frag<PO>(value + (U::P + U::lower(w, s) * PO) * 1024, lane, make_frag<PO>(u));
+                store_frag<PM>(value + (U::P + U::lower(w, s) * PM) * 1024, lane, make_frag<PM>(u));
             }
         }
         if (first)         // K' and Q': tiles of Dk rows, blocks of 32 tokens
@@ -610,10 +611,12 @@ __device__ __forceinline__ void load_columns(const E *p, long long token, unsign
             for (int e = 0; e < 8; ++e, q += token) u[s][e] = *behind(q, at);
     } else {
         p = behind(p, at) - 8 * g * token;
+        int first = 8 * g;
+        asm volatile("" : "+v"(first));        // its products with the distance belong here and not into registers that the loop's products need
 #pragma unroll
         for (int s = 0; s < LB; ++s)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[s][e] = p[32 * s + 8 * g + e < count ? (32 * s + 8 * g + e) * token : 0];
+            for (int e = 0; e < 8; ++e) u[s][e] = p[32 * s + first + e < count ? (32 * s + first + e) * token : 0];
     }
 }
 // Zeros in place of what does not count.
@@ -720,7 +723,7 @@ template <class E, int KB, int MODE>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head, int segments)
 {
     typedef DeltaUnits<E, KB> U;
-    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PO = U::PO, PM = DELTA_PM;
+    constexpr int L = U::L, NT = U::NT, LB = U::LB, DT = U::DT, PI = U::PI, PM = DELTA_PM;
     constexpr bool TAPE = MODE == SCAN_TAPE, EFFECTS = MODE == SCAN_EFFECTS;
     typedef ForwardLds<E, KB, MODE> Lds;
     constexpr int A_UNITS = EFFECTS ? U::Q : U::KT, VALUE_UNITS = EFFECTS ? U::P : U::VALUE_FORWARD;
@@ -852,7 +855,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 mm_many<3, false>(kf[kb & 1], Sf[kb], ks, NoWeave());
                 region_end();
             }
-            constexpr int MFMA = KB * NT * products(PI, PM, PO);
+            constexpr int MFMA = KB * NT * products(PI, PM, 3);
             auto pieces = weave<at_least_1(MFMA / (2 * LB)), 2 * LB>([&](int k) {
                 const int s = k >> 1, e = k & 1;
                 float u[4];
@@ -865,7 +868,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 for (int kb = 0; kb < KB; ++kb) {
                     if (kb + 1 < KB) read(U::Q, kb + 1, (KB + kb + 1) & 1);
                     region_end();
-                    mm_many<PO, true>(kf[(KB + kb) & 1], Sf[kb], qs, pieces);
+                    mm_many<3, true>(kf[(KB + kb) & 1], Sf[kb], qs, pieces);
                     region_end();
                 }
             pieces.rest();
@@ -878,7 +881,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         // the products of the next pair run; then the outputs' P U and the first part of S <- e^GL S + K' (e^(GL-G) U) while the last pair is split
         floatx4 Ee[NT];
         Frag<PM> W[LB];
-        Frag<PO> Uf[LB];
+        Frag<PM> Uf[LB];
         float be[LB][8], left[LB][8], decay_o[NT];
         Frag<PM> tf[2][2];
         auto read_t = [&](int s, int kb, int to) {
@@ -896,13 +899,13 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
                 u[r] = be[s][4 * e + r] * Ee[2 * s + e][r];
                 w[r] = left[s][4 * e + r] * u[r];
             }
-            if (!EFFECTS) set_four<PO>(Uf[s], e, u);
+            if (!EFFECTS) set_four<PM>(Uf[s], e, u);
             set_four<PM>(W[s], e, w);
         };
-        Frag<PO> pf[2][2];
+        Frag<PM> pf[2][2];
         auto read_p = [&](int s, int kb, int to) {
 #pragma unroll
-            for (int p = 0; p < 2; ++p) pf[to][p] = load_frag<PO>(ldsB + (U::P + U::lower(2 * s + p, kb) * PO) * 1024, lane);
+            for (int p = 0; p < 2; ++p) pf[to][p] = load_frag<PM>(ldsB + (U::P + U::lower(2 * s + p, kb) * PM) * 1024, lane);
         };
         {
             floatx4 *to[2] = {&Ee[0], &Ee[1]};
@@ -947,16 +950,16 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         read_k(0);
         read_k(1);
         if constexpr (LB > 1) {
-            constexpr int MFMA = (EFFECTS ? 0 : 4 * products(PO, PO, PO)) + KB * 2 * products(PI, PM, 3);
+            constexpr int MFMA = (EFFECTS ? 0 : 4 * products(PM, PM, 3)) + KB * 2 * products(PI, PM, 3);
             floatx4 *o1[2] = {&QS[2], &QS[3]};
             auto pieces = weave<MFMA / 3, 2>([&](int e) { split_u(1, e); });
             if constexpr (!EFFECTS) {
                 read_p(1, 0, 1);
                 region_end();
-                mm_many<PO, true>(pf[0], Uf[0], o0, pieces);
+                mm_many<3, true>(pf[0], Uf[0], o0, pieces);
                 read_p(1, 1, 0);
                 region_end();
-                mm_many<PO, true>(pf[1], Uf[0], o1, pieces);
+                mm_many<3, true>(pf[1], Uf[0], o1, pieces);
             }
 #pragma unroll
             for (int pair = 0; pair < KB; ++pair) {
@@ -986,7 +989,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
             }
             auto pieces = weave<2, 2>([&](int e) { split_s(KB - 1, e); });
             floatx4 *to[2] = {&QS[NT - 2], &QS[NT - 1]};
-            if constexpr (!EFFECTS) mm_many<PO, true>(pf[0], Uf[LB - 1], to, pieces);
+            if constexpr (!EFFECTS) mm_many<3, true>(pf[0], Uf[LB - 1], to, pieces);
             pieces.rest();
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) hold(Sf[kb]);

@@ -169,6 +169,30 @@ def test_keys_that_are_all_alike(tfno, dtype):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(2, 64, 1, 2, 64, 64), (40, 64, 2, 2, 128, 128), (1, 640, 1, 1, 128, 64)])
+def test_what_is_written_over_large_values(tfno, dtype, size):
+    """One key of length one for every token and beta = 1: a token's value takes the place of the one before, and the outputs are the values.  The first state holds
+    values a thousand times as large there, so what the outputs are made of (the products with the state and with the errors) cancels to a thousandth.  The bound: the rounding of
+    the outputs, and of some ten sums in float32 (a matrix instruction adds 32 terms at once) with operands 2^-22 off at most, 16 * 2^-24 of the old values' size."""
+    B, T, Hk, Hv, Dk, Dv = size
+    x = inputs(dtype, *size, seed=14, decay=0.0)
+    sign = torch.randn(1, 1, Hk, Dk, generator=torch.Generator("cuda").manual_seed(6), device="cuda").sign()
+    key = 0.125 * sign * (torch.arange(Dk, device="cuda") < 64)          # 64 entries of 1 / 8
+    for n in ("q", "k"):
+        x[n][:] = key
+    x["beta"][:] = 1.0
+    old = 1000 * torch.randn(B, Hv, 1, Dv, generator=torch.Generator("cuda").manual_seed(7), device="cuda")
+    x["initial"] = (key[0, 0].repeat_interleave(Hv // Hk, 0)[None, :, :, None] * old).contiguous()
+    wo, wfinal = want(x, False)
+    bound = 1000 * 16 * 2.0 ** -24
+    for tape in (None, tfno.gated_delta_rule_tape(x["q"], x["v"])):
+        say(f"[case] written over {dtype} {size} {tape is not None}")
+        o, final = forward(tfno, x, tape)
+        near("o", o[:, :64], wo[:, :64], (oracle.REL[BF16] if dtype is BF16 else 0) + bound)
+        near("final", final, wfinal, bound)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("bad", (float("nan"), float("inf"), float("-inf")))
 def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
     B, T = 7, 140
