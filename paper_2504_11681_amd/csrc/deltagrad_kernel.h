@@ -472,11 +472,10 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         return;
     }
 
-    // the waves of the states.  Factors of a token go into its operand, so that dq and dk add up without a second set of accumulators; what a member adds
-    // to q.dq and k.dk is then the difference of the sums behind and before it
+    // the waves of the states.  Factors of a token go into its operand, so that dq and dk add up in one set of accumulators.  They are one value head's: what it adds to q.dq and
+    // k.dk goes into the gradients of its gates (as the difference of running sums it would be lost beside a head whose gradients are some orders larger, and NaN behind one with
+    // a NaN).  The sum over the heads of a key head waits in memory between them, 64 KiB for heads of 128.
     floatx4 accq[DT], acck[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t) accq[t] = acck[t] = floatx4{0, 0, 0, 0};
     const int tok = tile_index(i, m);
     // sums over the state's rows of q times accq and k times x
     auto dots = [&](const floatx4 (&x)[DT], float &q_sum, float &k_sum) {
@@ -493,6 +492,12 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         }
         q_sum += __shfl_xor(q_sum, 16, 64), q_sum += __shfl_xor(q_sum, 32, 64);
         k_sum += __shfl_xor(k_sum, 16, 64), k_sum += __shfl_xor(k_sum, 32, 64);
+    };
+    // sums over the heads before: tile t of dq (of dk from DT on), 16 bytes a lane
+    auto sum_of = [&](int t) {
+        unsigned off = lane * 16;
+        asm volatile("" : "+v"(off));
+        return behind(uniform((floatx4 *)mem.sums + ((((long long)kh * mem.chunks + chunk) * NT + i) * 2 * DT + t) * 64), off);
     };
     const int count = group * rounds;
     struct { float e[8], y[8], o[8]; } next;
@@ -518,14 +523,14 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
     load_round(0);
     split_round(0, gates_of(0)->decay[tok]);
     if (count > 1) load_round(1);
-    float q_before = 0.0f, k_before = 0.0f, next_fe = gates_of(0)->left[tok], next_be = gates_of(0)->beta[tok], next_decay = gates_of(0)->decay[tok];
+    float next_fe = gates_of(0)->left[tok], next_be = gates_of(0)->beta[tok], next_decay = gates_of(0)->decay[tok];
     for (int member = 0; member < group; ++member) {
         const float fe = next_fe, be = next_be, decay = next_decay;
         const DeltaGates<L> *gates = gates_of(min(member + 1, group - 1));          // those of the next one come during this one's rounds
         next_fe = gates->left[tok], next_be = gates->beta[tok], next_decay = gates->decay[tok];
         floatx4 he[DT];
 #pragma unroll
-        for (int t = 0; t < DT; ++t) he[t] = floatx4{0, 0, 0, 0};
+        for (int t = 0; t < DT; ++t) accq[t] = acck[t] = he[t] = floatx4{0, 0, 0, 0};
         float q_sum, k_sum, e_sum, unused;
         for (int kb = 0; kb < rounds; ++kb) {
             const unsigned char *panel = lds + ((member * rounds + kb) & 1) * Lds::UNITS * 1024;
@@ -553,8 +558,21 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) acck[t][r] = fmaf(be * fe, he[t][r], acck[t][r]);
-        if (g == 0) token_g[tok] = (q_sum - q_before) + (k_sum - k_before), token_beta[tok] = tb;
-        q_before = q_sum, k_before = fmaf(be, tb, k_sum);
+        if (g == 0) token_g[tok] = q_sum + k_sum, token_beta[tok] = tb;
+        if (member > 0) {              // all loads of a half on their way before the first is waited for
+            floatx4 before[DT];
+#pragma unroll
+            for (int t = 0; t < DT; ++t) before[t] = *sum_of(t);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) accq[t] += before[t], before[t] = *sum_of(DT + t);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acck[t] += before[t];
+        }
+        if (member + 1 < group)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) *sum_of(t) = accq[t], *sum_of(DT + t) = acck[t];
         __syncthreads();
         __syncthreads();
     }

@@ -62,6 +62,7 @@ size_t backward_memory(const DeltaArgs &a, unsigned char *base, DeltaMemory *m)
     size_t at = 0;
     m->d_states = (float *)(base + at), at += values * U::DKP * dvp * sizeof(float);
     m->d_values = (float *)(base + at), at += values * U::L * dvp * sizeof(float);
+    if (a.Hv > a.Hk) m->sums = (float *)(base + at), at += (size_t)a.B * a.Hk * chunks * 2 * U::L * U::DKP * sizeof(float);
     if (segments > 1) {
         m->back_effects = (float *)(base + at), at += parts * U::DKP * dvp * sizeof(float);
         m->segment_d_states = (float *)(base + at), at += parts * U::DKP * dvp * sizeof(float);

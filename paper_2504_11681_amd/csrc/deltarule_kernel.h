@@ -218,6 +218,7 @@ struct DeltaMemory {
     float *logs;                     // tape: [b][hv][chunk][2][L] running sums of g in powers of two, as sums of two floats
     float *states, *errors;          // tape: S before each chunk [DKP][DVP], E [L][DVP]
     float *d_states, *d_values;      // backward: gradient of the state after each chunk, Y [L][DVP]
+    float *sums;                     // backward, where value heads share key heads: gradients of q and k from the value heads so far, [b][hk][chunk][2][L][DKP]
     int chunks, dvp, key_units, value_units;
     // Where there are few heads, the chunks of a head are walked through in segments at once: a segment's effect on the state is S -> A S + B.
     int segments, segment_chunks;

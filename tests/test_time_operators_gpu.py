@@ -210,6 +210,40 @@ def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(2, 150, 1, 2, 64, 48), (1, 70, 2, 8, 128, 128), (2, 200, 1, 3, 20, 33)])
+def test_heads_that_share_keys_keep_their_gradients_apart(tfno, dtype, size):
+    """The first value head of every key head has values and gradients 1e4 times the others', and then NaN: what the other heads get of their own is as near, and not NaN."""
+    B, T, Hk, Hv, Dk, Dv = size
+    group = Hv // Hk
+    x = inputs(dtype, *size, seed=15)
+    for n in ("v", "d_o"):
+        x[n][:, :, ::group] *= 1e4
+    for n in ("initial", "d_final"):
+        x[n][:, ::group] *= 1e4
+    say(f"[case] apart {dtype} {size}")
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    o, final = forward(tfno, x, tape)
+    d = backward(tfno, x, tape)
+    w = dict(zip(("o", "final", "q", "k", "v", "g", "beta", "initial"), want(x, True)))
+    for n in ("q", "k"):
+        near("d" + n, d[n], w[n], oracle.REL[dtype])
+    for h in range(Hv):
+        for n in ("v", "g", "beta"):
+            near(f"d{n} of head {h}", d[n][:, :, h], w[n][:, :, h], oracle.REL_GATES if n != "v" else oracle.REL[dtype])
+        near(f"o of head {h}", o[:, :, h], w["o"][:, :, h], oracle.REL[dtype])
+    x["v"][:, 5, ::group] = float("nan")
+    x["d_o"][:, T - 1, ::group] = float("nan")
+    o2, final2 = forward(tfno, x, tape)
+    d2 = backward(tfno, x, tape)
+    rest = [h for h in range(Hv) if h % group]
+    assert torch.isnan(o2[:, 5, 0]).all() and torch.isnan(d2["g"][:, 5, 0]).all()
+    assert torch.equal(o2[:, :, rest], o[:, :, rest]) and torch.equal(final2[:, rest], final[:, rest])
+    for n in ("v", "g", "beta"):
+        assert torch.equal(d2[n][:, :, rest], d[n][:, :, rest]), n
+    assert torch.equal(d2["initial"][:, rest], d["initial"][:, rest])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("size", [(1, 1100, 1, 1, 128, 128), (1, 1217, 2, 2, 64, 100), (3, 640, 1, 2, 33, 40), (2, 961, 1, 1, 100, 256), (4, 383, 1, 1, 16, 16)])
 def test_few_heads_of_long_sequences(tfno, dtype, size):
     """So few heads that a sequence is cut into segments of chunks; ends inside a chunk, chunks that no segment is full of."""
