@@ -312,7 +312,7 @@ tfno_status tfno_spectral_conv1d_auto(const void *x, const void *W, void *y,
  *    Sums, norms and states are held in float32 whatever the type.
  *  - Pointers are aligned to the size of an element (TFNO_ERR_ALIGN); every size, stride and alignment gives the same result, tensors whose
  *    rows are aligned to 16 bytes the faster one.
- *  - An output that overlaps an input or another output is TFNO_ERR_ALIAS; slices that interleave in one buffer do not overlap.
+ *  - An output that overlaps an input or another output is TFNO_ERR_ALIAS; slices that interleave in one buffer, along whichever axis, do not overlap.
  *  - Streams, ownership, workspace and the detection of errors before anything is launched are as above.  The descriptor is read during the call alone.
  *  - Equal calls give equal bits: no sum depends on the order in which workgroups run.
  */

@@ -47,30 +47,35 @@ bool distinct(const View &v)
     return true;
 }
 
-// Slices of `a` and `b` elements that lie apart in every period of a common buffer.
-bool apart(const View &a, long long na, const View &b, long long nb, long long period)
+// What a tensor covers of every period of a buffer, in bytes from its pointer on: axes that step over whole periods do not count.  More than a period where it is no slice.
+long long in_period(const View &v, long long period)
 {
-    if (period <= 0 || na > period || nb > period) return false;
-    const long long bytes = (long long)((uintptr_t)a.p - (uintptr_t)b.p);
-    if (bytes % a.elem) return false;
-    const long long off = ((bytes / a.elem) % period + period) % period;     // a's slice begins here in b's
-    return off >= nb && off + na <= period;
+    const std::pair<long long, long long> axes[3] = {{v.s.head, v.H}, {v.s.token, v.T}, {v.s.batch, v.B}};
+    long long covered = v.D * v.elem;
+    for (const auto &a : axes)
+        if (a.second > 1 && a.first * v.elem % period != 0) covered += (a.second - 1) * a.first * v.elem;
+    return covered;
 }
-// Whether two tensors may share memory.  Ranges that meet are no clash where both are slices of the rows of one buffer and lie apart there:
-// rows of tokens, or of batch elements.
+// Whether two tensors may share memory.  Ranges that meet are no clash where some axis of one of them is the period of a common buffer, in which both are slices that lie
+// apart: rows of tokens, of batch elements or of heads, in whatever order the axes lie.
 bool clash(const View &a, const View &b)
 {
     if (!a.there() || !b.there() || a.high() <= b.low() || b.high() <= a.low()) return false;
-    if (a.elem != b.elem || a.T != b.T || a.B != b.B) return true;
-    const long long ra = (a.H - 1) * a.s.head + a.D, rb = (b.H - 1) * b.s.head + b.D;
-    const bool whole_rows = a.B == 1 || (a.s.token > 0 && a.s.batch % a.s.token == 0 && b.s.batch % a.s.token == 0);
-    if (a.T > 1 && a.s.token == b.s.token && whole_rows && apart(a, ra, b, rb, a.s.token)) return false;
-    if (a.B > 1 && a.s.batch == b.s.batch && apart(a, (a.T - 1) * a.s.token + ra, b, (b.T - 1) * b.s.token + rb, a.s.batch)) return false;
+    for (const View *v : {&a, &b}) {
+        const std::pair<long long, long long> axes[3] = {{v->s.head, v->H}, {v->s.token, v->T}, {v->s.batch, v->B}};
+        for (const auto &axis : axes) {
+            const long long period = axis.first * v->elem;
+            if (axis.second <= 1 || period <= 0) continue;
+            const long long na = in_period(a, period), nb = in_period(b, period);
+            const long long off = ((long long)((uintptr_t)a.p - (uintptr_t)b.p) % period + period) % period;     // a's slice begins here in b's period
+            if (off >= nb && off + na <= period) return false;
+        }
+    }
     return true;
 }
 bool same(const View &a, const View &b)
 {
-    return a.p == b.p && a.s.batch == b.s.batch && a.s.token == b.s.token && a.s.head == b.s.head;
+    return a.p == b.p && (a.B <= 1 || a.s.batch == b.s.batch) && (a.T <= 1 || a.s.token == b.s.token) && (a.H <= 1 || a.s.head == b.s.head);
 }
 
 bool aligned(const void *p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }

@@ -1,6 +1,8 @@
 """What the operators along time refuse, on the host before anything is launched (no call here needs a GPU)."""
 import ctypes
+import itertools
 import os
+import random
 
 import pytest
 import torch
@@ -135,6 +137,78 @@ def test_slices_of_one_projection_are_no_aliases(L):
     assert call(L.tfno_gated_delta_rule, d, at) == tfno.ERR_WORKSPACE
     assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 6 * 8 * 256 - 2) == tfno.ERR_ALIAS
     assert call(L.tfno_gated_delta_rule, d, at, o=FAKE + 6 * 8 * 256 + 2) == tfno.ERR_ALIAS
+
+
+def elements(at, elem, sizes, strides, D):
+    """Addresses of all bytes of a tensor."""
+    first = [at + elem * sum(i * s for i, s in zip(index, strides)) for index in itertools.product(*map(range, sizes))]
+    return {x + y for x in first for y in range(elem * D)}
+
+
+def pair_layout(order, sizes, D):
+    """Strides (batch, token, head) and the distance of two tensors of one buffer whose axes, from the outermost on, are `order`, D values last."""
+    step, at = D, {}
+    for axis in reversed(order):
+        at[axis] = step
+        step *= sizes[axis]
+    return tfno._Strides(at["batch"], at["token"], at["head"]), at["slot"]
+
+
+@pytest.mark.parametrize("sizes", [dict(batch=2, token=8, head=4, slot=2), dict(batch=1, token=8, head=4, slot=3), dict(batch=3, token=1, head=4, slot=2),
+                                   dict(batch=2, token=5, head=1, slot=2), dict(batch=1, token=1, head=4, slot=2)])
+@pytest.mark.parametrize("order", list(itertools.permutations(("batch", "token", "head", "slot"))))
+def test_slices_that_interleave_along_any_axis_are_no_aliases(L, order, sizes):
+    """v and o, d_o and dv, dg and dbeta, dq and dk in place of q and k: slices of one buffer in every order of the axes.  They are refused for the workspace alone, and as aliases
+    when one lies an element closer to the other."""
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    B, T, H = sizes["batch"], sizes["token"], sizes["head"]
+    s, far = pair_layout(order, sizes, 64)
+    shape = dict(B=B, T=T, Hk=H, Hv=H, **{n: strides(T, H, 64) for n in ("q", "k", "dq", "dk")}, **{n: strides(T, H, 1) for n in ("g", "beta")})
+    d = rule_desc(**shape, v=s, o=s)
+    at = dict(RULE, v=FAKE + 200 * MB, o=FAKE + 200 * MB + 2 * far, tape=None)
+    assert call(L.tfno_gated_delta_rule, d, at) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_gated_delta_rule, d, at, o=at["o"] - 2) == tfno.ERR_ALIAS
+    gates, near = pair_layout(order, sizes, 1)
+    d = rule_desc(**shape, dg=gates, dbeta=gates, dv=s, o=s)
+    at = dict(RULE_BACK, tape=FAKE + 400 * MB, d_o=FAKE + 200 * MB, dv=FAKE + 200 * MB + 2 * far, dg=FAKE + 300 * MB, dbeta=FAKE + 300 * MB + 4 * near)
+    assert call(L.tfno_gated_delta_rule_backward, d, at) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_gated_delta_rule_backward, d, at, dv=at["dv"] - 2) == tfno.ERR_ALIAS
+    assert call(L.tfno_gated_delta_rule_backward, d, at, dbeta=at["dbeta"] - 4) == tfno.ERR_ALIAS
+    n = norm_desc(B=B, T=T, Hq=H, Hk=H, P=T, q=s, k=s, dq=s, dk=s, q_out=strides(T, H, 64), k_out=strides(T, H, 64))
+    at = dict(NORM_BACK, q=FAKE + 200 * MB, k=FAKE + 200 * MB + 2 * far, positions=None)
+    at["dq"], at["dk"] = at["q"], at["k"]
+    assert call(L.tfno_head_norm_rope_backward, n, at) == tfno.ERR_WORKSPACE
+    assert call(L.tfno_head_norm_rope_backward, n, at, dk=at["k"] - 2) == tfno.ERR_ALIAS
+
+
+def test_strides_of_axes_of_one_do_not_count_in_place(L):
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    n = norm_desc(T=1, q=tfno._Strides(256, 1 << 20, 64), dq=tfno._Strides(256, 256, 64))
+    assert call(L.tfno_head_norm_rope_backward, n, dict(NORM_BACK, dq=NORM_BACK["q"])) == tfno.ERR_WORKSPACE
+
+
+def test_tensors_that_share_bytes_are_always_aliases(L):
+    """Small tensors of random strides at random places close to each other, against the sets of their bytes."""
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    rng, shared, free = random.Random(5), 0, 0
+    for _ in range(4000):
+        B, T, H, D = rng.randint(1, 3), rng.randint(1, 4), rng.randint(1, 3), rng.choice((1, 2, 3, 8))
+        unit = rng.choice((1, D, 2 * D, 3 * D))
+
+        def random_strides():
+            return tuple(unit * rng.choice((0, 1, 2, 3, 4, 6, 8, 12, 24)) for _ in range(3))
+
+        sv, so, off = random_strides(), random_strides(), 2 * rng.randint(0, 40)
+        d = rule_desc(B=B, T=T, Hk=1, Hv=H, Dv=D, v=tfno._Strides(*sv), o=tfno._Strides(*so), q=strides(T, 1, 64), k=strides(T, 1, 64), g=strides(T, H, 1), beta=strides(T, H, 1))
+        at = dict(RULE, v=FAKE + 200 * MB, o=FAKE + 200 * MB + off, tape=None)
+        st = call(L.tfno_gated_delta_rule, d, at)
+        v, o = elements(at["v"], 2, (B, T, H), sv, D), elements(at["o"], 2, (B, T, H), so, D)
+        if v & o or len(o) < 2 * B * T * H * D:
+            assert st == tfno.ERR_ALIAS, (B, T, H, D, sv, so, off)
+            shared += 1
+        else:
+            free += st == tfno.ERR_WORKSPACE
+    assert shared > 500 and free > 200, (shared, free)
 
 
 def test_rule_memory(L):

@@ -333,6 +333,37 @@ def test_strides(tfno, dtype, way):
         near("d" + n, d[n], v, oracle.REL_GATES if n in ("g", "beta") else oracle.REL[d[n].dtype])
 
 
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_slices_that_interleave_by_heads(tfno, dtype):
+    """Queries, keys and values of a head beside each other, normalised in place; results and gradients as the halves of rows."""
+    B, T, H, D = 2, 77, 2, 64
+    x = inputs(dtype, B, T, H, H, D, D, seed=16)
+    packed = torch.stack([x[n] for n in "qkv"], 3)                        # [B, T, H, 3, D]
+    gen = torch.Generator("cuda").manual_seed(8)
+    cos, sin = torch.rand(T, D // 2, generator=gen, device="cuda"), torch.rand(T, D // 2, generator=gen, device="cuda")
+    weight = torch.full((D,), D ** -0.5, device="cuda")                   # keys of length one
+    normed = {n: oracle.norm(x[n], weight, cos, sin, None, 1e-6, False) for n in "qk"}
+    x["q"], x["k"], x["v"] = packed.unbind(3)
+    tfno.head_norm_rope(x["q"], x["k"], weight, weight, cos, sin, x["q"], x["k"])
+    say(f"[case] by heads {dtype}")
+    for n in "qk":
+        near(n, x[n], normed[n], oracle.REL[dtype])
+    rows = torch.empty(B, H, T, 2 * D, dtype=dtype, device="cuda").transpose(1, 2)
+    rows[..., :D] = x["v"]
+    x["v"], o = rows[..., :D], rows[..., D:]
+    gates = torch.empty(B, T, H, 2, device="cuda")
+    dqkv = torch.empty_like(packed)
+    grads = {**dict(zip("qkv", dqkv.unbind(3))), "g": gates[..., 0], "beta": gates[..., 1]}
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    got = forward(tfno, x, tape, o)
+    d = backward(tfno, x, tape, grads)
+    w = want(x, True)
+    near("o", got[0], w[0], oracle.REL[dtype])
+    near("final", got[1], w[1], oracle.REL[F32])
+    for n, v in zip(("q", "k", "v", "g", "beta", "initial"), w[2:]):
+        near("d" + n, d[n], v, oracle.REL_GATES if n in ("g", "beta") else oracle.REL[d[n].dtype])
+
+
 def test_offsets_past_32_bits(tfno):
     """Two trajectories further apart than 2^31 elements."""
     far, T, H, D = 2 ** 31 + 64, 70, 2, 64
