@@ -230,8 +230,10 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 const floatx4 y = quad_transpose(Y[i], lane);
-                const float u[4] = {y[0], y[1], y[2], y[3]};
                 const int row = t0 + 32 * (i >> 1) + 4 * (i & 1);
+                float u[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) u[r] = row + lane_token < len ? y[r] : 0.0f;       // past the end zeros beside a NaN too
                 E *to = dv + row * a.sdv.token;
                 if (plain) {
                     if (col0 < a.Dv) store4(behind(to, at_dv), u);
@@ -610,7 +612,7 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
         for (int s = 0; s < KB; ++s) {
             float u[8], w[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = accq[2 * s + (e >> 2)][e & 3], w[e] = acck[2 * s + (e >> 2)][e & 3];
+            for (int e = 0; e < 8; ++e) u[e] = token < len ? accq[2 * s + (e >> 2)][e & 3] : 0.0f, w[e] = token < len ? acck[2 * s + (e >> 2)][e & 3] : 0.0f;
             store8(dq + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dq, u);
             store8(dk + 32 * s + 8 * g, a.Dk - 32 * s - 8 * g, vec.dk, w);
         }

@@ -1004,7 +1004,9 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
         for (int i = 0; i < NT; ++i) {
             const int tile_token = t0 + 32 * (i >> 1) + 4 * (i & 1);
             E *to = o + tile_token * a.so.token + col0;
-            const float u[4] = {a.scale * QS[i][0], a.scale * QS[i][1], a.scale * QS[i][2], a.scale * QS[i][3]};
+            float u[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) u[r] = tile_token + lane_token < len ? a.scale * QS[i][r] : 0.0f;       // past the end zeros beside a NaN too
             if (plain) {
                 if (col0 < a.Dv) store4(behind(to, at_o), u);
             } else {

@@ -210,6 +210,25 @@ def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("T", (90, 128, 700))
+@pytest.mark.parametrize("what", ("initial", "k", "v", "d_o", "d_final"))
+def test_past_the_lengths_are_zeros_beside_a_nan(tfno, dtype, T, what):
+    """A NaN in the state or in a token that counts: outputs and gradients of the tokens past the lengths are zeros all the same."""
+    x = inputs(dtype, 3, T, 1, 2, 48, 40, seed=17)
+    x["lengths"] = torch.tensor([70, 1, T - 1], dtype=torch.int32, device="cuda")
+    x[what][:, 0] = float("nan")               # the first token, or the first head's state
+    live = oracle.tokens_of(x["lengths"], 3, T, "cuda")
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    for o in (forward(tfno, x)[0], forward(tfno, x, tape)[0]):
+        assert (o[~live] == 0).all()
+        assert torch.isnan(o).any() == (what not in ("d_o", "d_final"))
+    d = backward(tfno, x, tape)
+    for n in ("q", "k", "v", "g", "beta"):
+        assert (d[n][~live] == 0).all(), n
+    assert torch.isnan(d["k"]).any()           # the one gradient that every input has a part in
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("size", [(2, 150, 1, 2, 64, 48), (1, 70, 2, 8, 128, 128), (2, 200, 1, 3, 20, 33)])
 def test_heads_that_share_keys_keep_their_gradients_apart(tfno, dtype, size):
     """The first value head of every key head has values and gradients 1e4 times the others', and then NaN: what the other heads get of their own is as near, and not NaN."""
