@@ -362,7 +362,8 @@ size_t tfno_head_norm_rope_workspace_bytes(int D);
  * float32 [B, Hv, Dk, Dv], contiguous.  Hv is a multiple of Hk: value head h uses key head h / (Hv / Hk).  `lengths` (int32 [B] on the device, or
  * NULL) says how many tokens of each sequence count, as if cut to 0 .. T: the others are not read, their outputs and gradients are zeros, and
  * final is the state after the last one that counts.  Any decay and any beta are right; with |beta k'k| < 2 and g <= 0 the state stays bounded.
- * A NaN or an infinity in a token that counts makes its head's results NaN from the chunk of that token on (64 tokens, 32 for float32).
+ * A NaN or an infinity in a token that counts makes its head's results NaN from the chunk of that token on (64 tokens, 32 for float32); so does one in
+ * `initial` from the first token on, and a decay of 0 does not end that: a sequence that begins anew has no `initial`, or zeros there.
  *
  * The whole sequence: o, and final where it is not NULL.  With a tape (tfno_gated_delta_rule_tape_bytes bytes, aligned to 256) the call leaves
  * there what the backward call needs, else it needs tfno_gated_delta_rule_workspace_bytes(d, 0) bytes of workspace.
@@ -396,7 +397,7 @@ size_t tfno_gated_delta_rule_workspace_bytes(const tfno_delta_rule_desc *d, int 
 /*
  * One token of B sequences: the states [pool, Hv, Dk, Dv] (float32, contiguous) are advanced in place, and o is written.  Sequence b has the state
  * slots[b] (int32 [B] on the device; NULL: b).  A negative slot is a place without a sequence (o = 0), one that the pool does not hold gives NaN;
- * no state is touched for either.  A slot may not be given twice.  Descriptor, sizes and gates as above with T = 1; strides of tokens are not used.
+ * no state is touched for either.  A slot may not be given twice.  Where exp(g) is 0 the old state is not used, whatever it holds.  Descriptor, sizes and gates as above with T = 1; strides of tokens are not used.
  */
 tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void *q, const void *k, const void *v, const float *g,
                                        const float *beta, float *states, const int *slots, int pool, void *o, void *stream);

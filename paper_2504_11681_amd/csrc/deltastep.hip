@@ -68,7 +68,7 @@ __global__ __launch_bounds__(STEP_THREADS) void k_delta_step(DeltaStepArgs a, in
         const float kr = r < 128 ? ks[r] : 0.0f, qr = r < 128 ? qs[r] : 0.0f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            s[i][e] *= decay;
+            s[i][e] = decay == 0.0f ? 0.0f : s[i][e] * decay;          // forgotten whatever it was: a place of the pool that nobody wrote may hold NaN
             sk[e] = fmaf(kr, s[i][e], sk[e]);
             sq[e] = fmaf(qr, s[i][e], sq[e]);
         }

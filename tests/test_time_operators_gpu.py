@@ -513,6 +513,24 @@ def test_step(tfno, dtype, size):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(3, 2, 4, 64, 64), (2, 1, 1, 100, 33), (600, 1, 2, 32, 48)])
+def test_step_forgets_whatever_the_state_was(tfno, dtype, size):
+    """g = -inf in a place of the pool that holds NaN and infinities: the state is the token's alone.  Other heads keep theirs."""
+    B, Hk, Hv, Dk, Dv = size
+    x = inputs(dtype, B, 1, Hk, Hv, Dk, Dv, seed=22)
+    states = x["initial"].clone()
+    x["g"][0] = float("-inf")
+    states[0] = torch.tensor([float("nan"), float("inf"), float("-inf"), 1e38], device="cuda").repeat(states[0].numel() // 4 + 1)[:states[0].numel()].view(states[0].shape)
+    x["initial"][0] = 0.0
+    o = torch.full((B, Hv, Dv), 7.0, dtype=dtype, device="cuda")
+    say(f"[case] forgets {dtype} {size}")
+    tfno.gated_delta_rule_step(*(x[n][:, 0] for n in ("q", "k", "v", "g", "beta")), states, o, scale=x["scale"])
+    wo, wS = want(x, False)
+    near("o", o, wo[:, 0], oracle.REL[dtype])
+    near("states", states, wS, oracle.REL[F32])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 def test_steps_follow_the_whole_sequence(tfno, dtype):
     x = inputs(dtype, 2, 70, 2, 4, 64, 40, seed=21)
     states, outputs = x["initial"].clone(), []
