@@ -219,6 +219,7 @@ tfno_status tfno_gated_delta_rule(const tfno_delta_rule_desc *d, const void *q, 
     if (d->T > 0 && (!q || !k || !v || !beta || !o)) return TFNO_ERR_NULL;
     DeltaArgs a = rule_args(d);
     if (!tokens_near(a, a.sv) || !tokens_near(a, a.so)) return TFNO_ERR_UNSUPPORTED;
+    if (!delta_launches(a, tape != nullptr)) return TFNO_ERR_SHAPE;
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.Hv * a.Dk * a.Dv;
     const bool t = a.T > 0;
@@ -250,6 +251,7 @@ tfno_status tfno_gated_delta_rule_backward(const tfno_delta_rule_desc *d, const 
     if (d->T > 0 && (!q || !k || !v || !beta || !tape || !d_o || !dq || !dk || !dv || !dbeta)) return TFNO_ERR_NULL;
     DeltaArgs a = rule_args(d);
     if (!tokens_near(a, a.sdo) || !tokens_near(a, a.sdv)) return TFNO_ERR_UNSUPPORTED;
+    if (!delta_launches(a, true)) return TFNO_ERR_SHAPE;
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.Hv * a.Dk * a.Dv;
     const bool t = a.T > 0;

@@ -33,12 +33,14 @@ struct DeltaStepArgs {
     void *o;                            // [B, Hv, Dv]
     Strides sq, sk, sv, so, sg, sbeta;  // the token's stride is not used
     int B, Hk, Hv, Dk, Dv, pool;
+    int first;                          // of a launch's heads [B Hv]: more than one launch takes go in several
     float scale;
     bool bf16;
 };
 
 size_t delta_tape_bytes(const DeltaArgs &a);
 size_t delta_workspace_bytes(const DeltaArgs &a, bool backward);
+bool delta_launches(const DeltaArgs &a, bool whole);       // whether launches take the call: a batch `whole` (with a tape), or at least one sequence
 hipError_t delta_forward_launch(const DeltaArgs &a, hipStream_t s);
 hipError_t delta_backward_launch(const DeltaArgs &a, hipStream_t s);
 hipError_t delta_step_launch(const DeltaStepArgs &a, hipStream_t s);

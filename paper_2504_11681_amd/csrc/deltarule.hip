@@ -143,6 +143,18 @@ hipError_t scan_back(const DeltaArgs &a, const DeltaMemory &m, hipStream_t s)
     return hipGetLastError();
 }
 
+// Threads of the largest launch for a batch of B sequences: preparation, walk, gradients.  A launch takes less than 2^32.
+template <class E, int KB>
+long long launch_threads(const DeltaArgs &a, int B, bool tape)
+{
+    typedef DeltaUnits<E, KB> U;
+    const long long chunks = (a.T + U::L - 1) / U::L, heads = (long long)B * a.Hv;
+    const ScanShape sh = scan_shape(heads, (a.Dv + 31) / 32 * 2);
+    const long long walk = heads * sh.blocks * 64 * (sh.waves + 1), prepare = heads * chunks * 64 * U::NT;
+    return std::max({walk, prepare, tape ? (long long)B * a.Hk * chunks * 128 * U::NT : 0});
+}
+constexpr long long MOST_THREADS = (1LL << 32) - 1;
+
 // Sequences of a batch that go through preparation and walk before the next ones do, without a tape: what the one leaves for the other then stays in the
 // last-level cache (256 MB), in memory that the next ones use again, instead of passing through HBM.  Whole rounds of workgroups, one a CU, of up to 192 MB; not where
 // one round is more than the cache.  In us, in one piece and in such ones (B, T, heads, Dk = Dv): BF16 256, 1024, 2, 64 243 and 203, 512, 512, 4, 32 383 and 340, float32
@@ -153,13 +165,16 @@ int batch_piece(const DeltaArgs &a)
 {
     typedef DeltaUnits<E, KB> U;
     const int chunks = (a.T + U::L - 1) / U::L;
-    if (KB > 2 || a.B < 2 || chunks == 0 || segments_of(a, chunks) > 1) return a.B;
+    if (a.B < 2 || segments_of(a, chunks) > 1) return a.B;
+    int most = a.B;               // that launches take, and half of it more (next_piece)
+    while (most > 1 && launch_threads<E, KB>(a, most, false) > MOST_THREADS / 2) most = (most + 1) / 2;
+    if (KB > 2 || chunks == 0) return most;
     const long long key_units = U::PI == 1 ? U::QT - U::KT : U::KEY_FORWARD;
     const long long bytes = chunks * (a.Hk * key_units + a.Hv * (long long)U::VALUE_FORWARD) * 1024;
     const long long workgroups = a.Hv * (((a.Dv + 31) / 32 * 2 + SCAN_WAVES - 1) / SCAN_WAVES);
     const long long round = std::max<long long>(1, 256 / workgroups), fit = (192LL << 20) / bytes;
-    if (round * bytes > 256LL << 20) return a.B;
-    return (int)std::min<long long>(a.B, std::max(round, fit / round * round));
+    if (round * bytes > 256LL << 20) return most;
+    return (int)std::min<long long>(most, std::max(round, fit / round * round));
 }
 // How many of `left` sequences are next: what is less than half a piece goes with the last whole one.
 int next_piece(int left, int piece) { return left < piece + (piece + 1) / 2 ? left : piece; }
@@ -245,6 +260,10 @@ struct ForwardBytes {
         return most;
     }
 };
+struct Launches {
+    const DeltaArgs &a; bool whole;
+    template <class E, int KB> bool operator()() const { return launch_threads<E, KB>(a, whole ? a.B : 1, whole) <= MOST_THREADS; }
+};
 struct BackwardBytes {
     const DeltaArgs &a;
     template <class E, int KB> size_t operator()() const { DeltaMemory m{}; return backward_memory<E, KB>(a, nullptr, &m); }
@@ -256,6 +275,7 @@ auto by_kind(const DeltaArgs &a, F f) { return a.bf16 ? by_size<bf16>(a, f) : by
 
 size_t delta_tape_bytes(const DeltaArgs &a) { return by_kind(a, ForwardBytes{a, true}); }
 size_t delta_workspace_bytes(const DeltaArgs &a, bool backward) { return backward ? by_kind(a, BackwardBytes{a}) : by_kind(a, ForwardBytes{a, false}); }
+bool delta_launches(const DeltaArgs &a, bool whole) { return by_kind(a, Launches{a, whole}); }
 hipError_t delta_forward_launch(const DeltaArgs &a, hipStream_t s) { return by_kind(a, Forward{a, s}); }
 hipError_t delta_backward_launch(const DeltaArgs &a, hipStream_t s) { return by_kind(a, Backward{a, s}); }
 

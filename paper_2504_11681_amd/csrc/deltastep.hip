@@ -8,11 +8,13 @@
 // for 537 MB of states, 6.0 TB/s (a part of them stays in the last-level cache from step to step; a copy reaches 5.1).
 #include "deltarule.h"
 
+#include <algorithm>
+
 namespace tfno {
 
 namespace {
 
-constexpr int STEP_THREADS = 256;
+constexpr int STEP_THREADS = 256, STEP_BLOCKS = 1 << 23;      // a launch takes less than 2^32 threads
 
 template <class E, int VEC, int ROWS>
 __global__ __launch_bounds__(STEP_THREADS) void k_delta_step(DeltaStepArgs a, int lanes, int blocks_per_head)
@@ -21,7 +23,7 @@ __global__ __launch_bounds__(STEP_THREADS) void k_delta_step(DeltaStepArgs a, in
     __shared__ float sums[2][STEP_THREADS / 64][128];
     __shared__ float qk_part[2];
     const int tid = threadIdx.x, wave = tid >> 6, groups = STEP_THREADS / lanes, cl = tid & (lanes - 1), rg = tid / lanes;
-    const int block = blockIdx.x % blocks_per_head, head = blockIdx.x / blocks_per_head;
+    const int block = blockIdx.x % blocks_per_head, head = a.first + blockIdx.x / blocks_per_head;
     const int b = head / a.Hv, h = head - b * a.Hv, hk = h / (a.Hv / a.Hk);
     const int c = (block * lanes + cl) * VEC;
     const bool live = c < a.Dv;
@@ -121,13 +123,17 @@ hipError_t launch(const DeltaStepArgs &a, hipStream_t s)
     while (lanes < 32 && lanes * VEC < a.Dv) lanes <<= 1;
     while (lanes > 4 && heads * ((a.Dv + lanes * VEC - 1) / (lanes * VEC)) < 512) lanes >>= 1;
     const int per_head = (a.Dv + lanes * VEC - 1) / (lanes * VEC), groups = STEP_THREADS / lanes;
-    const unsigned grid = (unsigned)(heads * per_head);
-    const int rows = (a.Dk + groups - 1) / groups;
-    if (rows <= 1) k_delta_step<E, VEC, 1><<<grid, STEP_THREADS, 0, s>>>(a, lanes, per_head);
-    else if (rows <= 2) k_delta_step<E, VEC, 2><<<grid, STEP_THREADS, 0, s>>>(a, lanes, per_head);
-    else if (rows <= 4) k_delta_step<E, VEC, 4><<<grid, STEP_THREADS, 0, s>>>(a, lanes, per_head);
-    else if (rows <= 8) k_delta_step<E, VEC, 8><<<grid, STEP_THREADS, 0, s>>>(a, lanes, per_head);
-    else k_delta_step<E, VEC, 16><<<grid, STEP_THREADS, 0, s>>>(a, lanes, per_head);
+    const int rows = (a.Dk + groups - 1) / groups, most = STEP_BLOCKS / per_head;
+    for (long long first = 0; first < heads; first += most) {
+        DeltaStepArgs p = a;
+        p.first = (int)first;
+        const unsigned grid = (unsigned)(std::min<long long>(heads - first, most) * per_head);
+        if (rows <= 1) k_delta_step<E, VEC, 1><<<grid, STEP_THREADS, 0, s>>>(p, lanes, per_head);
+        else if (rows <= 2) k_delta_step<E, VEC, 2><<<grid, STEP_THREADS, 0, s>>>(p, lanes, per_head);
+        else if (rows <= 4) k_delta_step<E, VEC, 4><<<grid, STEP_THREADS, 0, s>>>(p, lanes, per_head);
+        else if (rows <= 8) k_delta_step<E, VEC, 8><<<grid, STEP_THREADS, 0, s>>>(p, lanes, per_head);
+        else k_delta_step<E, VEC, 16><<<grid, STEP_THREADS, 0, s>>>(p, lanes, per_head);
+    }
     return hipGetLastError();
 }
 

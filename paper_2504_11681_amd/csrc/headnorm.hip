@@ -37,9 +37,10 @@ hipError_t launch(const HeadNormArgs &a, int lpr, hipStream_t s)
         blocks[i] = (g.items[i] + groups - 1) / groups;
     }
     const unsigned long long all = (unsigned long long)blocks[0] + blocks[1];
-    if (BACKWARD && all > HEAD_NORM_BLOCKS)      // shared out as the work is, each kind that has work its own
+    const unsigned most = BACKWARD ? HEAD_NORM_BLOCKS : HEAD_NORM_LAUNCH;
+    if (all > most)      // shared out as the work is, each kind that has work its own
         for (int i = 0; i < 2; ++i)
-            if (blocks[i]) blocks[i] = 1 + (unsigned)((unsigned long long)blocks[i] * (HEAD_NORM_BLOCKS - 2) / all);
+            if (blocks[i]) blocks[i] = 1 + (unsigned)((unsigned long long)blocks[i] * (most - 2) / all);
     g.blocks_q = blocks[0];
     const unsigned grid = blocks[0] + blocks[1];
     if (grid) k_head_norm<E, VEC, ITER, NH, INTER, BACKWARD><<<grid, HEAD_NORM_THREADS, 0, s>>>(a, g);

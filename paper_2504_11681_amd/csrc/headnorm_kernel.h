@@ -19,6 +19,7 @@ constexpr int HEAD_NORM_THREADS = 256;
 // Workgroups of the backward kernel, at most: as many as the chip holds at four waves a SIMD, each with one partial sum of the weights' gradient (both
 // directions of the batch above: 104 us; with 768 111, with 512 128, with 2048 107).
 constexpr int HEAD_NORM_BLOCKS = 1024;
+constexpr unsigned HEAD_NORM_LAUNCH = 1u << 22;      // of the forward kernel: 2^30 threads, a launch takes less than 2^32
 
 struct HeadNormShape {
     int lpr;                        // lanes of a head

@@ -344,6 +344,22 @@ def test_rule_says_which_distances_it_does_not_support(L):
         assert call(L.tfno_gated_delta_rule_backward, rule_desc(**{n: far}), RULE_BACK) == tfno.ERR_UNSUPPORTED, n
 
 
+def test_sizes_that_no_launch_takes_are_refused(L):
+    """A launch takes less than 2^32 threads.  A walk of 256 columns has 1280 a head: 2^21 heads of a sequence are taken, 2^23 are not; of a batch, pieces are."""
+    assert L.tfno_set_workspace(None, 0) == tfno.OK
+    for n, T, status in ((1 << 21, 1, tfno.ERR_WORKSPACE), (1 << 23, 1, tfno.ERR_SHAPE), (1 << 23, 0, tfno.ERR_SHAPE), (1 << 25, 0, tfno.ERR_SHAPE)):
+        far = {m: FAKE + (i << 36) for i, m in enumerate(("q", "k", "v", "g", "beta", "lengths", "initial", "o", "final", "tape"))}
+        d = rule_desc(B=1, T=T, Hk=1, Hv=n, Dk=1, Dv=256, v=strides(T, n, 256), o=strides(T, n, 256), g=strides(T, n, 1), beta=strides(T, n, 1))
+        assert call(L.tfno_gated_delta_rule, d, far, tape=None) == status, (n, T)
+        if status != tfno.ERR_SHAPE:
+            d.B, d.Hk, d.Hv = 16 * n, 1, 1
+            for m in ("v", "o"):
+                setattr(d, m, strides(T, 1, 256))
+            for m in ("q", "k", "g", "beta"):
+                setattr(d, m, strides(T, 1, 1))
+            assert call(L.tfno_gated_delta_rule, d, far, tape=None) == status
+
+
 def test_key_holds_all_that_a_plan_depends_on(L):
     m = tfno._load_marshal()
     x = torch.zeros(2, 3, 4)

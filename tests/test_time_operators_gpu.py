@@ -547,6 +547,22 @@ def test_steps_follow_the_whole_sequence(tfno, dtype):
     near("o without decay", o, again[0][:, 0], oracle.REL[dtype])
 
 
+@pytest.mark.parametrize("B, Hv", [(1, 2 ** 24 + 3), (2 ** 24 + 3, 1), (3, 2 ** 23 - 5)])
+def test_step_of_more_heads_than_one_launch_takes(tfno, B, Hv):
+    """2^24 workgroups of 256 threads are 2^32: such calls go in several launches."""
+    gen = torch.Generator("cuda").manual_seed(23)
+    q, k = (torch.randn(B, 1, 1, generator=gen, device="cuda") for _ in range(2))
+    v, states = torch.randn(B, Hv, 1, generator=gen, device="cuda"), torch.randn(B, Hv, 1, 1, generator=gen, device="cuda")
+    g, beta = -torch.rand(B, Hv, generator=gen, device="cuda"), torch.rand(B, Hv, generator=gen, device="cuda")
+    o = torch.full_like(v, 7.0)
+    Sb = states[..., 0].double() * g.double().exp()[..., None]
+    S = Sb + (beta[..., None].double() * k.double()) * (v.double() - Sb * k.double())
+    say(f"[case] step of {B} x {Hv} heads")
+    tfno.gated_delta_rule_step(q, k, v, g, beta, states, o, scale=0.5)
+    near("o", o, 0.5 * S * q.double(), oracle.REL[F32])
+    near("states", states[..., 0], S, oracle.REL[F32])
+
+
 # ---------------------------------------------------------------- norm with rotation
 
 NORMS = [(1, 1, 1, 1, 1, 0), (2, 3, 2, 1, 2, 2), (1, 5, 3, 2, 3, 2), (2, 7, 4, 2, 7, 4), (1, 1, 8, 8, 64, 64), (3, 37, 6, 2, 80, 40), (2, 33, 2, 2, 96, 96),
@@ -639,3 +655,16 @@ def test_norm_of_nothing(tfno):
     tfno.head_norm_rope(q, q, None, None, None, None, q.clone(), q.clone())
     tfno.head_norm_rope_backward(q, q, None, None, None, None, q.clone(), q.clone(), q.clone(), q.clone(), dw, None)
     assert (dw == 0).all()
+
+
+def test_norm_of_more_heads_than_one_launch_takes(tfno):
+    """2^26 heads and a few, four a workgroup: 2^24 workgroups of 256 threads would be 2^32."""
+    B, H, D = 2 ** 20 + 1, 64, 129
+    gen = torch.Generator("cuda").manual_seed(34)
+    x = torch.randn(1, 1, H, D, generator=gen, device="cuda").to(BF16)
+    none = torch.empty(B, 1, 0, D, dtype=BF16, device="cuda")
+    out = torch.full((B, 1, H, D), 7.0, dtype=BF16, device="cuda")
+    say("[case] norm of 2^26 heads")
+    tfno.head_norm_rope(x.expand(B, 1, H, D), none, None, None, None, None, out, none)
+    near("the first", out[:1], oracle.norm(x, None, None, None, None, 1e-6, False), oracle.REL[BF16])
+    assert all(torch.equal(part, out[:1].expand_as(part)) for part in out.split(1 << 17))
