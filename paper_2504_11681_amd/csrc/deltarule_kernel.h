@@ -20,8 +20,9 @@
 // so that the two results of a pair hold in each lane just the eight consecutive indexes that an operand block needs: a result becomes
 // an operand without leaving its registers.
 //
-// Float32 values (the state, E, U, T, P, and float32 inputs) are operands as three BF16 parts that add up to them, and products of parts
-// below 2^-24 are left out, so sums have float32's accuracy.  BF16 inputs are one part.  What goes into a BF16 output alone (P, U, and S as the
+// Float32 values (the state, E, U, T, P, and float32 inputs) are operands as three BF16 parts that add up to them: the second is below 2^-7 of the value, the third
+// at most 2^-16 and of either sign.  Products of the second and the third are left out, 2^-22 of a product at most and 2^-24 in the mean square, so sums have float32's accuracy.
+// BF16 inputs are one part.  What goes into a BF16 output alone (P, U, and S as the
 // outputs read it) has three parts too: where a key is written over, Q S and P U are large and cancel, and with two parts, 2^-15 off, outputs a
 // thousandth of the old value were 2e-2 off.  That is a tenth of the time (256 x 1024 tokens, 2 heads of 64: 205 -> 224 us).
 #pragma once
@@ -56,14 +57,15 @@ __device__ __forceinline__ float minus_high(unsigned w, float x)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), __builtin_bit_cast(pair, c), x, false);
 }
 
-// Values 4 e .. 4 e + 3: two pairs in step, since a dot product's result is not there for the next instruction.
+// Values 4 e .. 4 e + 3: two pairs in step, since a dot product's result is not there for the next instruction.  The first part is cut off, which no value overflows,
+// the others are rounded to nearest: cut off too, the last one would have its value's sign, and what products leave out would add up.
 template <int P>
 __device__ __forceinline__ void set_four(Frag<P> &f, int e, const float (&x)[4])
 {
     float r[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const unsigned u = pack_bf16(r[0], r[1]), v = pack_bf16(r[2], r[3]);
+        const unsigned u = p ? bf16_pair(r[0], r[1]) : pack_bf16(r[0], r[1]), v = p ? bf16_pair(r[2], r[3]) : pack_bf16(r[2], r[3]);
         if (p + 1 < P) r[0] = minus_low(u, r[0]), r[1] = minus_high(u, r[1]), r[2] = minus_low(v, r[2]), r[3] = minus_high(v, r[3]);
         f.w[p][2 * e] = u, f.w[p][2 * e + 1] = v;
     }

@@ -209,6 +209,22 @@ def test_lengths_and_what_stands_past_them(tfno, dtype, bad):
     check_forward(tfno, x, "without tape")
 
 
+@pytest.mark.parametrize("tokens", (1, 40))
+def test_products_of_float32_are_not_off_to_one_side(tfno, tokens):
+    """All factors 1 + 2^-7 - 2^-23, whose digits are ones where an operand's second and third part are: parts that are cut off lose 2^-21 of every product, all on one side.
+    Nothing is written, so outputs are q times the state, and dq is d_o times it: one product of 32 terms, one rounding of at most 2^-23 and small ones below: 2^-22."""
+    x = inputs(F32, 1, tokens, 1, 1, 32, 32, seed=18)
+    for n in ("q", "initial", "d_o"):
+        x[n][:] = 1 + 2.0 ** -7 - 2.0 ** -23
+    x["beta"][:], x["g"], x["scale"] = 0.0, None, 1.0
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    want = 32 * (1 + 2.0 ** -7 - 2.0 ** -23) ** 2
+    for o in (forward(tfno, x)[0], forward(tfno, x, tape)[0], backward(tfno, x, tape)["q"]):
+        off = float((o.double() / want - 1).abs().max())
+        say(f"   {off:.3g} of {2.0 ** -22:.3g}")
+        assert off <= 2.0 ** -22
+
+
 @pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("T", (90, 128, 700))
 @pytest.mark.parametrize("what", ("initial", "k", "v", "d_o", "d_final"))
