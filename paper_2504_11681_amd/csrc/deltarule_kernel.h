@@ -471,6 +471,13 @@ __global__ __launch_bounds__((4 * DeltaKind<E>::L)) void k_delta_prepare(DeltaAr
                 if (TAPE) qk[i] = mm<3>(row_frag<PI>(Qs + at), kf, qk[i]);
             }
         }
+        // Results are read here, in the line of their products, and not behind the branches that follow: this kernel once gave a wrong inverse where products and the reads of their
+        // results had uniform branches between them, for a cause that was not found (the compiler leaves as many wait states there as in a line).
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            asm volatile("" : "+v"(kk[i]), "+v"(kq[i]));
+            if (TAPE) asm volatile("" : "+v"(qk[i]));
+        }
         const float hi_own = hi[own], lo_own = lo[own], beta_own = beta[own];
 #pragma unroll
         for (int s = 0; s < LB; ++s) {
