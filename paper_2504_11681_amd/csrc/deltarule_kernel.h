@@ -581,30 +581,25 @@ __device__ __forceinline__ T *uniform(T *p)
     const uintptr_t u = (uintptr_t)p;
     return (T *)((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)u));
 }
-// Units of 1024 bytes from global memory to LDS by one wave; they are there for the others after its wait for its loads (s_waitcnt 0) and a barrier.
-// In assembly, because the compiler takes every later read of LDS for one that may need them and would wait for the next chunk's blocks
-// before the first product of this one.  The instruction has no result register.
-__device__ __forceinline__ void units_to_lds(const unsigned char *from, const unsigned char *to, int units, int lane)
-{
-    const unsigned at = lane * 16;          // a uniform address and 32 bits a lane
-    from = uniform(from);
-    unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
-    for (int u = 0; u < units; ++u, lds += 1024, from += 1024)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(at), "s"(from));
-}
-
-// The same from 16 bytes of each lane's own.
-__device__ __forceinline__ void lanes_to_lds(const void *from, const unsigned char *to)
-{
-    const unsigned lds = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(from));
-}
-
 // The element `bytes` behind a uniform address: 32 bits a lane, so that the address stays scalar.
 template <class E>
 __device__ __forceinline__ const E *behind(const E *p, unsigned bytes) { return (const E *)((const char *)p + bytes); }
 template <class E>
 __device__ __forceinline__ E *behind(E *p, unsigned bytes) { return (E *)((char *)p + bytes); }
+
+// 16 bytes of each lane from global memory to LDS, 1024 bytes from `to` on, which is the same for all lanes.
+__device__ __forceinline__ void lanes_to_lds(const void *from, const unsigned char *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+// Units of 1024 bytes from global memory to LDS by one wave; they are there for the others after its wait for its loads (s_waitcnt 0) and a barrier.
+// The wave reads no LDS itself: before that the compiler would wait for all of them.
+__device__ __forceinline__ void units_to_lds(const unsigned char *from, const unsigned char *to, int units, int lane)
+{
+    const unsigned at = lane * 16;          // a uniform address and 32 bits a lane
+    from = uniform(from);
+    for (int u = 0; u < units; ++u, to += 1024, from += 1024) lanes_to_lds(behind(from, at), to);
+}
 
 // A wave's column of one chunk, eight consecutive tokens for each pair of tiles, from a tensor [token, column] whose first token counts.  `at`
 // is the lane's offset in bytes (8 g tokens and its column, or column 0 past the last one); distances of tokens are uniform.  In a chunk that ends early, the

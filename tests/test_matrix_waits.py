@@ -125,3 +125,11 @@ def test_preparation_reads_its_products_before_it_branches(kernels):
     for name in names:
         found = waits(kernels[name])
         assert ("v_mfma_f32_16x16x32_bf16", False) in found and ("v_mfma_f32_16x16x32_bf16", True) not in found, (name, found)
+
+
+def test_no_assembly_writes_registers_that_it_does_not_declare():
+    """m0 is the compiler's own: it may hold a value there across an assembly statement, which cannot declare that it changes it."""
+    for name in sorted(os.listdir(CSRC)):
+        with open(os.path.join(CSRC, name)) as f:
+            for statement in re.findall(r"\basm\b[^;]*;", f.read()):
+                assert not re.search(r"\bm0\b", statement), (name, statement)
