@@ -331,7 +331,7 @@ typedef struct { long long batch, token, head; } tfno_strides;   /* in elements 
  * A position outside 0 .. P-1 gives NaN in the values that it would turn.  y may be x itself (the same pointer and strides).
  *
  * The backward call takes the gradients of the results (at the places of q_out, k_out) and gives those of q, k and, where the pointers are
- * not NULL, of the weights.  It needs tfno_head_norm_rope_workspace_bytes(D) bytes of workspace.  dq may be q or dq_out itself.
+ * not NULL, of the weights, for which it needs tfno_head_norm_rope_workspace_bytes(D) bytes of workspace.  dq may be q or dq_out itself.
  *
  * Sizes: 1 <= D <= 512, R even, 0 <= R <= D, Hq + Hk >= 1, eps > 0, P >= T without positions (TFNO_ERR_SHAPE); B = 0 or T = 0 is an empty call,
  * whose weights' gradients are zeros.

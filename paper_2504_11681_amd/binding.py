@@ -506,7 +506,8 @@ def _head_norm_plan(q, k, q_out, k_out, dq, dk, positions, wq, wk, dwq, dwk, cos
     for (name, t), H in zip(names, (Hq, Hk) * 3):
         if t is not None:
             setattr(d, name, _strides4(name, t, (B, T, H, D)))
-    return ctypes.addressof(d), _entry("tfno_head_norm_rope_workspace_bytes")(D), q[1], d
+    need = 0 if dwq is None and dwk is None else _entry("tfno_head_norm_rope_workspace_bytes")(D)
+    return ctypes.addressof(d), need, q[1], d
 
 
 def head_norm_rope(q, k, wq, wk, cos, sin, q_out, k_out, positions=None, eps: float = 1e-6, interleaved: bool = False, stream=None):

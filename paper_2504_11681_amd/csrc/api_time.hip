@@ -149,7 +149,7 @@ tfno_status head_norm(const tfno_head_norm_desc *d, bool backward, const void *q
         const std::pair<int, int> in_place[] = {{0, 4}, {0, 6}, {1, 5}, {1, 7}};
         st = check_views(views, 4, in_place, 4);
         void *ws = nullptr;
-        if (st == TFNO_OK) st = workspace(head_norm_workspace_bytes(d->D), views, 13, &ws);
+        if (st == TFNO_OK && (dwq || dwk)) st = workspace(head_norm_workspace_bytes(d->D), views, 13, &ws);
         a.partial = (float *)ws;
         a.sdq = vdq.s, a.sdk = vdk.s;
     }

@@ -13,7 +13,7 @@ struct HeadNormArgs {
     const float *cos, *sin;             // [P, R / 2]
     const int *positions;               // [B, T] or NULL (the token's index)
     float *dwq, *dwk;                   // [D] or NULL
-    float *partial;                     // workspace of the weights' gradients: [blocks][2][D]
+    float *partial;                     // workspace of the weights' gradients, [blocks][D], or NULL where neither is asked for
     Strides sq, sk, sq_out, sk_out, sdq, sdk;
     long long positions_batch;
     int B, T, Hq, Hk, D, R, P;

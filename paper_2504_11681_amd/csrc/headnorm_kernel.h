@@ -192,6 +192,7 @@ __global__ __launch_bounds__(HEAD_NORM_THREADS) __attribute__((amdgpu_waves_per_
     }
 
     if constexpr (BACKWARD) {
+        if (!a.partial) return;          // nobody asks for the weights' gradient
         // the block's part of the weights' gradient: groups of a wave, then the waves, always in the same order
         __shared__ float sums[HEAD_NORM_THREADS / 64][512];
         const int wave = threadIdx.x >> 6;

@@ -665,6 +665,32 @@ def test_norm_gradient_against_differences(tfno):
         assert abs(float((d[n].double() * way).sum()) - slope) <= 4 * oracle.REL_GATES * float(d[n].norm()) + 1e-6 * abs(slope)
 
 
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(2, 9, 3, 1, 64, 32), (3, 200, 8, 2, 80, 40)])
+def test_norm_gradient_without_the_weights_needs_no_workspace(tfno, dtype, size):
+    B, T, Hq, Hk, D, R = size
+    gen = torch.Generator("cuda").manual_seed(35)
+    q, dy = (torch.randn(B, T, Hq, D, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    k, dz = (torch.randn(B, T, Hk, D, generator=gen, device="cuda").to(dtype) for _ in range(2))
+    angle = torch.rand(T, R // 2, generator=gen, device="cuda")
+    cos, sin = torch.cos(angle), torch.sin(angle)
+    before = tfno._workspace
+    try:
+        tfno.set_workspace(None)
+        dq, dk = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+        tfno.head_norm_rope_backward(q, k, None, None, cos, sin, dy, dz, dq, dk)
+        assert tfno._workspace is None
+    finally:
+        tfno.set_workspace(before)
+    near("dq", dq, oracle.norm(q, None, cos, sin, None, 1e-6, False, dy)[1], oracle.REL[dtype])
+    near("dk", dk, oracle.norm(k, None, cos, sin, None, 1e-6, False, dz)[1], oracle.REL[dtype])
+    dw = torch.empty(D, device="cuda")
+    for weights in ((dw, None), (None, dw)):
+        tfno.head_norm_rope_backward(q, k, None, None, cos, sin, dy, dz, dq, dk, *weights)
+        x, d = (q, dy) if weights[0] is dw else (k, dz)
+        near("dw", dw, oracle.norm(x, None, cos, sin, None, 1e-6, False, d)[2], oracle.REL[F32])
+
+
 def test_norm_of_nothing(tfno):
     q = torch.zeros(0, 4, 2, 16, device="cuda")
     dw = torch.full((16,), 7.0, device="cuda")
