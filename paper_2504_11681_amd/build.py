@@ -38,25 +38,31 @@ def _run(cmd, what: str) -> None:
         raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
 
 
-def _build_marshal() -> None:
-    import torch
+def _build_marshal() -> bool:
+    """_marshal.so, which the operators along time are called through from Python; without torch there is nothing to build it for."""
+    try:
+        import torch
+    except ImportError:
+        return False
     root = os.path.dirname(torch.__file__)
     include, lib = os.path.join(root, "include"), os.path.join(root, "lib")
     _run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
           os.path.join(CSRC, "marshal.cpp"), "-o", MARSHAL, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10", "-ldl"], "marshal.cpp")
+    return True
 
 
 def build(verbose: bool = True, jobs: int = 8) -> str:
+    """The library first: it needs hipcc alone, and is there whatever becomes of _marshal.so."""
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:
         marshal = ex.submit(_build_marshal)
         objs = list(ex.map(_compile, srcs))
-        marshal.result()
-    _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], "link")
+        _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], "link")
+    both = marshal.result()
     if verbose:
-        print(f"built {LIB} from {len(srcs)} sources, and {MARSHAL}", file=sys.stderr)
+        print(f"built {LIB} from {len(srcs)} sources, and {MARSHAL if both else 'no _marshal.so, since there is no torch'}", file=sys.stderr)
     return LIB
 
 

@@ -360,6 +360,27 @@ def test_sizes_that_no_launch_takes_are_refused(L):
             assert call(L.tfno_gated_delta_rule, d, far, tape=None) == status
 
 
+def test_the_library_is_built_without_torch_and_whatever_becomes_of_the_calls_from_python(monkeypatch, capsys):
+    import sys
+    from paper_2504_11681_amd import build
+    ran = []
+
+    def run(cmd, what):
+        ran.append(what)
+        if what == "marshal.cpp":
+            raise RuntimeError("no headers")
+
+    monkeypatch.setattr(build, "_compile", lambda src: src + ".o")
+    monkeypatch.setattr(build, "_run", run)
+    with pytest.raises(RuntimeError, match="no headers"):
+        build.build()
+    assert sorted(ran) == ["link", "marshal.cpp"]
+    ran.clear()
+    monkeypatch.setitem(sys.modules, "torch", None)
+    assert build.build() == build.LIB and ran == ["link"]
+    assert "no _marshal.so" in capsys.readouterr().err
+
+
 def test_key_holds_all_that_a_plan_depends_on(L):
     m = tfno._load_marshal()
     x = torch.zeros(2, 3, 4)
