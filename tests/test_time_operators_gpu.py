@@ -399,6 +399,39 @@ def test_slices_that_interleave_by_heads(tfno, dtype):
         near("d" + n, d[n], v, oracle.REL_GATES if n in ("g", "beta") else oracle.REL[d[n].dtype])
 
 
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("way", ("fused", "heads first", "tokens first", "one element off", "repeated", "wide rows", "odd wide rows"))
+@pytest.mark.parametrize("size", [(3, 77, 2, 4, 64, 64), (2, 130, 1, 2, 72, 40), (1, 700, 1, 1, 128, 96), (4, 65, 2, 2, 24, 32)])
+def test_strides_without_a_tape(tfno, dtype, way, size):
+    """Walks without a tape read BF16 keys and queries out of the caller's rows where these allow it, whole sequences and segments, to ends inside a chunk."""
+    B, T, Hk, Hv, Dk, Dv = size
+    x = inputs(dtype, *size, seed=19)
+    if way == "fused":
+        w = torch.empty(B, T, 2 * Hk * Dk + Hv * Dv, dtype=dtype, device="cuda")
+        q, k, v = w.split((Hk * Dk, Hk * Dk, Hv * Dv), -1)
+        for n, p in (("q", q.unflatten(-1, (Hk, Dk))), ("k", k.unflatten(-1, (Hk, Dk))), ("v", v.unflatten(-1, (Hv, Dv)))):
+            x[n] = p.copy_(x[n])
+    elif way in ("heads first", "tokens first"):
+        axes = (1, 2) if way == "heads first" else (0, 1)
+        for n in ("q", "k", "v", "g", "beta"):
+            x[n] = x[n].transpose(*axes).contiguous().transpose(*axes)
+    elif way == "one element off":
+        for n in ("q", "k"):
+            w = torch.empty(x[n].numel() + 1, dtype=dtype, device="cuda")[1:].view(x[n].shape)
+            x[n] = w.copy_(x[n])
+    elif way == "repeated":
+        x["q"] = x["q"][:1].expand(B, -1, -1, -1)
+        x["k"] = x["k"][:, :, :1].expand(-1, -1, Hk, -1)
+    else:
+        more = 8 if way == "wide rows" else 3
+        for n in ("q", "k", "v"):
+            w = torch.full((*x[n].shape[:-1], x[n].shape[-1] + more), float("nan"), dtype=dtype, device="cuda")[..., :-more]
+            x[n] = w.copy_(x[n])
+    check_forward(tfno, x, f"[case] strides without a tape {dtype} {way} {size}")
+    x["lengths"] = torch.arange(T, T - 23 * B, -23, dtype=torch.int32, device="cuda")
+    check_forward(tfno, x, "with lengths")
+
+
 def test_offsets_past_32_bits(tfno):
     """Two trajectories further apart than 2^31 elements."""
     far, T, H, D = 2 ** 31 + 64, 70, 2, 64
@@ -617,6 +650,36 @@ def test_norm(tfno, dtype, interleaved, size):
             # one value a head: its gradient is the small difference of two that cancel
             near("d" + n, dx.double() + (x.double() if D == 1 else 0), a[1] + (x.double() if D == 1 else 0), oracle.REL[dtype])
             near("dw" + n, dw, a[2], oracle.REL[F32])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("interleaved", (False, True))
+@pytest.mark.parametrize("size", [(8, 512, 13, 4, 128, 128), (8, 2049, 17, 3, 64, 32), (16, 260, 3, 7, 63, 20), (2, 4100, 1, 6, 100, 50), (700, 3, 5, 11, 200, 64), (1, 9000, 9, 0, 128, 64),
+                                  (5, 5000, 0, 7, 48, 48)])
+def test_norm_of_many_heads(tfno, dtype, interleaved, size):
+    """So many heads that a group of lanes takes four of them, heads that are no multiple of four, more groups than the gradient's workgroups take in one turn; and heads too wide for that."""
+    B, T, Hq, Hk, D, R = size
+    gen = torch.Generator("cuda").manual_seed(36)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    q, dy = (normal(B, T, Hq, D) * 3).to(dtype), normal(B, T, Hq, D).to(dtype)
+    k, dz = (normal(B, T, Hk, D) * 3).to(dtype), normal(B, T, Hk, D).to(dtype)
+    wq, wk = 1 + 0.3 * normal(D), 1 + 0.3 * normal(D)
+    angle = 6.3 * torch.rand(2 * T, R // 2, generator=gen, device="cuda")
+    cos, sin = torch.cos(angle), torch.sin(angle)
+    positions = torch.randint(0, 2 * T, (B, T), generator=gen, device="cuda", dtype=torch.int32)
+    say(f"[case] norm of many heads {dtype} {interleaved} {size}")
+    yq, yk = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    tfno.head_norm_rope(q, k, wq, wk, cos, sin, yq, yk, positions=positions, interleaved=interleaved)
+    dq, dk, dwq, dwk = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(wq, 7.0), torch.full_like(wk, 7.0)
+    tfno.head_norm_rope_backward(q, k, wq, wk, cos, sin, dy, dz, dq, dk, dwq, dwk, positions=positions, interleaved=interleaved)
+    for n, x, w, d, got, dx, dw in (("q", q, wq, dy, yq, dq, dwq), ("k", k, wk, dz, yk, dk, dwk)):
+        a = oracle.norm(x, w, cos, sin, positions, 1e-6, interleaved, d)
+        near(n, got, a[0], oracle.REL[dtype])
+        near("d" + n, dx, a[1], oracle.REL[dtype])
+        near("dw" + n, dw, a[2], oracle.REL[F32])
 
 
 def test_norm_in_place_without_weights_and_with_strides(tfno):
