@@ -1,7 +1,7 @@
 """Fields that move: a Fourier layer reads every frame, the gated delta rule carries what was seen, the next frame comes out.
 
 Each sequence is a periodic field of a few waves that travel at a speed of the sequence's own and fade; a single frame does not tell that speed, the
-frames before it do.  A frame u[N] goes through the Fourier layer of real fields (fno1d_real) and is sampled at a few points; queries, keys, values and
+frames before it do.  A frame u[N] goes through the Fourier layer of real fields (fno1d_real, with fixed random modes) and is sampled at a few points; queries, keys, values and
 the two gates are linear in that, queries and keys are normalised and rotated (head_norm_rope), the rule (gated_delta_rule) mixes along time, and a
 linear map gives the next frame's change.  Training runs whole sequences forward and backward; the rollout reads the first frames at once, keeps the
 state and goes on token by token (gated_delta_rule_step) on its own predictions.  The maps and the optimiser are PyTorch's, the rest is the library's.

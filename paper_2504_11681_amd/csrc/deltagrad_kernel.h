@@ -23,7 +23,7 @@ template <class E, int KB>
 struct BackwardLds : ScanLds<DeltaUnits<E, KB>::Q + 1 + 2 * DeltaUnits<E, KB>::TRI * DELTA_PM, DeltaUnits<E, KB>::KEY_TAPE - DeltaUnits<E, KB>::KT> {};
 
 // EFFECTS: what each segment but the first adds to the gradient of the state before it, without anything else.  Bound as the forward walk by the issue of a wave (B 4,
-// T 2048, 16 heads of 128 in BF16: 181 us, 5.7 a chunk); two chunks' K' and Q' do not fit LDS for heads of 128, they come during the chunk.
+// T 2048, 16 heads of 128 in BF16: 185 us, 5.8 a chunk); two chunks' K' and Q' do not fit LDS for heads of 128, they come during the chunk.
 template <class E, int KB, bool EFFECTS>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan_back(DeltaArgs a, DeltaMemory mem, int blocks_per_head)
 {
@@ -266,8 +266,9 @@ struct GradientLds {
 
 // One workgroup for a chunk of a key head.  L / 16 waves take the products of pairs of tokens and bring the states in, as many the products with the states,
 // each for 16 tokens, whose errors and values' gradients they bring in.  What comes is split once for all and left in LDS, a round of 32 columns ahead of its
-// products.  B 4, T 2048, 8 key heads and 16 value heads of 128 in BF16: 212 us for 450 MB, a round 8000 cycles, the products of a SIMD's two waves 3000 of them; the rest is the
-// splits and the loads' issue, which stands still while their queues are full, and some 20000 cycles a workgroup before the first round and after the last, alone on its CU.
+// products.  B 4, T 2048, 8 key heads and 16 value heads of 128 in BF16: 228 us for 580 MB, a round 8000 cycles, the products of a SIMD's two waves 3000 of them; the rest is the
+// splits and the loads' issue, which stands still while their queues are full, some 20000 cycles a workgroup before the first round and after the last, alone on its CU, and
+// some 8000 between two value heads, whose sums of dq and dk pass through memory (14 us of the call).
 // (All of it in every wave took 512 registers, so one wave a SIMD, and waited for memory in every round: 338 us; all loads and splits in the waves of the
 // states 266; loads one after the other behind all splits 256.)
 template <class E, int KB>

@@ -13,10 +13,10 @@ size_t pad(size_t n) { return (n + 255) / 256 * 256; }
 
 // Segments of a head's chunks that are walked through at once.  They cost: the effect of each is walked through beforehand with Dk more columns, and the
 // states between them are joined one after the other.  So they are for few heads, whose columns leave most of the chip idle, and many chunks.  Measured in
-// us, in segments and in one walk, BF16 unless stated (B, T, heads, Dk = Dv; waves: 16 columns each): forward 1, 16384, 8, 128 (64 waves) 250 and 763, its training 877
-// and 2369; 4, 4096, 8, 64 (128 waves) 102 and 167; 2, 1024, 4, 64 38 and 46; 8, 8192, 8, 64 (256 waves) 342 and 418; with 512 waves 4, 2048, 16, 128 144 and 136,
-// 16, 2048, 8, 64 142 and 133.  More segments than 1024 waves lose (the first one: 335 with 2048, 306 with 512).  Below some chunks they do too: 1, 512, 8, 128
-// 46 and 36, float32 8, 1000, 8, 64 83 and 80.  In chunks, two walks, slower where more than two waves a CU share it, and the joins make the estimate below.
+// us, in segments and in one walk, BF16 unless stated (B, T, heads, Dk = Dv; waves: 16 columns each): forward 1, 16384, 8, 128 (64 waves) 244 and 907, its training 830
+// and 2423; 4, 4096, 8, 64 (128 waves) 100 and 191; 2, 1024, 4, 64 38 and 51; 8, 8192, 8, 64 (256 waves) 352 and 480; with 512 waves about the same, 4, 2048, 16, 128 155 and 154,
+// 16, 2048, 8, 64 151 and 156.  More segments than 1024 waves lose, fewer too (the first one: 329 with 2048, 316 with 512).  Below some chunks they do: 1, 512, 8, 128
+// 48 and 40, float32 8, 1000, 8, 64 82 and 79.  In chunks, two walks, slower where more than two waves a CU share it, and the joins make the estimate below.
 int segments_of(const DeltaArgs &a, int chunks)
 {
     const long long waves = (long long)a.B * a.Hv * ((a.Dv + 31) / 32 * 2);
@@ -157,9 +157,9 @@ constexpr long long MOST_THREADS = (1LL << 32) - 1;
 
 // Sequences of a batch that go through preparation and walk before the next ones do, without a tape: what the one leaves for the other then stays in the
 // last-level cache (256 MB), in memory that the next ones use again, instead of passing through HBM.  Whole rounds of workgroups, one a CU, of up to 192 MB; not where
-// one round is more than the cache.  In us, in one piece and in such ones (B, T, heads, Dk = Dv): BF16 256, 1024, 2, 64 243 and 203, 512, 512, 4, 32 383 and 340, float32
-// 64, 512, 8, 64 236 and 196; rounds over 256 MB lose, float32 100, 777, 6, 48 405 and 439, BF16 32, 2048, 16, 64 463 and 473.  Heads over 64 are bound by the walk's
-// instructions and gain nothing: BF16 64, 512, 16, 128 398 and 393, 48, 512, 16, 128 288 and 297.
+// one round is more than the cache.  In us, in one piece and in such ones (B, T, heads, Dk = Dv): BF16 256, 1024, 2, 64 262 and 226, 512, 512, 4, 32 421 and 373, float32
+// 64, 512, 8, 64 237 and 198; rounds over 256 MB gain nothing or lose, BF16 32, 2048, 16, 64 504 and 503, float32 100, 777, 6, 48 412 and 448.  Heads over 64 are bound by the
+// walk's instructions and gain nothing: BF16 64, 512, 16, 128 471 and 477, 48, 512, 16, 128 350 and 358.
 template <class E, int KB>
 int batch_piece(const DeltaArgs &a)
 {

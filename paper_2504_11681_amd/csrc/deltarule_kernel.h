@@ -356,8 +356,8 @@ __device__ __forceinline__ void row_to_lds(const E *p, int n, bool vec, E *to)
 // exp(G_i - G_j) from running sums in powers of two that are sums of two floats: exact differences also after a reset.
 __device__ __forceinline__ float decay_between(float hi_i, float lo_i, float hi_j, float lo_j) { return __builtin_amdgcn_exp2f((hi_i - hi_j) + (lo_i - lo_j)); }
 
-// One workgroup for a chunk of a value head: L / 16 waves.  256 x 1024 tokens of 2 heads of 64 in BF16 without a tape: 100 us in one piece for 54 KiB a chunk, 4.4 TB/s
-// of the 5.1 that a copy reaches, 57 in each of two; its chain of barriers was the bound while its loads came one after the other (130 us).  Nothing passes through LDS
+// One workgroup for a chunk of a value head: L / 16 waves.  256 x 1024 tokens of 2 heads of 64 in BF16 without a tape: 105 us in one piece for 61 KiB a chunk, 4.9 TB/s
+// of the 5.1 that a copy reaches, 60 in each of two; its chain of barriers was the bound while its loads came one after the other (by a quarter).  Nothing passes through LDS
 // that need not: a wave takes the pairs of tokens whose column is in its own tile, and P comes out as an operand block as it is.  The inverse T of the unit lower triangular matrix I + N is found by blocks of 16: each diagonal
 // block by substitution, a column after the other, the blocks below it from T_IJ = -T_II sum_{J<=M<I} N_IM T_MJ, one wave for a block column.
 // Substitution and not the product (I - N)(I + N^2)(I + N^4)..: its powers grow like binomials where keys are alike, and cancel.
@@ -717,12 +717,12 @@ struct ForwardLds : ScanLds<(MODE == SCAN_EFFECTS ? DeltaUnits<E, KB>::Q + Delta
 constexpr int SCAN_WAVES = 4, SCAN_THREADS = 64 * (SCAN_WAVES + 1);       // waves that compute, at most, and one that loads
 
 // A workgroup walks through the chunks of one head, or of one segment of it, with 16 columns of its state a wave, which stay in the wave's registers.
-// One more wave does nothing but bring the next chunk's blocks to LDS (75 cycles of issue each, 79 of them for heads of 128: a wave that
-// computes would lose 3000 cycles to a half of them); K', where two chunks' do not fit, comes while the chunk's first products run.  Blocks are read from LDS
-// one group ahead of their products, a group has several accumulators, and the splits stand between the products: 182 of them are 2900 cycles,
-// a chunk takes 7700 (B 1, T 16384, 8 heads of 128 in 16 segments: 62 us for the outputs, 86 for the effects) and 9050 with a tape (B 4, T 2048, 16 heads of 128:
-// 158 us), bound by one wave's issue; with many heads (256 x 1024 tokens, 2 heads of 64) it moves 70 KiB a chunk, in one piece in 152 us, 3.9 TB/s, in two, whose
-// blocks come from the last-level cache, in 55 us each, 5.2 TB/s.  256 registers a wave, none of them accumulation registers, whose copies would cost as
+// One more wave does nothing but bring the next chunk's blocks to LDS (75 cycles of issue each, 85 of them for heads of 128: a wave that
+// computes would lose 3000 cycles to a half of them); K', where two chunks' do not fit (heads over 64), comes while the chunk's first products run.  Blocks are read from LDS
+// one group ahead of their products, a group has several accumulators, and the splits stand between the products: 216 of them are 3500 cycles or 1.5 us,
+// a chunk takes 4.6 us (B 1, T 16384, 8 heads of 128 in 16 segments: 73 us for the outputs; 86 for the effects) and 6.0 with a tape (B 4, T 2048, 16 heads of 128:
+// 192 us), bound by one wave's issue; with many heads (256 x 1024 tokens, 2 heads of 64) it moves 77 KiB a chunk, in one piece in 167 us, 3.9 TB/s, in two, whose
+// blocks come from the last-level cache, in 63 us each, 5.1 TB/s.  256 registers a wave, none of them accumulation registers, whose copies would cost as
 // much as the splits.  Effects: columns of B start from zeros, columns of A from the identity, without values.
 template <class E, int KB, int MODE>
 __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_delta_scan(DeltaArgs a, DeltaMemory mem, int blocks_per_head, int segments)
@@ -1035,7 +1035,7 @@ __global__ __launch_bounds__(SCAN_THREADS) __attribute__((amdgpu_waves_per_eu(2,
 // The states before the segments, one after the other: S <- A S + B.  BACK: the gradients of the states after them, from the last one:
 // dS <- A' dS + b.  A workgroup takes four tiles of columns of a head, two waves a tile, each with half of the state's rows: the waves split A
 // and their part of the state for all of them in LDS, and fetch the next segment's A and B meanwhile.  Each segment waits for the one before: 16 segments of 8 heads of
-// 128 take 74 us (with one wave a tile and nothing fetched ahead the whole call took 157 us more).
+// 128 take 73 us (with one wave a tile and nothing fetched ahead the whole call took 157 us more).
 constexpr int JOIN_TILES = 4, JOIN_THREADS = 512;
 template <int KB>
 struct JoinLds { static constexpr int DT = 2 * KB, A = DT * KB * DELTA_PM, BYTES = (A + JOIN_TILES * KB * DELTA_PM) * 1024; };
