@@ -310,6 +310,13 @@ def test_segments_that_forget_all_or_nothing(tfno, dtype):
     check_both(tfno, x, f"[case] segments at the gates' ends {dtype}")
 
 
+def test_more_sequences_without_tokens_than_one_launch_takes(tfno):
+    """2^25 walks of 192 threads: they go in pieces.  Every final state is the initial one."""
+    x = inputs(F32, 2 ** 25, 0, 1, 1, 1, 1, seed=7)
+    say("[case] 2^25 sequences of no tokens")
+    assert torch.equal(forward(tfno, x)[1], x["initial"])
+
+
 def test_no_tokens_at_all(tfno):
     x = inputs(F32, 3, 0, 2, 2, 16, 16, seed=7)
     tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
