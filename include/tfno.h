@@ -369,7 +369,7 @@ size_t tfno_head_norm_rope_workspace_bytes(int D);
  * there what the backward call needs, else it needs tfno_gated_delta_rule_workspace_bytes(d, 0) bytes of workspace.
  *
  * The backward call takes the same inputs, the tape (which it only reads), the gradient d_o of o and d_final of final (NULL: zeros), and gives the
- * gradients of q, k, v, beta and, where not NULL, of g and initial.  Value heads that share a key head add up in dq and dk.  It needs
+ * gradients of q, k, v, beta and, where not NULL, of g (0 where exp(g) is) and initial.  Value heads that share a key head add up in dq and dk.  It needs
  * tfno_gated_delta_rule_workspace_bytes(d, 1) bytes of workspace.
  *
  * Sizes: B >= 0, T >= 0, Hk, Hv, Dk, Dv >= 1, a launch's threads (up to 1280 a head, 256 a chunk of 64 and head) less than 2^32 (TFNO_ERR_SHAPE), Dk <= 128, Dv <= 256, and tokens of v, o and their gradients less than 2^24

@@ -10,7 +10,7 @@
 //   dq = e^G (dO S') + (M . D beta) K,
 //   dk = -e^G (Y S') + e^(GL-G) beta (E dS'') + (M . D beta)' Q - (W + W') K,   W = strict(M . C beta),
 //   dG_i = sum_j X_ij beta_j - beta_i sum_j X_ji + q_i e^G (dO S')_i - k_i e^G (Y S')_i - c_i,   c_i = e^(GL-G_i) beta_i k_i (dS' E_i),
-//   dG_L += sum c + e^GL <S, dS'>,   dg = sum of dG from the token on.
+//   dG_L += sum c + e^GL <S, dS'>,   dg = sum of dG from the token on, up to the next decay of 0 (whose own dg is 0).
 //
 // Value heads that share a key head are summed by the workgroup of that key head, in their order.
 #pragma once
@@ -449,10 +449,15 @@ __global__ __launch_bounds__((8 * DeltaKind<E>::L)) __attribute__((amdgpu_waves_
                 float dG = lane < L ? row_sums[tok] - beta[tok] * column + token_g[tok] - c : 0.0f;
                 const float sum = group_sum(c, 64);
                 if (lane == L - 1) dG += sum + whole * all;
+                // Sums from each token on.  A decay of 0 ends them: what comes from there on adds up to nothing, and would leave its rounding with the tokens before it.
+                const float factor = lane > 0 ? decay_between(hi[tok], lo[tok], hi[lane < L ? lane - 1 : 0], lo[lane < L ? lane - 1 : 0]) : __builtin_amdgcn_exp2f(hi[0] + lo[0]);
+                const unsigned long long resets = __ballot(lane < L && factor == 0.0f), behind_it = lane < 63 ? resets >> (lane + 1) : 0;
+                const int end = behind_it ? lane + 1 + __builtin_ctzll(behind_it) : 64;
                 for (int step = 1; step < 64; step <<= 1) {
                     const float u = __shfl_down(dG, step, 64);
-                    if (lane + step < 64) dG += u;
+                    if (lane + step < end) dG += u;
                 }
+                if (resets >> lane & 1) dG = 0.0f;
                 const int t = t0 + lane;
                 if (lane < L && t < a.T) {
                     const bool live = t < len;

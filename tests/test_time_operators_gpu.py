@@ -153,6 +153,30 @@ def test_gates_at_their_ends(tfno, dtype):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("T, resets", [(128, (40,)), (200, (0, 3, 63, 64, 100, 101)), (700, (31, 32, 333, 640))])
+def test_gradients_before_a_reset_do_not_see_what_follows(tfno, dtype, T, resets):
+    """Sequences one after the other in one, each forgotten where the next begins, and the last one with 1e4 times the values and gradients: those of the ones before are as near as
+    theirs alone.  The decay of a reset is 0, and so is its gradient."""
+    x = inputs(dtype, 2, T, 1, 2, 64, 48, seed=24)
+    for r in resets:
+        x["g"][:, r] = float("-inf")
+    for n in ("v", "d_o"):
+        x[n][:, resets[-1]:] *= 1e4
+    x["d_final"] *= 1e4
+    say(f"[case] before a reset {dtype} {T} {resets}")
+    tape = tfno.gated_delta_rule_tape(x["q"], x["v"])
+    forward(tfno, x, tape)
+    d = backward(tfno, x, tape)
+    w = dict(zip(("o", "final", "q", "k", "v", "g", "beta", "initial"), want(x, True)))
+    edges = [0, *resets, T]
+    for first, last in zip(edges, edges[1:]):
+        for n in ("q", "k", "v", "g", "beta"):
+            if last > first:
+                near(f"d{n} of {first} .. {last - 1}", d[n][:, first:last], w[n][:, first:last], oracle.REL_GATES if n in ("g", "beta") else oracle.REL[dtype])
+    assert (d["g"][:, list(resets)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 def test_no_decay(tfno, dtype):
     x = inputs(dtype, 2, 130, 1, 2, 32, 32, seed=4)
     x["g"] = None
