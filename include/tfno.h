@@ -302,9 +302,10 @@ tfno_status tfno_spectral_conv1d_auto(const void *x, const void *W, void *y,
 /*
  * Operators along time
  * --------------------
- * The layers above mix a field over the whole transformed axis.  The two operators below mix a trajectory of fields causally along
+ * The layers above mix a field over the whole transformed axis.  Operators below mix a trajectory of fields causally along
  * time and can be advanced by one frame at constant cost: the gated delta rule, a matrix-valued state per head that each token
- * corrects, and the norm of its queries and keys with the rotation by position.
+ * corrects, with the norm of its queries and keys and the rotation by position, and the gated linear recurrence, a state per channel.  With them come the norms, gate and residual
+ * between two such blocks, and the clipping of gradients by their norm, which training needs.
  *
  *  - Tensors are [batch, token, head, value] with the last axis contiguous and the other strides given, in elements and not negative; inputs
  *    may repeat elements (stride 0), outputs may not.  So slices of one fused projection are taken as they are.
@@ -401,6 +402,109 @@ size_t tfno_gated_delta_rule_workspace_bytes(const tfno_delta_rule_desc *d, int 
  */
 tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void *q, const void *k, const void *v, const float *g,
                                        const float *beta, float *states, const int *slots, int pool, void *o, void *stream);
+
+/*
+ * Gated linear recurrence: a state for each channel, which each token lets decay and adds to,
+ *
+ *   h = exp(l) h + u,    y = h,    l = -rate sigmoid(gate), or gate itself where rate is NULL,
+ *   u = x, times sigmoid(input_gate) where that is not NULL, times sqrt(1 - exp(2 l)) where `normalise` is set
+ *
+ * with x, gate, input_gate, y [B, T, C], rate float32 [C], not negative, and states float32 [B, C], contiguous; h starts from `initial` (NULL: zeros).
+ * Where exp(l) is 0 in float32 (l = -inf, say) the state is forgotten, whatever it holds.  l should be 0 or less: above that the state grows, which is right as long as the
+ * growth over any run of tokens is finite, and `normalise` gives NaN.  `lengths` as for the rule above: tokens past them are not read, their outputs
+ * and gradients are zeros.  A NaN or an infinity in a token makes its channel NaN from there to the next decay of 0.
+ *
+ * The whole sequence: y, and the last state into `final` where it is not NULL.  With a tape (tfno_gated_recurrence_tape_bytes bytes, aligned to 256) the call leaves there
+ * the states (float32) that the backward call starts from.  Both need tfno_gated_recurrence_workspace_bytes(d, backward) bytes of workspace, which may be 0.
+ *
+ * The backward call takes the same inputs but for `initial`, the tape (which it only reads), the gradient d_y of y and d_final of final (NULL: zeros), and gives the
+ * gradients of x, gate and, where not NULL, of input_gate (NULL only with input_gate), rate (float32, summed over all tokens) and initial.  Of l = 0 and `normalise`, where the root has no
+ * slope, only what goes through the decay counts.
+ *
+ * Sizes: B, T >= 0, C >= 1, T <= 2^30, B C and B ceil(T / 32) C less than 2^40 (TFNO_ERR_SHAPE).  Strides of heads are not used.
+ */
+typedef struct {
+    int dtype;                    /* tfno_dtype of x, gate, input_gate, y and of their gradients */
+    int B, T, C;
+    int normalise;
+    tfno_strides x, gate, input_gate, y;          /* backward: y is d_y's */
+    tfno_strides dx, dgate, dinput_gate;          /* backward only */
+} tfno_gated_recurrence_desc;
+
+tfno_status tfno_gated_recurrence(const tfno_gated_recurrence_desc *d, const void *x, const void *gate, const void *input_gate, const float *rate,
+                                  const int *lengths, const float *initial, void *y, float *final, void *tape, void *stream);
+tfno_status tfno_gated_recurrence_backward(const tfno_gated_recurrence_desc *d, const void *x, const void *gate, const void *input_gate,
+                                           const float *rate, const int *lengths, const void *tape, const void *d_y, const float *d_final,
+                                           void *dx, void *dgate, void *dinput_gate, float *drate, float *d_initial, void *stream);
+size_t tfno_gated_recurrence_tape_bytes(const tfno_gated_recurrence_desc *d);
+size_t tfno_gated_recurrence_workspace_bytes(const tfno_gated_recurrence_desc *d, int backward);
+
+/*
+ * One token of B sequences: the states [pool, C] (float32, contiguous) are advanced in place, and y is written.  Sequence b has the state slots[b] (int32 [B] on
+ * the device; NULL: b).  A negative slot is a place without a sequence (y = 0), one that the pool does not hold gives NaN; no state is touched for
+ * either.  A slot may not be given twice.  Descriptor and sizes as above with T = 1; strides of tokens are not used.
+ */
+tfno_status tfno_gated_recurrence_step(const tfno_gated_recurrence_desc *d, const void *x, const void *gate, const void *input_gate,
+                                       const float *rate, float *states, const int *slots, int pool, void *y, void *stream);
+
+/*
+ * What stands between two blocks, in one pass over the rows of [B, T, C]: the norm of the first block's output y, its gate, the residual r, and the norm
+ * that the second block begins with:
+ *
+ *   m = y w_after / sqrt(mean_c y^2 + eps), or y itself where `norm_after` is not set (w_after is not read then),
+ *   r_out = residual_scale r + act(gate) m,    n_out = r_out w_before / sqrt(mean_c r_out^2 + eps)
+ *
+ * without the first term where r is NULL, and without the factor where there is no gate (d->gate_kind).  The gate is of y's type with a value for each token
+ * (TFNO_GATE_TOKEN), or float32 and shared by a sequence's tokens ([B, C], TFNO_GATE_SEQUENCE: strides of batch elements) or by all ([C], TFNO_GATE_CHANNEL); act is as
+ * d->activation says, act(z) = z, z sigmoid(z) or sigmoid(z).  Weights are float32 [C] (NULL: ones).  Either result may be NULL, not both; n_out is the norm
+ * of r_out as it is before its rounding.  y and n_out have the type d->dtype; r and r_out have d->residual_dtype, which is dtype or float32.  r_out may be r itself and
+ * n_out y (the same pointer and strides).  Tokens past `lengths` (int32 [B] or NULL) are not read, and count in no sum; results and gradients there are zeros.
+ *
+ * The backward call takes the same inputs and the gradients d_r_out and d_n_out of the results (NULL: zeros, not both), and gives dy and, where not NULL, dr, dgate (as the
+ * gate: of y's type, or float32 and contiguous, summed over the tokens that share it), dw_after and dw_before (float32 [C]).  Where it sums over
+ * tokens (dw_after, dw_before, dgate of a shared gate) it needs tfno_block_norm_workspace_bytes bytes of workspace.  dr may be d_r_out itself and dy d_n_out.
+ *
+ * Sizes: B, T >= 0, B T < 2^31, C >= 1, eps > 0, no dw_after without norm_after (TFNO_ERR_SHAPE), C <= 8192 (else TFNO_ERR_UNSUPPORTED).  Strides of heads are not used.
+ */
+typedef enum { TFNO_GATE_NONE = 0, TFNO_GATE_TOKEN = 1, TFNO_GATE_SEQUENCE = 2, TFNO_GATE_CHANNEL = 3 } tfno_gate;
+typedef enum { TFNO_ACTIVATION_NONE = 0, TFNO_ACTIVATION_SILU = 1, TFNO_ACTIVATION_SIGMOID = 2 } tfno_activation;
+
+typedef struct {
+    int dtype, residual_dtype;    /* tfno_dtype */
+    int B, T, C;
+    int gate_kind, activation;    /* tfno_gate, tfno_activation */
+    int norm_after;
+    float residual_scale, eps;
+    tfno_strides y, r, gate, r_out, n_out;        /* backward: r_out and n_out are their gradients' */
+    tfno_strides dy, dr, dgate;                   /* backward only */
+} tfno_block_norm_desc;
+
+tfno_status tfno_block_norm(const tfno_block_norm_desc *d, const void *y, const void *r, const void *gate, const float *w_after,
+                            const float *w_before, const int *lengths, void *r_out, void *n_out, void *stream);
+tfno_status tfno_block_norm_backward(const tfno_block_norm_desc *d, const void *y, const void *r, const void *gate, const float *w_after,
+                                     const float *w_before, const int *lengths, const void *d_r_out, const void *d_n_out, void *dy,
+                                     void *dr, void *dgate, float *dw_after, float *dw_before, void *stream);
+size_t tfno_block_norm_workspace_bytes(const tfno_block_norm_desc *d);
+
+/*
+ * The norm over all elements of many tensors (of gradients, say), and the clipping to it:
+ *
+ *   norm = sqrt(sum x^2),    x <- x limit / norm where norm > limit
+ *
+ * in place, with squares and the scale in float64.  norm is a float32 on the device (NULL: not wanted).  limit = INFINITY gives the norm alone.  A norm that is NaN or
+ * infinite leaves the tensors as they are.  Tensors are contiguous, float32 or BF16, each its own memory (TFNO_ERR_ALIAS); the array
+ * is read during the call alone.  Two launches for every 128 tensors; tfno_clip_grad_norm_workspace_bytes(count) bytes of workspace.
+ *
+ * Sizes: count >= 0, 0 <= elements < 2^40, limit >= 0 (TFNO_ERR_SHAPE).
+ */
+typedef struct {
+    void *data;
+    long long elements;
+    int dtype;                    /* tfno_dtype */
+} tfno_tensor;
+
+tfno_status tfno_clip_grad_norm(const tfno_tensor *tensors, int count, double limit, float *norm, void *stream);
+size_t tfno_clip_grad_norm_workspace_bytes(int count);
 
 /*
  * Workspace (device memory for intermediates) that an entry point needs for a

@@ -48,6 +48,16 @@ EXPORTS = (
     "tfno_gated_delta_rule_tape_bytes",
     "tfno_gated_delta_rule_workspace_bytes",
     "tfno_gated_delta_rule_step",
+    "tfno_gated_recurrence",
+    "tfno_gated_recurrence_backward",
+    "tfno_gated_recurrence_tape_bytes",
+    "tfno_gated_recurrence_workspace_bytes",
+    "tfno_gated_recurrence_step",
+    "tfno_block_norm",
+    "tfno_block_norm_backward",
+    "tfno_block_norm_workspace_bytes",
+    "tfno_clip_grad_norm",
+    "tfno_clip_grad_norm_workspace_bytes",
 )
 
 CONV_EXPORTS = EXPORTS[:8]   # the entry points with the (x, W, y, B, C_in, C_out, N, K, stream) signature
@@ -126,6 +136,21 @@ class _DeltaRuleDesc(ctypes.Structure):
                 [(n, _Strides) for n in ("q", "k", "v", "o", "g", "beta", "dq", "dk", "dv", "dg", "dbeta")])
 
 
+class _RecurrenceDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "B", "T", "C", "normalise")] +
+                [(n, _Strides) for n in ("x", "gate", "input_gate", "y", "dx", "dgate", "dinput_gate")])
+
+
+class _BlockNormDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int) for n in ("dtype", "residual_dtype", "B", "T", "C", "gate_kind", "activation", "norm_after")] +
+                [("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)] +
+                [(n, _Strides) for n in ("y", "r", "gate", "r_out", "n_out", "dy", "dr", "dgate")])
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("elements", ctypes.c_longlong), ("dtype", ctypes.c_int)]
+
+
 class TfnoError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -181,6 +206,20 @@ def lib() -> ctypes.CDLL:
         L.tfno_gated_delta_rule_tape_bytes.argtypes = [vp]
         L.tfno_gated_delta_rule_workspace_bytes.restype = ctypes.c_size_t
         L.tfno_gated_delta_rule_workspace_bytes.argtypes = [vp, ci]
+        for name, pointers in (("tfno_gated_recurrence", 9), ("tfno_gated_recurrence_backward", 13), ("tfno_block_norm", 8),
+                               ("tfno_block_norm_backward", 13)):
+            fn = getattr(L, name)
+            fn.restype = ci
+            fn.argtypes = [vp] * (pointers + 2)      # the descriptor before them, the stream after
+        L.tfno_gated_recurrence_step.restype = ci
+        L.tfno_gated_recurrence_step.argtypes = [vp] * 7 + [ci, vp, vp]
+        L.tfno_clip_grad_norm.restype = ci
+        L.tfno_clip_grad_norm.argtypes = [vp, ci, ctypes.c_double, vp, vp]
+        for name, arguments in (("tfno_gated_recurrence_tape_bytes", [vp]), ("tfno_gated_recurrence_workspace_bytes", [vp, ci]),
+                                ("tfno_block_norm_workspace_bytes", [vp]), ("tfno_clip_grad_norm_workspace_bytes", [ci])):
+            fn = getattr(L, name)
+            fn.restype = ctypes.c_size_t
+            fn.argtypes = arguments
         _lib = L
     return _lib
 
@@ -441,19 +480,19 @@ def _plan(key, make, tensors, *args):
     return plan
 
 
-def _element_type(dtype) -> int:
+def _element_type(dtype, what="q, k and v") -> int:
     torch = _torch or _load_torch()
     if dtype is torch.bfloat16:
         return 1
     if dtype is torch.float32:
         return 0
-    raise TypeError("q, k and v must be float32 or bfloat16")
+    raise TypeError(f"{what} must be float32 or bfloat16")
 
 
-def _check_types(first, same, f32=(), i32=(), u8=()):
+def _check_types(first, same, f32=(), i32=(), u8=(), what="q"):
     """Device tensors on one device: `same` of the type of the first one, the others of the types named; each given as (name, _of(tensor))."""
     torch = _torch or _load_torch()
-    _element_type(first[0])
+    _element_type(first[0], "q, k and v" if what == "q" else what)
     for dtype, tensors in ((first[0], same), (torch.float32, f32), (torch.int32, i32), (torch.uint8, u8)):
         for name, t in tensors:
             if t is None:
@@ -461,7 +500,7 @@ def _check_types(first, same, f32=(), i32=(), u8=()):
             if t[0] is not dtype:
                 raise TypeError(f"{name} must be {dtype}")
             if t[1] < 0 or t[1] != first[1]:
-                raise TypeError(f"{name} must be a tensor on the device of q")
+                raise TypeError(f"{name} must be a tensor on the device of {what}")
 
 
 def _strides4(name, t, shape):
@@ -644,3 +683,208 @@ def gated_delta_rule_step(q, k, v, g, beta, states, o, slots=None, scale=None, s
     if st != OK:
         raise TfnoError(st, "tfno_gated_delta_rule_step")
     return o
+
+
+def _strides3(name, t, shape):
+    """Strides of a [B, T, C] tensor with its last axis contiguous."""
+    if tuple(t[2]) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t[2])}")
+    if shape[2] > 1 and t[3][2] != 1:
+        raise ValueError(f"the last axis of {name} must be contiguous")
+    return _Strides(t[3][0], t[3][1], 0)
+
+
+def _recurrence_plan(x, gate, input_gate, rate, y, dx, dgate, dinput_gate, drate, lengths, tape, initial, final, other, normalise):
+    names = (("x", x), ("gate", gate), ("input_gate", input_gate), ("y", y), ("dx", dx), ("dgate", dgate), ("dinput_gate", dinput_gate))
+    states = (("the initial state", initial), ("the final state or its gradient", final), ("the gradient of the initial state", other))
+    _check_types(x, names, f32=(("rate", rate), ("drate", drate)) + states, i32=(("lengths", lengths),), u8=(("the tape", tape),), what="x")
+    if len(x[2]) != 3:
+        raise ValueError("x must be [B, T, C]")
+    B, T, C = x[2]
+    d = _RecurrenceDesc(_element_type(x[0], "x"), B, T, C, normalise)
+    for name, t in names:
+        if t is not None:
+            setattr(d, name, _strides3(name, t, (B, T, C)))
+    _check_contiguous((C,), ("rate", rate), ("drate", drate))
+    _check_contiguous((B, C), *states)
+    _check_contiguous((B,), ("lengths", lengths))
+    at = ctypes.addressof(d)
+    need = _entry("tfno_gated_recurrence_tape_bytes")(at)
+    if tape is not None and (len(tape[2]) != 1 or (tape[2][0] > 1 and tape[3][0] != 1) or tape[2][0] < need):
+        raise ValueError(f"the tape must be contiguous and hold {need} bytes")
+    ask = _entry("tfno_gated_recurrence_workspace_bytes")
+    return at, need, ask(at, 0), ask(at, 1), x[1], d
+
+
+def gated_recurrence_tape(x):
+    """A tape for gated_recurrence and gated_recurrence_backward on tensors of the sizes of x [B, T, C]."""
+    torch = _torch or _load_torch()
+    m = _marshal or _load_marshal()
+    key = ("recurrence tape", m.key(x))
+    plan = _plans.get(key) or _plan(key, _recurrence_plan, (x, *(None,) * 13), False)
+    return torch.empty(plan[1], dtype=torch.uint8, device=x.device)
+
+
+def gated_recurrence(x, gate, input_gate, rate, y, normalise: bool = False, initial_state=None, final_state=None, lengths=None, tape=None, stream=None):
+    """The gated linear recurrence h = exp(l) h + u, y = h, over whole sequences: x, gate, input_gate, y [B, T, C] (float32 or bfloat16, any strides with the last axis
+    contiguous).  l = -rate sigmoid(gate) with rate float32 [C], or gate itself where rate is None; u = x, times sigmoid(input_gate) where that is not None, times
+    sqrt(1 - exp(2 l)) with `normalise`.  States are float32 [B, C], lengths int32 [B].  With a tape (gated_recurrence_tape) the gradient can be taken afterwards."""
+    m = _marshal or _load_marshal()
+    tensors = (x, gate, input_gate, rate, y, None, None, None, None, lengths, tape, initial_state, final_state, None)
+    key = ("recurrence", m.key(*tensors), normalise := bool(normalise))
+    plan = _plans.get(key) or _plan(key, _recurrence_plan, tensors, normalise)
+    ensure_workspace(plan[2], x.device)
+    st = m.tfno_gated_recurrence(plan[0], x, gate, input_gate, rate, lengths, initial_state, y, final_state, tape, _raw_stream(plan[4]) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_gated_recurrence")
+    return y
+
+
+def gated_recurrence_backward(x, gate, input_gate, rate, d_y, dx, dgate, dinput_gate, drate, tape, normalise: bool = False, d_final_state=None,
+                              d_initial_state=None, lengths=None, stream=None):
+    """Gradients of gated_recurrence with the same inputs, from its tape and the gradients d_y of y and d_final_state of the final state (None: zeros).  drate (float32
+    [C], summed over all tokens) and d_initial_state may be None."""
+    m = _marshal or _load_marshal()
+    tensors = (x, gate, input_gate, rate, d_y, dx, dgate, dinput_gate, drate, lengths, tape, None, d_final_state, d_initial_state)
+    key = ("recurrence", m.key(*tensors), normalise := bool(normalise))
+    plan = _plans.get(key) or _plan(key, _recurrence_plan, tensors, normalise)
+    ensure_workspace(plan[3], x.device)
+    st = m.tfno_gated_recurrence_backward(plan[0], x, gate, input_gate, rate, lengths, tape, d_y, d_final_state, dx, dgate, dinput_gate, drate, d_initial_state,
+                                          _raw_stream(plan[4]) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_gated_recurrence_backward")
+    return dx, dgate, dinput_gate, drate
+
+
+def _recurrence_step_plan(x, gate, input_gate, rate, y, states, slots, normalise):
+    names = (("x", x), ("gate", gate), ("input_gate", input_gate), ("y", y))
+    _check_types(x, names, f32=(("rate", rate), ("states", states)), i32=(("slots", slots),), what="x")
+    if len(x[2]) != 2:
+        raise ValueError("x must be [B, C]")
+    B, C = x[2]
+    if len(states[2]) != 2:
+        raise ValueError("states must be [pool, C]")
+    d = _RecurrenceDesc(_element_type(x[0], "x"), B, 1, C, normalise)
+    for name, t in names:
+        if t is not None:
+            if len(t[2]) != 2:
+                raise ValueError(f"{name} must be {[B, C]}, not {list(t[2])}")
+            setattr(d, name, _strides3(name, (t[0], t[1], (t[2][0], 1, t[2][1]), (t[3][0], 0, t[3][1])), (B, 1, C)))
+    _check_contiguous((C,), ("rate", rate))
+    _check_contiguous((states[2][0], C), ("states", states))
+    _check_contiguous((B,), ("slots", slots))
+    return ctypes.addressof(d), x[1], d
+
+
+def gated_recurrence_step(x, gate, input_gate, rate, states, y, normalise: bool = False, slots=None, stream=None):
+    """One token of the gated linear recurrence: x, gate, input_gate, y [B, C]; the states float32 [pool, C] of the slots int32 [B] (None: 0 .. B - 1;
+    negative: no sequence) are advanced in place."""
+    m = _marshal or _load_marshal()
+    tensors = (x, gate, input_gate, rate, y, states, slots)
+    key = ("recurrence step", m.key(*tensors), normalise := bool(normalise))
+    plan = _plans.get(key) or _plan(key, _recurrence_step_plan, tensors, normalise)
+    st = m.tfno_gated_recurrence_step(plan[0], x, gate, input_gate, rate, states, slots, states.size(0), y, _raw_stream(plan[1]) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_gated_recurrence_step")
+    return y
+
+
+# ---------------------------------------------------------------- between two blocks
+
+_ACTIVATIONS = {"none": 0, "silu": 1, "sigmoid": 2}
+
+
+def _block_norm_ways(norm_after, activation, residual_scale, eps):
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {list(_ACTIVATIONS)}")
+    return bool(norm_after), _ACTIVATIONS[activation], float(residual_scale), float(eps)
+
+
+def _block_norm_plan(y, r, gate, w_after, w_before, r_out, n_out, dy, dr, dgate, dw_after, dw_before, lengths, norm_after, activation, residual_scale, eps):
+    torch = _torch or _load_torch()
+    if len(y[2]) != 3:
+        raise ValueError("y must be [B, T, C]")
+    B, T, C = y[2]
+    kind = 0 if gate is None else {3: 1, 2: 2, 1: 3}.get(len(gate[2]), -1)
+    if kind < 0:
+        raise ValueError("gate must be [B, T, C], [B, C] or [C]")
+    gates, weights = (("gate", gate), ("dgate", dgate)), (("w_after", w_after), ("w_before", w_before), ("dw_after", dw_after), ("dw_before", dw_before))
+    _check_types(y, (("y", y), ("n_out", n_out), ("dy", dy)) + (gates if kind == 1 else ()), f32=weights + (gates if kind != 1 else ()),
+                 i32=(("lengths", lengths),), what="y")
+    residuals = (("r", r), ("r_out", r_out), ("dr", dr))
+    residual = next((t for _, t in residuals if t is not None), y)
+    if residual[0] is not y[0] and residual[0] is not torch.float32:
+        raise TypeError(f"r must be {y[0]} or float32")
+    _check_types(residual, residuals, what="y")
+    if residual[1] != y[1]:
+        raise TypeError("r and r_out must be tensors on the device of y")
+    d = _BlockNormDesc(_element_type(y[0], "y"), _element_type(residual[0], "r"), B, T, C, kind, activation, norm_after, residual_scale, eps)
+    for name, t in (("y", y), ("n_out", n_out), ("dy", dy)) + residuals + (gates if kind == 1 else ()):
+        if t is not None:
+            setattr(d, name, _strides3(name, t, (B, T, C)))
+    if kind == 2:
+        if tuple(gate[2]) != (B, C) or (C > 1 and gate[3][1] != 1):
+            raise ValueError("the gate of sequences must be [B, C] with contiguous rows")
+        d.gate = _Strides(gate[3][0], 0, 0)
+        _check_contiguous((B, C), ("dgate", dgate))
+        d.dgate = _Strides(C, 0, 0)
+    elif kind != 1:
+        _check_contiguous((C,), *gates)
+    _check_contiguous((C,), *weights)
+    _check_contiguous((B,), ("lengths", lengths))
+    at = ctypes.addressof(d)
+    sums = dw_after is not None or dw_before is not None or (dgate is not None and kind != 1)
+    return at, _entry("tfno_block_norm_workspace_bytes")(at) if sums else 0, y[1], d
+
+
+def block_norm(y, r, gate, w_after, w_before, r_out, n_out, norm_after: bool = True, activation="none", residual_scale: float = 1.0, eps: float = 1e-6,
+               lengths=None, stream=None):
+    """What stands between two blocks, in one pass: r_out = residual_scale r + act(gate) Norm(y) w_after and n_out = Norm(r_out) w_before, where
+    Norm(x) = x / sqrt(mean x^2 + eps).  y, n_out [B, T, C] float32 or bfloat16, r and r_out of that type or float32, any strides with the last axis contiguous; gate [B, T, C]
+    of y's type, or float32 [B, C] or [C], or None; activation "none", "silu" or "sigmoid"; weights float32 [C] or None (ones).  Without norm_after y goes in as it
+    is; r, and either result, may be None.  r_out may be r and n_out y."""
+    m = _marshal or _load_marshal()
+    tensors = (y, r, gate, w_after, w_before, r_out, n_out, None, None, None, None, None, lengths)
+    ways = _block_norm_ways(norm_after, activation, residual_scale, eps)
+    key = ("block norm", m.key(*tensors), ways)
+    plan = _plans.get(key) or _plan(key, _block_norm_plan, tensors, *ways)
+    st = m.tfno_block_norm(plan[0], y, r, gate, w_after, w_before, lengths, r_out, n_out, _raw_stream(plan[2]) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_block_norm")
+    return r_out, n_out
+
+
+def block_norm_backward(y, r, gate, w_after, w_before, d_r_out, d_n_out, dy, dr, dgate, dw_after, dw_before, norm_after: bool = True, activation="none",
+                        residual_scale: float = 1.0, eps: float = 1e-6, lengths=None, stream=None):
+    """Gradients of block_norm with the same inputs from those of its results, d_r_out and d_n_out (None: zeros).  dr, dgate, dw_after and dw_before may be None; a
+    gradient of weights or of a gate that tokens share is float32 and summed over them.  dr may be d_r_out and dy d_n_out."""
+    m = _marshal or _load_marshal()
+    tensors = (y, r, gate, w_after, w_before, d_r_out, d_n_out, dy, dr, dgate, dw_after, dw_before, lengths)
+    ways = _block_norm_ways(norm_after, activation, residual_scale, eps)
+    key = ("block norm", m.key(*tensors), ways)
+    plan = _plans.get(key) or _plan(key, _block_norm_plan, tensors, *ways)
+    ensure_workspace(plan[1], y.device)
+    st = m.tfno_block_norm_backward(plan[0], y, r, gate, w_after, w_before, lengths, d_r_out, d_n_out, dy, dr, dgate, dw_after, dw_before,
+                                    _raw_stream(plan[2]) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_block_norm_backward")
+    return dy, dr, dgate, dw_after, dw_before
+
+
+# ---------------------------------------------------------------- gradients
+
+def clip_grad_norm(gradients, limit: float, norm=None, stream=None):
+    """Scales the gradients (float32, bfloat16 or complex64 tensors on one device, each filling its own memory) in place so that the norm over all their elements is at
+    most `limit`; math.inf gives the norm alone.  norm: one float32 on the device for the norm before that, or None.  Gradients whose norm is not finite stay as they are."""
+    m = _marshal or _load_marshal()
+    gradients = gradients if isinstance(gradients, (list, tuple)) else list(gradients)
+    if not gradients and norm is None:
+        return norm
+    device = (norm if norm is not None else gradients[0]).device
+    if device.type != "cuda":
+        raise TypeError("gradients must be tensors on the device")
+    ensure_workspace(_entry("tfno_clip_grad_norm_workspace_bytes")(len(gradients)), device)
+    st = m.tfno_clip_grad_norm(gradients, limit, norm, device.index, _raw_stream(device.index) if stream is None else stream)
+    if st != OK:
+        raise TfnoError(st, "tfno_clip_grad_norm")
+    return norm

@@ -1,0 +1,311 @@
+// m = Norm(y) w_after,   s = scale r + act(gate) m,   n = Norm(s) w_before,   Norm(x) = x (mean x^2 + eps)^-1/2, for every row in one pass, and its gradient
+//
+//   d = d_s + q (b - s q^2 mean(b s)),   b = d_n w_before,   q = (mean s^2 + eps)^-1/2,
+//   dr = scale d,   dgate = d m act'(gate),   f = d act(gate),   dy = p (f w_after - y p^2 mean(f w_after y)),   p = (mean y^2 + eps)^-1/2,
+//   dw_after = sum f y p,   dw_before = sum d_n s q.
+//
+// Bound by bytes: every row is read once and written once.  A group of lanes (up to a whole workgroup) holds a row in registers, eight or sixteen values a lane;
+// the backward pass makes s again from y, r and the gate instead of reading it back: as many bytes, and s as it was before its rounding.  Sums over
+// tokens (of the weights' gradients, of a gate that tokens share) stay in registers over a group's rows, then a workgroup leaves one row of each in the
+// workspace, which k_column_sums adds up in their order.
+#pragma once
+#include "blocknorm.h"
+
+namespace tfno {
+
+constexpr int BLOCK_NORM_THREADS = 256, BLOCK_NORM_MOST = 512;      // of a workgroup whose rows are narrow, and of one that holds a wide row
+enum { GATE_NONE = 0, GATE_TOKEN = 1, GATE_SEQUENCE = 2, GATE_CHANNEL = 3 };
+enum { ACT_NONE = 0, ACT_SILU = 1, ACT_SIGMOID = 2 };
+
+struct BlockNormShape {
+    int group_log2;                 // threads of a row
+    unsigned outer, outer_stride;   // parts of the batch, and how many are worked on at once
+    int by_group;                   // a part is a group's; else a workgroup's, whose groups share its rows
+    unsigned long long rows;        // of a part
+    unsigned parts;                 // of a sequence (parts are sequences' where a gate is theirs)
+    int whole;                      // a part is a whole sequence: its gate's gradient needs no further sum
+    float *part_after, *part_before, *part_gate;
+};
+
+// Eight values of a thread: neighbours where VEC, else `step` apart.  `count` of them are inside the row.
+template <bool VEC>
+__device__ __forceinline__ void load8(const float *p, int step, int count, float (&v)[8])
+{
+    if constexpr (VEC) {
+        const float4 lo = reinterpret_cast<const float4 *>(p)[0], hi = reinterpret_cast<const float4 *>(p)[1];
+        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? p[i * step] : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const bf16 *p, int step, int count, float (&v)[8])
+{
+    if constexpr (VEC) {
+        const uint4 t = *reinterpret_cast<const uint4 *>(p);
+        const unsigned w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? to_float(p[i * step]) : 0.0f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(float *p, int step, int count, const float (&v)[8])
+{
+    if constexpr (VEC) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) p[i * step] = v[i];
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(bf16 *p, int step, int count, const float (&v)[8])
+{
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) store_element(p + i * step, v[i]);
+    }
+}
+
+// act(z), and its slope.
+__device__ __forceinline__ void activate(int kind, float z, float &value, float &slope)
+{
+    value = z, slope = 1.0f;
+    if (kind == ACT_NONE) return;
+    const float e = expf(-fabsf(z)), big = 1.0f / (1.0f + e), small = e * big;
+    const float s = z < 0.0f ? small : big, rest = z < 0.0f ? big : small;
+    value = kind == ACT_SILU ? z * s : s;
+    slope = kind == ACT_SILU ? fmaf(z * s, rest, s) : s * rest;
+}
+
+// Sums of N values over the threads of a row.  Rows wider than a wave have the workgroup to themselves and meet in LDS, in two buffers by turns.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int group_log2, float (*meet)[2][16], int &turn)
+{
+    const int width = min(1 << group_log2, 64);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = group_sum(v[n], width);
+    if (group_log2 <= 6) return;
+    const int waves = 1 << (group_log2 - 6);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int n = 0; n < N; ++n) meet[turn][n][threadIdx.x >> 6] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        float all = 0.0f;
+        for (int w = 0; w < waves; ++w) all += meet[turn][n][w];
+        v[n] = all;
+    }
+    turn ^= 1;
+}
+
+// A row of one sum over tokens: the groups of a workgroup add up in their order.
+template <bool VEC, int ITER>
+__device__ __forceinline__ void leave(float (&v)[ITER][8], int group_log2, const int (&count)[ITER], const int (&column)[ITER], int step, float *out, float (*meet)[8])
+{
+    const int width = 1 << group_log2;
+    if (width >= (int)blockDim.x) {
+#pragma unroll
+        for (int i = 0; i < ITER; ++i)
+            if (count[i] > 0) store8<false>(out + column[i], VEC ? 1 : step, count[i], v[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) meet[threadIdx.x][e] = v[i][e];
+        __syncthreads();
+        if ((int)threadIdx.x < width && count[i] > 0) {
+            float sum[8] = {};
+            for (int g = threadIdx.x; g < (int)blockDim.x; g += width)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += meet[g][e];
+            store8<false>(out + column[i], VEC ? 1 : step, count[i], sum);
+        }
+    }
+    __syncthreads();
+}
+
+// E: type of y, n and of a token's gate.  R: type of the residual.  A thread has ITER times eight values of a row.
+template <class E, class R, bool VEC, int ITER, bool BACKWARD>
+__global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a, BlockNormShape s)
+{
+    __shared__ float meet[2][2][16];
+    __shared__ float sums[BACKWARD ? BLOCK_NORM_THREADS : 1][8];
+    const int width = 1 << s.group_log2, lane = threadIdx.x & (width - 1), group = threadIdx.x >> s.group_log2, groups = blockDim.x >> s.group_log2;
+    const int step = width;
+    int column[ITER], count[ITER], turn = 0;
+    float wa[ITER][8], wb[ITER][8], gate_c[ITER][8];
+#pragma unroll
+    for (int i = 0; i < ITER; ++i) {
+        column[i] = VEC ? (i * width + lane) * 8 : i * width * 8 + lane;
+        count[i] = VEC ? (column[i] < a.C ? 8 : 0) : max(0, min(8, (a.C - column[i] + step - 1) / step));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = column[i] + (VEC ? e : e * step);
+            const bool in = e < count[i];
+            wa[i][e] = in ? a.w_after && a.norm_after ? a.w_after[c] : 1.0f : 0.0f;
+            wb[i][e] = in ? a.w_before ? a.w_before[c] : 1.0f : 0.0f;
+            gate_c[i][e] = in && a.gate_kind == GATE_CHANNEL ? ((const float *)a.gate)[c] : 0.0f;
+        }
+    }
+    float d_after[ITER][8] = {}, d_before[ITER][8] = {}, d_gate[ITER][8] = {};
+    const float over_C = 1.0f / (float)a.C;
+    const unsigned first = s.by_group ? blockIdx.x * groups + group : blockIdx.x;
+    const unsigned long long row_first = s.by_group ? 0 : group, row_step = s.by_group ? 1 : groups;
+    for (unsigned part = first; part < s.outer; part += s.outer_stride) {
+        for (unsigned long long row = row_first; row < s.rows; row += row_step) {
+            const unsigned long long all = (unsigned long long)part * s.rows + row;
+            unsigned b, t;
+            if (a.gate_kind == GATE_SEQUENCE) {
+                b = part / s.parts;
+                const unsigned long long at = (part - b * s.parts) * s.rows + row;
+                if (at >= (unsigned)a.T) break;
+                t = (unsigned)at;
+            } else {
+                if (all >= (unsigned long long)a.B * a.T) break;
+                b = (unsigned)(all / (unsigned)a.T), t = (unsigned)(all - (unsigned long long)b * a.T);
+            }
+            const bool there = !a.lengths || (int)t < a.lengths[b];
+            float y[ITER][8], r[ITER][8], z[ITER][8], dn[ITER][8], ds[ITER][8];
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[i][e] = r[i][e] = dn[i][e] = ds[i][e] = 0.0f, z[i][e] = gate_c[i][e];
+                if (!there || count[i] == 0) continue;
+                load8<VEC>((const E *)a.y + b * a.sy.batch + t * a.sy.token + column[i], step, count[i], y[i]);
+                if (a.r) load8<VEC>((const R *)a.r + b * a.sr.batch + t * a.sr.token + column[i], step, count[i], r[i]);
+                if (a.gate_kind == GATE_TOKEN) load8<VEC>((const E *)a.gate + b * a.sgate.batch + t * a.sgate.token + column[i], step, count[i], z[i]);
+                if (a.gate_kind == GATE_SEQUENCE) load8<VEC>((const float *)a.gate + b * a.sgate.batch + column[i], step, count[i], z[i]);
+                if constexpr (BACKWARD) {
+                    if (a.d_r_out) load8<VEC>((const R *)a.d_r_out + b * a.sr_out.batch + t * a.sr_out.token + column[i], step, count[i], ds[i]);
+                    if (a.d_n_out) load8<VEC>((const E *)a.d_n_out + b * a.sn_out.batch + t * a.sn_out.token + column[i], step, count[i], dn[i]);
+                }
+            }
+            float p = 1.0f;
+            if (a.norm_after) {
+                float ss[1] = {};
+#pragma unroll
+                for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ss[0] = fmaf(y[i][e], y[i][e], ss[0]);
+                row_sums(ss, s.group_log2, meet, turn);
+                p = 1.0f / sqrtf(fmaf(ss[0], over_C, a.eps));
+            }
+            float st[ITER][8], open[ITER][8], slope[ITER][8], two[2] = {};
+#pragma unroll
+            for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float m = y[i][e] * p * wa[i][e];
+                    open[i][e] = 1.0f, slope[i][e] = 0.0f;
+                    if (a.gate_kind != GATE_NONE) activate(a.activation, z[i][e], open[i][e], slope[i][e]);
+                    st[i][e] = m * open[i][e];
+                    if (a.r) st[i][e] = fmaf(a.residual_scale, r[i][e], st[i][e]);
+                    two[0] = fmaf(st[i][e], st[i][e], two[0]);
+                    if constexpr (BACKWARD) two[1] = fmaf(dn[i][e] * wb[i][e], st[i][e], two[1]);
+                }
+            float q = 0.0f;
+            const bool before = BACKWARD ? a.d_n_out != nullptr : a.n_out != nullptr;
+            if (before) {
+                if constexpr (BACKWARD) {
+                    row_sums(two, s.group_log2, meet, turn);
+                } else {
+                    float one[1] = {two[0]};
+                    row_sums(one, s.group_log2, meet, turn);
+                    two[0] = one[0];
+                }
+                q = 1.0f / sqrtf(fmaf(two[0], over_C, a.eps));
+            }
+            if constexpr (!BACKWARD) {
+#pragma unroll
+                for (int i = 0; i < ITER; ++i) {
+                    if (count[i] == 0) continue;
+                    float n[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        n[e] = there ? st[i][e] * q * wb[i][e] : 0.0f;
+                        st[i][e] = there ? st[i][e] : 0.0f;
+                    }
+                    if (a.r_out) store8<VEC>((R *)a.r_out + b * a.sr_out.batch + t * a.sr_out.token + column[i], step, count[i], st[i]);
+                    if (a.n_out) store8<VEC>((E *)a.n_out + b * a.sn_out.batch + t * a.sn_out.token + column[i], step, count[i], n);
+                }
+            } else {
+                const float back = q * q * q * two[1] * over_C;
+                float dot[1] = {};
+#pragma unroll
+                for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float m = y[i][e] * p * wa[i][e];
+                        float d = ds[i][e];
+                        if (before) {
+                            d += fmaf(q * wb[i][e], dn[i][e], -back * st[i][e]);
+                            d_before[i][e] = fmaf(dn[i][e] * q, st[i][e], d_before[i][e]);
+                        }
+                        const float f = d * open[i][e], dz = d * m * slope[i][e];
+                        d_after[i][e] = fmaf(f * p, y[i][e], d_after[i][e]);
+                        d_gate[i][e] += dz;
+                        slope[i][e] = dz;
+                        r[i][e] = a.residual_scale * d;
+                        z[i][e] = f * wa[i][e];
+                        dot[0] = fmaf(z[i][e], y[i][e], dot[0]);
+                    }
+                float along = 0.0f;
+                if (a.norm_after) {
+                    row_sums(dot, s.group_log2, meet, turn);
+                    along = p * p * p * dot[0] * over_C;
+                }
+#pragma unroll
+                for (int i = 0; i < ITER; ++i) {
+                    if (count[i] == 0) continue;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        y[i][e] = there ? fmaf(p, z[i][e], -along * y[i][e]) : 0.0f;
+                        r[i][e] = there ? r[i][e] : 0.0f;
+                        slope[i][e] = there ? slope[i][e] : 0.0f;
+                    }
+                    store8<VEC>((E *)a.dy + b * a.sdy.batch + t * a.sdy.token + column[i], step, count[i], y[i]);
+                    if (a.dr) store8<VEC>((R *)a.dr + b * a.sdr.batch + t * a.sdr.token + column[i], step, count[i], r[i]);
+                    if (a.dgate && a.gate_kind == GATE_TOKEN)
+                        store8<VEC>((E *)a.dgate + b * a.sdgate.batch + t * a.sdgate.token + column[i], step, count[i], slope[i]);
+                }
+            }
+        }
+        if constexpr (BACKWARD) {
+            if (a.gate_kind == GATE_SEQUENCE && a.dgate) {
+                // one row of the gate's gradient for the part: where it is a whole sequence, that is the gradient
+                float *out = s.whole ? (float *)a.dgate + (long long)part * a.sdgate.batch : s.part_gate + (size_t)part * a.C;
+                if (s.by_group) {
+#pragma unroll
+                    for (int i = 0; i < ITER; ++i)
+                        if (count[i] > 0) store8<false>(out + column[i], VEC ? 1 : step, count[i], d_gate[i]);
+                } else {
+                    leave<VEC>(d_gate, s.group_log2, count, column, step, out, sums);
+                }
+#pragma unroll
+                for (int i = 0; i < ITER; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d_gate[i][e] = 0.0f;
+            }
+        }
+    }
+    if constexpr (BACKWARD) {
+        if (a.dw_after) leave<VEC>(d_after, s.group_log2, count, column, step, s.part_after + (size_t)blockIdx.x * a.C, sums);
+        if (a.dw_before) leave<VEC>(d_before, s.group_log2, count, column, step, s.part_before + (size_t)blockIdx.x * a.C, sums);
+        if (a.dgate && a.gate_kind == GATE_CHANNEL) leave<VEC>(d_gate, s.group_log2, count, column, step, s.part_gate + (size_t)blockIdx.x * a.C, sums);
+    }
+}
+
+}  // namespace tfno

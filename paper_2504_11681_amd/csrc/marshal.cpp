@@ -14,6 +14,7 @@
 #include <tuple>
 #include <type_traits>
 #include <utility>
+#include <vector>
 
 #include "../../include/tfno.h"
 
@@ -27,6 +28,12 @@ struct Library {
     decltype(&tfno_gated_delta_rule) rule;
     decltype(&tfno_gated_delta_rule_backward) rule_backward;
     decltype(&tfno_gated_delta_rule_step) step;
+    decltype(&tfno_gated_recurrence) recurrence;
+    decltype(&tfno_gated_recurrence_backward) recurrence_backward;
+    decltype(&tfno_gated_recurrence_step) recurrence_step;
+    decltype(&tfno_block_norm) block_norm;
+    decltype(&tfno_block_norm_backward) block_norm_backward;
+    decltype(&tfno_clip_grad_norm) clip;
 } library;
 
 // Numbers of any size in few bytes: seven bits in each, the last one below 128.
@@ -110,6 +117,66 @@ PyObject *rule(PyObject *, PyObject *const *args, Py_ssize_t count) { return cal
 PyObject *rule_backward(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.rule_backward, args, count); }
 PyObject *step(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.step, args, count); }
 
+PyObject *recurrence(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.recurrence, args, count); }
+PyObject *recurrence_backward(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.recurrence_backward, args, count); }
+PyObject *recurrence_step(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.recurrence_step, args, count); }
+PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.block_norm, args, count); }
+PyObject *block_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.block_norm_backward, args, count); }
+
+// Tensors of any number as the entry point takes them, and its call: (tensors, limit, norm or None, device, stream).  Here are all checks of the tensors' types and
+// layouts: through Python they took longer than the kernels of a small model.
+PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    if (!library.clip) return PyErr_Format(PyExc_RuntimeError, "the library is not open");
+    if (count != 5) return PyErr_Format(PyExc_TypeError, "5 arguments are expected, not %d", (int)count);
+    const double limit = PyFloat_AsDouble(args[1]);
+    const long device = PyLong_AsLong(args[3]);
+    void *stream = PyLong_AsVoidPtr(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    PyObject *list = PySequence_Fast(args[0], "the tensors must be a sequence");
+    if (!list) return nullptr;
+    PyObject *result = nullptr;
+    try {
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+        PyObject **items = PySequence_Fast_ITEMS(list);
+        std::vector<tfno_tensor> tensors((size_t)n);
+        const char *wrong = nullptr;
+        for (Py_ssize_t i = 0; i < n && !wrong; ++i) {
+            if (!THPVariable_Check(items[i])) {
+                wrong = "gradients must be tensors";
+                break;
+            }
+            const at::Tensor &t = THPVariable_Unpack(items[i]);
+            const at::ScalarType type = t.scalar_type();
+            if (t.layout() != at::kStrided || !t.is_cuda() || t.get_device() != device) wrong = "gradients must be dense tensors on one device";
+            else if (type != at::kFloat && type != at::kBFloat16 && type != at::kComplexFloat) wrong = "gradients must be float32, bfloat16 or complex64";
+            else if (!t.is_non_overlapping_and_dense()) wrong = "gradients must fill their memory, in whatever order of axes";
+            else tensors[i] = {t.numel() ? t.data_ptr() : nullptr, (long long)t.numel() * (type == at::kComplexFloat ? 2 : 1), type == at::kBFloat16 ? TFNO_BF16 : TFNO_F32};
+        }
+        float *norm = nullptr;
+        if (!wrong && args[2] != Py_None) {
+            const bool tensor = THPVariable_Check(args[2]);
+            if (!tensor || THPVariable_Unpack(args[2]).scalar_type() != at::kFloat || THPVariable_Unpack(args[2]).numel() != 1 ||
+                !THPVariable_Unpack(args[2]).is_cuda() || THPVariable_Unpack(args[2]).get_device() != device)
+                wrong = "norm must be one float32 on the device of the gradients";
+            else norm = (float *)THPVariable_Unpack(args[2]).data_ptr();
+        }
+        if (wrong) {
+            PyErr_SetString(PyExc_TypeError, wrong);
+        } else {
+            tfno_status st;
+            Py_BEGIN_ALLOW_THREADS
+            st = library.clip(tensors.data(), (int)n, limit, norm, stream);
+            Py_END_ALLOW_THREADS
+            result = PyLong_FromLong(st);
+        }
+    } catch (const std::exception &e) {       // a tensor without memory, or none on the host
+        PyErr_Format(PyExc_RuntimeError, "%.300s", e.what());
+    }
+    Py_DECREF(list);
+    return result;
+}
+
 PyObject *open_library(PyObject *, PyObject *path)
 {
     const char *name = PyUnicode_AsUTF8(path);
@@ -124,7 +191,9 @@ PyObject *open_library(PyObject *, PyObject *path)
     };
     if (!find(found.norm, "tfno_head_norm_rope") || !find(found.norm_backward, "tfno_head_norm_rope_backward") ||
         !find(found.rule, "tfno_gated_delta_rule") || !find(found.rule_backward, "tfno_gated_delta_rule_backward") ||
-        !find(found.step, "tfno_gated_delta_rule_step"))
+        !find(found.step, "tfno_gated_delta_rule_step") || !find(found.recurrence, "tfno_gated_recurrence") ||
+        !find(found.recurrence_backward, "tfno_gated_recurrence_backward") || !find(found.recurrence_step, "tfno_gated_recurrence_step") ||
+        !find(found.block_norm, "tfno_block_norm") || !find(found.block_norm_backward, "tfno_block_norm_backward") || !find(found.clip, "tfno_clip_grad_norm"))
         return nullptr;
     library = found;
     Py_RETURN_NONE;
@@ -140,6 +209,12 @@ PyMethodDef methods[] = {
     {"tfno_gated_delta_rule", fast(rule), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
     {"tfno_gated_delta_rule_backward", fast(rule_backward), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
     {"tfno_gated_delta_rule_step", fast(step), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_gated_recurrence", fast(recurrence), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_gated_recurrence_backward", fast(recurrence_backward), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_gated_recurrence_step", fast(recurrence_step), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_block_norm", fast(block_norm), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_block_norm_backward", fast(block_norm_backward), METH_FASTCALL, "The entry point; tensors or addresses for its pointers."},
+    {"tfno_clip_grad_norm", fast(clip), METH_FASTCALL, "The entry point for tensors, a limit, the norm's tensor or None, a device and a stream."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
