@@ -21,8 +21,16 @@ tfno_status recurrence_sizes(const tfno_gated_recurrence_desc *d)
 {
     if (!d) return TFNO_ERR_NULL;
     if (!type_ok(d->dtype) || d->B < 0 || d->T < 0 || d->C < 1 || d->T > (1 << 30)) return TFNO_ERR_SHAPE;
-    if ((long double)d->B * std::max(1.0L, ((long double)d->T + 31) / 32) * d->C >= 1099511627776.0L || d->C > (1 << 30)) return TFNO_ERR_SHAPE;
+    if ((long double)d->B * std::max(1.0L, ((long double)d->T + 31) / 32) * d->C >= 1099511627776.0L || d->C > (1 << 28)) return TFNO_ERR_SHAPE;
     return TFNO_OK;
+}
+
+// The kernels reach the tokens of a wave with 32-bit offsets.
+bool tokens_near(int T, std::initializer_list<const tfno_strides *> of)
+{
+    for (const tfno_strides *s : of)
+        if (T > 1 && s->token >= (1 << 23)) return false;
+    return true;
 }
 
 RecurrenceArgs recurrence_args(const tfno_gated_recurrence_desc *d, const void *x, const void *gate, const void *input_gate, const float *rate)
@@ -56,6 +64,7 @@ tfno_status tfno_gated_recurrence(const tfno_gated_recurrence_desc *d, const voi
     if (st != TFNO_OK) return st;
     if (d->B == 0 || (d->T == 0 && !final)) return TFNO_OK;
     if (d->T > 0 && (!x || !gate || !y)) return TFNO_ERR_NULL;
+    if (!tokens_near(d->T, {&d->x, &d->gate, &d->y}) || (input_gate && !tokens_near(d->T, {&d->input_gate}))) return TFNO_ERR_UNSUPPORTED;
     RecurrenceArgs a = recurrence_args(d, x, gate, input_gate, rate);
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.C;
@@ -82,6 +91,8 @@ tfno_status tfno_gated_recurrence_backward(const tfno_gated_recurrence_desc *d, 
     const bool empty = d->B == 0 || d->T == 0;
     if (empty && !drate && (d->B == 0 || !d_initial)) return TFNO_OK;
     if (!empty && (!x || !gate || !tape || !d_y || !dx || !dgate || (!input_gate) != (!dinput_gate) || (drate && !rate))) return TFNO_ERR_NULL;
+    if (!tokens_near(d->T, {&d->x, &d->gate, &d->y, &d->dx, &d->dgate}) || (input_gate && !tokens_near(d->T, {&d->input_gate, &d->dinput_gate})))
+        return TFNO_ERR_UNSUPPORTED;
     RecurrenceArgs a = recurrence_args(d, x, gate, input_gate, rate);
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.C;

@@ -8,37 +8,34 @@ namespace tfno {
 
 namespace {
 
-constexpr int TOKENS = 8;                                   // of a group in a tile
-constexpr unsigned RECURRENCE_LAUNCH = 1u << 23;            // workgroups: a launch takes less than 2^32 threads
+constexpr unsigned RECURRENCE_LAUNCH = 1u << 21;            // workgroups: a launch takes less than 2^32 threads
 
-// Lanes of a group, and segments.
-RecurrenceShape shape_of(int B, int T, int C, int V)
+struct Geometry {
+    RecurrenceShape s;
+    int threads;
+};
+
+// Lanes of a group, threads of a workgroup and segments: whole lines of channels and small workgroups where these fill the chip, else more of a sequence in a workgroup, then half
+// lines, then segments.
+Geometry shape_of(int B, int T, int C, bool bf16, int tokens)
 {
-    RecurrenceShape s{};
-    s.lanes_log2 = 6;
-    const auto blocks = [&] { return (unsigned)((C + (V << s.lanes_log2) - 1) / (V << s.lanes_log2)); };
-    while (s.lanes_log2 > 4 && (long long)B * blocks() < 1024) --s.lanes_log2;
-    s.channel_blocks = blocks();
-    const int tile = (RECURRENCE_THREADS >> s.lanes_log2) * TOKENS;
-    const long long groups = (long long)B * s.channel_blocks, tiles = (T + tile - 1) / tile;
-    const long long wanted = groups < 512 ? std::max(1LL, std::min({1024 / std::max(groups, 1LL), tiles / 2, 64LL})) : 1;
-    s.segment = (int)std::max((tiles + wanted - 1) / wanted, 1LL) * tile;
+    Geometry g{};
+    RecurrenceShape &s = g.s;
+    s.lanes_log2 = 6, g.threads = 256;
+    const auto blocks = [&] { return (long long)B * ((C + (1 << s.lanes_log2) - 1) >> s.lanes_log2); };
+    const auto tile = [&] { return (g.threads >> s.lanes_log2) * tokens; };
+    while (s.lanes_log2 > 5 && C <= 1 << (s.lanes_log2 - 1)) --s.lanes_log2;
+    constexpr long long full = 256 * 1024;       // threads: four waves a SIMD
+    if (blocks() * g.threads < full && tile() < T) g.threads = 512;
+    while (s.lanes_log2 > 5 && blocks() * g.threads < full && tile() < T) --s.lanes_log2;
+    if (blocks() * g.threads < full / 2) g.threads = 256;
+    const long long tiles = (T + tile() - 1) / tile();
+    long long wanted = 1;
+    if (blocks() * g.threads < full / 4) wanted = std::max(1LL, std::min({full / std::max(blocks() * g.threads, 1LL), tiles, 64LL}));
+    s.channel_blocks = (unsigned)((C + (1 << s.lanes_log2) - 1) >> s.lanes_log2);
+    s.segment = (int)std::max((tiles + wanted - 1) / wanted, 1LL) * tile();
     s.segments = std::max(1, (T + s.segment - 1) / s.segment);
-    return s;
-}
-
-bool pairs(const RecurrenceArgs &a, bool backward)
-{
-    const uintptr_t mask = a.bf16 ? 3 : 7;
-    uintptr_t p = (uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.input_gate | (uintptr_t)(backward ? a.dy : a.y);
-    long long s = a.sx.batch | a.sx.token | a.sgate.batch | a.sgate.token | a.sy.batch | a.sy.token;
-    if (a.input_gate) s |= a.sinput.batch | a.sinput.token;
-    if (backward) {
-        p |= (uintptr_t)a.dx | (uintptr_t)a.dgate | (uintptr_t)a.dinput_gate;
-        s |= a.sdx.batch | a.sdx.token | a.sdgate.batch | a.sdgate.token;
-        if (a.input_gate) s |= a.sdinput.batch | a.sdinput.token;
-    }
-    return a.C % 2 == 0 && (p & mask) == 0 && (s & 1) == 0;
+    return g;
 }
 
 template <class F>
@@ -50,26 +47,26 @@ void in_launches(RecurrenceShape s, long long items, F launch)
     }
 }
 
-template <class E, int V>
-hipError_t forward(const RecurrenceArgs &a, hipStream_t st)
+template <class E, bool ALL, int THREADS>
+hipError_t forward(const RecurrenceArgs &a, const RecurrenceShape &s, hipStream_t st)
 {
-    const RecurrenceShape s = shape_of(a.B, a.T, a.C, V);
+    constexpr int S = RECURRENCE_TOKENS;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
     if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, V, TOKENS, false><<<grid, RECURRENCE_THREADS, 0, st>>>(a, p); });
-    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence<E, V, TOKENS><<<grid, RECURRENCE_THREADS, 0, st>>>(a, p); });
+        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, ALL, S, THREADS, false><<<grid, THREADS, 0, st>>>(a, p); });
+    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence<E, ALL, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     return hipGetLastError();
 }
 
-template <class E, int V>
-hipError_t backward(RecurrenceArgs a, hipStream_t st)
+template <class E, bool ALL, int THREADS>
+hipError_t backward(RecurrenceArgs a, const RecurrenceShape &s, hipStream_t st)
 {
-    const RecurrenceShape s = shape_of(a.B, a.T, a.C, V);
+    constexpr int S = RECURRENCE_TOKENS_BACK;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
     a.partial = (float *)(a.effects + (s.segments > 1 ? (size_t)a.B * s.segments * a.C : 0));
     if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, V, TOKENS, true><<<grid, RECURRENCE_THREADS, 0, st>>>(a, p); });
-    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, V, TOKENS><<<grid, RECURRENCE_THREADS, 0, st>>>(a, p); });
+        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, ALL, S, THREADS, true><<<grid, THREADS, 0, st>>>(a, p); });
+    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, ALL, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     if (a.drate) {
         const ColumnSumsArgs<1> sums{{{a.partial, a.drate, (unsigned)a.B * s.segments}}, {0, 1}, a.C};
         k_column_sums<1><<<dim3((a.C + 15) / 16, 1), 1024, 0, st>>>(sums);
@@ -77,9 +74,34 @@ hipError_t backward(RecurrenceArgs a, hipStream_t st)
     return hipGetLastError();
 }
 
+template <class E, bool ALL>
+hipError_t run(const RecurrenceArgs &a, bool back, hipStream_t st)
+{
+    const Geometry g = shape_of(a.B, a.T, a.C, a.bf16, back ? RECURRENCE_TOKENS_BACK : RECURRENCE_TOKENS);
+    if (g.threads == 256) return back ? backward<E, ALL, 256>(a, g.s, st) : forward<E, ALL, 256>(a, g.s, st);
+    return back ? backward<E, ALL, 512>(a, g.s, st) : forward<E, ALL, 512>(a, g.s, st);
+}
+
 constexpr int STEP_THREADS = 256;
 
-// One token: bound by the bytes of states, inputs and outputs, for a single sequence by the launch.
+// One token: bound by the bytes of states, inputs and outputs, for a single sequence by the launch.  A thread takes four neighbouring channels where every address allows it.
+template <class E, int V>
+struct Few;
+template <class E>
+struct Few<E, 4> {
+    Quad<E> at;
+    __device__ __forceinline__ void load(const E *p) { at.load(p); }
+    __device__ __forceinline__ void values(float (&v)[4]) const { at.values(v); }
+    __device__ __forceinline__ static void store(E *p, const float (&v)[4]) { store4(p, v); }
+};
+template <class E>
+struct Few<E, 1> {
+    E at;
+    __device__ __forceinline__ void load(const E *p) { at = *p; }
+    __device__ __forceinline__ void values(float (&v)[1]) const { v[0] = to_float(at); }
+    __device__ __forceinline__ static void store(E *p, const float (&v)[1]) { store_element(p, v[0]); }
+};
+
 template <class E, int V>
 __global__ __launch_bounds__(STEP_THREADS) void k_recurrence_step(RecurrenceArgs a, unsigned first)
 {
@@ -90,25 +112,33 @@ __global__ __launch_bounds__(STEP_THREADS) void k_recurrence_step(RecurrenceArgs
     E *y = (E *)a.y + b * a.sy.batch + c;
     if ((unsigned)slot >= (unsigned)a.pool) {            // no sequence here (zeros), or one that the pool does not hold (NaN)
         float none[V];
+#pragma unroll
         for (int e = 0; e < V; ++e) none[e] = slot < 0 ? 0.0f : __uint_as_float(0x7fc00000u);
-        store_some(y, none);
+        Few<E, V>::store(y, none);
         return;
     }
     float *state = a.states + (long long)slot * a.C + c;
-    Some<E, V> x, gate, input{};
-    Some<float, V> h;
-    x.load((const E *)a.x + b * a.sx.batch + c);
-    gate.load((const E *)a.gate + b * a.sgate.batch + c);
-    if (a.input_gate) input.load((const E *)a.input_gate + b * a.sinput.batch + c);
-    h.load(state);
-    Decay d[V];
-    float rate[V], u[V], out[V], log[V] = {};
-    load_rates(a, c, rate);
-    decay_and_input<E, V>(a, rate, x, gate, input, true, d, u, log);
+    Few<float, V> in_h, in_rate{};
+    Few<E, V> in_x, in_gate, in_input{};
+    in_h.load(state);
+    in_x.load((const E *)a.x + b * a.sx.batch + c);
+    in_gate.load((const E *)a.gate + b * a.sgate.batch + c);
+    if (a.input_gate) in_input.load((const E *)a.input_gate + b * a.sinput.batch + c);
+    if (a.rate) in_rate.load(a.rate + c);
+    float h[V], x[V], gate[V], input[V], rate[V];
+    in_h.values(h), in_x.values(x), in_gate.values(gate), in_input.values(input), in_rate.values(rate);
 #pragma unroll
-    for (int e = 0; e < V; ++e) out[e] = d[e].of(h.value(e), u[e]);
-    store_some(state, out);
-    store_some(y, out);
+    for (int e = 0; e < V; ++e) {
+        float u = x[e], full, less;
+        const float l = log_of(a.rate, rate[e], gate[e]);
+        if (a.input_gate) u *= sigmoid(input[e]);
+        Decay d(l, full, less);
+        if (l < HARDLY) d.hardly(l);
+        if (a.normalise) u *= __builtin_amdgcn_sqrtf(less * (2.0f - less));
+        h[e] = d.of(h[e], u);
+    }
+    Few<float, V>::store(state, h);
+    Few<E, V>::store(y, h);
 }
 
 template <class E, int V>
@@ -120,39 +150,36 @@ hipError_t step(const RecurrenceArgs &a, hipStream_t st)
     return hipGetLastError();
 }
 
+bool fours(const RecurrenceArgs &a)
+{
+    const uintptr_t of_elements = (uintptr_t)a.x | (uintptr_t)a.gate | (uintptr_t)a.input_gate | (uintptr_t)a.y, of_floats = (uintptr_t)a.states | (uintptr_t)a.rate;
+    const long long s = a.sx.batch | a.sgate.batch | (a.input_gate ? a.sinput.batch : 0) | a.sy.batch | a.C;
+    return (of_elements & (a.bf16 ? 7 : 15)) == 0 && (of_floats & 15) == 0 && (s & 3) == 0;
+}
+
 }  // namespace
 
-hipError_t recurrence_launch(const RecurrenceArgs &a, hipStream_t s)
+static hipError_t typed(const RecurrenceArgs &a, bool back, hipStream_t s)
 {
-    const bool two = pairs(a, false);
-    if (a.bf16) return two ? forward<bf16, 2>(a, s) : forward<bf16, 1>(a, s);
-    return two ? forward<float, 2>(a, s) : forward<float, 1>(a, s);
+    const bool all = a.rate && a.input_gate && a.normalise;
+    if (a.bf16) return all ? run<bf16, true>(a, back, s) : run<bf16, false>(a, back, s);
+    return all ? run<float, true>(a, back, s) : run<float, false>(a, back, s);
 }
 
-hipError_t recurrence_backward_launch(const RecurrenceArgs &a, hipStream_t s)
+hipError_t recurrence_launch(const RecurrenceArgs &a, hipStream_t s) { return typed(a, false, s); }
+hipError_t recurrence_backward_launch(const RecurrenceArgs &a, hipStream_t s) { return typed(a, true, s); }
+hipError_t recurrence_step_launch(const RecurrenceArgs &a, hipStream_t s) 
 {
-    const bool two = pairs(a, true);
-    if (a.bf16) return two ? backward<bf16, 2>(a, s) : backward<bf16, 1>(a, s);
-    return two ? backward<float, 2>(a, s) : backward<float, 1>(a, s);
-}
-
-hipError_t recurrence_step_launch(const RecurrenceArgs &a, hipStream_t s)
-{
-    const bool two = pairs(a, false) && ((uintptr_t)a.states & 7) == 0;
-    if (a.bf16) return two ? step<bf16, 2>(a, s) : step<bf16, 1>(a, s);
-    return two ? step<float, 2>(a, s) : step<float, 1>(a, s);
+    if (a.bf16) return fours(a) ? step<bf16, 4>(a, s) : step<bf16, 1>(a, s);
+    return fours(a) ? step<float, 4>(a, s) : step<float, 1>(a, s);
 }
 
 size_t recurrence_tape_bytes(int B, int T, int C) { return 4 * (size_t)B * ((T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) * C; }
 
-size_t recurrence_workspace_bytes(int B, int T, int C, bool, bool backward)
+size_t recurrence_workspace_bytes(int B, int T, int C, bool bf16, bool backward)
 {
-    size_t most = 0;
-    for (int V = 1; V <= 2; ++V) {
-        const size_t maps = (size_t)B * shape_of(B, T, C, V).segments;
-        most = std::max(most, (maps > (size_t)B ? 8 * maps * C : 0) + (backward ? 4 * maps * C : 0));
-    }
-    return most;
+    const size_t maps = (size_t)B * shape_of(B, T, C, bf16, backward ? RECURRENCE_TOKENS_BACK : RECURRENCE_TOKENS).s.segments;
+    return (maps > (size_t)B ? 8 * maps * C : 0) + (backward ? 4 * maps * C : 0);
 }
 
 }  // namespace tfno

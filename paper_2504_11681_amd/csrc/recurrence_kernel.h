@@ -2,50 +2,24 @@
 //
 //   D_t = dy_t + a_{t+1} D_{t+1},   du = D,   dl = D a h_{t-1} - D x sigmoid(input_gate) a^2 / sqrt(1 - a^2).
 //
-// Bound by bytes: every input is read once and every output written once.  A workgroup takes `lanes` neighbouring pairs of channels and walks
-// through a sequence in tiles; a tile is shared out over time among groups of lanes, each with S tokens in a row, whose loads are all under way while the tile
-// before is worked on.  A group makes of its tokens one map h -> a h + B (backward also e -> a e + R for what comes from later tokens), the
-// maps meet in LDS, and each group then walks its tokens from the state that the maps before it give.
-// Sequences too few to fill the chip are cut into segments, whose maps a kernel of its own finds first.
-//
+// Every input is read once and every output written once; the gates of a value are some 60 instructions, five of them of the slow kind (exp2, 1/x, square root), so with BF16
+// both sides are near.  A workgroup takes `lanes` neighbouring channels and walks through a sequence in tiles; a tile is shared out over time among groups of
+// lanes, each with S tokens in a row, whose loads are all under way while the tile before is worked on.  A group makes of its tokens one map h -> a h + B (backward also
+// e -> a e + R for what comes from later tokens); the maps are joined along the wave by shuffles and along the workgroup in LDS, and each group then walks its
+// tokens from the state that the maps before it give.  Sequences too few to fill the chip are cut into segments, whose maps a kernel of its own finds first.
 #pragma once
 #include "recurrence.h"
 
 namespace tfno {
 
-constexpr int RECURRENCE_THREADS = 256;
+constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;      // of a group in a tile: what waits in registers fits four waves a SIMD
 
+// ALL of a kernel: with rates, an input gate and `normalise`, as nearly all calls have them; else each is asked for.
 struct RecurrenceShape {
     int lanes_log2;                 // lanes of a group
     unsigned channel_blocks, segments, first;
     int segment;                    // tokens of a segment
 };
-
-// V neighbouring elements as they stand in memory.
-template <class E, int V>
-struct Some;
-template <class E>
-struct Some<E, 1> {
-    E at;
-    __device__ __forceinline__ void load(const E *p) { at = *p; }
-    __device__ __forceinline__ float value(int) const { return to_float(at); }
-};
-template <>
-struct Some<float, 2> {
-    float2 at;
-    __device__ __forceinline__ void load(const float *p) { at = *reinterpret_cast<const float2 *>(p); }
-    __device__ __forceinline__ float value(int i) const { return i ? at.y : at.x; }
-};
-template <>
-struct Some<bf16, 2> {
-    unsigned at;
-    __device__ __forceinline__ void load(const bf16 *p) { at = *reinterpret_cast<const unsigned *>(p); }
-    __device__ __forceinline__ float value(int i) const { return __uint_as_float(i ? at & 0xffff0000u : at << 16); }
-};
-__device__ __forceinline__ void store_some(float *p, const float (&v)[1]) { *p = v[0]; }
-__device__ __forceinline__ void store_some(bf16 *p, const float (&v)[1]) { store_element(p, v[0]); }
-__device__ __forceinline__ void store_some(float *p, const float (&v)[2]) { *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]); }
-__device__ __forceinline__ void store_some(bf16 *p, const float (&v)[2]) { *reinterpret_cast<unsigned *>(p) = bf16_pair(v[0], v[1]); }
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
@@ -57,58 +31,131 @@ __device__ __forceinline__ void sigmoid(float z, float &s, float &rest)
     s = z < 0.0f ? small : big;
     rest = z < 0.0f ? big : small;
 }
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 // A decay a = exp(l).  Near 1, where states last long, its distance from 1 is what matters: it is kept as -(1 - a), sign bit set, and from the series
-// -l (1 + l/2 + l^2/6 + ...), whose first term left out is l^7 / 40320 of the whole, 2e-8 at the border; rounded to a float32 itself, a decay of 0.9999 would be
+// -l (1 + l/2 + l^2/6 + ...), whose first term left out is l^5 / 720 of the whole, 4e-8 at the border; rounded to a float32 itself, a decay of 0.9999 would be
 // 3e-4 of its distance off, always to the same side.  Elsewhere (and above 1) it is a itself, at least 2^-126.  +0 is a decay of exactly 0, which forgets the state whatever it
 // holds: that of one token where exp(l) rounds to 0 in float32; of a sum of logarithms only where one of them was that of 0, whatever the others make of it.
-constexpr float NOTHING_LEFT = -104.0f;
+constexpr float NOTHING_LEFT = -104.0f, HARDLY = -87.0f;
 struct Decay {
     float at;
     __device__ __forceinline__ Decay() {}
-    // a and 1 - a too
-    __device__ __forceinline__ Decay(float l, float &a, float &less, float nothing = NOTHING_LEFT)
+    // For l no less than HARDLY (or NaN); a and 1 - a too.
+    __device__ __forceinline__ Decay(float l, float &a, float &less)
     {
-        float p = fmaf(l, 1.0f / 5040.0f, 1.0f / 720.0f);
-        p = fmaf(l, p, 1.0f / 120.0f);
-        p = fmaf(l, p, 1.0f / 24.0f);
+        float p = fmaf(l, 1.0f / 120.0f, 1.0f / 24.0f);
         p = fmaf(l, p, 1.0f / 6.0f);
         p = fmaf(l, p, 0.5f);
-        p = fmaf(l, p, 1.0f);
+        p = fmaf(l, p, 1.0f) * l;
         a = __builtin_amdgcn_exp2f(l * LOG2E);
-        a = a == 0.0f ? 1.17549435e-38f : a;
-        const bool near = l > -0.35f && l <= 0.0f;
-        less = near ? fabsf(l * p) : 1.0f - a;
-        at = near ? -less : l < nothing ? 0.0f : a;
+        const bool near = __float_as_uint(l) - 0x80000000u < 0x3e000000u;      // -0.125 < l <= -0
+        less = near ? -p : 1.0f - a;
+        at = near ? p : a;
     }
-    __device__ __forceinline__ static Decay of_sum(float l)
+    // For any l, which is no more than HARDLY.
+    __device__ __forceinline__ void hardly(float l, float nothing = NOTHING_LEFT) { at = l < nothing ? 0.0f : 1.17549435e-38f; }
+    __device__ __forceinline__ explicit Decay(float l, float nothing = NOTHING_LEFT)
     {
         float a, less;
-        return Decay(l, a, less, -3.4e38f);
+        *this = Decay(l, a, less);
+        if (l < HARDLY) hardly(l, nothing);
     }
+    __device__ __forceinline__ static Decay of_sum(float l) { return Decay(l, -3.4e38f); }
     __device__ __forceinline__ bool forgets() const { return __float_as_uint(at) == 0; }
+    // a h, and a h + u
     __device__ __forceinline__ float of(float h) const { return forgets() ? 0.0f : fmaf(at, h, (int)__float_as_uint(at) < 0 ? h : 0.0f); }
-    // a h + u
     __device__ __forceinline__ float of(float h, float u) const { return forgets() ? u : fmaf(at, h, ((int)__float_as_uint(at) < 0 ? h : 0.0f) + u); }
 };
-// The part of a sum of logarithms that a token has.
+// The same with what the sign bit says as a factor, for the walks through tokens: two instructions where none of a wave's tokens forgets, which nearly always holds.
+struct TokenDecay {
+    float at, whole;
+    __device__ __forceinline__ TokenDecay() {}
+    __device__ __forceinline__ TokenDecay(float l, float &a, float &less)
+    {
+        const Decay d(l, a, less);
+        at = d.at, whole = (int)__float_as_uint(d.at) < 0 ? 1.0f : 0.0f;
+    }
+    __device__ __forceinline__ void hardly(float l) { at = l < NOTHING_LEFT ? 0.0f : 1.17549435e-38f; }
+    template <bool RESETS>
+    __device__ __forceinline__ float of(float h) const { return RESETS && __float_as_uint(at) == 0 ? 0.0f : fmaf(at, h, whole * h); }
+    template <bool RESETS>
+    __device__ __forceinline__ float of(float h, float u) const { return RESETS && __float_as_uint(at) == 0 ? u : fmaf(at, h, fmaf(whole, h, u)); }
+};
+// The logarithm of a token's decay, and its part of a sum of them.
+__device__ __forceinline__ float log_of(bool rated, float rate, float gate) { return rated ? -rate * sigmoid(gate) : gate; }
 __device__ __forceinline__ float part_of_sum(float l) { return l < NOTHING_LEFT ? -INFINITY : l; }
 
-// What tokens in their order do to the state before them: h -> a h + B.
-struct Map { Decay a; float B; };
+__device__ __forceinline__ void set(float &v, float to) { v = to; }
+__device__ __forceinline__ void set(bf16 &v, float to) { v.bits = (unsigned short)(__float_as_uint(to) >> 16); }       // 0 and infinity
+// Tokens as if they were not there: they add nothing, and their decay is 1.
+template <int S, class E>
+__device__ __forceinline__ void leave_out(bool rated, int t, int last, E (&x)[S], E (&gate)[S])
+{
+#pragma unroll
+    for (int j = 0; j < S; ++j)
+        if (t + j > last) set(x[j], 0.0f), set(gate[j], rated ? -INFINITY : 0.0f);
+}
+// Decays that are hardly more than 0, or not: seldom, and then looked for in a wave's whole tile, whose gates are read again.
+template <int S, class E>
+__device__ __forceinline__ bool find_resets(bool rated, float rate, const E (&gate)[S], int t, int last, TokenDecay (&d)[S], float &log)
+{
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
+        const float l = t + j <= last ? log_of(rated, rate, to_float(gate[j])) : 0.0f;
+        if (l < HARDLY) d[j].hardly(l);
+        found = found || l < NOTHING_LEFT;
+    }
+    if (found) log = -INFINITY;
+    return __any(found);
+}
+
+// What tokens in their order do to the state before them, h -> a h + B, by the decay and by the sum of the logarithms of their decays.
+struct Map {
+    float log, B;
+    __device__ __forceinline__ float of(float h) const { return Decay::of_sum(log).of(h, B); }
+};
+struct Joined {
+    Decay a;
+    float B;
+    __device__ __forceinline__ float of(float h) const { return a.of(h, B); }
+};
+__device__ __forceinline__ Joined joined(Map m) { return Joined{Decay::of_sum(m.log), m.B}; }
+__device__ __forceinline__ Map after(Map first, Map second) { return Map{first.log + second.log, second.of(first.B)}; }
+
+// Maps of the groups of a wave, each joined with those before it (behind it, where BACK), without its own; and all of them.
+template <bool BACK>
+__device__ __forceinline__ void join(int lanes, Map own, Map &others, Map &all)
+{
+    const int lane = threadIdx.x & 63, order = BACK ? 63 - lane : lane;
+    for (int d = lanes; d < 64; d <<= 1) {
+        const Map p = {BACK ? __shfl_down(own.log, d, 64) : __shfl_up(own.log, d, 64), BACK ? __shfl_down(own.B, d, 64) : __shfl_up(own.B, d, 64)};
+        if (order >= d) own = after(p, own);
+    }
+    others = {0.0f, 0.0f};
+    if (lanes < 64) {
+        const Map p = {BACK ? __shfl_down(own.log, lanes, 64) : __shfl_up(own.log, lanes, 64), BACK ? __shfl_down(own.B, lanes, 64) : __shfl_up(own.B, lanes, 64)};
+        if (order >= lanes) others = p;
+    }
+    all = own;      // where order is last
+}
 
 // What the workgroup's place in the launch means.
-template <int V>
 struct Place {
-    int b, segment, group, groups, c, len, begin, end;      // tokens begin .. end - 1 of the segment
-    bool live;                                             // the lane has channels
+    int b, segment, lane, wave, group, c, len, begin, end;      // tokens begin .. end - 1 of the segment; group: in its wave
+    bool live;                                                 // the lane has a channel
     __device__ __forceinline__ Place(const RecurrenceArgs &a, const RecurrenceShape &s)
     {
         const unsigned item = s.first + blockIdx.x, block = item % s.channel_blocks, rest = item / s.channel_blocks;
         segment = rest % s.segments;
         b = rest / s.segments;
-        const int lane = threadIdx.x & ((1 << s.lanes_log2) - 1);
-        group = threadIdx.x >> s.lanes_log2, groups = RECURRENCE_THREADS >> s.lanes_log2;
-        c = ((int)(block << s.lanes_log2) + lane) * V;
+        lane = threadIdx.x & ((1 << s.lanes_log2) - 1);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        group = (threadIdx.x & 63) >> s.lanes_log2;
+        c = (int)(block << s.lanes_log2) + lane;
         live = c < a.C;
         if (!live) c = 0;           // loads stay inside
         len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
@@ -116,338 +163,433 @@ struct Place {
     }
 };
 
-// The decays and inputs of S tokens of the thread from token t on, past `end` as if they were not there.
-template <class E, int V, int S>
-struct Tile {
-    Some<E, V> x[S], gate[S], input[S];
-    __device__ __forceinline__ void load(const RecurrenceArgs &a, int b, int c, int t, int last)
-    {
+// The state before the segment (the gradient behind it, where BACK): the maps of the other segments, shared out among the workgroup's groups.
+template <bool BACK, int WAVES>
+__device__ __forceinline__ float through_segments(const RecurrenceArgs &a, const RecurrenceShape &s, const Place &at, float start, Joined (&maps)[WAVES][64])
+{
+    const int n = BACK ? (int)s.segments - 1 - at.segment : at.segment, groups = 64 >> s.lanes_log2, lanes = 1 << s.lanes_log2;
+    if (n == 0) return start;
+    const int each = (n + groups * WAVES - 1) / (groups * WAVES), from = (at.wave * groups + at.group) * each;
+    Map own = {0.0f, 0.0f};
+    for (int i = from; i < min(from + each, n); ++i) {
+        const float2 m = a.effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - i : i)) * a.C + at.c];
+        own = after(own, Map{m.x, m.y});
+    }
+    Map others, all;
+    join<false>(lanes, own, others, all);
+    if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = joined(all);
+    __syncthreads();
 #pragma unroll
-        for (int j = 0; j < S; ++j) {
-            const long long at = min(t + j, last);
-            x[j].load((const E *)a.x + b * a.sx.batch + at * a.sx.token + c);
-            gate[j].load((const E *)a.gate + b * a.sgate.batch + at * a.sgate.token + c);
-            if (a.input_gate) input[j].load((const E *)a.input_gate + b * a.sinput.batch + at * a.sinput.token + c);
+    for (int w = 0; w < WAVES; ++w) start = maps[w][at.lane].of(start);
+    __syncthreads();
+    return start;
+}
+
+// A tensor's elements of the thread: S tokens from `first` (of the wave) + `ahead` (of its group) on, in one channel.  A token's address is scalar, a lane's offset from it has 32
+// bits of bytes, the same for all: tokens of a wave, 64 at most, are less than 2^23 elements apart.
+template <class E>
+struct Row {
+    char *at;                   // of the sequence
+    long long wide;             // bytes from token to token
+    unsigned offset;            // of the lane
+    __device__ __forceinline__ Row(const void *p, const Strides &s, int b, int c, int ahead)
+        : at((char *)p + b * s.batch * (long long)sizeof(E)), wide(s.token * (long long)sizeof(E)), offset((unsigned)ahead * (unsigned)wide + (unsigned)c * (unsigned)sizeof(E)) {}
+    // The lane's offset, made to look new each time: kept as an address it would be two registers a token instead of none.
+    __device__ __forceinline__ unsigned here() const
+    {
+        unsigned o = offset;
+        asm volatile("" : "+v"(o));
+        return o;
+    }
+    // From a token's scalar offset to its element, and on to the next token.
+    __device__ __forceinline__ long long from(int token) const { return token * wide; }
+    __device__ __forceinline__ E *next(long long &k, unsigned here) const
+    {
+        E *p = (E *)(at + k + here);
+        k += wide;
+        asm volatile("" : "+s"(k));         // a sum, not a product for every token
+        return p;
+    }
+    __device__ __forceinline__ E *before(long long &k, unsigned here) const
+    {
+        E *p = (E *)(at + k + here);
+        k -= wide;
+        asm volatile("" : "+s"(k));
+        return p;
+    }
+    // S tokens; those past the last one that counts, which is not negative, are that one again: their values are not used.
+    template <bool FULL, int S>
+    __device__ __forceinline__ void load(int first, int ahead, int c, int last, E (&v)[S]) const
+    {
+        if (FULL) {
+            const unsigned o = here();
+            long long k = from(first);
+#pragma unroll
+            for (int j = 0; j < S; ++j) v[j] = *next(k, o);
+            // the loads of both kinds stay apart: as common code behind them the compiler would take addresses of 64 bits from either
+            asm volatile("; whole");
+        } else {
+            const char *p = at + min(first, last) * wide;
+            unsigned o = c * (unsigned)sizeof(E) + (unsigned)(min(first + ahead, last) - min(first, last)) * (unsigned)wide;
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                v[j] = *(const E *)(p + o);
+                o += first + ahead + j < last ? (unsigned)wide : 0u;
+            }
+            asm volatile("; cut");
         }
     }
 };
 
-template <class E, int V>
-__device__ __forceinline__ void decay_and_input(const RecurrenceArgs &a, const float (&rate)[V], const Some<E, V> &x, const Some<E, V> &gate,
-                                                const Some<E, V> &input, bool there, Decay (&decay)[V], float (&u)[V], float (&log)[V])
+template <class E, bool ALL, int S, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, RecurrenceShape s)
 {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        float l = gate.value(e), full, less;
-        if (a.rate) l = -rate[e] * sigmoid(l);
-        l = there ? l : 0.0f;
-        decay[e] = Decay(l, full, less);
-        float w = x.value(e);
-        if (a.input_gate) w *= sigmoid(input.value(e));
-        if (a.normalise) w *= __builtin_amdgcn_sqrtf(less * (2.0f - less));       // 1 - a^2
-        u[e] = there ? w : 0.0f;
-        log[e] += part_of_sum(l);
-    }
-}
-
-template <int V>
-__device__ __forceinline__ void load_rates(const RecurrenceArgs &a, int c, float (&rate)[V])
-{
-#pragma unroll
-    for (int e = 0; e < V; ++e) rate[e] = a.rate ? a.rate[c + e] : 0.0f;
-}
-
-template <class E, int V, int S>
-__global__ __launch_bounds__(RECURRENCE_THREADS) void k_recurrence(RecurrenceArgs a, RecurrenceShape s)
-{
-    __shared__ Map maps[2][V][RECURRENCE_THREADS];
-    const Place<V> at(a, s);
-    const int lanes = 1 << s.lanes_log2, lane = threadIdx.x & (lanes - 1), tile = at.groups * S;
-    float rate[V], carry[V];
-    load_rates(a, at.c, rate);
+    constexpr int WAVES = THREADS / 64;
+    __shared__ Joined maps[2][WAVES][64];
+    const Place at(a, s);
+    const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
+    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const float rate = rated ? a.rate[at.c] : 0.0f;
     // the state before the segment
+    float carry = a.initial ? a.initial[(long long)at.b * a.C + at.c] : 0.0f;
+    carry = through_segments<false, WAVES>(a, s, at, carry, maps[0]);
+    const int last = max(min(at.len, at.end) - 1, 0), tape_rows = (a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE;
+    const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
+    const Row<E> y(a.y, a.sy, at.b, at.c, ahead);
+    E in_x[S], in_gate[S], in_input[S];
+    const auto load = [&](int first) {          // of the wave
+        const auto all = [&](auto full) {
+            x.template load<full.value>(first, ahead, at.c, last, in_x);
+            gate.template load<full.value>(first, ahead, at.c, last, in_gate);
+            if (gated) input.template load<full.value>(first, ahead, at.c, last, in_input);
+        };
+        if (first + per_wave - 1 <= last) all(Yes());
+        else all(No());
+    };
+    int first = at.begin + at.wave * per_wave, buffer = 0;
+    if (at.begin < at.len) load(first);
+    for (int start = at.begin; start < at.end; start += tile, first += tile, buffer ^= 1) {
+        const int t = first + ahead;
+        if (start >= at.len) {
+            long long k = y.from(first);    // past the sequence: zeros, and nothing on the tape, which is not read there
 #pragma unroll
-    for (int e = 0; e < V; ++e) carry[e] = a.initial ? a.initial[(long long)at.b * a.C + at.c + e] : 0.0f;
-    for (int i = 0; i < at.segment; ++i) {
-        const float2 *m = a.effects + ((long long)at.b * s.segments + i) * a.C + at.c;
-#pragma unroll
-        for (int e = 0; e < V; ++e) carry[e] = Decay::of_sum(m[e].x).of(carry[e], m[e].y);
-    }
-    const int last = max(min(at.len, at.end) - 1, 0);
-    E *y = (E *)a.y + at.b * a.sy.batch + at.c;
-    Tile<E, V, S> in;
-    int t = at.begin + at.group * S, buffer = 0;
-    if (at.begin < at.len) in.load(a, at.b, at.c, t, last);
-    for (int start = at.begin; start < at.end; start += tile, t += tile, buffer ^= 1) {
-        if (start >= at.len) {              // past the sequence: zeros, and nothing on the tape, which is not read there
-            const float zeros[V] = {};
-#pragma unroll
-            for (int j = 0; j < S; ++j)
-                if (t + j < at.end && at.live) store_some(y + (long long)(t + j) * a.sy.token, zeros);
+            for (int j = 0; j < S; ++j) {
+                E *p = y.next(k, y.offset);
+                if (t + j < at.end && at.live) store_element(p, 0.0f);
+            }
             continue;
         }
-        Decay d[S][V];
-        float u[S][V], log[V] = {};
+        TokenDecay d[S];
+        float u[S];
+        Map own = {0.0f, 0.0f};
+        if (first + per_wave - 1 > last) leave_out(rated, t, last, in_x, in_gate);
+        float lowest = 0.0f;
+        const unsigned next_x = x.here(), next_gate = gate.here(), next_input = input.here();
+        long long kx = x.from(first + tile), kg = gate.from(first + tile), ki = input.from(first + tile);
+        // a token's place in the registers is free once its gates are made: the next tile's is asked for there and then, so that its latency lies under all the rest
+        const auto gates = [&](auto next) {
 #pragma unroll
-        for (int j = 0; j < S; ++j) decay_and_input<E, V>(a, rate, in.x[j], in.gate[j], in.input[j], t + j <= last, d[j], u[j], log);
-        in.load(a, at.b, at.c, t + tile, last);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float B = u[0][e];
-#pragma unroll
-            for (int j = 1; j < S; ++j) B = d[j][e].of(B, u[j][e]);
-            maps[buffer][e][threadIdx.x] = Map{Decay::of_sum(log[e]), B};
-        }
-        __syncthreads();                    // the other buffer is written next: a wave that is here has read it
-        float h[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float all = carry[e];
-            h[e] = all;
-            for (int g = 0; g < at.groups; ++g) {
-                h[e] = g == at.group ? all : h[e];
-                const Map m = maps[buffer][e][g * lanes + lane];
-                all = m.a.of(all, m.B);
+            for (int j = 0; j < S; ++j) {
+                float part, less;
+                const float l = log_of(rated, rate, to_float(in_gate[j]));
+                d[j] = TokenDecay(l, part, less);
+                u[j] = to_float(in_x[j]);
+                if (gated) u[j] *= sigmoid(to_float(in_input[j]));
+                if (normalise) u[j] *= __builtin_amdgcn_sqrtf(less * (2.0f - less));       // 1 - a^2
+                own.log += l;
+                lowest = fminf(lowest, l);
+                if (next.value) {
+                    in_x[j] = *x.next(kx, next_x);
+                    in_gate[j] = *gate.next(kg, next_gate);
+                    if (gated) in_input[j] = *input.next(ki, next_input);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            carry[e] = all;
+        };
+        if (first + tile + per_wave - 1 <= last) {
+            gates(Yes());
+        } else {
+            gates(No());
+            load(first + tile);
         }
-        if (a.tape && (t & (RECURRENCE_TAPE - 1)) == 0 && t < at.end && at.live)
+        bool resets = false;
+        if (__any(lowest < HARDLY)) {
+            E again[S];
+            gate.template load<false>(first, ahead, at.c, last, again);
+            resets = find_resets(rated, rate, again, t, last, d, own.log);
+        }
+        const auto run = [&](float h, auto can, auto each) {
 #pragma unroll
-            for (int e = 0; e < V; ++e)
-                a.tape[((long long)at.b * ((a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) + t / RECURRENCE_TAPE) * a.C + at.c + e] = h[e];
+            for (int j = 0; j < S; ++j) each(j, h = d[j].template of<can.value>(h, u[j]));
+            return h;
+        };
+        const auto nothing = [](int, float) {};
+        own.B = resets ? run(0.0f, Yes(), nothing) : run(0.0f, No(), nothing);
+        Map before, all;
+        join<false>(lanes, own, before, all);
+        if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[buffer][at.wave][at.lane] = joined(all);
+        __syncthreads();                    // the other buffer is written next: a wave that is here has read it
+        float h = carry;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            h = w == at.wave ? carry : h;
+            carry = maps[buffer][w][at.lane].of(carry);
+        }
+        if (lanes < 64) h = before.of(h);
+        if (a.tape && (t & (RECURRENCE_TAPE - 1)) == 0 && t < at.end && at.live) a.tape[((long long)at.b * tape_rows + t / RECURRENCE_TAPE) * a.C + at.c] = h;
+        const unsigned o = y.here();
+        long long k = y.from(first);
+        if (!resets && first + per_wave <= at.end && first + per_wave <= at.len) {
+            if (at.live) run(h, No(), [&](int, float v) { store_element(y.next(k, o), v); });
+        } else {
+            run(h, Yes(), [&](int j, float v) {
+                E *p = y.next(k, o);
+                if (t + j < at.end && at.live) store_element(p, t + j < at.len ? v : 0.0f);
+            });
+        }
+    }
+    if (a.final_state && at.segment == (int)s.segments - 1 && at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = carry;
+}
+
+// What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every group finds the map of its part.
+template <class E, bool ALL, int S, int THREADS, bool BACKWARD>
+__global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a, RecurrenceShape s)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float2 maps[WAVES][64];
+    const Place at(a, s);
+    if (at.segment == (BACKWARD ? 0 : (int)s.segments - 1)) return;          // nobody asks
+    const int lanes = 1 << s.lanes_log2, groups = (64 >> s.lanes_log2) * WAVES, part = s.segment / groups;      // a multiple of S: a segment is whole tiles
+    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const float rate = rated ? a.rate[at.c] : 0.0f;
+    const int stop = min(at.end, at.len), last = max(stop - 1, 0), of_wave = at.begin + at.wave * (64 >> s.lanes_log2) * part, ahead = at.group * part;
+    const long long from = (long long)of_wave + ahead;
+    const E *x = (const E *)a.x + at.b * a.sx.batch + at.c, *gate = (const E *)a.gate + at.b * a.sgate.batch + at.c;
+    const E *input = gated ? (const E *)a.input_gate + at.b * a.sinput.batch + at.c : nullptr, *dy = BACKWARD ? (const E *)a.dy + at.b * a.sy.batch + at.c : nullptr;
+    Map own = {0.0f, 0.0f};
+    E in_x[S], in_gate[S], in_input[S];
+    const auto load = [&](int i) {
+        const long long t = BACKWARD ? from + part - S - i : from + i;
 #pragma unroll
         for (int j = 0; j < S; ++j) {
-            float out[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                h[e] = d[j][e].of(h[e], u[j][e]);
-                out[e] = t + j < at.len ? h[e] : 0.0f;
-            }
-            if (t + j < at.end && at.live) store_some(y + (long long)(t + j) * a.sy.token, out);
+            const long long k = min(max(t + j, 0LL), (long long)last);
+            in_x[j] = BACKWARD ? dy[k * a.sy.token] : x[k * a.sx.token];
+            in_gate[j] = gate[k * a.sgate.token];
+            if (!BACKWARD && gated) in_input[j] = input[k * a.sinput.token];
         }
+    };
+    if (of_wave < stop) load(0);
+    for (int i = 0; i < part && of_wave < stop; i += S) {
+        const long long t = BACKWARD ? from + part - S - i : from + i;
+        Decay d[S];
+        float u[S];
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            const bool there = t + j < stop;
+            float l = to_float(in_gate[j]), full, less;
+            if (rated) l = -rate * sigmoid(l);
+            l = there ? l : 0.0f;
+            d[j] = Decay(l, full, less);
+            if (l < HARDLY) d[j].hardly(l);
+            u[j] = to_float(in_x[j]);
+            if (!BACKWARD && gated) u[j] *= sigmoid(to_float(in_input[j]));
+            if (!BACKWARD && normalise) u[j] *= __builtin_amdgcn_sqrtf(less * (2.0f - less));
+            u[j] = there ? u[j] : 0.0f;
+            own.log += part_of_sum(l);
+        }
+        load(i + S);
+#pragma unroll
+        for (int j = 0; j < S; ++j) own.B = BACKWARD ? d[S - 1 - j].of(own.B + u[S - 1 - j]) : d[j].of(own.B, u[j]);
     }
-    if (a.final_state && at.segment == (int)s.segments - 1 && at.group == 0 && at.live)
-#pragma unroll
-        for (int e = 0; e < V; ++e) a.final_state[(long long)at.b * a.C + at.c + e] = carry[e];
-}
-
-// What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every group finds the map of its part, the first group joins them.
-template <class E, int V, int S, bool BACKWARD>
-__global__ __launch_bounds__(RECURRENCE_THREADS) void k_recurrence_effects(RecurrenceArgs a, RecurrenceShape s)
-{
-    __shared__ float2 maps[V][RECURRENCE_THREADS];       // logarithm of the decay, B
-    const Place<V> at(a, s);
-    if (at.segment == (BACKWARD ? 0 : (int)s.segments - 1)) return;          // nobody asks
-    const int lanes = 1 << s.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    float rate[V], log[V] = {}, B[V] = {};
-    load_rates(a, at.c, rate);
-    const int stop = min(at.end, at.len), part = (s.segment / at.groups + S - 1) / S * S;
-    const int from = at.begin + at.group * part, to = min(from + part, stop);
-    const int last = max(stop - 1, 0);
-    if (BACKWARD) {
-        const E *dy = (const E *)a.dy + at.b * a.sy.batch + at.c;
-        for (int t = from + part - S; t >= from && at.begin < at.len; t -= S) {
-            Some<E, V> gate[S], in[S];
-#pragma unroll
-            for (int j = 0; j < S; ++j) {
-                const long long k = min(t + j, last);
-                gate[j].load((const E *)a.gate + at.b * a.sgate.batch + k * a.sgate.token + at.c);
-                in[j].load(dy + k * a.sy.token);
-            }
-#pragma unroll
-            for (int j = S - 1; j >= 0; --j)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float l = gate[j].value(e);
-                    if (a.rate) l = -rate[e] * sigmoid(l);
-                    const bool there = t + j < to;
-                    l = there ? l : 0.0f;
-                    float full, less;
-                    B[e] = Decay(l, full, less).of(B[e] + (there ? in[j].value(e) : 0.0f));
-                    log[e] += part_of_sum(l);
-                }
-        }
-    } else {
-        for (int t = from; t < to; t += S) {
-            Tile<E, V, S> in;
-            in.load(a, at.b, at.c, t, last);
-#pragma unroll
-            for (int j = 0; j < S; ++j) {
-                Decay d[V];
-                float u[V];
-                decay_and_input<E, V>(a, rate, in.x[j], in.gate[j], in.input[j], t + j < to, d, u, log);
-#pragma unroll
-                for (int e = 0; e < V; ++e) B[e] = d[e].of(B[e], u[e]);
-            }
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) maps[e][threadIdx.x] = make_float2(log[e], B[e]);
+    Map others, all;
+    join<BACKWARD>(lanes, own, others, all);
+    if (BACKWARD ? (int)(threadIdx.x & 63) < lanes : (int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = make_float2(all.log, all.B);
     __syncthreads();
-    if (at.group != 0 || !at.live) return;
+    if (at.wave != 0 || at.group != 0 || !at.live) return;
+    Map joined = {0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        float2 all = make_float2(0.0f, 0.0f);
-        for (int i = 0; i < at.groups; ++i) {
-            const float2 m = maps[e][(BACKWARD ? at.groups - 1 - i : i) * lanes + lane];
-            all = make_float2(all.x + m.x, Decay::of_sum(m.x).of(all.y, m.y));
-        }
-        a.effects[((long long)at.b * s.segments + at.segment) * a.C + at.c + e] = all;
+    for (int w = 0; w < WAVES; ++w) {
+        const float2 m = maps[BACKWARD ? WAVES - 1 - w : w][at.lane];
+        joined = after(joined, Map{m.x, m.y});
     }
+    a.effects[((long long)at.b * s.segments + at.segment) * a.C + at.c] = make_float2(joined.log, joined.B);
 }
 
-template <class E, int V, int S>
-__global__ __launch_bounds__(RECURRENCE_THREADS) void k_recurrence_back(RecurrenceArgs a, RecurrenceShape s)
+template <class E, bool ALL, int S, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, RecurrenceShape s)
 {
-    __shared__ Map maps[2][V][RECURRENCE_THREADS];
-    __shared__ float later[2][V][RECURRENCE_THREADS];
-    const Place<V> at(a, s);
-    const int lanes = 1 << s.lanes_log2, lane = threadIdx.x & (lanes - 1), tile = at.groups * S;
-    float rate[V], carry[V], drate[V];          // carry: the gradient that reaches the state before the tile from its later tokens
-    load_rates(a, at.c, rate);
-#pragma unroll
-    for (int e = 0; e < V; ++e) carry[e] = a.d_final ? a.d_final[(long long)at.b * a.C + at.c + e] : 0.0f, drate[e] = 0.0f;
-    for (int i = (int)s.segments - 1; i > at.segment; --i) {
-        const float2 *m = a.effects + ((long long)at.b * s.segments + i) * a.C + at.c;
-#pragma unroll
-        for (int e = 0; e < V; ++e) carry[e] = Decay::of_sum(m[e].x).of(carry[e], m[e].y);
-    }
+    constexpr int WAVES = THREADS / 64;
+    __shared__ Joined maps[2][WAVES][64];
+    __shared__ float later[2][WAVES][64];
+    const Place at(a, s);
+    const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
+    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const float rate = rated ? a.rate[at.c] : 0.0f;
+    float drate = 0.0f, carry = a.d_final ? a.d_final[(long long)at.b * a.C + at.c] : 0.0f;      // carry: the gradient that reaches the state before the tile from its later tokens
+    carry = through_segments<true, WAVES>(a, s, at, carry, maps[0]);
     const int last = max(min(at.len, at.end) - 1, 0), tiles = (at.end - at.begin + tile - 1) / tile;
     const float *tape = a.tape + (long long)at.b * ((a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) * a.C + at.c;
-    const E *dy = (const E *)a.dy + at.b * a.sy.batch + at.c;
-    E *dx = (E *)a.dx + at.b * a.sdx.batch + at.c, *dgate = (E *)a.dgate + at.b * a.sdgate.batch + at.c;
-    E *dinput = (E *)a.dinput_gate + at.b * a.sdinput.batch + at.c;
-    Tile<E, V, S> in;
-    Some<E, V> in_dy[S];
-    float in_h[V] = {};
-    int start = at.begin + (tiles - 1) * tile, t = start + at.group * S, buffer = 0;
-    const auto load = [&](int t, int start) {
-        in.load(a, at.b, at.c, t, last);
-#pragma unroll
-        for (int j = 0; j < S; ++j) in_dy[j].load(dy + (long long)min(t + j, last) * a.sy.token);
-#pragma unroll
-        for (int e = 0; e < V; ++e) in_h[e] = tape[(long long)(start / RECURRENCE_TAPE) * a.C + e];
+    const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
+    const Row<E> dy(a.dy, a.sy, at.b, at.c, ahead);
+    const Row<E> dx(a.dx, a.sdx, at.b, at.c, ahead), dgate(a.dgate, a.sdgate, at.b, at.c, ahead), dinput(a.dinput_gate, a.sdinput, at.b, at.c, ahead);
+    E in_x[S], in_gate[S], in_input[S], in_dy[S];
+    float in_h = 0.0f;
+    const auto load = [&](int first, int start) {
+        const auto all = [&](auto full) {
+            x.template load<full.value>(first, ahead, at.c, last, in_x);
+            gate.template load<full.value>(first, ahead, at.c, last, in_gate);
+            dy.template load<full.value>(first, ahead, at.c, last, in_dy);
+            if (gated) input.template load<full.value>(first, ahead, at.c, last, in_input);
+        };
+        if (first + per_wave - 1 <= last) all(Yes());
+        else all(No());
+        in_h = tape[(long long)(start / RECURRENCE_TAPE) * a.C];
     };
-    for (; start >= at.begin && start >= at.len; start -= tile, t -= tile) {      // past the sequence: zeros
-        const float zeros[V] = {};
-#pragma unroll
-        for (int j = 0; j < S; ++j)
-            if (t + j < at.end && at.live) {
-                store_some(dx + (long long)(t + j) * a.sdx.token, zeros);
-                store_some(dgate + (long long)(t + j) * a.sdgate.token, zeros);
-                if (a.input_gate) store_some(dinput + (long long)(t + j) * a.sdinput.token, zeros);
-            }
-    }
-    if (start >= at.begin) load(t, start);
-    for (; start >= at.begin; start -= tile, t -= tile, buffer ^= 1) {
-        // of each token: decay, input, and with the state before it known: dx = D by_x, dinput = D by_input, dl = D by_log, dgate = dl by_gate, drate = dl by_rate
-        Decay d[S][V];
-        float log[V] = {}, u[S][V], by_x[S][V], by_input[S][V], by_log[S][V], by_gate[S][V], by_rate[S][V], g[S][V];
+    int start = at.begin + (tiles - 1) * tile, first = start + at.wave * per_wave, buffer = 0;
+    for (; start >= at.begin && start >= at.len; start -= tile, first -= tile) {    // past the sequence: zeros
+        long long kx = dx.from(first), kg = dgate.from(first), ki = dinput.from(first);
 #pragma unroll
         for (int j = 0; j < S; ++j) {
-            const bool there = t + j <= last;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float l = in.gate[j].value(e), sigma, rest;
-                by_gate[j][e] = 1.0f, by_rate[j][e] = 0.0f;
-                if (a.rate) {
-                    sigmoid(l, sigma, rest);
-                    l = -rate[e] * sigma;
-                    by_gate[j][e] = l * rest, by_rate[j][e] = -sigma;
-                }
-                l = there ? l : 0.0f;
-                float full, less;
-                d[j][e] = Decay(l, full, less);
-                log[e] += part_of_sum(l);
-                const float x = in.x[j].value(e);
-                float open = 1.0f, left = 1.0f, by_open = 0.0f;
-                if (a.input_gate) {
-                    sigmoid(in.input[j].value(e), open, rest);
-                    by_open = open * rest;
-                }
-                by_log[j][e] = 0.0f;
-                if (a.normalise) {
-                    left = __builtin_amdgcn_sqrtf(less * (2.0f - less));
-                    by_log[j][e] = left == 0.0f ? 0.0f : -x * open * full * full * __builtin_amdgcn_rcpf(left);
-                }
-                by_x[j][e] = open * left, by_input[j][e] = x * left * by_open;
-                u[j][e] = there ? x * by_x[j][e] : 0.0f;
-                g[j][e] = there ? in_dy[j].value(e) : 0.0f;
-            }
-        }
-        float first[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) first[e] = in_h[e];
-        if (start > at.begin) load(t - tile, start - tile);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float B = u[0][e], R = 0.0f;
-#pragma unroll
-            for (int j = 1; j < S; ++j) B = d[j][e].of(B, u[j][e]);
-#pragma unroll
-            for (int j = S - 1; j >= 0; --j) R = d[j][e].of(g[j][e] + R);
-            maps[buffer][e][threadIdx.x] = Map{Decay::of_sum(log[e]), B};
-            later[buffer][e][threadIdx.x] = R;
-        }
-        __syncthreads();
-        float h[V], D[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float all = first[e], back = carry[e];
-            for (int i = 0; i < at.group; ++i) {
-                const Map m = maps[buffer][e][i * lanes + lane];
-                all = m.a.of(all, m.B);
-            }
-            for (int i = at.groups - 1; i >= 0; --i) {
-                D[e] = i == at.group ? back : D[e];
-                back = maps[buffer][e][i * lanes + lane].a.of(back, later[buffer][e][i * lanes + lane]);
-            }
-            h[e] = all, carry[e] = back;
-        }
-#pragma unroll
-        for (int j = 0; j < S; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float kept = d[j][e].of(h[e]);
-                by_log[j][e] += kept;
-                h[e] = kept + u[j][e];
-            }
-#pragma unroll
-        for (int j = S - 1; j >= 0; --j) {
-            const bool there = t + j < at.len;
-            float ox[V], og[V], oi[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                D[e] += g[j][e];
-                const float dl = D[e] * by_log[j][e];
-                ox[e] = there ? D[e] * by_x[j][e] : 0.0f;
-                oi[e] = there ? D[e] * by_input[j][e] : 0.0f;
-                og[e] = there ? dl * by_gate[j][e] : 0.0f;
-                drate[e] += there ? dl * by_rate[j][e] : 0.0f;
-                D[e] = d[j][e].of(D[e]);
-            }
-            if (t + j < at.end && at.live) {
-                store_some(dx + (long long)(t + j) * a.sdx.token, ox);
-                store_some(dgate + (long long)(t + j) * a.sdgate.token, og);
-                if (a.input_gate) store_some(dinput + (long long)(t + j) * a.sdinput.token, oi);
+            E *px = dx.next(kx, dx.offset), *pg = dgate.next(kg, dgate.offset), *pi = dinput.next(ki, dinput.offset);
+            if (first + ahead + j < at.end && at.live) {
+                store_element(px, 0.0f);
+                store_element(pg, 0.0f);
+                if (gated) store_element(pi, 0.0f);
             }
         }
     }
-    if (a.d_initial && at.segment == 0 && at.group == 0 && at.live)
+    if (start >= at.begin) load(first, start);
+    for (; start >= at.begin; start -= tile, first -= tile, buffer ^= 1) {
+        const int t = first + ahead;
+        // of each token: decay, input, and with the state before it known: dx = D by_x, dinput = D by_input, dl = D by_log, dgate = dl by_gate, drate = dl by_rate
+        TokenDecay d[S];
+        float u[S], by_x[S], by_input[S], by_log[S], by_gate[S], by_rate[S], g[S];
+        Map own = {0.0f, 0.0f};
+        if (first + per_wave - 1 > last) {
+            leave_out(rated, t, last, in_x, in_gate);
 #pragma unroll
-        for (int e = 0; e < V; ++e) a.d_initial[(long long)at.b * a.C + at.c + e] = carry[e];
-    if (!a.drate) return;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < V; ++e) later[0][e][threadIdx.x] = drate[e];
-    __syncthreads();
-    if (at.group == 0 && at.live)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            float sum = 0.0f;
-            for (int i = 0; i < at.groups; ++i) sum += later[0][e][i * lanes + lane];
-            a.partial[((long long)at.b * s.segments + at.segment) * a.C + at.c + e] = sum;
+            for (int j = 0; j < S; ++j)
+                if (t + j > last) set(in_dy[j], 0.0f), set(in_input[j], 0.0f);
         }
+        float lowest = 0.0f;
+        const unsigned next_x = x.here(), next_gate = gate.here(), next_input = input.here(), next_dy = dy.here();
+        long long kx = x.from(first - tile), kg = gate.from(first - tile), ki = input.from(first - tile), kd = dy.from(first - tile);
+        const auto gates = [&](auto next) {
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                float l = to_float(in_gate[j]), part, less, sigma, rest;
+                by_gate[j] = 1.0f, by_rate[j] = 0.0f;
+                if (rated) {
+                    sigmoid(l, sigma, rest);
+                    l = -rate * sigma;
+                    by_gate[j] = l * rest, by_rate[j] = -sigma;
+                }
+                d[j] = TokenDecay(l, part, less);
+                own.log += l;
+                lowest = fminf(lowest, l);
+                const float in = to_float(in_x[j]);
+                float open = 1.0f, left = 1.0f, by_open = 0.0f;
+                if (gated) {
+                    sigmoid(to_float(in_input[j]), open, rest);
+                    by_open = open * rest;
+                }
+                by_log[j] = 0.0f;
+                if (normalise) {
+                    left = __builtin_amdgcn_sqrtf(less * (2.0f - less));
+                    by_log[j] = left == 0.0f ? 0.0f : -in * open * part * part * __builtin_amdgcn_rcpf(left);
+                }
+                by_x[j] = open * left, by_input[j] = in * left * by_open;
+                u[j] = in * by_x[j];
+                g[j] = to_float(in_dy[j]);
+                if (next.value) {
+                    in_x[j] = *x.next(kx, next_x);
+                    in_gate[j] = *gate.next(kg, next_gate);
+                    in_dy[j] = *dy.next(kd, next_dy);
+                    if (gated) in_input[j] = *input.next(ki, next_input);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        // the tile before is whole wherever there is one, since tokens are missing at a sequence's end alone
+        const float state = in_h;
+        if (start > at.begin) {
+            gates(Yes());
+            in_h = tape[(long long)((start - tile) / RECURRENCE_TAPE) * a.C];
+        } else {
+            gates(No());
+        }
+        bool resets = false;
+        if (__any(lowest < HARDLY)) {
+            E again[S];
+            gate.template load<false>(first, ahead, at.c, last, again);
+            resets = find_resets(rated, rate, again, t, last, d, own.log);
+        }
+        const auto local = [&](auto can) {
+            float R = 0.0f;
+#pragma unroll
+            for (int j = 0; j < S; ++j) own.B = d[j].template of<can.value>(own.B, u[j]);
+#pragma unroll
+            for (int j = S - 1; j >= 0; --j) R = d[j].template of<can.value>(g[j] + R);
+            return R;
+        };
+        const float R = resets ? local(Yes()) : local(No());
+        Map before, behind, all, all_back;
+        join<false>(lanes, own, before, all);
+        join<true>(lanes, Map{own.log, R}, behind, all_back);
+        if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[buffer][at.wave][at.lane] = joined(all);
+        if ((int)(threadIdx.x & 63) < lanes) later[buffer][at.wave][at.lane] = all_back.B;
+        __syncthreads();
+        float h = state, D = carry;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float next = maps[buffer][w][at.lane].of(h);
+            h = w < at.wave ? next : h;
+        }
+#pragma unroll
+        for (int w = WAVES - 1; w >= 0; --w) {
+            D = w == at.wave ? carry : D;
+            carry = maps[buffer][w][at.lane].a.of(carry, later[buffer][w][at.lane]);
+        }
+        if (lanes < 64) h = before.of(h), D = behind.of(D);
+        const unsigned ox = dx.here(), og = dgate.here(), oi = dinput.here();
+        long long qx = dx.from(first + S - 1), qg = dgate.from(first + S - 1), qi = dinput.from(first + S - 1);
+        const auto walk = [&](auto can, auto full) {
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                const float kept = d[j].template of<can.value>(h);
+                by_log[j] += kept;
+                h = kept + u[j];
+            }
+#pragma unroll
+            for (int j = S - 1; j >= 0; --j) {
+                const bool there = full.value || t + j < at.len;
+                D += g[j];
+                const float dl = D * by_log[j];
+                drate += there ? dl * by_rate[j] : 0.0f;
+                E *px = dx.before(qx, ox), *pg = dgate.before(qg, og), *pi = dinput.before(qi, oi);
+                if ((full.value || t + j < at.end) && at.live) {
+                    store_element(px, there ? D * by_x[j] : 0.0f);
+                    store_element(pg, there ? dl * by_gate[j] : 0.0f);
+                    if (gated) store_element(pi, there ? D * by_input[j] : 0.0f);
+                }
+                D = d[j].template of<can.value>(D);
+            }
+        };
+        if (!resets && first + per_wave <= at.end && first + per_wave <= at.len) walk(No(), Yes());
+        else walk(Yes(), No());
+    }
+    if (a.d_initial && at.segment == 0 && at.wave == 0 && at.group == 0 && at.live) a.d_initial[(long long)at.b * a.C + at.c] = carry;
+    if (!a.drate) return;
+    // the groups' parts in their order
+    for (int k = lanes; k < 64; k <<= 1) drate += __shfl_xor(drate, k, 64);
+    __syncthreads();
+    later[0][at.wave][threadIdx.x & 63] = drate;
+    __syncthreads();
+    if (at.wave == 0 && at.group == 0 && at.live) {
+        float sum = 0.0f;
+        for (int w = 0; w < WAVES; ++w) sum += later[0][w][at.lane];
+        a.partial[((long long)at.b * s.segments + at.segment) * a.C + at.c] = sum;
+    }
 }
 
 }  // namespace tfno
