@@ -9,8 +9,8 @@ namespace tfno {
 namespace {
 
 // Workgroups of the backward kernel, at most: each leaves a row of every sum over tokens.
-unsigned most_blocks(int C) { return std::max(256u, std::min(1024u, (4u << 20) / (unsigned)C)); }
-constexpr unsigned FORWARD_BLOCKS = 1u << 22;
+unsigned most_blocks(int C, int gate_kind) { return std::max(256u, std::min(gate_kind == GATE_TOKEN ? 768u : 512u, (4u << 20) / (unsigned)C)); }
+constexpr unsigned FORWARD_WAVES = 256 * 20;         // five waves a SIMD, which its registers allow
 
 int group_log2_of(int C)
 {
@@ -24,35 +24,36 @@ int threads_of(int group_log2) { return group_log2 > 6 ? 1 << group_log2 : BLOCK
 unsigned parts_of(int B, int T, int C)
 {
     const int groups = threads_of(group_log2_of(C)) >> group_log2_of(C);
-    if (T <= 2 * groups || (unsigned)B >= most_blocks(C)) return 1;
-    const unsigned wanted = (most_blocks(C) + B - 1) / B, most = (T + groups - 1) / groups;
+    if (T <= 2 * groups || (unsigned)B >= most_blocks(C, GATE_SEQUENCE)) return 1;
+    const unsigned wanted = (most_blocks(C, GATE_SEQUENCE) + B - 1) / B, most = (T + groups - 1) / groups;
     const unsigned rows = (T + std::min(wanted, most) - 1) / std::min(wanted, most);
     return (T + rows - 1) / rows;
 }
 
-template <class E, class R, bool VEC, int ITER, bool BACKWARD>
+template <class E, class R, bool VEC, int ITER, bool TOKEN, bool BACKWARD>
 hipError_t launch(const BlockNormArgs &a, hipStream_t st)
 {
     BlockNormShape s{};
     s.group_log2 = group_log2_of(a.C);
     const int threads = threads_of(s.group_log2), groups = threads >> s.group_log2;
-    const unsigned most = BACKWARD ? most_blocks(a.C) : FORWARD_BLOCKS;
-    unsigned long long work;        // workgroups that would each have work for once
+    const unsigned rows = (unsigned)a.B * (unsigned)a.T;
+    unsigned work, most = BACKWARD ? most_blocks(a.C, a.gate_kind) : FORWARD_WAVES * 64 / threads;        // work: workgroups that each have work once
     if (BACKWARD && a.gate_kind == GATE_SEQUENCE && a.dgate) {
         s.parts = parts_of(a.B, a.T, a.C), s.whole = s.parts == 1;
         s.by_group = s.whole && (groups == 1 || a.B >= groups * 64 || a.T <= 2 * groups);
         s.outer = a.B * s.parts, s.rows = (a.T + s.parts - 1) / s.parts;
         work = s.by_group ? (s.outer + groups - 1) / groups : s.outer;
     } else {
-        s.by_group = 1, s.outer = (unsigned)a.B * (unsigned)a.T, s.rows = 1, s.parts = a.T;
-        work = (s.outer + groups - 1) / groups;
+        s.outer = rows > 0;
+        s.rows = (unsigned)std::max(1ull, ((unsigned long long)rows + (unsigned long long)most * groups - 1) / ((unsigned long long)most * groups));
+        work = (unsigned)(((unsigned long long)rows + (unsigned long long)s.rows * groups - 1) / ((unsigned long long)s.rows * groups));
     }
-    const unsigned grid = (unsigned)std::min<unsigned long long>(work, most);
-    s.outer_stride = s.by_group ? grid * groups : grid;
+    const unsigned grid = std::min(work, most);
+    s.outer_stride = s.parts == 0 ? 1 : s.by_group ? grid * groups : grid;
     if (BACKWARD) {
         s.part_after = a.workspace, s.part_before = s.part_after + (size_t)grid * a.C, s.part_gate = s.part_before + (size_t)grid * a.C;
     }
-    if (grid) k_block_norm<E, R, VEC, ITER, BACKWARD><<<grid, threads, 0, st>>>(a, s);
+    if (grid) k_block_norm<E, R, VEC, ITER, TOKEN, BACKWARD><<<grid, threads, 0, st>>>(a, s);
     if (BACKWARD) {
         ColumnSumsArgs<3> sums{};
         const bool of_sequences = a.gate_kind == GATE_SEQUENCE && a.dgate && !s.whole && grid;
@@ -87,12 +88,17 @@ bool vectors(const BlockNormArgs &a, bool backward)
     return (p & 15) == 0 && (s & 7) == 0;
 }
 
-template <class E, class R, bool BACKWARD>
+template <class E, class R, bool TOKEN, bool BACKWARD>
 hipError_t choose(const BlockNormArgs &a, hipStream_t s)
 {
     const bool vec = vectors(a, BACKWARD);
-    if ((8 << group_log2_of(a.C)) < a.C) return vec ? launch<E, R, true, 2, BACKWARD>(a, s) : launch<E, R, false, 2, BACKWARD>(a, s);
-    return vec ? launch<E, R, true, 1, BACKWARD>(a, s) : launch<E, R, false, 1, BACKWARD>(a, s);
+    if ((8 << group_log2_of(a.C)) < a.C) return vec ? launch<E, R, true, 2, TOKEN, BACKWARD>(a, s) : launch<E, R, false, 2, TOKEN, BACKWARD>(a, s);
+    return vec ? launch<E, R, true, 1, TOKEN, BACKWARD>(a, s) : launch<E, R, false, 1, TOKEN, BACKWARD>(a, s);
+}
+template <class E, class R, bool BACKWARD>
+hipError_t choose(const BlockNormArgs &a, hipStream_t s)
+{
+    return a.gate_kind == GATE_TOKEN ? choose<E, R, true, BACKWARD>(a, s) : choose<E, R, false, BACKWARD>(a, s);
 }
 
 template <bool BACKWARD>
@@ -109,8 +115,8 @@ hipError_t block_norm_backward_launch(const BlockNormArgs &a, hipStream_t s) { r
 
 size_t block_norm_workspace_bytes(int B, int T, int C, int gate_kind)
 {
-    size_t rows = 3 * (size_t)most_blocks(C);
-    if (gate_kind == GATE_SEQUENCE) rows = 2 * (size_t)most_blocks(C) + (size_t)B * parts_of(B, T, C);
+    size_t rows = 3 * (size_t)most_blocks(C, gate_kind);
+    if (gate_kind == GATE_SEQUENCE) rows = 2 * (size_t)most_blocks(C, gate_kind) + (size_t)B * parts_of(B, T, C);
     return sizeof(float) * rows * C;
 }
 

@@ -10,6 +10,7 @@
 // workspace, which k_column_sums adds up in their order.
 #pragma once
 #include "blocknorm.h"
+#include "gates.h"
 
 namespace tfno {
 
@@ -19,73 +20,69 @@ enum { ACT_NONE = 0, ACT_SILU = 1, ACT_SIGMOID = 2 };
 
 struct BlockNormShape {
     int group_log2;                 // threads of a row
+    int by_group;                   // a part's rows are one group's; else a workgroup's, whose groups share them
     unsigned outer, outer_stride;   // parts of the batch, and how many are worked on at once
-    int by_group;                   // a part is a group's; else a workgroup's, whose groups share its rows
-    unsigned long long rows;        // of a part
-    unsigned parts;                 // of a sequence (parts are sequences' where a gate is theirs)
+    unsigned parts, rows;           // parts of a sequence, and their rows; without parts (0) a group takes `rows` rows of the batch in all
     int whole;                      // a part is a whole sequence: its gate's gradient needs no further sum
     float *part_after, *part_before, *part_gate;
 };
 
-// Eight values of a thread: neighbours where VEC, else `step` apart.  `count` of them are inside the row.
-template <bool VEC>
-__device__ __forceinline__ void load8(const float *p, int step, int count, float (&v)[8])
-{
-    if constexpr (VEC) {
-        const float4 lo = reinterpret_cast<const float4 *>(p)[0], hi = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-    } else {
+// Eight values of a thread as they stand in memory: neighbours where VEC, else `step` apart.  `count` of them are inside the row.
+template <class E, bool VEC>
+struct Eight {
+    E at[8];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? p[i * step] : 0.0f;
+        for (int i = 0; i < 8; ++i) at[i] = E{};
     }
-}
-template <bool VEC>
-__device__ __forceinline__ void load8(const bf16 *p, int step, int count, float (&v)[8])
-{
-    if constexpr (VEC) {
-        const uint4 t = *reinterpret_cast<const uint4 *>(p);
-        const unsigned w[4] = {t.x, t.y, t.z, t.w};
+    __device__ __forceinline__ void load(const E *p, int step, int count)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < count ? to_float(p[i * step]) : 0.0f;
+        for (int i = 0; i < 8; ++i) at[i] = i < count ? p[i * step] : E{};
     }
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(float *p, int step, int count, const float (&v)[8])
-{
-    if constexpr (VEC) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < count) p[i * step] = v[i];
+        for (int i = 0; i < 8; ++i) v[i] = to_float(at[i]);
     }
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(bf16 *p, int step, int count, const float (&v)[8])
-{
-    if constexpr (VEC) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
-    } else {
+    __device__ __forceinline__ static void store(E *p, int step, int count, const float (&v)[8])
+    {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < count) store_element(p + i * step, v[i]);
     }
-}
-
-// act(z), and its slope.
-__device__ __forceinline__ void activate(int kind, float z, float &value, float &slope)
-{
-    value = z, slope = 1.0f;
-    if (kind == ACT_NONE) return;
-    const float e = expf(-fabsf(z)), big = 1.0f / (1.0f + e), small = e * big;
-    const float s = z < 0.0f ? small : big, rest = z < 0.0f ? big : small;
-    value = kind == ACT_SILU ? z * s : s;
-    slope = kind == ACT_SILU ? fmaf(z * s, rest, s) : s * rest;
-}
+};
+template <>
+struct Eight<float, true> {
+    float4 lo, hi;
+    __device__ __forceinline__ void clear() { lo = hi = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
+    __device__ __forceinline__ void load(const float *p, int, int) { lo = reinterpret_cast<const float4 *>(p)[0], hi = reinterpret_cast<const float4 *>(p)[1]; }
+    __device__ __forceinline__ void values(float (&v)[8]) const { v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w; }
+    __device__ __forceinline__ static void store(float *p, int, int, const float (&v)[8])
+    {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+};
+template <>
+struct Eight<bf16, true> {
+    uint4 at;
+    __device__ __forceinline__ void clear() { at = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const bf16 *p, int, int) { at = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+        const unsigned w[4] = {at.x, at.y, at.z, at.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    __device__ __forceinline__ static void store(bf16 *p, int, int, const float (&v)[8])
+    {
+        // whole lines that nobody reads soon (16 x 8192 heads of 128, both directions: 70 -> 65 us); the two halves of a lane's float32 values would be parts of lines
+        typedef unsigned vector __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(vector{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, (vector *)p);
+    }
+};
 
 // Sums of N values over the threads of a row.  Rows wider than a wave have the workgroup to themselves and meet in LDS, in two buffers by turns.
 template <int N>
@@ -117,7 +114,7 @@ __device__ __forceinline__ void leave(float (&v)[ITER][8], int group_log2, const
     if (width >= (int)blockDim.x) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
-            if (count[i] > 0) store8<false>(out + column[i], VEC ? 1 : step, count[i], v[i]);
+            if (count[i] > 0) Eight<float, false>::store(out + column[i], VEC ? 1 : step, count[i], v[i]);
         return;
     }
 #pragma unroll
@@ -131,22 +128,22 @@ __device__ __forceinline__ void leave(float (&v)[ITER][8], int group_log2, const
             for (int g = threadIdx.x; g < (int)blockDim.x; g += width)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += meet[g][e];
-            store8<false>(out + column[i], VEC ? 1 : step, count[i], sum);
+            Eight<float, false>::store(out + column[i], VEC ? 1 : step, count[i], sum);
         }
     }
     __syncthreads();
 }
 
-// E: type of y, n and of a token's gate.  R: type of the residual.  A thread has ITER times eight values of a row.
-template <class E, class R, bool VEC, int ITER, bool BACKWARD>
-__global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a, BlockNormShape s)
+// E: type of y, n and of a token's gate.  R: type of the residual.  TOKEN: each token has a gate of its own; else they share one, or there is none.  A thread has ITER times eight values of a row; the next row's are on their way while it works on one.
+template <class E, class R, bool VEC, int ITER, bool TOKEN, bool BACKWARD>
+__global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu(BACKWARD && TOKEN && ITER == 1 ? 3 : 2))) void k_block_norm(BlockNormArgs a, BlockNormShape s)
 {
     __shared__ float meet[2][2][16];
     __shared__ float sums[BACKWARD ? BLOCK_NORM_THREADS : 1][8];
     const int width = 1 << s.group_log2, lane = threadIdx.x & (width - 1), group = threadIdx.x >> s.group_log2, groups = blockDim.x >> s.group_log2;
     const int step = width;
     int column[ITER], count[ITER], turn = 0;
-    float wa[ITER][8], wb[ITER][8], gate_c[ITER][8];
+    float wa[ITER][8], wb[ITER][8], gate[TOKEN ? 1 : ITER][8];       // gate: of the channels, or of the sequence that the rows are in
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         column[i] = VEC ? (i * width + lane) * 8 : i * width * 8 + lane;
@@ -157,42 +154,78 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
             const bool in = e < count[i];
             wa[i][e] = in ? a.w_after && a.norm_after ? a.w_after[c] : 1.0f : 0.0f;
             wb[i][e] = in ? a.w_before ? a.w_before[c] : 1.0f : 0.0f;
-            gate_c[i][e] = in && a.gate_kind == GATE_CHANNEL ? ((const float *)a.gate)[c] : 0.0f;
+            if constexpr (!TOKEN) gate[i][e] = in && a.gate_kind == GATE_CHANNEL ? ((const float *)a.gate)[c] : 0.0f;
         }
     }
-    float d_after[ITER][8] = {}, d_before[ITER][8] = {}, d_gate[ITER][8] = {};
+    float d_after[ITER][8] = {}, d_before[ITER][8] = {}, d_gate[TOKEN ? 1 : ITER][8] = {};
     const float over_C = 1.0f / (float)a.C;
-    const unsigned first = s.by_group ? blockIdx.x * groups + group : blockIdx.x;
-    const unsigned long long row_first = s.by_group ? 0 : group, row_step = s.by_group ? 1 : groups;
-    for (unsigned part = first; part < s.outer; part += s.outer_stride) {
-        for (unsigned long long row = row_first; row < s.rows; row += row_step) {
-            const unsigned long long all = (unsigned long long)part * s.rows + row;
-            unsigned b, t;
-            if (a.gate_kind == GATE_SEQUENCE) {
-                b = part / s.parts;
-                const unsigned long long at = (part - b * s.parts) * s.rows + row;
-                if (at >= (unsigned)a.T) break;
-                t = (unsigned)at;
-            } else {
-                if (all >= (unsigned long long)a.B * a.T) break;
-                b = (unsigned)(all / (unsigned)a.T), t = (unsigned)(all - (unsigned long long)b * a.T);
-            }
-            const bool there = !a.lengths || (int)t < a.lengths[b];
-            float y[ITER][8], r[ITER][8], z[ITER][8], dn[ITER][8], ds[ITER][8];
+    const bool before = BACKWARD ? a.d_n_out != nullptr : a.n_out != nullptr;
+    const unsigned here = blockIdx.x * groups + group;
+    for (unsigned part = s.parts && !s.by_group ? blockIdx.x : s.parts ? here : 0; part < s.outer; part += s.outer_stride) {
+        // the group's rows
+        unsigned row, end;
+        if (s.parts == 0) {
+            const unsigned long long from = (unsigned long long)here * s.rows, all = (unsigned long long)a.B * a.T;
+            row = (unsigned)min(from, all), end = (unsigned)min(from + s.rows, all);
+        } else {
+            const unsigned b = part / s.parts, from = (part - b * s.parts) * s.rows, to = min(from + s.rows, (unsigned)a.T);
+            const unsigned each = s.by_group ? to - from : (to - from + groups - 1) / groups, first = s.by_group ? from : from + group * each;
+            row = b * a.T + min(first, to), end = b * a.T + min(first + each, to);
+        }
+        unsigned b = a.T ? row / a.T : 0, t = row - b * a.T;
+        int seen = -1;                              // the sequence whose gate is in the registers
+        int length = a.lengths && row < end ? a.lengths[b] : a.T;
+        Eight<E, VEC> in_y[ITER], in_z[TOKEN ? ITER : 1], in_n[BACKWARD ? ITER : 1];
+        Eight<R, VEC> in_r[ITER], in_s[BACKWARD ? ITER : 1];
+        const auto load = [&] {
+            const bool there = (int)t < length;
 #pragma unroll
             for (int i = 0; i < ITER; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[i][e] = r[i][e] = dn[i][e] = ds[i][e] = 0.0f, z[i][e] = gate_c[i][e];
+                in_y[i].clear(), in_r[i].clear();
+                if constexpr (TOKEN) in_z[i].clear();
+                if constexpr (BACKWARD) in_n[i].clear(), in_s[i].clear();
                 if (!there || count[i] == 0) continue;
-                load8<VEC>((const E *)a.y + b * a.sy.batch + t * a.sy.token + column[i], step, count[i], y[i]);
-                if (a.r) load8<VEC>((const R *)a.r + b * a.sr.batch + t * a.sr.token + column[i], step, count[i], r[i]);
-                if (a.gate_kind == GATE_TOKEN) load8<VEC>((const E *)a.gate + b * a.sgate.batch + t * a.sgate.token + column[i], step, count[i], z[i]);
-                if (a.gate_kind == GATE_SEQUENCE) load8<VEC>((const float *)a.gate + b * a.sgate.batch + column[i], step, count[i], z[i]);
+                in_y[i].load((const E *)a.y + b * a.sy.batch + t * a.sy.token + column[i], step, count[i]);
+                if (a.r) in_r[i].load((const R *)a.r + b * a.sr.batch + t * a.sr.token + column[i], step, count[i]);
+                if constexpr (TOKEN) in_z[i].load((const E *)a.gate + b * a.sgate.batch + t * a.sgate.token + column[i], step, count[i]);
                 if constexpr (BACKWARD) {
-                    if (a.d_r_out) load8<VEC>((const R *)a.d_r_out + b * a.sr_out.batch + t * a.sr_out.token + column[i], step, count[i], ds[i]);
-                    if (a.d_n_out) load8<VEC>((const E *)a.d_n_out + b * a.sn_out.batch + t * a.sn_out.token + column[i], step, count[i], dn[i]);
+                    if (a.d_r_out) in_s[i].load((const R *)a.d_r_out + b * a.sr_out.batch + t * a.sr_out.token + column[i], step, count[i]);
+                    if (a.d_n_out) in_n[i].load((const E *)a.d_n_out + b * a.sn_out.batch + t * a.sn_out.token + column[i], step, count[i]);
                 }
             }
+        };
+        if (row < end) load();
+        while (row < end) {
+            const unsigned cb = b, ct = t;
+            const bool there = (int)t < length;
+            float y[ITER][8], r[ITER][8], z[ITER][8], dn[ITER][8], ds[ITER][8];
+            if (!TOKEN && a.gate_kind == GATE_SEQUENCE && seen != (int)b) {
+                seen = (int)b;
+#pragma unroll
+                for (int i = 0; i < ITER; ++i) {
+                    Eight<float, VEC> shared;
+                    shared.clear();
+                    if (count[i] > 0) shared.load((const float *)a.gate + b * a.sgate.batch + column[i], step, count[i]);
+                    shared.values(gate[TOKEN ? 0 : i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < ITER; ++i) {
+                in_y[i].values(y[i]), in_r[i].values(r[i]);
+                if constexpr (BACKWARD) in_n[i].values(dn[i]), in_s[i].values(ds[i]);
+                if constexpr (TOKEN) {
+                    in_z[i].values(z[i]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[i][e] = gate[i][e];
+                }
+            }
+            ++row;
+            if (++t == (unsigned)a.T) {
+                t = 0, ++b;
+                if (a.lengths && row < end) length = a.lengths[b];
+            }
+            if (row < end) load();
             float p = 1.0f;
             if (a.norm_after) {
                 float ss[1] = {};
@@ -201,23 +234,37 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
 #pragma unroll
                     for (int e = 0; e < 8; ++e) ss[0] = fmaf(y[i][e], y[i][e], ss[0]);
                 row_sums(ss, s.group_log2, meet, turn);
-                p = 1.0f / sqrtf(fmaf(ss[0], over_C, a.eps));
+                p = rsqrtf(fmaf(ss[0], over_C, a.eps));
             }
-            float st[ITER][8], open[ITER][8], slope[ITER][8], two[2] = {};
+            // z: act(gate), slope: its slope
+            float st[ITER][8], slope[ITER][8], two[2] = {};
 #pragma unroll
-            for (int i = 0; i < ITER; ++i)
+            for (int i = 0; i < ITER; ++i) {
+                if (!TOKEN && a.gate_kind == GATE_NONE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[i][e] = 1.0f, slope[i][e] = 0.0f;
+                } else if (a.activation == ACT_NONE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) slope[i][e] = 1.0f;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float open, rest;
+                        sigmoid(z[i][e], open, rest);
+                        const float through = a.activation == ACT_SILU ? z[i][e] * open : open;
+                        slope[i][e] = a.activation == ACT_SILU ? fmaf(through, rest, open) : open * rest;
+                        z[i][e] = through;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float m = y[i][e] * p * wa[i][e];
-                    open[i][e] = 1.0f, slope[i][e] = 0.0f;
-                    if (a.gate_kind != GATE_NONE) activate(a.activation, z[i][e], open[i][e], slope[i][e]);
-                    st[i][e] = m * open[i][e];
+                    st[i][e] = y[i][e] * p * wa[i][e] * z[i][e];
                     if (a.r) st[i][e] = fmaf(a.residual_scale, r[i][e], st[i][e]);
                     two[0] = fmaf(st[i][e], st[i][e], two[0]);
                     if constexpr (BACKWARD) two[1] = fmaf(dn[i][e] * wb[i][e], st[i][e], two[1]);
                 }
+            }
             float q = 0.0f;
-            const bool before = BACKWARD ? a.d_n_out != nullptr : a.n_out != nullptr;
             if (before) {
                 if constexpr (BACKWARD) {
                     row_sums(two, s.group_log2, meet, turn);
@@ -226,7 +273,7 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
                     row_sums(one, s.group_log2, meet, turn);
                     two[0] = one[0];
                 }
-                q = 1.0f / sqrtf(fmaf(two[0], over_C, a.eps));
+                q = rsqrtf(fmaf(two[0], over_C, a.eps));
             }
             if constexpr (!BACKWARD) {
 #pragma unroll
@@ -238,8 +285,8 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
                         n[e] = there ? st[i][e] * q * wb[i][e] : 0.0f;
                         st[i][e] = there ? st[i][e] : 0.0f;
                     }
-                    if (a.r_out) store8<VEC>((R *)a.r_out + b * a.sr_out.batch + t * a.sr_out.token + column[i], step, count[i], st[i]);
-                    if (a.n_out) store8<VEC>((E *)a.n_out + b * a.sn_out.batch + t * a.sn_out.token + column[i], step, count[i], n);
+                    if (a.r_out) Eight<R, VEC>::store((R *)a.r_out + cb * a.sr_out.batch + ct * a.sr_out.token + column[i], step, count[i], st[i]);
+                    if (a.n_out) Eight<E, VEC>::store((E *)a.n_out + cb * a.sn_out.batch + ct * a.sn_out.token + column[i], step, count[i], n);
                 }
             } else {
                 const float back = q * q * q * two[1] * over_C;
@@ -248,16 +295,16 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
                 for (int i = 0; i < ITER; ++i)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float m = y[i][e] * p * wa[i][e];
+                        const float scaled = y[i][e] * p;
                         float d = ds[i][e];
                         if (before) {
                             d += fmaf(q * wb[i][e], dn[i][e], -back * st[i][e]);
                             d_before[i][e] = fmaf(dn[i][e] * q, st[i][e], d_before[i][e]);
                         }
-                        const float f = d * open[i][e], dz = d * m * slope[i][e];
-                        d_after[i][e] = fmaf(f * p, y[i][e], d_after[i][e]);
-                        d_gate[i][e] += dz;
-                        slope[i][e] = dz;
+                        const float f = d * z[i][e], dz = d * (scaled * wa[i][e]) * slope[i][e];
+                        d_after[i][e] = fmaf(f, scaled, d_after[i][e]);
+                        if constexpr (TOKEN) slope[i][e] = dz;
+                        else d_gate[i][e] += dz;
                         r[i][e] = a.residual_scale * d;
                         z[i][e] = f * wa[i][e];
                         dot[0] = fmaf(z[i][e], y[i][e], dot[0]);
@@ -276,21 +323,21 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
                         r[i][e] = there ? r[i][e] : 0.0f;
                         slope[i][e] = there ? slope[i][e] : 0.0f;
                     }
-                    store8<VEC>((E *)a.dy + b * a.sdy.batch + t * a.sdy.token + column[i], step, count[i], y[i]);
-                    if (a.dr) store8<VEC>((R *)a.dr + b * a.sdr.batch + t * a.sdr.token + column[i], step, count[i], r[i]);
-                    if (a.dgate && a.gate_kind == GATE_TOKEN)
-                        store8<VEC>((E *)a.dgate + b * a.sdgate.batch + t * a.sdgate.token + column[i], step, count[i], slope[i]);
+                    Eight<E, VEC>::store((E *)a.dy + cb * a.sdy.batch + ct * a.sdy.token + column[i], step, count[i], y[i]);
+                    if (a.dr) Eight<R, VEC>::store((R *)a.dr + cb * a.sdr.batch + ct * a.sdr.token + column[i], step, count[i], r[i]);
+                    if (TOKEN && a.dgate)
+                        Eight<E, VEC>::store((E *)a.dgate + cb * a.sdgate.batch + ct * a.sdgate.token + column[i], step, count[i], slope[i]);
                 }
             }
         }
-        if constexpr (BACKWARD) {
-            if (a.gate_kind == GATE_SEQUENCE && a.dgate) {
+        if constexpr (BACKWARD && !TOKEN) {
+            if (s.parts && a.gate_kind == GATE_SEQUENCE && a.dgate) {
                 // one row of the gate's gradient for the part: where it is a whole sequence, that is the gradient
                 float *out = s.whole ? (float *)a.dgate + (long long)part * a.sdgate.batch : s.part_gate + (size_t)part * a.C;
                 if (s.by_group) {
 #pragma unroll
                     for (int i = 0; i < ITER; ++i)
-                        if (count[i] > 0) store8<false>(out + column[i], VEC ? 1 : step, count[i], d_gate[i]);
+                        if (count[i] > 0) Eight<float, false>::store(out + column[i], VEC ? 1 : step, count[i], d_gate[i]);
                 } else {
                     leave<VEC>(d_gate, s.group_log2, count, column, step, out, sums);
                 }
@@ -304,7 +351,8 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) void k_block_norm(BlockNormArgs a,
     if constexpr (BACKWARD) {
         if (a.dw_after) leave<VEC>(d_after, s.group_log2, count, column, step, s.part_after + (size_t)blockIdx.x * a.C, sums);
         if (a.dw_before) leave<VEC>(d_before, s.group_log2, count, column, step, s.part_before + (size_t)blockIdx.x * a.C, sums);
-        if (a.dgate && a.gate_kind == GATE_CHANNEL) leave<VEC>(d_gate, s.group_log2, count, column, step, s.part_gate + (size_t)blockIdx.x * a.C, sums);
+        if constexpr (!TOKEN)
+            if (a.dgate && a.gate_kind == GATE_CHANNEL) leave<VEC>(d_gate, s.group_log2, count, column, step, s.part_gate + (size_t)blockIdx.x * a.C, sums);
     }
 }
 

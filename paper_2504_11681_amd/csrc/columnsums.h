@@ -29,6 +29,7 @@ __global__ __launch_bounds__(1024) void k_column_sums(ColumnSumsArgs<JOBS> a)
     const size_t at = blockIdx.y - a.first[k];
     float sum = 0.0f;
     if (c < (unsigned)a.C)
+#pragma unroll 8
         for (unsigned r = group; r < job.rows; r += 64) sum += job.part[(at * job.rows + r) * a.C + c];
     sums[group][threadIdx.x & 15] = sum;
     __syncthreads();

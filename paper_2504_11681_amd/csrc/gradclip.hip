@@ -2,8 +2,8 @@
 //
 // Bound by bytes: all tensors are read once for the norm, and read and written where there is something to clip.  Squares are added up in float64, so
 // that no value over- or underflows and no order matters beyond a float32's last bit.  A launch takes a table of tensors, cut into pieces that its
-// workgroups take by turns; the second launch adds up what the workgroups of the first left, each the same way, and goes through the pieces from the end: the
-// last ones read are still in the last-level cache.
+// workgroups take by turns, all of them close together in memory (each its own stretch: 118 -> 133 us for 486 MB); the second launch adds up what the workgroups of the
+// first left, each the same way, and goes through the pieces from the end.
 #include "gradclip.h"
 
 #include <algorithm>
@@ -15,6 +15,9 @@ namespace {
 constexpr int CLIP_THREADS = 256, CLIP_TENSORS = 128, CLIP_BLOCKS = 2048;
 constexpr int CLIP_ROUND = CLIP_THREADS * 4;        // vectors of 16 bytes in a piece
 
+// Loads and stores that leave the last-level cache alone: what is read next is as large as what it holds (both passes over 486 MB in BF16 314 -> 277 us; the stores alone 293).
+typedef unsigned Vector __attribute__((ext_vector_type(4)));
+
 struct ClipTable {
     void *p[CLIP_TENSORS];
     long long n[CLIP_TENSORS];                      // elements
@@ -23,25 +26,45 @@ struct ClipTable {
     int count;
 };
 
+// A workgroup looks for its first piece's tensor and then goes on from there, in either direction.
 struct Piece {
-    void *p;                                        // of the tensor, down to a multiple of 16 bytes
-    long long skip, end;                            // elements from there on that are the tensor's: skip .. end - 1
-    long long vector;                               // the first vector of the piece
-    bool bf16;
+    int tensor;
+    Vector *p;                                      // the tensor, down to a multiple of 16 bytes, from the piece on
+    long long from, to;                             // elements from p on that are the tensor's
+    int per;                                        // elements of a vector
+    bool bf16, whole;
     __device__ __forceinline__ Piece(const ClipTable &t, unsigned piece)
     {
-        int lo = 0, hi = t.count - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (t.first[mid] <= piece) lo = mid;
+        int hi = t.count - 1;
+        tensor = 0;
+        while (tensor < hi) {
+            const int mid = (tensor + hi + 1) >> 1;
+            if (t.first[mid] <= piece) tensor = mid;
             else hi = mid - 1;
         }
-        bf16 = t.bf16_mask[lo >> 5] >> (lo & 31) & 1;
-        const uintptr_t at = (uintptr_t)t.p[lo];
-        p = (void *)(at & ~(uintptr_t)15);
-        skip = (long long)(at & 15) / (bf16 ? 2 : 4);
-        end = skip + t.n[lo];
-        vector = (long long)(piece - t.first[lo]) * CLIP_ROUND;
+        set(t, piece);
+    }
+    __device__ __forceinline__ void go(const ClipTable &t, unsigned piece)
+    {
+        while (t.first[tensor] > piece) --tensor;
+        while (t.first[tensor + 1] <= piece) ++tensor;
+        set(t, piece);
+    }
+    __device__ __forceinline__ void set(const ClipTable &t, unsigned piece)
+    {
+        bf16 = t.bf16_mask[tensor >> 5] >> (tensor & 31) & 1;
+        per = bf16 ? 8 : 4;
+        const uintptr_t at = (uintptr_t)t.p[tensor];
+        const long long vector = (long long)(piece - t.first[tensor]) * CLIP_ROUND, skip = (long long)(at & 15) / (bf16 ? 2 : 4);
+        p = (Vector *)(at & ~(uintptr_t)15) + vector;
+        from = max(skip - vector * per, 0ll);
+        to = min(skip + t.n[tensor] - vector * per, (long long)CLIP_ROUND * per);
+        whole = from == 0 && to == (long long)CLIP_ROUND * per;
+    }
+    __device__ __forceinline__ void load(Vector (&in)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) in[i] = __builtin_nontemporal_load(p + threadIdx.x + i * CLIP_THREADS);
     }
 };
 
@@ -53,7 +76,7 @@ unsigned pieces_of(const tfno_tensor &t)
 }
 
 __device__ __forceinline__ double square(float x) { return (double)x * (double)x; }
-__device__ __forceinline__ double squares(uint4 v, bool bf16)
+__device__ __forceinline__ double squares(Vector v, bool bf16)
 {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
     double sum = 0.0;
@@ -80,20 +103,26 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_squares(ClipTable t, doub
 {
     __shared__ double meet[CLIP_THREADS / 64];
     double sum = 0.0;
-    for (unsigned piece = blockIdx.x; piece < t.first[t.count]; piece += gridDim.x) {
-        const Piece at(t, piece);
-        const int per = at.bf16 ? 8 : 4;
-        if (at.vector * per >= at.skip && (at.vector + CLIP_ROUND) * per <= at.end) {
-            const uint4 *v = (const uint4 *)at.p + at.vector + threadIdx.x;
-            uint4 in[4];
+    const unsigned end = t.first[t.count];
+    unsigned piece = blockIdx.x;
+    Piece at(t, piece);
+    Vector next[4];
+    if (at.whole) at.load(next);
+    while (piece < end) {
+        const Piece now = at;
+        Vector in[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) in[i] = v[i * CLIP_THREADS];
+        for (int i = 0; i < 4; ++i) in[i] = next[i];
+        if ((piece += gridDim.x) < end) {
+            at.go(t, piece);
+            if (at.whole) at.load(next);
+        }
+        if (now.whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += squares(in[i], at.bf16);
+            for (int i = 0; i < 4; ++i) sum += squares(in[i], now.bf16);
         } else {
-            const long long from = max(at.vector * per, at.skip), to = min((at.vector + CLIP_ROUND) * per, at.end);
-            for (long long i = from + threadIdx.x; i < to; i += CLIP_THREADS)
-                sum += square(at.bf16 ? to_float(((const bf16 *)at.p)[i]) : ((const float *)at.p)[i]);
+            for (long long i = now.from + threadIdx.x; i < now.to; i += CLIP_THREADS)
+                sum += square(now.bf16 ? to_float(((const bf16 *)now.p)[i]) : ((const float *)now.p)[i]);
         }
     }
     sum = block_sum(sum, meet);
@@ -112,31 +141,39 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(ClipTable t, const 
     if (!(all > limit) || isinf(all)) return;      // nothing to clip, or nothing to clip it by
     const double scale = limit / all;
     const unsigned pieces = t.first[t.count];
-    for (unsigned i = blockIdx.x; i < pieces; i += gridDim.x) {
-        const Piece at(t, pieces - 1 - i);
-        const int per = at.bf16 ? 8 : 4;
-        if (at.vector * per >= at.skip && (at.vector + CLIP_ROUND) * per <= at.end) {
-            uint4 *v = (uint4 *)at.p + at.vector + threadIdx.x;
-            uint4 in[4];
+    if (blockIdx.x >= pieces) return;
+    unsigned piece = pieces - 1 - blockIdx.x;
+    Piece at(t, piece);
+    Vector next[4];
+    if (at.whole) at.load(next);
+    for (;;) {
+        const Piece now = at;
+        Vector in[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) in[k] = v[k * CLIP_THREADS];
+        for (int k = 0; k < 4; ++k) in[k] = next[k];
+        const bool more = piece >= gridDim.x;
+        if (more) {
+            at.go(t, piece -= gridDim.x);
+            if (at.whole) at.load(next);
+        }
+        if (now.whole) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 unsigned w[4] = {in[k].x, in[k].y, in[k].z, in[k].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if (at.bf16) w[e] = bf16_pair(scaled(__uint_as_float(w[e] << 16), scale), scaled(__uint_as_float(w[e] & 0xffff0000u), scale));
+                    if (now.bf16) w[e] = bf16_pair(scaled(__uint_as_float(w[e] << 16), scale), scaled(__uint_as_float(w[e] & 0xffff0000u), scale));
                     else w[e] = __float_as_uint(scaled(__uint_as_float(w[e]), scale));
                 }
-                v[k * CLIP_THREADS] = make_uint4(w[0], w[1], w[2], w[3]);
+                __builtin_nontemporal_store(Vector{w[0], w[1], w[2], w[3]}, now.p + threadIdx.x + k * CLIP_THREADS);
             }
         } else {
-            const long long from = max(at.vector * per, at.skip), to = min((at.vector + CLIP_ROUND) * per, at.end);
-            for (long long k = from + threadIdx.x; k < to; k += CLIP_THREADS) {
-                if (at.bf16) store_element((bf16 *)at.p + k, scaled(to_float(((const bf16 *)at.p)[k]), scale));
-                else ((float *)at.p)[k] = scaled(((const float *)at.p)[k], scale);
+            for (long long k = now.from + threadIdx.x; k < now.to; k += CLIP_THREADS) {
+                if (now.bf16) store_element((bf16 *)now.p + k, scaled(to_float(((const bf16 *)now.p)[k]), scale));
+                else ((float *)now.p)[k] = scaled(((const float *)now.p)[k], scale);
             }
         }
+        if (!more) return;
     }
 }
 

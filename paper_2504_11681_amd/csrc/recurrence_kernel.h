@@ -8,6 +8,7 @@
 // e -> a e + R for what comes from later tokens); the maps are joined along the wave by shuffles and along the workgroup in LDS, and each group then walks its
 // tokens from the state that the maps before it give.  Sequences too few to fill the chip are cut into segments, whose maps a kernel of its own finds first.
 #pragma once
+#include "gates.h"
 #include "recurrence.h"
 
 namespace tfno {
@@ -20,17 +21,6 @@ struct RecurrenceShape {
     unsigned channel_blocks, segments, first;
     int segment;                    // tokens of a segment
 };
-
-constexpr float LOG2E = 1.44269504088896340736f;
-
-// 1 / (1 + exp(-z)), and what is left of 1.
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * z)); }
-__device__ __forceinline__ void sigmoid(float z, float &s, float &rest)
-{
-    const float e = __builtin_amdgcn_exp2f(-LOG2E * fabsf(z)), big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
-    s = z < 0.0f ? small : big;
-    rest = z < 0.0f ? big : small;
-}
 
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
