@@ -76,7 +76,7 @@ tfno_status tfno_gated_recurrence(const tfno_gated_recurrence_desc *d, const voi
     if (const size_t need = recurrence_workspace_bytes(a.B, a.T, a.C, a.bf16, false)) {
         void *ws = nullptr;
         if ((st = workspace(need, views, 9, &ws)) != TFNO_OK) return st;
-        a.effects = (float2 *)ws;
+        a.effects = (float *)ws;
     }
     a.lengths = lengths, a.initial = initial, a.y = y, a.final_state = final, a.tape = (float *)tape;
     return status(recurrence_launch(a, (hipStream_t)stream));
@@ -107,7 +107,7 @@ tfno_status tfno_gated_recurrence_backward(const tfno_gated_recurrence_desc *d, 
     if (const size_t need = recurrence_workspace_bytes(a.B, a.T, a.C, a.bf16, true)) {
         void *ws = nullptr;
         if ((st = workspace(need, views, 13, &ws)) != TFNO_OK) return st;
-        a.effects = (float2 *)ws;
+        a.effects = (float *)ws;
     }
     a.lengths = lengths, a.tape = (float *)tape, a.dy = d_y, a.d_final = d_final;
     a.dx = dx, a.dgate = dgate, a.dinput_gate = dinput_gate, a.drate = drate, a.d_initial = d_initial;

@@ -20,7 +20,7 @@ struct RecurrenceArgs {
     float *drate, *d_initial;
     float *states;                      // step: [pool, C]
     const int *slots;
-    float2 *effects;                    // workspace: what each segment does to the state
+    float *effects;                     // workspace: what each segment does to the state, three numbers each
     float *partial;                     // workspace: each workgroup's part of drate
     Strides sx, sgate, sinput, sy, sdx, sdgate, sdinput;      // sy: y, or dy
     int B, T, C, pool;

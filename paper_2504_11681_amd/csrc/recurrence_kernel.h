@@ -28,8 +28,8 @@ struct No { static constexpr bool value = false; };
 // A decay a = exp(l).  Near 1, where states last long, its distance from 1 is what matters: it is kept as -(1 - a), sign bit set, and from the series
 // -l (1 + l/2 + l^2/6 + ...), whose first term left out is l^5 / 720 of the whole, 4e-8 at the border; rounded to a float32 itself, a decay of 0.9999 would be
 // 3e-4 of its distance off, always to the same side.  Elsewhere (and above 1) it is a itself, at least 2^-126.  +0 is a decay of exactly 0, which forgets the state whatever it
-// holds: that of one token where exp(l) rounds to 0 in float32; of a sum of logarithms only where one of them was that of 0, whatever the others make of it.
-constexpr float NOTHING_LEFT = -104.0f, HARDLY = -87.0f;
+// holds: where exp(l) rounds to 0 in float32.
+constexpr float NOTHING_LEFT = -104.0f, HARDLY = -87.0f, LEAST = 1.17549435e-38f;
 struct Decay {
     float at;
     __device__ __forceinline__ Decay() {}
@@ -46,14 +46,7 @@ struct Decay {
         at = near ? p : a;
     }
     // For any l, which is no more than HARDLY.
-    __device__ __forceinline__ void hardly(float l, float nothing = NOTHING_LEFT) { at = l < nothing ? 0.0f : 1.17549435e-38f; }
-    __device__ __forceinline__ explicit Decay(float l, float nothing = NOTHING_LEFT)
-    {
-        float a, less;
-        *this = Decay(l, a, less);
-        if (l < HARDLY) hardly(l, nothing);
-    }
-    __device__ __forceinline__ static Decay of_sum(float l) { return Decay(l, -3.4e38f); }
+    __device__ __forceinline__ void hardly(float l) { at = l < NOTHING_LEFT ? 0.0f : LEAST; }
     __device__ __forceinline__ bool forgets() const { return __float_as_uint(at) == 0; }
     // a h, and a h + u
     __device__ __forceinline__ float of(float h) const { return forgets() ? 0.0f : fmaf(at, h, (int)__float_as_uint(at) < 0 ? h : 0.0f); }
@@ -68,15 +61,14 @@ struct TokenDecay {
         const Decay d(l, a, less);
         at = d.at, whole = (int)__float_as_uint(d.at) < 0 ? 1.0f : 0.0f;
     }
-    __device__ __forceinline__ void hardly(float l) { at = l < NOTHING_LEFT ? 0.0f : 1.17549435e-38f; }
+    __device__ __forceinline__ void hardly(float l) { at = l < NOTHING_LEFT ? 0.0f : LEAST; }
     template <bool RESETS>
     __device__ __forceinline__ float of(float h) const { return RESETS && __float_as_uint(at) == 0 ? 0.0f : fmaf(at, h, whole * h); }
     template <bool RESETS>
     __device__ __forceinline__ float of(float h, float u) const { return RESETS && __float_as_uint(at) == 0 ? u : fmaf(at, h, fmaf(whole, h, u)); }
 };
-// The logarithm of a token's decay, and its part of a sum of them.
+// The logarithm of a token's decay.
 __device__ __forceinline__ float log_of(bool rated, float rate, float gate) { return rated ? -rate * sigmoid(gate) : gate; }
-__device__ __forceinline__ float part_of_sum(float l) { return l < NOTHING_LEFT ? -INFINITY : l; }
 
 __device__ __forceinline__ void set(float &v, float to) { v = to; }
 __device__ __forceinline__ void set(bf16 &v, float to) { v.bits = (unsigned short)(__float_as_uint(to) >> 16); }       // 0 and infinity
@@ -88,9 +80,31 @@ __device__ __forceinline__ void leave_out(bool rated, int t, int last, E (&x)[S]
     for (int j = 0; j < S; ++j)
         if (t + j > last) set(x[j], 0.0f), set(gate[j], rated ? -INFINITY : 0.0f);
 }
+// What tokens in their order do to the state before them, h -> a h + B: their decays' product, its distance from 1 without taking the difference, and B.
+struct Span {
+    float a, less, B;
+    __device__ __forceinline__ void longer(float more, float more_less) { less = fmaf(a, more_less, less), a *= more; }
+    __device__ __forceinline__ Decay decay() const
+    {
+        Decay d;
+        d.at = less > 0.0f && a > 0.5f ? -less : a;
+        return d;
+    }
+};
+// A product that underflows does not forget; one with a 0 in it does.
+__device__ __forceinline__ Span after(Span first, Span second)
+{
+    const float a = first.a * second.a;
+    return Span{a == 0.0f && first.a != 0.0f && second.a != 0.0f ? LEAST : a, fmaf(first.a, second.less, first.less), second.decay().of(first.B, second.B)};
+}
+struct Joined {
+    Decay a;
+    float B;
+    __device__ __forceinline__ float of(float h) const { return a.of(h, B); }
+};
 // Decays that are hardly more than 0, or not: seldom, and then looked for in a wave's whole tile, whose gates are read again.
 template <int S, class E>
-__device__ __forceinline__ bool find_resets(bool rated, float rate, const E (&gate)[S], int t, int last, TokenDecay (&d)[S], float &log)
+__device__ __forceinline__ bool find_resets(bool rated, float rate, const E (&gate)[S], int t, int last, TokenDecay (&d)[S], Span &own)
 {
     bool found = false;
 #pragma unroll
@@ -99,38 +113,29 @@ __device__ __forceinline__ bool find_resets(bool rated, float rate, const E (&ga
         if (l < HARDLY) d[j].hardly(l);
         found = found || l < NOTHING_LEFT;
     }
-    if (found) log = -INFINITY;
+    own.a = found ? 0.0f : own.a == 0.0f ? LEAST : own.a;
     return __any(found);
 }
 
-// What tokens in their order do to the state before them, h -> a h + B, by the decay and by the sum of the logarithms of their decays.
-struct Map {
-    float log, B;
-    __device__ __forceinline__ float of(float h) const { return Decay::of_sum(log).of(h, B); }
-};
-struct Joined {
-    Decay a;
-    float B;
-    __device__ __forceinline__ float of(float h) const { return a.of(h, B); }
-};
-__device__ __forceinline__ Joined joined(Map m) { return Joined{Decay::of_sum(m.log), m.B}; }
-__device__ __forceinline__ Map after(Map first, Map second) { return Map{first.log + second.log, second.of(first.B)}; }
+__device__ __forceinline__ Joined joined(Span s) { return Joined{s.decay(), s.B}; }
 
-// Maps of the groups of a wave, each joined with those before it (behind it, where BACK), without its own; and all of them.
+__device__ __forceinline__ Span moved(Span m, int d, bool back)
+{
+    return Span{back ? __shfl_down(m.a, d, 64) : __shfl_up(m.a, d, 64), back ? __shfl_down(m.less, d, 64) : __shfl_up(m.less, d, 64),
+                back ? __shfl_down(m.B, d, 64) : __shfl_up(m.B, d, 64)};
+}
+// What the groups of a wave do, each joined with those before it (behind it, where BACK), without its own, where `others` is true on return; and all of them, in the last group.
 template <bool BACK>
-__device__ __forceinline__ void join(int lanes, Map own, Map &others, Map &all)
+__device__ __forceinline__ bool join(int lanes, Span own, Span &others, Span &all)
 {
     const int lane = threadIdx.x & 63, order = BACK ? 63 - lane : lane;
     for (int d = lanes; d < 64; d <<= 1) {
-        const Map p = {BACK ? __shfl_down(own.log, d, 64) : __shfl_up(own.log, d, 64), BACK ? __shfl_down(own.B, d, 64) : __shfl_up(own.B, d, 64)};
+        const Span p = moved(own, d, BACK);
         if (order >= d) own = after(p, own);
     }
-    others = {0.0f, 0.0f};
-    if (lanes < 64) {
-        const Map p = {BACK ? __shfl_down(own.log, lanes, 64) : __shfl_up(own.log, lanes, 64), BACK ? __shfl_down(own.B, lanes, 64) : __shfl_up(own.B, lanes, 64)};
-        if (order >= lanes) others = p;
-    }
-    all = own;      // where order is last
+    if (lanes < 64) others = moved(own, lanes, BACK);
+    all = own;
+    return order >= lanes;
 }
 
 // What the workgroup's place in the launch means.
@@ -139,7 +144,8 @@ struct Place {
     bool live;                                                 // the lane has a channel
     __device__ __forceinline__ Place(const RecurrenceArgs &a, const RecurrenceShape &s)
     {
-        const unsigned item = s.first + blockIdx.x, block = item % s.channel_blocks, rest = item / s.channel_blocks;
+        const unsigned place = xcd_contiguous(blockIdx.x, gridDim.x);
+        const unsigned item = s.first + place, block = item % s.channel_blocks, rest = item / s.channel_blocks;
         segment = rest % s.segments;
         b = rest / s.segments;
         lane = threadIdx.x & ((1 << s.lanes_log2) - 1);
@@ -160,12 +166,11 @@ __device__ __forceinline__ float through_segments(const RecurrenceArgs &a, const
     const int n = BACK ? (int)s.segments - 1 - at.segment : at.segment, groups = 64 >> s.lanes_log2, lanes = 1 << s.lanes_log2;
     if (n == 0) return start;
     const int each = (n + groups * WAVES - 1) / (groups * WAVES), from = (at.wave * groups + at.group) * each;
-    Map own = {0.0f, 0.0f};
-    for (int i = from; i < min(from + each, n); ++i) {
-        const float2 m = a.effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - i : i)) * a.C + at.c];
-        own = after(own, Map{m.x, m.y});
-    }
-    Map others, all;
+    Span own = {1.0f, 0.0f, 0.0f};
+    const Span *effects = (const Span *)a.effects;
+    for (int i = from; i < min(from + each, n); ++i)
+        own = after(own, effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - i : i)) * a.C + at.c]);
+    Span others, all;
     join<false>(lanes, own, others, all);
     if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = joined(all);
     __syncthreads();
@@ -236,6 +241,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
 {
     constexpr int WAVES = THREADS / 64;
     __shared__ Joined maps[2][WAVES][64];
+    __shared__ float state[2][64];          // before a tile
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
     const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
@@ -243,6 +249,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
     // the state before the segment
     float carry = a.initial ? a.initial[(long long)at.b * a.C + at.c] : 0.0f;
     carry = through_segments<false, WAVES>(a, s, at, carry, maps[0]);
+    if (at.wave == 0 && at.group == 0) state[1][at.lane] = carry;
     const int last = max(min(at.len, at.end) - 1, 0), tape_rows = (a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE;
     const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
     const Row<E> y(a.y, a.sy, at.b, at.c, ahead);
@@ -261,6 +268,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
     for (int start = at.begin; start < at.end; start += tile, first += tile, buffer ^= 1) {
         const int t = first + ahead;
         if (start >= at.len) {
+            buffer ^= 1;                    // the state stays where it is
             long long k = y.from(first);    // past the sequence: zeros, and nothing on the tape, which is not read there
 #pragma unroll
             for (int j = 0; j < S; ++j) {
@@ -271,9 +279,8 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
         }
         TokenDecay d[S];
         float u[S];
-        Map own = {0.0f, 0.0f};
+        Span own = {1.0f, 0.0f, 0.0f};
         if (first + per_wave - 1 > last) leave_out(rated, t, last, in_x, in_gate);
-        float lowest = 0.0f;
         const unsigned next_x = x.here(), next_gate = gate.here(), next_input = input.here();
         long long kx = x.from(first + tile), kg = gate.from(first + tile), ki = input.from(first + tile);
         // a token's place in the registers is free once its gates are made: the next tile's is asked for there and then, so that its latency lies under all the rest
@@ -286,8 +293,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
                 u[j] = to_float(in_x[j]);
                 if (gated) u[j] *= sigmoid(to_float(in_input[j]));
                 if (normalise) u[j] *= __builtin_amdgcn_sqrtf(less * (2.0f - less));       // 1 - a^2
-                own.log += l;
-                lowest = fminf(lowest, l);
+                own.longer(part, less);
                 if (next.value) {
                     in_x[j] = *x.next(kx, next_x);
                     in_gate[j] = *gate.next(kg, next_gate);
@@ -303,10 +309,10 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
             load(first + tile);
         }
         bool resets = false;
-        if (__any(lowest < HARDLY)) {
+        if (__any(own.a == 0.0f)) {
             E again[S];
             gate.template load<false>(first, ahead, at.c, last, again);
-            resets = find_resets(rated, rate, again, t, last, d, own.log);
+            resets = find_resets(rated, rate, again, t, last, d, own);
         }
         const auto run = [&](float h, auto can, auto each) {
 #pragma unroll
@@ -315,94 +321,98 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
         };
         const auto nothing = [](int, float) {};
         own.B = resets ? run(0.0f, Yes(), nothing) : run(0.0f, No(), nothing);
-        Map before, all;
-        join<false>(lanes, own, before, all);
+        Span before, all;
+        const bool some = join<false>(lanes, own, before, all);
         if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[buffer][at.wave][at.lane] = joined(all);
         __syncthreads();                    // the other buffer is written next: a wave that is here has read it
-        float h = carry;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            h = w == at.wave ? carry : h;
-            carry = maps[buffer][w][at.lane].of(carry);
-        }
-        if (lanes < 64) h = before.of(h);
+        float h = state[buffer ^ 1][at.lane];
+        for (int w = 0; w < at.wave; ++w) h = maps[buffer][w][at.lane].of(h);
+        if (lanes < 64) h = some ? before.decay().of(h, before.B) : h;
         if (a.tape && (t & (RECURRENCE_TAPE - 1)) == 0 && t < at.end && at.live) a.tape[((long long)at.b * tape_rows + t / RECURRENCE_TAPE) * a.C + at.c] = h;
         const unsigned o = y.here();
         long long k = y.from(first);
         if (!resets && first + per_wave <= at.end && first + per_wave <= at.len) {
-            if (at.live) run(h, No(), [&](int, float v) { store_element(y.next(k, o), v); });
+            h = run(h, No(), [&](int, float v) {
+                E *p = y.next(k, o);
+                if (at.live) store_element(p, v);
+            });
         } else {
-            run(h, Yes(), [&](int j, float v) {
+            h = run(h, Yes(), [&](int j, float v) {
                 E *p = y.next(k, o);
                 if (t + j < at.end && at.live) store_element(p, t + j < at.len ? v : 0.0f);
             });
         }
+        // the last group has the state behind the tile; who reads it is past the next barrier
+        if (at.wave == WAVES - 1 && (int)(threadIdx.x & 63) >= 64 - lanes) state[buffer][at.lane] = h;
     }
-    if (a.final_state && at.segment == (int)s.segments - 1 && at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = carry;
+    if (!a.final_state || at.segment != (int)s.segments - 1) return;
+    __syncthreads();
+    if (at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = state[buffer ^ 1][at.lane];
 }
 
-// What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every group finds the map of its part.
+// What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every wave goes through a part of it by itself.
 template <class E, bool ALL, int S, int THREADS, bool BACKWARD>
 __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a, RecurrenceShape s)
 {
     constexpr int WAVES = THREADS / 64;
-    __shared__ float2 maps[WAVES][64];
+    __shared__ Span maps[WAVES][64];
     const Place at(a, s);
     if (at.segment == (BACKWARD ? 0 : (int)s.segments - 1)) return;          // nobody asks
-    const int lanes = 1 << s.lanes_log2, groups = (64 >> s.lanes_log2) * WAVES, part = s.segment / groups;      // a multiple of S: a segment is whole tiles
-    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, part = s.segment / WAVES;      // whole tiles, so whole rounds of a wave
+    const bool rated = ALL || a.rate, gated = !BACKWARD && (ALL || a.input_gate), normalise = !BACKWARD && (ALL || a.normalise);
     const float rate = rated ? a.rate[at.c] : 0.0f;
-    const int stop = min(at.end, at.len), last = max(stop - 1, 0), of_wave = at.begin + at.wave * (64 >> s.lanes_log2) * part, ahead = at.group * part;
-    const long long from = (long long)of_wave + ahead;
-    const E *x = (const E *)a.x + at.b * a.sx.batch + at.c, *gate = (const E *)a.gate + at.b * a.sgate.batch + at.c;
-    const E *input = gated ? (const E *)a.input_gate + at.b * a.sinput.batch + at.c : nullptr, *dy = BACKWARD ? (const E *)a.dy + at.b * a.sy.batch + at.c : nullptr;
-    Map own = {0.0f, 0.0f};
+    const int last = max(min(at.end, at.len) - 1, 0), from = at.begin + at.wave * part, end = min(from + part, min(at.end, at.len));
+    // in: x, or dy
+    const Row<E> in(BACKWARD ? a.dy : a.x, BACKWARD ? a.sy : a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead);
+    const Row<E> input(gated ? a.input_gate : a.gate, gated ? a.sinput : a.sgate, at.b, at.c, ahead);
     E in_x[S], in_gate[S], in_input[S];
-    const auto load = [&](int i) {
-        const long long t = BACKWARD ? from + part - S - i : from + i;
-#pragma unroll
-        for (int j = 0; j < S; ++j) {
-            const long long k = min(max(t + j, 0LL), (long long)last);
-            in_x[j] = BACKWARD ? dy[k * a.sy.token] : x[k * a.sx.token];
-            in_gate[j] = gate[k * a.sgate.token];
-            if (!BACKWARD && gated) in_input[j] = input[k * a.sinput.token];
-        }
+    const auto load = [&](int first) {
+        const auto all = [&](auto full) {
+            in.template load<full.value>(first, ahead, at.c, last, in_x);
+            gate.template load<full.value>(first, ahead, at.c, last, in_gate);
+            if (gated) input.template load<full.value>(first, ahead, at.c, last, in_input);
+        };
+        if (first + per_wave - 1 <= last) all(Yes());
+        else all(No());
     };
-    if (of_wave < stop) load(0);
-    for (int i = 0; i < part && of_wave < stop; i += S) {
-        const long long t = BACKWARD ? from + part - S - i : from + i;
-        Decay d[S];
+    Span sum = {1.0f, 0.0f, 0.0f};
+    const int rounds = end > from ? (end - from + per_wave - 1) / per_wave : 0;
+    if (rounds > 0) load(BACKWARD ? from + (rounds - 1) * per_wave : from);
+    for (int i = 0; i < rounds; ++i) {
+        const int first = from + (BACKWARD ? rounds - 1 - i : i) * per_wave, t = first + ahead;
+        if (first + per_wave - 1 > last) leave_out(rated, t, last, in_x, in_gate);
+        TokenDecay d[S];
         float u[S];
+        Span own = {1.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < S; ++j) {
-            const bool there = t + j < stop;
-            float l = to_float(in_gate[j]), full, less;
-            if (rated) l = -rate * sigmoid(l);
-            l = there ? l : 0.0f;
-            d[j] = Decay(l, full, less);
-            if (l < HARDLY) d[j].hardly(l);
+            float decay, less;
+            const float l = log_of(rated, rate, to_float(in_gate[j]));
+            d[j] = TokenDecay(l, decay, less);
             u[j] = to_float(in_x[j]);
-            if (!BACKWARD && gated) u[j] *= sigmoid(to_float(in_input[j]));
-            if (!BACKWARD && normalise) u[j] *= __builtin_amdgcn_sqrtf(less * (2.0f - less));
-            u[j] = there ? u[j] : 0.0f;
-            own.log += part_of_sum(l);
+            if (gated) u[j] *= sigmoid(to_float(in_input[j]));
+            if (normalise) u[j] *= __builtin_amdgcn_sqrtf(less * (2.0f - less));
+            own.longer(decay, less);
         }
-        load(i + S);
+        if (i + 1 < rounds) load(BACKWARD ? first - per_wave : first + per_wave);
+        if (__any(own.a == 0.0f)) {
+            E again[S];
+            gate.template load<false>(first, ahead, at.c, last, again);
+            find_resets(rated, rate, again, t, last, d, own);
+        }
 #pragma unroll
-        for (int j = 0; j < S; ++j) own.B = BACKWARD ? d[S - 1 - j].of(own.B + u[S - 1 - j]) : d[j].of(own.B, u[j]);
+        for (int j = 0; j < S; ++j) own.B = BACKWARD ? d[S - 1 - j].template of<true>(own.B + u[S - 1 - j]) : d[j].template of<true>(own.B, u[j]);
+        Span others, all;
+        join<BACKWARD>(lanes, own, others, all);
+        sum = after(sum, all);
     }
-    Map others, all;
-    join<BACKWARD>(lanes, own, others, all);
-    if (BACKWARD ? (int)(threadIdx.x & 63) < lanes : (int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = make_float2(all.log, all.B);
+    if (BACKWARD ? (int)(threadIdx.x & 63) < lanes : (int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = sum;
     __syncthreads();
     if (at.wave != 0 || at.group != 0 || !at.live) return;
-    Map joined = {0.0f, 0.0f};
+    Span all = {1.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        const float2 m = maps[BACKWARD ? WAVES - 1 - w : w][at.lane];
-        joined = after(joined, Map{m.x, m.y});
-    }
-    a.effects[((long long)at.b * s.segments + at.segment) * a.C + at.c] = make_float2(joined.log, joined.B);
+    for (int w = 0; w < WAVES; ++w) all = after(all, maps[BACKWARD ? WAVES - 1 - w : w][at.lane]);
+    ((Span *)a.effects)[((long long)at.b * s.segments + at.segment) * a.C + at.c] = all;
 }
 
 template <class E, bool ALL, int S, int THREADS>
@@ -411,12 +421,14 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
     constexpr int WAVES = THREADS / 64;
     __shared__ Joined maps[2][WAVES][64];
     __shared__ float later[2][WAVES][64];
+    __shared__ float gradient[2][64];       // that reaches a tile from its later tokens
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
     const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
     const float rate = rated ? a.rate[at.c] : 0.0f;
     float drate = 0.0f, carry = a.d_final ? a.d_final[(long long)at.b * a.C + at.c] : 0.0f;      // carry: the gradient that reaches the state before the tile from its later tokens
     carry = through_segments<true, WAVES>(a, s, at, carry, maps[0]);
+    if (at.wave == 0 && at.group == 0) gradient[1][at.lane] = carry;
     const int last = max(min(at.len, at.end) - 1, 0), tiles = (at.end - at.begin + tile - 1) / tile;
     const float *tape = a.tape + (long long)at.b * ((a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) * a.C + at.c;
     const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
@@ -454,14 +466,13 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
         // of each token: decay, input, and with the state before it known: dx = D by_x, dinput = D by_input, dl = D by_log, dgate = dl by_gate, drate = dl by_rate
         TokenDecay d[S];
         float u[S], by_x[S], by_input[S], by_log[S], by_gate[S], by_rate[S], g[S];
-        Map own = {0.0f, 0.0f};
+        Span own = {1.0f, 0.0f, 0.0f};
         if (first + per_wave - 1 > last) {
             leave_out(rated, t, last, in_x, in_gate);
 #pragma unroll
             for (int j = 0; j < S; ++j)
                 if (t + j > last) set(in_dy[j], 0.0f), set(in_input[j], 0.0f);
         }
-        float lowest = 0.0f;
         const unsigned next_x = x.here(), next_gate = gate.here(), next_input = input.here(), next_dy = dy.here();
         long long kx = x.from(first - tile), kg = gate.from(first - tile), ki = input.from(first - tile), kd = dy.from(first - tile);
         const auto gates = [&](auto next) {
@@ -475,8 +486,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
                     by_gate[j] = l * rest, by_rate[j] = -sigma;
                 }
                 d[j] = TokenDecay(l, part, less);
-                own.log += l;
-                lowest = fminf(lowest, l);
+                own.longer(part, less);
                 const float in = to_float(in_x[j]);
                 float open = 1.0f, left = 1.0f, by_open = 0.0f;
                 if (gated) {
@@ -509,10 +519,10 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
             gates(No());
         }
         bool resets = false;
-        if (__any(lowest < HARDLY)) {
+        if (__any(own.a == 0.0f)) {
             E again[S];
             gate.template load<false>(first, ahead, at.c, last, again);
-            resets = find_resets(rated, rate, again, t, last, d, own.log);
+            resets = find_resets(rated, rate, again, t, last, d, own);
         }
         const auto local = [&](auto can) {
             float R = 0.0f;
@@ -523,24 +533,19 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
             return R;
         };
         const float R = resets ? local(Yes()) : local(No());
-        Map before, behind, all, all_back;
-        join<false>(lanes, own, before, all);
-        join<true>(lanes, Map{own.log, R}, behind, all_back);
+        Span before, behind, all, all_back;
+        const bool some_before = join<false>(lanes, own, before, all);
+        const bool some_behind = join<true>(lanes, Span{own.a, own.less, R}, behind, all_back);
         if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[buffer][at.wave][at.lane] = joined(all);
         if ((int)(threadIdx.x & 63) < lanes) later[buffer][at.wave][at.lane] = all_back.B;
         __syncthreads();
-        float h = state, D = carry;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float next = maps[buffer][w][at.lane].of(h);
-            h = w < at.wave ? next : h;
+        float h = state, D = gradient[buffer ^ 1][at.lane];
+        for (int w = 0; w < at.wave; ++w) h = maps[buffer][w][at.lane].of(h);
+        for (int w = WAVES - 1; w > at.wave; --w) D = maps[buffer][w][at.lane].a.of(D, later[buffer][w][at.lane]);
+        if (lanes < 64) {
+            h = some_before ? before.decay().of(h, before.B) : h;
+            D = some_behind ? behind.decay().of(D, behind.B) : D;
         }
-#pragma unroll
-        for (int w = WAVES - 1; w >= 0; --w) {
-            D = w == at.wave ? carry : D;
-            carry = maps[buffer][w][at.lane].a.of(carry, later[buffer][w][at.lane]);
-        }
-        if (lanes < 64) h = before.of(h), D = behind.of(D);
         const unsigned ox = dx.here(), og = dgate.here(), oi = dinput.here();
         long long qx = dx.from(first + S - 1), qg = dgate.from(first + S - 1), qi = dinput.from(first + S - 1);
         const auto walk = [&](auto can, auto full) {
@@ -567,8 +572,11 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
         };
         if (!resets && first + per_wave <= at.end && first + per_wave <= at.len) walk(No(), Yes());
         else walk(Yes(), No());
+        // the first group has the gradient that reaches the state before the tile; who reads it is past the next barrier
+        if (at.wave == 0 && at.group == 0) gradient[buffer][at.lane] = D;
     }
-    if (a.d_initial && at.segment == 0 && at.wave == 0 && at.group == 0 && at.live) a.d_initial[(long long)at.b * a.C + at.c] = carry;
+    // that of the first token is the first group's own
+    if (a.d_initial && at.segment == 0 && at.wave == 0 && at.group == 0 && at.live) a.d_initial[(long long)at.b * a.C + at.c] = gradient[buffer ^ 1][at.lane];
     if (!a.drate) return;
     // the groups' parts in their order
     for (int k = lanes; k < 64; k <<= 1) drate += __shfl_xor(drate, k, 64);
