@@ -49,26 +49,26 @@ void in_launches(RecurrenceShape s, long long items, F launch)
     }
 }
 
-template <class E, bool ALL, int THREADS>
+template <class E, int GATES, int THREADS>
 hipError_t forward(const RecurrenceArgs &a, const RecurrenceShape &s, hipStream_t st)
 {
     constexpr int S = RECURRENCE_TOKENS;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
     if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, ALL, S, THREADS, false><<<grid, THREADS, 0, st>>>(a, p); });
-    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence<E, ALL, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
+        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, false><<<grid, THREADS, 0, st>>>(a, p); });
+    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence<E, GATES, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     return hipGetLastError();
 }
 
-template <class E, bool ALL, int THREADS>
+template <class E, int GATES, int THREADS>
 hipError_t backward(RecurrenceArgs a, const RecurrenceShape &s, hipStream_t st)
 {
     constexpr int S = RECURRENCE_TOKENS_BACK;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
     a.partial = a.effects + (s.segments > 1 ? 3 * (size_t)a.B * s.segments * a.C : 0);
     if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, ALL, S, THREADS, true><<<grid, THREADS, 0, st>>>(a, p); });
-    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, ALL, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
+        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, true><<<grid, THREADS, 0, st>>>(a, p); });
+    in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, GATES, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     if (a.drate) {
         const ColumnSumsArgs<1> sums{{{a.partial, a.drate, (unsigned)a.B * s.segments}}, {0, 1}, a.C};
         k_column_sums<1><<<dim3((a.C + 15) / 16, 1), 1024, 0, st>>>(sums);
@@ -76,13 +76,13 @@ hipError_t backward(RecurrenceArgs a, const RecurrenceShape &s, hipStream_t st)
     return hipGetLastError();
 }
 
-template <class E, bool ALL>
+template <class E, int GATES>
 hipError_t run(const RecurrenceArgs &a, bool back, hipStream_t st)
 {
     const Geometry g = shape_of(a.B, a.T, a.C, a.bf16, back, back ? RECURRENCE_TOKENS_BACK : RECURRENCE_TOKENS);
-    if (g.threads == 256) return back ? backward<E, ALL, 256>(a, g.s, st) : forward<E, ALL, 256>(a, g.s, st);
-    if (g.threads == 1024) return forward<E, ALL, 1024>(a, g.s, st);
-    return back ? backward<E, ALL, 512>(a, g.s, st) : forward<E, ALL, 512>(a, g.s, st);
+    if (g.threads == 256) return back ? backward<E, GATES, 256>(a, g.s, st) : forward<E, GATES, 256>(a, g.s, st);
+    if (g.threads == 1024) return forward<E, GATES, 1024>(a, g.s, st);
+    return back ? backward<E, GATES, 512>(a, g.s, st) : forward<E, GATES, 512>(a, g.s, st);
 }
 
 constexpr int STEP_THREADS = 256;
@@ -164,9 +164,9 @@ bool fours(const RecurrenceArgs &a)
 
 static hipError_t typed(const RecurrenceArgs &a, bool back, hipStream_t s)
 {
-    const bool all = a.rate && a.input_gate && a.normalise;
-    if (a.bf16) return all ? run<bf16, true>(a, back, s) : run<bf16, false>(a, back, s);
-    return all ? run<float, true>(a, back, s) : run<float, false>(a, back, s);
+    const bool all = a.rate && a.input_gate && a.normalise, none = !a.rate && !a.input_gate && !a.normalise;
+    if (a.bf16) return all ? run<bf16, ALL>(a, back, s) : none ? run<bf16, NONE>(a, back, s) : run<bf16, ANY>(a, back, s);
+    return all ? run<float, ALL>(a, back, s) : none ? run<float, NONE>(a, back, s) : run<float, ANY>(a, back, s);
 }
 
 hipError_t recurrence_launch(const RecurrenceArgs &a, hipStream_t s) { return typed(a, false, s); }

@@ -15,7 +15,8 @@ namespace tfno {
 
 constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;      // of a group in a tile: what waits in registers fits four waves a SIMD
 
-// ALL of a kernel: with rates, an input gate and `normalise`, as nearly all calls have them; else each is asked for.
+// What a kernel knows of its gates: ALL has rates, an input gate and `normalise`, NONE neither; ANY asks.
+enum { ANY = 0, ALL = 1, NONE = 2 };
 struct RecurrenceShape {
     int lanes_log2;                 // lanes of a group
     unsigned channel_blocks, segments, first;
@@ -168,8 +169,17 @@ __device__ __forceinline__ float through_segments(const RecurrenceArgs &a, const
     const int each = (n + groups * WAVES - 1) / (groups * WAVES), from = (at.wave * groups + at.group) * each;
     Span own = {1.0f, 0.0f, 0.0f};
     const Span *effects = (const Span *)a.effects;
-    for (int i = from; i < min(from + each, n); ++i)
-        own = after(own, effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - i : i)) * a.C + at.c]);
+    for (int i = from; i < min(from + each, n); i += 4) {          // four on their way at once
+        Span some[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int which = min(i + k, n - 1);
+            some[k] = effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - which : which)) * a.C + at.c];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i + k < min(from + each, n)) own = after(own, some[k]);
+    }
     Span others, all;
     join<false>(lanes, own, others, all);
     if ((int)(threadIdx.x & 63) >= 64 - lanes) maps[at.wave][at.lane] = joined(all);
@@ -236,7 +246,7 @@ struct Row {
     }
 };
 
-template <class E, bool ALL, int S, int THREADS>
+template <class E, int GATES, int S, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, RecurrenceShape s)
 {
     constexpr int WAVES = THREADS / 64;
@@ -244,7 +254,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
     __shared__ float state[2][64];          // before a tile
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
-    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES == ALL : a.normalise;
     const float rate = rated ? a.rate[at.c] : 0.0f;
     // the state before the segment
     float carry = a.initial ? a.initial[(long long)at.b * a.C + at.c] : 0.0f;
@@ -351,7 +361,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
 }
 
 // What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every wave goes through a part of it by itself.
-template <class E, bool ALL, int S, int THREADS, bool BACKWARD>
+template <class E, int GATES, int S, int THREADS, bool BACKWARD>
 __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a, RecurrenceShape s)
 {
     constexpr int WAVES = THREADS / 64;
@@ -359,7 +369,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a
     const Place at(a, s);
     if (at.segment == (BACKWARD ? 0 : (int)s.segments - 1)) return;          // nobody asks
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, part = s.segment / WAVES;      // whole tiles, so whole rounds of a wave
-    const bool rated = ALL || a.rate, gated = !BACKWARD && (ALL || a.input_gate), normalise = !BACKWARD && (ALL || a.normalise);
+    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = !BACKWARD && (GATES ? GATES == ALL : a.input_gate != nullptr), normalise = !BACKWARD && (GATES ? GATES == ALL : a.normalise);
     const float rate = rated ? a.rate[at.c] : 0.0f;
     const int last = max(min(at.end, at.len) - 1, 0), from = at.begin + at.wave * part, end = min(from + part, min(at.end, at.len));
     // in: x, or dy
@@ -415,7 +425,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a
     ((Span *)a.effects)[((long long)at.b * s.segments + at.segment) * a.C + at.c] = all;
 }
 
-template <class E, bool ALL, int S, int THREADS>
+template <class E, int GATES, int S, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, RecurrenceShape s)
 {
     constexpr int WAVES = THREADS / 64;
@@ -424,7 +434,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
     __shared__ float gradient[2][64];       // that reaches a tile from its later tokens
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
-    const bool rated = ALL || a.rate, gated = ALL || a.input_gate, normalise = ALL || a.normalise;
+    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES == ALL : a.normalise;
     const float rate = rated ? a.rate[at.c] : 0.0f;
     float drate = 0.0f, carry = a.d_final ? a.d_final[(long long)at.b * a.C + at.c] : 0.0f;      // carry: the gradient that reaches the state before the tile from its later tokens
     carry = through_segments<true, WAVES>(a, s, at, carry, maps[0]);
