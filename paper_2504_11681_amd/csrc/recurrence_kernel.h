@@ -260,6 +260,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
     float carry = a.initial ? a.initial[(long long)at.b * a.C + at.c] : 0.0f;
     carry = through_segments<false, WAVES>(a, s, at, carry, maps[0]);
     if (at.wave == 0 && at.group == 0) state[1][at.lane] = carry;
+    if (a.final_state && at.len == 0 && at.segment == 0 && at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = carry;
     const int last = max(min(at.len, at.end) - 1, 0), tape_rows = (a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE;
     const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
     const Row<E> y(a.y, a.sy, at.b, at.c, ahead);
@@ -352,12 +353,10 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
                 if (t + j < at.end && at.live) store_element(p, t + j < at.len ? v : 0.0f);
             });
         }
+        if (a.final_state && at.live && t < at.len && t + S >= at.len) a.final_state[(long long)at.b * a.C + at.c] = h;
         // the last group has the state behind the tile; who reads it is past the next barrier
         if (at.wave == WAVES - 1 && (int)(threadIdx.x & 63) >= 64 - lanes) state[buffer][at.lane] = h;
     }
-    if (!a.final_state || at.segment != (int)s.segments - 1) return;
-    __syncthreads();
-    if (at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = state[buffer ^ 1][at.lane];
 }
 
 // What each segment does to the state (to the gradient that comes from later tokens, where BACKWARD): every wave goes through a part of it by itself.

@@ -668,3 +668,80 @@ def test_another_stream_and_a_graph(tfno):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
         assert all(torch.equal(a, b) for a, b in zip(block(tfno, p, *data[1]), eager[1]))
+
+
+def test_two_graphs_share_the_workspace(tfno):
+    """Two captured runs of different sizes, replayed by turns with eager calls between them: nothing is expected to be left of an earlier call."""
+    gen = torch.Generator("cuda").manual_seed(7)
+    runs = []
+    for C, T in ((32, 1500), (80, 300)):
+        p = parameters(C, gen)
+        u, r = torch.randn(2, T, C, generator=gen, device="cuda"), torch.randn(2, T, C, generator=gen, device="cuda")
+        want = [t.clone() for t in block(tfno, p, u, r)]
+        runs.append((p, u, r, want))
+    for p, u, r, _ in runs:                                     # the larger workspace is there before anything is captured
+        block(tfno, p, u, r)
+    torch.cuda.synchronize()
+    graphs = []
+    for p, u, r, _ in runs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            graphs.append((graph, block(tfno, p, u, r)))
+    for turn in range(6):
+        graph, out = graphs[turn % 2]
+        for t in out:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, runs[turn % 2][3])), turn
+        p, u, r, want = runs[(turn + 1) % 2]
+        assert all(torch.equal(a, b) for a, b in zip(block(tfno, p, u, r), want)), turn
+
+
+def test_more_sequences_than_one_launch_takes(tfno):
+    B = 2 ** 21 + 3
+    gen = torch.Generator("cuda").manual_seed(8)
+    x, gate = torch.randn(B, 2, 1, generator=gen, device="cuda"), -torch.rand(B, 2, 1, generator=gen, device="cuda")
+    h, y, final = torch.randn(B, 1, generator=gen, device="cuda"), torch.empty(B, 2, 1, device="cuda"), torch.empty(B, 1, device="cuda")
+    tape = tfno.gated_recurrence_tape(x)
+    tfno.gated_recurrence(x, gate, None, None, y, initial_state=h, final_state=final, tape=tape)
+    a = gate.double().exp()
+    first = a[:, 0] * h.double() + x[:, 0].double()
+    near("y", y, torch.stack((first, a[:, 1] * first + x[:, 1].double()), 1), oracle.REL[F32])
+    assert torch.equal(final, y[:, 1])
+    dx, dgate, d_initial = torch.empty_like(x), torch.empty_like(x), torch.empty_like(h)
+    tfno.gated_recurrence_backward(x, gate, None, None, torch.ones_like(x), dx, dgate, None, None, tape, d_initial_state=d_initial)
+    near("dx", dx, torch.stack((1 + a[:, 1], torch.ones_like(a[:, 1])), 1), oracle.REL[F32])
+    near("dinitial", d_initial, a[:, 0] * (1 + a[:, 1]), oracle.REL[F32])
+    states, o = h.clone(), torch.empty(B, 1, device="cuda")
+    tfno.gated_recurrence_step(x[:, 0], gate[:, 0], None, None, states, o)
+    assert torch.equal(states, o)
+    near("step", o, first, oracle.REL[F32])
+
+
+def test_norms_offsets_past_32_bits(tfno):
+    far, T, C = 2 ** 31 + 64, 9, 64
+    memory = torch.empty(far + 2 * T * C, dtype=BF16, device="cuda")
+    x = between_inputs(BF16, F32, 2, T, C, "token", "silu", seed=8)
+    x["y"] = memory.as_strided((2, T, C), (far, C, 1)).copy_(x["y"])
+    n = memory[T * C:].as_strided((2, T, C), (far, C, 1))
+    r = empty(x["r"])
+    tfno.block_norm(*(x[k] for k in PARTS), r, n, **x["ways"])
+    w = between_wanted(x)
+    near("r", r, w[0], oracle.REL[F32])
+    near("n", n, w[1], oracle.REL[BF16])
+
+
+def test_norms_gradient_without_sums_needs_no_workspace(tfno):
+    x = between_inputs(BF16, F32, 3, 50, 96, "token", "silu", seed=9)
+    d = [empty(x[n]) for n in PARTS]
+    tfno.block_norm_backward(*(x[n] for n in PARTS), x["d_r"], x["d_n"], *d, **x["ways"])
+    kept = tfno._workspace
+    try:
+        tfno.set_workspace(None)
+        again = [empty(x[n]) for n in PARTS[:3]]
+        tfno.block_norm_backward(*(x[n] for n in PARTS), x["d_r"], x["d_n"], *again, None, None, **x["ways"])
+        assert tfno._workspace is None
+    finally:
+        tfno.set_workspace(kept)
+    assert all(torch.equal(a, b) for a, b in zip(again, d))
