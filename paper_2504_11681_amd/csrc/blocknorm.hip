@@ -64,7 +64,7 @@ hipError_t launch(const BlockNormArgs &a, hipStream_t st)
         sums.first[2] = sums.first[1] + (a.dw_before ? 1 : 0);
         sums.first[3] = sums.first[2] + (a.dgate && a.gate_kind == GATE_CHANNEL ? 1 : of_sequences ? a.B : 0);
         sums.C = a.C;
-        if (sums.first[3]) k_column_sums<3><<<dim3((a.C + 15) / 16, sums.first[3]), 1024, 0, st>>>(sums);
+        column_sums(sums, st);
     }
     return hipGetLastError();
 }

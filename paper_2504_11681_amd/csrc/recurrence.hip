@@ -71,7 +71,7 @@ hipError_t backward(RecurrenceArgs a, const RecurrenceShape &s, hipStream_t st)
     in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, GATES, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     if (a.drate) {
         const ColumnSumsArgs<1> sums{{{a.partial, a.drate, (unsigned)a.B * s.segments}}, {0, 1}, a.C};
-        k_column_sums<1><<<dim3((a.C + 15) / 16, 1), 1024, 0, st>>>(sums);
+        column_sums(sums, st);
     }
     return hipGetLastError();
 }
