@@ -22,6 +22,7 @@ tfno_status recurrence_sizes(const tfno_gated_recurrence_desc *d)
     if (!d) return TFNO_ERR_NULL;
     if (!type_ok(d->dtype) || d->B < 0 || d->T < 0 || d->C < 1 || d->T > (1 << 30)) return TFNO_ERR_SHAPE;
     if ((long double)d->B * std::max(1.0L, ((long double)d->T + 31) / 32) * d->C >= 1099511627776.0L || d->C > (1 << 28)) return TFNO_ERR_SHAPE;
+    if ((long double)d->B * ((d->C + 31) / 32) >= 2147483648.0L) return TFNO_ERR_SHAPE;       // workgroups
     return TFNO_OK;
 }
 
@@ -29,7 +30,7 @@ tfno_status recurrence_sizes(const tfno_gated_recurrence_desc *d)
 bool tokens_near(int T, std::initializer_list<const tfno_strides *> of)
 {
     for (const tfno_strides *s : of)
-        if (T > 1 && s->token >= (1 << 23)) return false;
+        if (T > 1 && s->token >= (1 << 24)) return false;
     return true;
 }
 

@@ -7,7 +7,8 @@
 // Bound by bytes: every row is read once and written once.  A group of lanes (up to a whole workgroup) holds a row in registers, eight or sixteen values a lane;
 // the backward pass makes s again from y, r and the gate instead of reading it back: as many bytes, and s as it was before its rounding.  Sums over
 // tokens (of the weights' gradients, of a gate that tokens share) stay in registers over a group's rows, then a workgroup leaves one row of each in the
-// workspace, which k_column_sums adds up in their order.
+// workspace, which k_column_sums adds up in their order.  A group's rows lie one behind the other, and the next one's values wait in registers as they stand in memory (16 x 1024
+// tokens of 2048 in BF16 with a float32 residual: forward 173 -> 79 us, 403 MB, 5.1 TB/s, with a row a workgroup and its weights read for each; gradient 187 -> 140, 604 MB).
 #pragma once
 #include "blocknorm.h"
 #include "gates.h"

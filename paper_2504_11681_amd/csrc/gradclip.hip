@@ -2,7 +2,7 @@
 //
 // Bound by bytes: all tensors are read once for the norm, and read and written where there is something to clip.  Squares are added up in float64, so
 // that no value over- or underflows and no order matters beyond a float32's last bit.  A launch takes a table of tensors, cut into pieces that its
-// workgroups take by turns, all of them close together in memory (each its own stretch: 118 -> 133 us for 486 MB); the second launch adds up what the workgroups of the
+// workgroups take by turns, all of them close together in memory (each its own stretch: 118 -> 133 us for 510 MB); the second launch adds up what the workgroups of the
 // first left, each the same way, and goes through the pieces from the end.
 #include "gradclip.h"
 
@@ -15,7 +15,7 @@ namespace {
 constexpr int CLIP_THREADS = 256, CLIP_TENSORS = 128, CLIP_BLOCKS = 2048;
 constexpr int CLIP_ROUND = CLIP_THREADS * 4;        // vectors of 16 bytes in a piece
 
-// Loads and stores that leave the last-level cache alone: what is read next is as large as what it holds (both passes over 486 MB in BF16 314 -> 277 us; the stores alone 293).
+// Loads and stores that leave the last-level cache alone: what is read next is as large as what it holds (both passes over 510 MB in BF16 314 -> 277 us; the stores alone 293).
 typedef unsigned Vector __attribute__((ext_vector_type(4)));
 
 struct ClipTable {

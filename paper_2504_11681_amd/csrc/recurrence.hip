@@ -16,7 +16,8 @@ struct Geometry {
 };
 
 // Lanes of a group, threads of a workgroup and segments: whole lines of channels and small workgroups where these fill the chip, else more of a sequence in a workgroup, then half
-// lines, then segments.
+// lines, then segments, in workgroups that are small again (one sequence of 16384 tokens of 512 channels: 64 segments 29 us, 32 31, 128 35; 5 x 777 of 205 in float32 39 -> 32
+// with 256 threads instead of 512).
 Geometry shape_of(int B, int T, int C, bool bf16, bool back, int tokens)
 {
     Geometry g{};

@@ -2,18 +2,22 @@
 //
 //   D_t = dy_t + a_{t+1} D_{t+1},   du = D,   dl = D a h_{t-1} - D x sigmoid(input_gate) a^2 / sqrt(1 - a^2).
 //
-// Every input is read once and every output written once; the gates of a value are some 60 instructions, five of them of the slow kind (exp2, 1/x, square root), so with BF16
-// both sides are near.  A workgroup takes `lanes` neighbouring channels and walks through a sequence in tiles; a tile is shared out over time among groups of
-// lanes, each with S tokens in a row, whose loads are all under way while the tile before is worked on.  A group makes of its tokens one map h -> a h + B (backward also
-// e -> a e + R for what comes from later tokens); the maps are joined along the wave by shuffles and along the workgroup in LDS, and each group then walks its
-// tokens from the state that the maps before it give.  Sequences too few to fill the chip are cut into segments, whose maps a kernel of its own finds first.
+// Every input is read once and every output written once; a value takes 46 vector instructions (backward 100), five of them of the slow kind (exp2, 1/x, square root), so with
+// BF16 both sides are near: 256 x 1024 tokens of 128 channels 63 us (269 MB, 4.3 TB/s; vector pipes 50 us).  A workgroup takes 64 or 32 neighbouring channels and walks through a sequence
+// in tiles; a tile is shared out over time among groups of as many lanes, each with S tokens in a row, whose loads are all under way while the tile before is worked on.  A
+// group makes of its tokens one map h -> a h + B (backward also e -> a e + R for what comes from later tokens); the maps are joined along the wave by shuffles and along the
+// workgroup in LDS, and each group then walks its tokens from the state that the maps before it give.  Sequences too few to fill the chip are cut into segments, whose maps a
+// kernel of its own finds first.  One channel a lane: with two the maps of a lane are joined twice and the gradient has 256 registers.  Workgroups that are neighbours in memory share an XCD: half lines of
+// channels were read twice otherwise (4 x 2048 tokens of 2048 channels, both directions, 144 -> 131 us).
 #pragma once
 #include "gates.h"
 #include "recurrence.h"
 
 namespace tfno {
 
-constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;      // of a group in a tile: what waits in registers fits four waves a SIMD
+// Tokens of a group in a tile.  Forward four waves a SIMD have registers for that (with 16, which two have, 77 -> 85 us for the batch above); backward two (with 4 and four waves
+// 131 -> 137 us for the two directions above: twice the joining).
+constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;
 
 // What a kernel knows of its gates: ALL has rates, an input gate and `normalise`, NONE neither; ANY asks.
 enum { ANY = 0, ALL = 1, NONE = 2 };
@@ -191,7 +195,7 @@ __device__ __forceinline__ float through_segments(const RecurrenceArgs &a, const
 }
 
 // A tensor's elements of the thread: S tokens from `first` (of the wave) + `ahead` (of its group) on, in one channel.  A token's address is scalar, a lane's offset from it has 32
-// bits of bytes, the same for all: tokens of a wave, 64 at most, are less than 2^23 elements apart.
+// bits of bytes, the same for all: tokens of a wave, 16 at most, are less than 2^24 elements apart.
 template <class E>
 struct Row {
     char *at;                   // of the sequence

@@ -67,11 +67,11 @@ def test_recurrence_refuses(L, workspace):
         assert call(fn, None, args) == tfno.ERR_NULL
         for n in needed:
             assert call(fn, recurrence_desc(), args, **{n: None}) == tfno.ERR_NULL, n
-        for bad in (dict(dtype=2), dict(dtype=-1), dict(B=-1), dict(T=-1), dict(C=0), dict(T=(1 << 30) + 1), dict(C=(1 << 28) + 1), dict(B=1 << 20, C=1 << 20),
+        for bad in (dict(dtype=2), dict(dtype=-1), dict(B=-1), dict(T=-1), dict(C=0), dict(T=(1 << 30) + 1), dict(C=(1 << 28) + 1), dict(B=1 << 20, C=1 << 20), dict(B=(1 << 31) - 1, C=33),
                     dict(x=tfno._Strides(-1, 64, 0)), dict(gate=tfno._Strides(1 << 40, 64, 0))):
             assert call(fn, recurrence_desc(**bad), args) == tfno.ERR_SHAPE, bad
         for n in ("x", "gate", "input_gate", "y"):
-            assert call(fn, recurrence_desc(**{n: tfno._Strides(0, 1 << 23, 0)}), args) == tfno.ERR_UNSUPPORTED, n
+            assert call(fn, recurrence_desc(**{n: tfno._Strides(0, 1 << 24, 0)}), args) == tfno.ERR_UNSUPPORTED, n
         for n in needed:
             assert call(fn, recurrence_desc(), args, **{n: args[n] + 1}) == tfno.ERR_ALIGN, n
         assert call(fn, recurrence_desc(), args, tape=args["tape"] + 128) == tfno.ERR_ALIGN
