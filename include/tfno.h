@@ -421,7 +421,7 @@ tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void
  * gradients of x, gate and, where not NULL, of input_gate (NULL only with input_gate), rate (float32, summed over all tokens) and initial.  Of l = 0 and `normalise`, where the root has no
  * slope, only what goes through the decay counts.
  *
- * Sizes: B, T >= 0, 1 <= C <= 2^28, T <= 2^30, B C and B ceil(T / 32) C less than 2^40, B ceil(C / 32) less than 2^31 (TFNO_ERR_SHAPE), tokens of every tensor less than 2^24 elements apart (else
+ * Sizes: B, T >= 0, 1 <= C <= 2^28, T <= 2^30, B C and B ceil(T / 8) C less than 2^40, B ceil(C / 32) less than 2^31 (TFNO_ERR_SHAPE), tokens of every tensor less than 2^24 elements apart (else
  * TFNO_ERR_UNSUPPORTED).  Strides of heads are not used.
  */
 typedef struct {

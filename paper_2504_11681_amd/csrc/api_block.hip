@@ -21,7 +21,7 @@ tfno_status recurrence_sizes(const tfno_gated_recurrence_desc *d)
 {
     if (!d) return TFNO_ERR_NULL;
     if (!type_ok(d->dtype) || d->B < 0 || d->T < 0 || d->C < 1 || d->T > (1 << 30)) return TFNO_ERR_SHAPE;
-    if ((long double)d->B * std::max(1.0L, ((long double)d->T + 31) / 32) * d->C >= 1099511627776.0L || d->C > (1 << 28)) return TFNO_ERR_SHAPE;
+    if ((long double)d->B * std::max(1.0L, ((long double)d->T + 7) / 8) * d->C >= 1099511627776.0L || d->C > (1 << 28)) return TFNO_ERR_SHAPE;
     if ((long double)d->B * ((d->C + 31) / 32) >= 2147483648.0L) return TFNO_ERR_SHAPE;       // workgroups
     return TFNO_OK;
 }
@@ -69,7 +69,7 @@ tfno_status tfno_gated_recurrence(const tfno_gated_recurrence_desc *d, const voi
     RecurrenceArgs a = recurrence_args(d, x, gate, input_gate, rate);
     const int elem = a.bf16 ? 2 : 4;
     const long long states = (long long)a.B * a.C;
-    const View views[] = {tokens(y, elem, a.B, a.T, a.C, d->y), flat(final, states), flat(a.T > 0 ? tape : nullptr, (long long)recurrence_tape_bytes(a.B, a.T, a.C), 1),
+    const View views[] = {tokens(y, elem, a.B, a.T, a.C, d->y), flat(final, states), flat(a.T > 0 ? tape : nullptr, (long long)recurrence_tape_bytes(a.B, a.T, a.C, a.bf16), 1),
                           tokens(x, elem, a.B, a.T, a.C, d->x), tokens(gate, elem, a.B, a.T, a.C, d->gate),
                           tokens(input_gate, elem, a.B, a.T, a.C, d->input_gate), flat(rate, a.C), flat(initial, states), flat(lengths, a.B)};
     if ((st = check_views(views, 3, nullptr, 0)) != TFNO_OK) return st;
@@ -102,7 +102,7 @@ tfno_status tfno_gated_recurrence_backward(const tfno_gated_recurrence_desc *d, 
                           tokens(x, elem, a.B, a.T, a.C, d->x), tokens(gate, elem, a.B, a.T, a.C, d->gate),
                           tokens(input_gate, elem, a.B, a.T, a.C, d->input_gate), tokens(d_y, elem, a.B, a.T, a.C, d->y), flat(rate, a.C),
                           flat(a.B > 0 ? d_final : nullptr, states), flat(a.B > 0 ? lengths : nullptr, a.B),
-                          flat(empty ? nullptr : tape, (long long)recurrence_tape_bytes(a.B, a.T, a.C), 1)};
+                          flat(empty ? nullptr : tape, (long long)recurrence_tape_bytes(a.B, a.T, a.C, a.bf16), 1)};
     if ((st = check_views(views, 5, nullptr, 0)) != TFNO_OK) return st;
     if (!aligned(tape, 256)) return TFNO_ERR_ALIGN;
     if (const size_t need = recurrence_workspace_bytes(a.B, a.T, a.C, a.bf16, true)) {
@@ -117,7 +117,7 @@ tfno_status tfno_gated_recurrence_backward(const tfno_gated_recurrence_desc *d, 
 
 size_t tfno_gated_recurrence_tape_bytes(const tfno_gated_recurrence_desc *d)
 {
-    return recurrence_sizes(d) == TFNO_OK ? recurrence_tape_bytes(d->B, d->T, d->C) : 0;
+    return recurrence_sizes(d) == TFNO_OK ? recurrence_tape_bytes(d->B, d->T, d->C, d->dtype == TFNO_BF16) : 0;
 }
 
 size_t tfno_gated_recurrence_workspace_bytes(const tfno_gated_recurrence_desc *d, int backward)

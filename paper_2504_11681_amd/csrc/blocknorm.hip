@@ -8,9 +8,6 @@ namespace tfno {
 
 namespace {
 
-// Workgroups of the backward kernel, at most: each leaves a row of every sum over tokens.  As many as are there at once: three waves a SIMD where tokens have gates of their own (131072 heads
-// of 128, both directions: 70 us, with 512 76), else two (16 x 1024 tokens of 2048: 231, with 768 240).
-unsigned most_blocks(int C, int gate_kind) { return std::max(256u, std::min(gate_kind == GATE_TOKEN ? 768u : 512u, (4u << 20) / (unsigned)C)); }
 constexpr unsigned FORWARD_WAVES = 256 * 20;         // five waves a SIMD, which its registers allow
 
 int group_log2_of(int C)
@@ -20,6 +17,9 @@ int group_log2_of(int C)
     return g;
 }
 int threads_of(int group_log2) { return group_log2 > 6 ? 1 << group_log2 : BLOCK_NORM_THREADS; }
+// Workgroups of the backward kernel, at most: each leaves a row of every sum over tokens.  As many as are there at once: three waves a SIMD where tokens have gates of their own (131072 heads
+// of 128, both directions: 70 us, with two 76), else two (16 x 1024 tokens of 2048: 231, with three 240).
+unsigned most_blocks(int C, int gate_kind) { return 1024u * (gate_kind == GATE_TOKEN ? 3 : 2) * 64 / threads_of(group_log2_of(C)); }
 
 // Parts of a sequence for workgroups that sum up a gate's gradient: as many as fill the launch, none without rows.
 unsigned parts_of(int B, int T, int C)
@@ -58,9 +58,9 @@ hipError_t launch(const BlockNormArgs &a, hipStream_t st)
     if (BACKWARD) {
         ColumnSumsArgs<3> sums{};
         const bool of_sequences = a.gate_kind == GATE_SEQUENCE && a.dgate && !s.whole && grid;
-        sums.kind[0] = {s.part_after, a.dw_after, grid};
-        sums.kind[1] = {s.part_before, a.dw_before, grid};
-        sums.kind[2] = {s.part_gate, (float *)a.dgate, of_sequences ? s.parts : grid};
+        sums.kind[0] = {s.part_after, a.dw_after, grid, grid};
+        sums.kind[1] = {s.part_before, a.dw_before, grid, grid};
+        sums.kind[2] = {s.part_gate, (float *)a.dgate, of_sequences ? s.parts : grid, of_sequences ? s.parts * a.B : grid};
         sums.first[1] = a.dw_after ? 1 : 0;
         sums.first[2] = sums.first[1] + (a.dw_before ? 1 : 0);
         sums.first[3] = sums.first[2] + (a.dgate && a.gate_kind == GATE_CHANNEL ? 1 : of_sequences ? a.B : 0);

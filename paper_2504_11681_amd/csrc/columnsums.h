@@ -7,7 +7,7 @@ namespace tfno {
 struct ColumnSums {
     const float *part;      // [jobs][rows][C]
     float *out;             // [jobs][C]
-    unsigned rows;
+    unsigned rows, all;     // of a job, and of all of them: the last one may have less
 };
 template <int KINDS>
 struct ColumnSumsArgs {
@@ -31,8 +31,9 @@ __global__ __launch_bounds__(1024) void k_column_sums(ColumnSumsArgs<KINDS> a)
     float sum[V] = {};
     if (c < (unsigned)a.C) {
         const float *p = job.part + at * job.rows * a.C + c;
+        const unsigned rows = min(job.rows, job.all - (unsigned)at * job.rows);
 #pragma unroll 8
-        for (unsigned r = group; r < job.rows; r += groups) {
+        for (unsigned r = group; r < rows; r += groups) {
             if constexpr (V == 4) {
                 const float4 v = *reinterpret_cast<const float4 *>(p + (size_t)r * a.C);
                 sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;

@@ -4,8 +4,6 @@
 
 namespace tfno {
 
-constexpr int RECURRENCE_TAPE = 32;       // tokens between two states on the tape
-
 struct RecurrenceArgs {
     const void *x, *gate, *input_gate;  // [B, T, C]; input_gate may be NULL (open)
     const float *rate;                  // [C], or NULL: gate is the logarithm of the decay itself
@@ -13,7 +11,7 @@ struct RecurrenceArgs {
     const float *initial;               // [B, C] or NULL
     void *y;                            // forward
     float *final_state;                 // [B, C] or NULL
-    float *tape;                        // [B, ceil(T / RECURRENCE_TAPE), C]: the state before each block of tokens; NULL: none is kept
+    float *tape;                        // [B, ceil(T / 2^tape_log2), C]: the state before every so many tokens; NULL: none is kept
     const void *dy;                     // backward
     const float *d_final;               // [B, C] or NULL
     void *dx, *dgate, *dinput_gate;
@@ -23,14 +21,14 @@ struct RecurrenceArgs {
     float *effects;                     // workspace: what each segment does to the state, three numbers each
     float *partial;                     // workspace: each workgroup's part of drate
     Strides sx, sgate, sinput, sy, sdx, sdgate, sdinput;      // sy: y, or dy
-    int B, T, C, pool;
+    int B, T, C, pool, tape_log2;
     bool bf16, normalise;
 };
 
 hipError_t recurrence_launch(const RecurrenceArgs &a, hipStream_t s);
 hipError_t recurrence_backward_launch(const RecurrenceArgs &a, hipStream_t s);
 hipError_t recurrence_step_launch(const RecurrenceArgs &a, hipStream_t s);
-size_t recurrence_tape_bytes(int B, int T, int C);
+size_t recurrence_tape_bytes(int B, int T, int C, bool bf16);
 size_t recurrence_workspace_bytes(int B, int T, int C, bool bf16, bool backward);
 
 }  // namespace tfno

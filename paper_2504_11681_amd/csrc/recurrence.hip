@@ -27,18 +27,34 @@ Geometry shape_of(int B, int T, int C, bool bf16, bool back, int tokens)
     const auto tile = [&] { return (g.threads >> s.lanes_log2) * tokens; };
     while (s.lanes_log2 > 5 && C <= 1 << (s.lanes_log2 - 1)) --s.lanes_log2;
     constexpr long long full = 256 * 1024;       // threads: four waves a SIMD
-    if (blocks() * g.threads < full && tile() < T) g.threads = 512;
+    // sequences enough for waves that share little or nothing (BF16, 4096 sequences of 16 tokens of 512 channels 145 -> 72 us, of 64 of 256 in 1024 36 -> 34; float32 62 -> 66 there, so
+    // that asks for more), or so short that more waves would have no tokens (4096 of 8 of 512 137 -> 42)
+    for (const int few : {128, 64})
+        if (blocks() * few >= (bf16 ? full : 4 * full) || (few >> s.lanes_log2) * tokens >= T) g.threads = few;
+    if (g.threads == 256 && blocks() * g.threads < full && tile() < T) g.threads = 512;
     while (s.lanes_log2 > 5 && blocks() * g.threads < full && tile() < T) --s.lanes_log2;
-    if (blocks() * g.threads < full / 2) g.threads = 256;
+    if (g.threads == 512 && blocks() * g.threads < full / 2) g.threads = 256;
     // forward alone: the backward kernel has registers for two waves a SIMD (4 x 2048 tokens of 2048 channels: forward 46 -> 39 us)
     if (g.threads == 512 && !back && blocks() * 1024 <= full && 2 * tile() <= T) g.threads = 1024;
     const long long tiles = (T + tile() - 1) / tile();
     long long wanted = 1;
-    if (blocks() * g.threads < full / 4) wanted = std::max(1LL, std::min({full / std::max(blocks() * g.threads, 1LL), tiles, 64LL}));
+    if (g.threads == 256 && blocks() * g.threads < full / 4) wanted = std::max(1LL, std::min({full / std::max(blocks() * g.threads, 1LL), tiles, 256LL}));
     s.channel_blocks = (unsigned)((C + (1 << s.lanes_log2) - 1) >> s.lanes_log2);
     s.segment = (int)std::max((tiles + wanted - 1) / wanted, 1LL) * tile();
     s.segments = std::max(1, (T + s.segment - 1) / s.segment);
     return g;
+}
+
+// Rows of parts of drate that are added up by themselves where there are many, and how many such pieces there are; a grid has 65535 of them at most.
+constexpr unsigned SUMS_PIECE = 256;
+unsigned pieces_of(unsigned rows) { return rows > 4 * SUMS_PIECE && rows / SUMS_PIECE < 65535 ? (rows + SUMS_PIECE - 1) / SUMS_PIECE : 1; }
+
+// The tape has the state before every tile of the backward kernel, whose tokens are a power of two, but at least before every 32 tokens: a small tile in workgroups of one or two waves.
+int tape_log2_of(int B, int T, int C, bool bf16)
+{
+    const Geometry g = shape_of(B, T, C, bf16, true, RECURRENCE_TOKENS_BACK);
+    const int tile = (g.threads >> g.s.lanes_log2) * RECURRENCE_TOKENS_BACK;
+    return tile >= 32 ? 5 : tile >= 16 ? 4 : 3;
 }
 
 template <class F>
@@ -55,8 +71,8 @@ hipError_t forward(const RecurrenceArgs &a, const RecurrenceShape &s, hipStream_
 {
     constexpr int S = RECURRENCE_TOKENS;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
-    if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, false><<<grid, THREADS, 0, st>>>(a, p); });
+    if constexpr (THREADS == 256)
+        if (s.segments > 1) in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, false><<<grid, THREADS, 0, st>>>(a, p); });
     in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence<E, GATES, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     return hipGetLastError();
 }
@@ -67,20 +83,26 @@ hipError_t backward(RecurrenceArgs a, const RecurrenceShape &s, hipStream_t st)
     constexpr int S = RECURRENCE_TOKENS_BACK;
     const long long items = (long long)a.B * s.channel_blocks * s.segments;
     a.partial = a.effects + (s.segments > 1 ? 3 * (size_t)a.B * s.segments * a.C : 0);
-    if (s.segments > 1)
-        in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, true><<<grid, THREADS, 0, st>>>(a, p); });
+    if constexpr (THREADS == 256)
+        if (s.segments > 1) in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_effects<E, GATES, S, THREADS, true><<<grid, THREADS, 0, st>>>(a, p); });
     in_launches(s, items, [&](const RecurrenceShape &p, unsigned grid) { k_recurrence_back<E, GATES, S, THREADS><<<grid, THREADS, 0, st>>>(a, p); });
     if (a.drate) {
-        const ColumnSumsArgs<1> sums{{{a.partial, a.drate, (unsigned)a.B * s.segments}}, {0, 1}, a.C};
-        column_sums(sums, st);
+        // many sequences' parts first by themselves in pieces: few columns are few workgroups
+        const unsigned rows = (unsigned)a.B * s.segments, pieces = pieces_of(rows);
+        float *joined = a.partial + (size_t)rows * a.C;
+        if (pieces > 1) column_sums(ColumnSumsArgs<1>{{{a.partial, joined, SUMS_PIECE, rows}}, {0, pieces}, a.C}, st);
+        column_sums(ColumnSumsArgs<1>{{{pieces > 1 ? joined : a.partial, a.drate, pieces > 1 ? pieces : rows, pieces > 1 ? pieces : rows}}, {0, 1}, a.C}, st);
     }
     return hipGetLastError();
 }
 
 template <class E, int GATES>
-hipError_t run(const RecurrenceArgs &a, bool back, hipStream_t st)
+hipError_t run(RecurrenceArgs a, bool back, hipStream_t st)
 {
+    a.tape_log2 = tape_log2_of(a.B, a.T, a.C, a.bf16);
     const Geometry g = shape_of(a.B, a.T, a.C, a.bf16, back, back ? RECURRENCE_TOKENS_BACK : RECURRENCE_TOKENS);
+    if (g.threads == 64) return back ? backward<E, GATES, 64>(a, g.s, st) : forward<E, GATES, 64>(a, g.s, st);
+    if (g.threads == 128) return back ? backward<E, GATES, 128>(a, g.s, st) : forward<E, GATES, 128>(a, g.s, st);
     if (g.threads == 256) return back ? backward<E, GATES, 256>(a, g.s, st) : forward<E, GATES, 256>(a, g.s, st);
     if (g.threads == 1024) return forward<E, GATES, 1024>(a, g.s, st);
     return back ? backward<E, GATES, 512>(a, g.s, st) : forward<E, GATES, 512>(a, g.s, st);
@@ -163,11 +185,15 @@ bool fours(const RecurrenceArgs &a)
 
 }  // namespace
 
+template <class E>
+static hipError_t gates(const RecurrenceArgs &a, bool back, hipStream_t s)
+{
+    if (a.rate && a.normalise) return a.input_gate ? run<E, ALL>(a, back, s) : run<E, RATES>(a, back, s);
+    return !a.rate && !a.input_gate && !a.normalise ? run<E, NONE>(a, back, s) : run<E, ANY>(a, back, s);
+}
 static hipError_t typed(const RecurrenceArgs &a, bool back, hipStream_t s)
 {
-    const bool all = a.rate && a.input_gate && a.normalise, none = !a.rate && !a.input_gate && !a.normalise;
-    if (a.bf16) return all ? run<bf16, ALL>(a, back, s) : none ? run<bf16, NONE>(a, back, s) : run<bf16, ANY>(a, back, s);
-    return all ? run<float, ALL>(a, back, s) : none ? run<float, NONE>(a, back, s) : run<float, ANY>(a, back, s);
+    return a.bf16 ? gates<bf16>(a, back, s) : gates<float>(a, back, s);
 }
 
 hipError_t recurrence_launch(const RecurrenceArgs &a, hipStream_t s) { return typed(a, false, s); }
@@ -178,12 +204,16 @@ hipError_t recurrence_step_launch(const RecurrenceArgs &a, hipStream_t s)
     return fours(a) ? step<float, 4>(a, s) : step<float, 1>(a, s);
 }
 
-size_t recurrence_tape_bytes(int B, int T, int C) { return 4 * (size_t)B * ((T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) * C; }
+size_t recurrence_tape_bytes(int B, int T, int C, bool bf16)
+{
+    const int every = tape_log2_of(B, T, C, bf16);
+    return 4 * (size_t)B * (((size_t)T + (1 << every) - 1) >> every) * C;
+}
 
 size_t recurrence_workspace_bytes(int B, int T, int C, bool bf16, bool backward)
 {
     const size_t maps = (size_t)B * shape_of(B, T, C, bf16, backward, backward ? RECURRENCE_TOKENS_BACK : RECURRENCE_TOKENS).s.segments;
-    return (maps > (size_t)B ? 12 * maps * C : 0) + (backward ? 4 * maps * C : 0);
+    return (maps > (size_t)B ? 12 * maps * C : 0) + (backward ? 4 * (maps + pieces_of((unsigned)maps)) * C : 0);
 }
 
 }  // namespace tfno

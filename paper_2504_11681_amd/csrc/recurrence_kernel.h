@@ -19,8 +19,8 @@ namespace tfno {
 // 131 -> 137 us for the two directions above: twice the joining).
 constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;
 
-// What a kernel knows of its gates: ALL has rates, an input gate and `normalise`, NONE neither; ANY asks.
-enum { ANY = 0, ALL = 1, NONE = 2 };
+// What a kernel knows of its gates: ALL has rates, an input gate and `normalise`, NONE neither, RATES all but an input gate; ANY asks.
+enum { ANY = 0, ALL = 1, NONE = 2, RATES = 3 };
 struct RecurrenceShape {
     int lanes_log2;                 // lanes of a group
     unsigned channel_blocks, segments, first;
@@ -173,15 +173,15 @@ __device__ __forceinline__ float through_segments(const RecurrenceArgs &a, const
     const int each = (n + groups * WAVES - 1) / (groups * WAVES), from = (at.wave * groups + at.group) * each;
     Span own = {1.0f, 0.0f, 0.0f};
     const Span *effects = (const Span *)a.effects;
-    for (int i = from; i < min(from + each, n); i += 4) {          // four on their way at once
-        Span some[4];
+    for (int i = from; i < min(from + each, n); i += 8) {          // eight on their way at once
+        Span some[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 8; ++k) {
             const int which = min(i + k, n - 1);
             some[k] = effects[((long long)at.b * s.segments + (BACK ? (int)s.segments - 1 - which : which)) * a.C + at.c];
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 8; ++k)
             if (i + k < min(from + each, n)) own = after(own, some[k]);
     }
     Span others, all;
@@ -258,14 +258,14 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
     __shared__ float state[2][64];          // before a tile
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
-    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES == ALL : a.normalise;
+    const bool rated = GATES ? GATES != NONE : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES != NONE : a.normalise;
     const float rate = rated ? a.rate[at.c] : 0.0f;
     // the state before the segment
     float carry = a.initial ? a.initial[(long long)at.b * a.C + at.c] : 0.0f;
     carry = through_segments<false, WAVES>(a, s, at, carry, maps[0]);
     if (at.wave == 0 && at.group == 0) state[1][at.lane] = carry;
     if (a.final_state && at.len == 0 && at.segment == 0 && at.wave == 0 && at.group == 0 && at.live) a.final_state[(long long)at.b * a.C + at.c] = carry;
-    const int last = max(min(at.len, at.end) - 1, 0), tape_rows = (a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE;
+    const int last = max(min(at.len, at.end) - 1, 0), tape_every = 1 << a.tape_log2, tape_rows = (a.T + tape_every - 1) >> a.tape_log2;
     const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
     const Row<E> y(a.y, a.sy, at.b, at.c, ahead);
     E in_x[S], in_gate[S], in_input[S];
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
         float h = state[buffer ^ 1][at.lane];
         for (int w = 0; w < at.wave; ++w) h = maps[buffer][w][at.lane].of(h);
         if (lanes < 64) h = some ? before.decay().of(h, before.B) : h;
-        if (a.tape && (t & (RECURRENCE_TAPE - 1)) == 0 && t < at.end && at.live) a.tape[((long long)at.b * tape_rows + t / RECURRENCE_TAPE) * a.C + at.c] = h;
+        if (a.tape && (t & (tape_every - 1)) == 0 && t < at.end && at.live) a.tape[((long long)at.b * tape_rows + (t >> a.tape_log2)) * a.C + at.c] = h;
         const unsigned o = y.here();
         long long k = y.from(first);
         if (!resets && first + per_wave <= at.end && first + per_wave <= at.len) {
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a
     const Place at(a, s);
     if (at.segment == (BACKWARD ? 0 : (int)s.segments - 1)) return;          // nobody asks
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, part = s.segment / WAVES;      // whole tiles, so whole rounds of a wave
-    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = !BACKWARD && (GATES ? GATES == ALL : a.input_gate != nullptr), normalise = !BACKWARD && (GATES ? GATES == ALL : a.normalise);
+    const bool rated = GATES ? GATES != NONE : a.rate != nullptr, gated = !BACKWARD && (GATES ? GATES == ALL : a.input_gate != nullptr), normalise = !BACKWARD && (GATES ? GATES != NONE : a.normalise);
     const float rate = rated ? a.rate[at.c] : 0.0f;
     const int last = max(min(at.end, at.len) - 1, 0), from = at.begin + at.wave * part, end = min(from + part, min(at.end, at.len));
     // in: x, or dy
@@ -437,13 +437,13 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
     __shared__ float gradient[2][64];       // that reaches a tile from its later tokens
     const Place at(a, s);
     const int lanes = 1 << s.lanes_log2, ahead = at.group * S, per_wave = (64 >> s.lanes_log2) * S, tile = per_wave * WAVES;
-    const bool rated = GATES ? GATES == ALL : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES == ALL : a.normalise;
+    const bool rated = GATES ? GATES != NONE : a.rate != nullptr, gated = GATES ? GATES == ALL : a.input_gate != nullptr, normalise = GATES ? GATES != NONE : a.normalise;
     const float rate = rated ? a.rate[at.c] : 0.0f;
     float drate = 0.0f, carry = a.d_final ? a.d_final[(long long)at.b * a.C + at.c] : 0.0f;      // carry: the gradient that reaches the state before the tile from its later tokens
     carry = through_segments<true, WAVES>(a, s, at, carry, maps[0]);
     if (at.wave == 0 && at.group == 0) gradient[1][at.lane] = carry;
     const int last = max(min(at.len, at.end) - 1, 0), tiles = (at.end - at.begin + tile - 1) / tile;
-    const float *tape = a.tape + (long long)at.b * ((a.T + RECURRENCE_TAPE - 1) / RECURRENCE_TAPE) * a.C + at.c;
+    const float *tape = a.tape + (long long)at.b * ((a.T + (1 << a.tape_log2) - 1) >> a.tape_log2) * a.C + at.c;      // a tile begins where one is
     const Row<E> x(a.x, a.sx, at.b, at.c, ahead), gate(a.gate, a.sgate, at.b, at.c, ahead), input(gated ? a.input_gate : a.x, gated ? a.sinput : a.sx, at.b, at.c, ahead);
     const Row<E> dy(a.dy, a.sy, at.b, at.c, ahead);
     const Row<E> dx(a.dx, a.sdx, at.b, at.c, ahead), dgate(a.dgate, a.sdgate, at.b, at.c, ahead), dinput(a.dinput_gate, a.sdinput, at.b, at.c, ahead);
@@ -458,7 +458,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
         };
         if (first + per_wave - 1 <= last) all(Yes());
         else all(No());
-        in_h = tape[(long long)(start / RECURRENCE_TAPE) * a.C];
+        in_h = tape[(long long)(start >> a.tape_log2) * a.C];
     };
     int start = at.begin + (tiles - 1) * tile, first = start + at.wave * per_wave, buffer = 0;
     for (; start >= at.begin && start >= at.len; start -= tile, first -= tile) {    // past the sequence: zeros
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
         const float state = in_h;
         if (start > at.begin) {
             gates(Yes());
-            in_h = tape[(long long)((start - tile) / RECURRENCE_TAPE) * a.C];
+            in_h = tape[(long long)((start - tile) >> a.tape_log2) * a.C];
         } else {
             gates(No());
         }

@@ -119,6 +119,28 @@ def test_recurrence_of_long_sequences_and_many_channels(tfno, dtype, size):
 
 
 @pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("size", [(3000, 5, 9), (4200, 13, 70), (2100, 30, 64), (1, 9000, 3)])
+def test_recurrence_of_many_short_sequences_and_of_a_very_long_one(tfno, dtype, size):
+    """So many sequences that each is one wave's, and that their parts of the rates' gradient are added up in pieces; so long a one that it goes in more than a hundred segments."""
+    for gates in ("both", "one") if size[0] > 1 else ("both",):
+        check_recurrence(tfno, recurrence_inputs(dtype, *size, gates, seed=13), f"[case] many {dtype} {gates} {size}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("T", (100, 1100))
+def test_recurrence_of_strong_decays(tfno, dtype, T):
+    """Products of decays that underflow within a few tokens, without a decay of 0 among them; then some of those too."""
+    x = recurrence_inputs(dtype, 2, T, 20, "decay", seed=14)
+    gen = torch.Generator("cuda").manual_seed(14)
+    x["gate"] = (-40.0 * torch.rand(2, T, 20, generator=gen, device="cuda") ** 3).to(dtype)
+    x["gate"][:, ::7, ::3] = -95.0
+    check_recurrence(tfno, x, f"[case] strong {dtype} {T}")
+    x["gate"][:, 3::11, 1::4] = -120.0
+    x["gate"][:, 5::13, 2::4] = -math.inf
+    check_recurrence(tfno, x, f"[case] strong with resets {dtype} {T}")
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("T", (70, 700, 1500))
 def test_recurrence_lengths_and_what_stands_past_them(tfno, dtype, T):
     x = recurrence_inputs(dtype, 8, T, 24, seed=2)
