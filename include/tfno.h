@@ -409,7 +409,7 @@ tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void
  *   h = exp(l) h + u,    y = h,    l = -rate sigmoid(gate), or gate itself where rate is NULL,
  *   u = x, times sigmoid(input_gate) where that is not NULL, times sqrt(1 - exp(2 l)) where `normalise` is set
  *
- * with x, gate, input_gate, y [B, T, C], rate float32 [C], not negative, and states float32 [B, C], contiguous; h starts from `initial` (NULL: zeros).
+ * with x, gate, input_gate, y [B, T, C], rate float32 [C], finite and not negative, and states float32 [B, C], contiguous; h starts from `initial` (NULL: zeros).
  * Where exp(l) is 0 in float32 (l = -inf, say) the state is forgotten, whatever it holds.  l should be 0 or less: above that the state grows, which is right as long as the
  * growth over any run of tokens is finite, and `normalise` gives NaN.  `lengths` as for the rule above: tokens past them are not read, their outputs
  * and gradients are zeros.  A NaN or an infinity in a token makes its channel NaN from there to the next decay of 0.
