@@ -96,18 +96,20 @@ struct Span {
         return d;
     }
 };
-// A product that underflows does not forget; one with a 0 in it does.
+// A product that underflows does not forget; one with a 0 in it does, whatever else is in it: 0 times a NaN or an infinity is no decay, and what such tokens leave behind the 0 is in B.
 __device__ __forceinline__ Span after(Span first, Span second)
 {
     const float a = first.a * second.a;
-    return Span{a == 0.0f && first.a != 0.0f && second.a != 0.0f ? LEAST : a, fmaf(first.a, second.less, first.less), second.decay().of(first.B, second.B)};
+    return Span{first.a == 0.0f || second.a == 0.0f ? 0.0f : a == 0.0f ? LEAST : a, fmaf(first.a, second.less, first.less), second.decay().of(first.B, second.B)};
 }
 struct Joined {
     Decay a;
     float B;
     __device__ __forceinline__ float of(float h) const { return a.of(h, B); }
 };
-// Decays that are hardly more than 0, or not: seldom, and then looked for in a wave's whole tile, whose gates are read again.
+// Decays that are hardly more than 0, or not: seldom, and then looked for in a wave's whole tile, whose gates are read again.  A product that is 0 or NaN (0 times a NaN or an
+// infinity) may have one in it.
+__device__ __forceinline__ bool may_reset(Span own) { return !(own.a > 0.0f); }
 template <int S, class E>
 __device__ __forceinline__ bool find_resets(bool rated, float rate, const E (&gate)[S], int t, int last, TokenDecay (&d)[S], Span &own)
 {
@@ -324,7 +326,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence(RecurrenceArgs a, Recurr
             load(first + tile);
         }
         bool resets = false;
-        if (__any(own.a == 0.0f)) {
+        if (__any(may_reset(own))) {
             E again[S];
             gate.template load<false>(first, ahead, at.c, last, again);
             resets = find_resets(rated, rate, again, t, last, d, own);
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_effects(RecurrenceArgs a
             own.longer(decay, less);
         }
         if (i + 1 < rounds) load(BACKWARD ? first - per_wave : first + per_wave);
-        if (__any(own.a == 0.0f)) {
+        if (__any(may_reset(own))) {
             E again[S];
             gate.template load<false>(first, ahead, at.c, last, again);
             find_resets(rated, rate, again, t, last, d, own);
@@ -532,7 +534,7 @@ __global__ __launch_bounds__(THREADS) void k_recurrence_back(RecurrenceArgs a, R
             gates(No());
         }
         bool resets = false;
-        if (__any(own.a == 0.0f)) {
+        if (__any(may_reset(own))) {
             E again[S];
             gate.template load<false>(first, ahead, at.c, last, again);
             resets = find_resets(rated, rate, again, t, last, d, own);

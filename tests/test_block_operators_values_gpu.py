@@ -1,0 +1,97 @@
+"""The operators of a block along time on the GPU at values where one channel, row or sequence could go wrong beneath the others."""
+import math
+
+import pytest
+import torch
+
+import block_oracle as oracle
+from block_oracle import BF16, F32
+from test_block_operators_gpu import INPUTS, recur, recur_back, recurrence_inputs, recurrence_wanted, say, tfno  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def same_where_finite(name, got, want, bound):
+    """Finite where the wanted values are, and as near there as `bound`."""
+    finite = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), finite), f"{name}: {int((torch.isfinite(got) != finite).sum())} values finite in one alone"
+    off = oracle.rel(torch.where(finite, got.double(), 0.0), torch.where(finite, want, 0.0))
+    say(f"   {name}: {off:.3g} of {bound:.3g}, {int((~finite).sum())} not finite")
+    assert off <= bound, name
+
+
+# ---------------------------------------------------------------- gated linear recurrence
+
+# tokens of a bad gate and of decays of 0: within one group of eight tokens, in either order; in neighbouring groups, in another wave, in another tile; several of each
+BAD_AND_RESETS = [([3], [5]), ([5], [3]), ([3], [3]), ([3], [12]), ([12], [3]), ([3], [20]), ([3], [64]), ([3], [130]), ([7], [8]), ([8], [7]), ([0], [1]), ([2, 40], [4, 41, 90])]
+
+
+def check_bad_gates(tfno, x, bad, resets, value, what, clean=True):
+    """`value` in the gates of the tokens `bad` of two channels of three, decays of 0 at the tokens `resets` of one of them and, where `clean`, of the third."""
+    say(what)
+    dtype, B, T, C = x["x"].dtype, *x["x"].shape
+    if x["rate"] is not None:
+        x["rate"][:] = x["rate"].clamp(0.05, 2.0)
+        x["rate"][0::3] = x["rate"][1::3] = 1000.0              # a gate that is open makes the decay 0, one that is nearly closed leaves something
+        x["gate"][:, :, 0::3] -= 7.5
+        x["gate"][:, :, 1::3] -= 7.5
+    for t in resets:
+        for c in (0, 1)[:1 + clean]:
+            x["gate"][:, t, c::3] = 90.0 if x["rate"] is not None else -math.inf
+    for t in bad:
+        x["gate"][:, t, 0::3] = value
+        x["gate"][:, t, 2::3] = value
+    tape = tfno.gated_recurrence_tape(x["x"])
+    y, final = recur(tfno, x, tape)
+    w = recurrence_wanted(x)
+    same_where_finite("y", y, w[0], oracle.REL[dtype])
+    same_where_finite("final", final, w[1], oracle.REL[F32])
+    d = recur_back(tfno, x, tape)
+    same_where_finite("dx", d["x"], w[2], oracle.REL[dtype])
+    for t in resets:                                            # 0 times a gradient that is not finite: either answer will do
+        either = ~torch.isfinite(w[2][:, t])
+        d["gate"][:, t][either], w[3][:, t][either] = 0.0, 0.0
+    same_where_finite("dgate", d["gate"], w[3], oracle.REL_GATES[dtype])
+    for n, v in (("input_gate", w[4]), ("rate", w[5])):
+        if d[n] is not None:
+            same_where_finite("d" + n, d[n], v, oracle.REL_SUMS if n == "rate" else oracle.REL[dtype])
+    same_where_finite("dinitial", d["initial"], w[6], oracle.REL[F32])
+    return y
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("gates", ("decay", "decay of inputs", "both", "one"))
+@pytest.mark.parametrize("where", range(len(BAD_AND_RESETS)))
+def test_recurrence_gates_of_nan_up_to_the_next_reset(tfno, dtype, gates, where):  # noqa: F811
+    """A NaN in a gate stays in its channel up to the next decay of 0, forward, and back to the one before, in gradients."""
+    bad, resets = BAD_AND_RESETS[where]
+    for C, clean in ((7, True), (70, True), (7, False), (70, False)):
+        check_bad_gates(tfno, recurrence_inputs(dtype, 2, 150, C, gates, seed=21), bad, resets, math.nan, f"[case] NaN gates {dtype} {gates} {C} {bad} {resets} {clean}", clean)
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("gates", ("decay", "both"))
+def test_recurrence_gates_of_nan_in_segments_and_short_sequences(tfno, dtype, gates):  # noqa: F811
+    for size, bad, resets in (((1, 1500, 6), [3], [700]), ((1, 1500, 6), [700], [3]), ((1, 1500, 6), [3, 900], [10, 1200]), ((3, 1100, 40), [500], [520]),
+                              ((4200, 13, 70), [2], [5]), ((4200, 30, 70), [2], [17]), ((300, 70, 64), [10], [40])):
+        check_bad_gates(tfno, recurrence_inputs(dtype, *size, gates, seed=22), bad, resets, math.nan, f"[case] NaN gates {dtype} {gates} {size} {bad} {resets}")
+
+
+@pytest.mark.parametrize("where", range(len(BAD_AND_RESETS)))
+def test_recurrence_infinite_growth_up_to_the_next_reset(tfno, where):  # noqa: F811
+    """A decay of infinity: what comes of it is not finite up to the next decay of 0."""
+    bad, resets = BAD_AND_RESETS[where]
+    for size in ((2, 150, 7), (1, 1500, 7)):
+        check_bad_gates(tfno, recurrence_inputs(F32, *size, "decay", seed=23), bad, resets, math.inf, f"[case] infinite growth {size} {bad} {resets}")
+
+
+@pytest.mark.parametrize("gates", ("decay", "both"))
+def test_recurrence_steps_forget_nans_where_sequences_do(tfno, gates):  # noqa: F811
+    x = recurrence_inputs(F32, 2, 40, 7, gates, seed=24)
+    y = check_bad_gates(tfno, x, [3, 20], [5, 30], math.nan, f"[case] steps {gates}")
+    state = x["initial"].clone()
+    for t in range(40):
+        o = torch.empty(2, 7, device="cuda")
+        one = [None if x[n] is None else x[n] if n == "rate" else x[n][:, t] for n in INPUTS]
+        tfno.gated_recurrence_step(*one, state, o, normalise=x["normalise"])
+        same_where_finite(f"step {t}", o, y[:, t].double(), oracle.REL[F32])
