@@ -459,7 +459,8 @@ tfno_status tfno_gated_recurrence_step(const tfno_gated_recurrence_desc *d, cons
  * (TFNO_GATE_TOKEN), or float32 and shared by a sequence's tokens ([B, C], TFNO_GATE_SEQUENCE: strides of batch elements) or by all ([C], TFNO_GATE_CHANNEL); act is as
  * d->activation says, act(z) = z, z sigmoid(z) or sigmoid(z).  Weights are float32 [C] (NULL: ones).  Either result may be NULL, not both; n_out is the norm
  * of r_out as it is before its rounding.  y and n_out have the type d->dtype; r and r_out have d->residual_dtype, which is dtype or float32.  r_out may be r itself and
- * n_out y (the same pointer and strides).  Tokens past `lengths` (int32 [B] or NULL) are not read, and count in no sum; results and gradients there are zeros.
+ * n_out y (the same pointer and strides).  Tokens past `lengths` (int32 [B] or NULL) are not read, and count in no sum, whatever their gate and the weights are; results and
+ * gradients there are zeros, the gradient of a gate of a sequence without tokens too.
  *
  * The backward call takes the same inputs and the gradients d_r_out and d_n_out of the results (NULL: zeros, not both), and gives dy and, where not NULL, dr, dgate (as the
  * gate: of y's type, or float32 and contiguous, summed over the tokens that share it), dw_after and dw_before (float32 [C]).  Where it sums over

@@ -292,6 +292,7 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu
             } else {
                 const float back = q * q * q * two[1] * over_C;
                 float dot[1] = {};
+                // a row that is not there counts in no sum, whatever gate and weights it would have: selected, not skipped, which took registers (rows of 8192 285 -> 301 us)
 #pragma unroll
                 for (int i = 0; i < ITER; ++i)
 #pragma unroll
@@ -300,12 +301,12 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu
                         float d = ds[i][e];
                         if (before) {
                             d += fmaf(q * wb[i][e], dn[i][e], -back * st[i][e]);
-                            d_before[i][e] = fmaf(dn[i][e] * q, st[i][e], d_before[i][e]);
+                            d_before[i][e] = there ? fmaf(dn[i][e] * q, st[i][e], d_before[i][e]) : d_before[i][e];
                         }
                         const float f = d * z[i][e], dz = d * (scaled * wa[i][e]) * slope[i][e];
-                        d_after[i][e] = fmaf(f, scaled, d_after[i][e]);
+                        d_after[i][e] = there ? fmaf(f, scaled, d_after[i][e]) : d_after[i][e];
                         if constexpr (TOKEN) slope[i][e] = dz;
-                        else d_gate[i][e] += dz;
+                        else d_gate[i][e] += there ? dz : 0.0f;
                         r[i][e] = a.residual_scale * d;
                         z[i][e] = f * wa[i][e];
                         dot[0] = fmaf(z[i][e], y[i][e], dot[0]);

@@ -6,7 +6,8 @@ import torch
 
 import block_oracle as oracle
 from block_oracle import BF16, F32
-from test_block_operators_gpu import INPUTS, recur, recur_back, recurrence_inputs, recurrence_wanted, say, tfno  # noqa: F401
+from test_block_operators_gpu import (INPUTS, PARTS, TYPES, between_inputs, between_wanted, empty, near, recur, recur_back, recurrence_inputs,  # noqa: F401
+                                      recurrence_wanted, say, tfno)
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +96,52 @@ def test_recurrence_steps_forget_nans_where_sequences_do(tfno, gates):  # noqa: 
         one = [None if x[n] is None else x[n] if n == "rate" else x[n][:, t] for n in INPUTS]
         tfno.gated_recurrence_step(*one, state, o, normalise=x["normalise"])
         same_where_finite(f"step {t}", o, y[:, t].double(), oracle.REL[F32])
+
+
+# ---------------------------------------------------------------- norms around a block
+
+def norms_and_gradients(tfno, x):
+    out = [empty(x["y"], x["d_r"].dtype), empty(x["y"])]
+    tfno.block_norm(*(x[n] for n in PARTS), *out, **x["ways"])
+    d = [empty(x[n]) for n in PARTS]
+    tfno.block_norm_backward(*(x[n] for n in PARTS), x["d_r"], x["d_n"], *d, **x["ways"])
+    return dict(zip(("r_out", "n_out", *("d" + n for n in PARTS)), (*out, *d)))
+
+
+def bound_of(name, t):
+    if name in ("r_out", "n_out"):
+        return oracle.REL[t.dtype]
+    return oracle.REL_GATES[BF16] if t.dtype == BF16 else oracle.REL_SUMS
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("activation", ("none", "silu", "sigmoid"))
+@pytest.mark.parametrize("size", [(6, 50, 40), (6, 50, 100), (5, 33, 1024), (4, 7, 5000), (300, 3, 40), (70, 40, 256), (3, 1300, 64)])
+def test_norms_gates_of_sequences_without_tokens(tfno, types, activation, size):  # noqa: F811
+    """The gate of a sequence of no tokens counts in no sum, whatever it is."""
+    B, T, C = size
+    x = between_inputs(*types, *size, "sequence", activation, seed=21)
+    lengths = [(b * 7 + 2) % (T + 1) for b in range(B)]
+    lengths[0], lengths[1], lengths[-1] = T, 0, -1
+    x["ways"]["lengths"] = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    none = x["ways"]["lengths"] <= 0
+    x["gate"][none] = 0.0
+    w = dict(zip(("r_out", "n_out", *("d" + n for n in PARTS)), between_wanted(x)))
+    for bad in (math.nan, math.inf, -math.inf):
+        say(f"[case] gates of nothing {types} {activation} {size} {bad}")
+        x["gate"][none] = bad
+        for n, got in norms_and_gradients(tfno, x).items():
+            near(n, got, w[n], bound_of(n, got))
+            if n == "dgate":
+                assert (got[none] == 0).all()
+
+
+@pytest.mark.parametrize("gate", ("token", "sequence", "channel"))
+@pytest.mark.parametrize("C", (40, 1024))
+def test_norms_of_no_tokens_at_all_have_sums_of_zero(tfno, gate, C):  # noqa: F811
+    x = between_inputs(F32, F32, 4, 9, C, gate, "silu", seed=22)
+    x["ways"]["lengths"] = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for n in ("y", "r", "gate", "w_after", "w_before", "d_r", "d_n"):
+        x[n].fill_(math.nan)
+    for n, got in norms_and_gradients(tfno, x).items():
+        assert (got == 0).all(), n
