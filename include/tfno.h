@@ -466,6 +466,8 @@ tfno_status tfno_gated_recurrence_step(const tfno_gated_recurrence_desc *d, cons
  * gate: of y's type, or float32 and contiguous, summed over the tokens that share it), dw_after and dw_before (float32 [C]).  Where it sums over
  * tokens (dw_after, dw_before, dgate of a shared gate) it needs tfno_block_norm_workspace_bytes bytes of workspace.  dr may be d_r_out itself and dy d_n_out.
  *
+ * Squares are added up in float32: rows whose sum of squares is above its range (values of 1e19 / sqrt(C) and more) are infinite there, and their norm 0.
+ *
  * Sizes: B, T >= 0, B T < 2^31, C >= 1, eps > 0, no dw_after without norm_after (TFNO_ERR_SHAPE), C <= 8192 (else TFNO_ERR_UNSUPPORTED).  Strides of heads are not used.
  */
 typedef enum { TFNO_GATE_NONE = 0, TFNO_GATE_TOKEN = 1, TFNO_GATE_SEQUENCE = 2, TFNO_GATE_CHANNEL = 3 } tfno_gate;

@@ -1,7 +1,7 @@
 // m = Norm(y) w_after,   s = scale r + act(gate) m,   n = Norm(s) w_before,   Norm(x) = x (mean x^2 + eps)^-1/2, for every row in one pass, and its gradient
 //
-//   d = d_s + q (b - s q^2 mean(b s)),   b = d_n w_before,   q = (mean s^2 + eps)^-1/2,
-//   dr = scale d,   dgate = d m act'(gate),   f = d act(gate),   dy = p (f w_after - y p^2 mean(f w_after y)),   p = (mean y^2 + eps)^-1/2,
+//   d = d_s + q (b - s q (q mean(b s))),   b = d_n w_before,   q = (mean s^2 + eps)^-1/2,
+//   dr = scale d,   dgate = d m act'(gate),   f = d act(gate),   dy = p (f w_after - y p (p mean(f w_after y))),   p = (mean y^2 + eps)^-1/2,
 //   dw_after = sum f y p,   dw_before = sum d_n s q.
 //
 // Bound by bytes: every row is read once and written once.  A group of lanes (up to a whole workgroup) holds a row in registers, eight or sixteen values a lane;
@@ -290,7 +290,8 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu
                     if (a.n_out) Eight<E, VEC>::store((E *)a.n_out + cb * a.sn_out.batch + ct * a.sn_out.token + column[i], step, count[i], n);
                 }
             } else {
-                const float back = q * q * q * two[1] * over_C;
+                // products in an order that stays in range: the third power of an inverse root would not, for rows of 1e13 or 1e-13
+                const float back = q * two[1] * over_C * q;
                 float dot[1] = {};
                 // a row that is not there counts in no sum, whatever gate and weights it would have: selected, not skipped, which took registers (rows of 8192 285 -> 301 us)
 #pragma unroll
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu
                         const float scaled = y[i][e] * p;
                         float d = ds[i][e];
                         if (before) {
-                            d += fmaf(q * wb[i][e], dn[i][e], -back * st[i][e]);
+                            d = fmaf(q, fmaf(wb[i][e], dn[i][e], -back * st[i][e]), d);
                             d_before[i][e] = there ? fmaf(dn[i][e] * q, st[i][e], d_before[i][e]) : d_before[i][e];
                         }
                         const float f = d * z[i][e], dz = d * (scaled * wa[i][e]) * slope[i][e];
@@ -314,14 +315,14 @@ __global__ __launch_bounds__(BLOCK_NORM_MOST) __attribute__((amdgpu_waves_per_eu
                 float along = 0.0f;
                 if (a.norm_after) {
                     row_sums(dot, s.group_log2, meet, turn);
-                    along = p * p * p * dot[0] * over_C;
+                    along = p * dot[0] * over_C * p;
                 }
 #pragma unroll
                 for (int i = 0; i < ITER; ++i) {
                     if (count[i] == 0) continue;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        y[i][e] = there ? fmaf(p, z[i][e], -along * y[i][e]) : 0.0f;
+                        y[i][e] = there ? p * fmaf(-along, y[i][e], z[i][e]) : 0.0f;
                         r[i][e] = there ? r[i][e] : 0.0f;
                         slope[i][e] = there ? slope[i][e] : 0.0f;
                     }

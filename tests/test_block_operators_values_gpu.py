@@ -145,3 +145,36 @@ def test_norms_of_no_tokens_at_all_have_sums_of_zero(tfno, gate, C):  # noqa: F8
         x[n].fill_(math.nan)
     for n, got in norms_and_gradients(tfno, x).items():
         assert (got == 0).all(), n
+
+
+def near_by_row(name, got, want, bound):
+    """Every row by itself: got and want are [..., C]."""
+    assert torch.isfinite(got).all(), name
+    off, size = (got.double() - want).norm(dim=-1), want.norm(dim=-1)
+    worst = float(torch.where(size > 0, off / size, off).max())
+    say(f"   {name}: {worst:.3g} of {bound:.3g} in the worst row")
+    assert worst <= bound, name
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("after", (True, False))
+@pytest.mark.parametrize("C", (40, 205, 1024, 4099))
+def test_norms_and_gradient_of_rows_of_any_size(tfno, types, after, C):  # noqa: F811
+    """Rows from 1e-15 to 1e17, whose inverse roots' third powers are far out of float32's range, and of zeros; the squares' sums are not."""
+    sizes = torch.tensor([1e-15, 1e-10, 1e-5, 1.0, 1e5, 1e10, 1e13, 1e15, 1e17, 0.0], device="cuda")
+    x = between_inputs(*types, 2, len(sizes), C, "token", "silu", seed=23, after=after)
+    gen = torch.Generator("cuda").manual_seed(23)
+    for n in ("y", "r"):
+        x[n] = (torch.randn(2, len(sizes), C, generator=gen, device="cuda") * sizes[:, None]).to(x[n].dtype)
+    x["ways"]["eps"] = 1e-30
+    say(f"[case] sizes of rows {types} {after} {C}")
+    out, d = [empty(x["y"], types[1]), empty(x["y"])], [empty(x[n]) for n in PARTS]
+    tfno.block_norm(*(x[n] for n in PARTS), *out, **x["ways"])
+    if not after:
+        d[3] = None
+    tfno.block_norm_backward(*(x[n] for n in PARTS), x["d_r"], x["d_n"], *d, **x["ways"])
+    w = between_wanted(x)
+    for n, got, want in zip(("r_out", "n_out", "dy", "dr", "dgate"), (*out, *d), w):
+        near_by_row(n, got, want, bound_of(n, got))
+    for got in d[3:]:
+        assert got is None or torch.isfinite(got).all()
