@@ -33,9 +33,11 @@ Geometry shape_of(int B, int T, int C, bool bf16, bool back, int tokens)
         if (blocks() * few >= (bf16 ? full : 4 * full) || (few >> s.lanes_log2) * tokens >= T) g.threads = few;
     if (g.threads == 256 && blocks() * g.threads < full && tile() < T) g.threads = 512;
     while (s.lanes_log2 > 5 && blocks() * g.threads < full && tile() < T) --s.lanes_log2;
-    if (g.threads == 512 && blocks() * g.threads < full / 2) g.threads = 256;
-    // forward alone: the backward kernel has registers for two waves a SIMD (4 x 2048 tokens of 2048 channels: forward 46 -> 39 us)
-    if (g.threads == 512 && !back && blocks() * 1024 <= full && 2 * tile() <= T) g.threads = 1024;
+    // A workgroup a CU, as large as they come, where most CUs get one and none two.  2048 tokens in BF16, 160 to 252 blocks of channels: 48 to 63 -> 34 to 37 us with 1024 threads instead
+    // of segments, 256 blocks 45 -> 37 instead of 512 threads, 260 62 -> 68; 16384 tokens with decays given 144 blocks 200 -> 195, 129 160 -> 180; float32 gains more.  Forward
+    // alone: the backward kernel has registers for two waves a SIMD.
+    if (g.threads == 512 && !back && blocks() >= 144 && blocks() <= 256 && 2 * tile() <= T) g.threads = 1024;
+    else if (g.threads == 512 && blocks() * g.threads < full / 2) g.threads = 256;
     const long long tiles = (T + tile() - 1) / tile();
     long long wanted = 1;
     if (g.threads == 256 && blocks() * g.threads < full / 4) wanted = std::max(1LL, std::min({full / std::max(blocks() * g.threads, 1LL), tiles, 256LL}));

@@ -109,6 +109,16 @@ def test_recurrence_memory(L):
     assert L.tfno_set_workspace(None, 0) == tfno.OK
 
 
+def test_recurrence_of_a_workgroup_a_cu_goes_without_segments(L):
+    """Blocks of 32 channels, of all sequences: with 144 to 256 of them no size is apart from its neighbours."""
+    def need(B, C, back=0):
+        return L.tfno_gated_recurrence_workspace_bytes(ctypes.byref(recurrence_desc(B=B, T=2048, C=C)), back)
+
+    assert not any(need(B, 20) for B in range(144, 257)) and need(143, 20) > 0
+    assert not any(need(4, C) for C in range(36 * 32, 64 * 32 + 1)) and need(4, 35 * 32) > 0
+    assert all(need(B, 20, 1) > 12 * 20 * B for B in range(144, 256))                    # the gradient goes in segments there
+
+
 def test_step_refuses(L):
     args = pointers("x", "gate", "input_gate", "rate", "states", "slots")
 

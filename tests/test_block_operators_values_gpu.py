@@ -6,7 +6,7 @@ import torch
 
 import block_oracle as oracle
 from block_oracle import BF16, F32
-from test_block_operators_gpu import (INPUTS, PARTS, TYPES, between_inputs, between_wanted, empty, near, recur, recur_back, recurrence_inputs,  # noqa: F401
+from test_block_operators_gpu import (INPUTS, PARTS, TYPES, between_inputs, between_wanted, check_recurrence, empty, near, recur, recur_back, recurrence_inputs,  # noqa: F401
                                       recurrence_wanted, say, tfno)
 
 pytestmark = pytest.mark.gpu
@@ -96,6 +96,17 @@ def test_recurrence_steps_forget_nans_where_sequences_do(tfno, gates):  # noqa: 
         one = [None if x[n] is None else x[n] if n == "rate" else x[n][:, t] for n in INPUTS]
         tfno.gated_recurrence_step(*one, state, o, normalise=x["normalise"])
         same_where_finite(f"step {t}", o, y[:, t].double(), oracle.REL[F32])
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("gates", ("both", "one", "decay", "decay of inputs"))
+@pytest.mark.parametrize("size", [(8, 700, 1000), (8, 600, 640), (5, 520, 933), (255, 520, 20), (144, 513, 31), (143, 513, 31), (257, 520, 20), (8, 700, 1030)])
+def test_recurrence_of_a_workgroup_a_cu(tfno, dtype, gates, size):  # noqa: F811
+    """144 to 256 blocks of 32 channels, for which the forward kernel has its largest workgroups, and the sizes next to them; of different lengths."""
+    B, T, C = size
+    x = recurrence_inputs(dtype, *size, gates, seed=25)
+    x["lengths"] = torch.tensor([T, 0, 1, T - 1, 256, *((b * 101 + 7) % (T + 1) for b in range(5, B))], dtype=torch.int32, device="cuda")
+    check_recurrence(tfno, x, f"[case] a workgroup a CU {dtype} {gates} {size}")
 
 
 # ---------------------------------------------------------------- norms around a block
