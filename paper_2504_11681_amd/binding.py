@@ -875,12 +875,14 @@ def block_norm_backward(y, r, gate, w_after, w_before, d_r_out, d_n_out, dy, dr,
 
 def clip_grad_norm(gradients, limit: float, norm=None, stream=None):
     """Scales the gradients (float32, bfloat16 or complex64 tensors on one device, each filling its own memory) in place so that the norm over all their elements is at
-    most `limit`; math.inf gives the norm alone.  norm: one float32 on the device for the norm before that, or None.  Gradients whose norm is not finite stay as they are."""
+    most `limit`; math.inf gives the norm alone.  A gradient may be None (of a parameter that has none).  norm: one float32 on the device for the norm before that, or None.
+    Gradients whose norm is not finite stay as they are."""
     m = _marshal or _load_marshal()
     gradients = gradients if isinstance(gradients, (list, tuple)) else list(gradients)
-    if not gradients and norm is None:
+    first = norm if norm is not None else next((g for g in gradients if g is not None), None)
+    if first is None:
         return norm
-    device = (norm if norm is not None else gradients[0]).device
+    device = first.device
     if device.type != "cuda":
         raise TypeError("gradients must be tensors on the device")
     ensure_workspace(_entry("tfno_clip_grad_norm_workspace_bytes")(len(gradients)), device)

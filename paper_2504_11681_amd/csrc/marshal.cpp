@@ -123,7 +123,7 @@ PyObject *recurrence_step(PyObject *, PyObject *const *args, Py_ssize_t count) {
 PyObject *block_norm(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.block_norm, args, count); }
 PyObject *block_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t count) { return call(library.block_norm_backward, args, count); }
 
-// Tensors of any number as the entry point takes them, and its call: (tensors, limit, norm or None, device, stream).  Here are all checks of the tensors' types and
+// Tensors of any number (None is skipped) as the entry point takes them, and its call: (tensors, limit, norm or None, device, stream).  Here are all checks of the tensors' types and
 // layouts: through Python they took longer than the kernels of a small model.
 PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t count)
 {
@@ -141,7 +141,9 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t count)
         PyObject **items = PySequence_Fast_ITEMS(list);
         std::vector<tfno_tensor> tensors((size_t)n);
         const char *wrong = nullptr;
+        size_t there = 0;
         for (Py_ssize_t i = 0; i < n && !wrong; ++i) {
+            if (items[i] == Py_None) continue;         // of a parameter without a gradient
             if (!THPVariable_Check(items[i])) {
                 wrong = "gradients must be tensors";
                 break;
@@ -151,7 +153,7 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t count)
             if (t.layout() != at::kStrided || !t.is_cuda() || t.get_device() != device) wrong = "gradients must be dense tensors on one device";
             else if (type != at::kFloat && type != at::kBFloat16 && type != at::kComplexFloat) wrong = "gradients must be float32, bfloat16 or complex64";
             else if (!t.is_non_overlapping_and_dense()) wrong = "gradients must fill their memory, in whatever order of axes";
-            else tensors[i] = {t.numel() ? t.data_ptr() : nullptr, (long long)t.numel() * (type == at::kComplexFloat ? 2 : 1), type == at::kBFloat16 ? TFNO_BF16 : TFNO_F32};
+            else tensors[there++] = {t.numel() ? t.data_ptr() : nullptr, (long long)t.numel() * (type == at::kComplexFloat ? 2 : 1), type == at::kBFloat16 ? TFNO_BF16 : TFNO_F32};
         }
         float *norm = nullptr;
         if (!wrong && args[2] != Py_None) {
@@ -166,7 +168,7 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t count)
         } else {
             tfno_status st;
             Py_BEGIN_ALLOW_THREADS
-            st = library.clip(tensors.data(), (int)n, limit, norm, stream);
+            st = library.clip(tensors.data(), (int)there, limit, norm, stream);
             Py_END_ALLOW_THREADS
             result = PyLong_FromLong(st);
         }

@@ -189,3 +189,26 @@ def test_norms_and_gradient_of_rows_of_any_size(tfno, types, after, C):  # noqa:
         near_by_row(n, got, want, bound_of(n, got))
     for got in d[3:]:
         assert got is None or torch.isfinite(got).all()
+
+
+# ---------------------------------------------------------------- clipping
+
+def test_clip_skips_parameters_without_a_gradient(tfno):  # noqa: F811
+    """As a list of parameters' gradients has them: None where a weight is frozen or was not used."""
+    model = torch.nn.Sequential(torch.nn.Linear(30, 40), torch.nn.Linear(40, 50), torch.nn.Linear(50, 3)).cuda()
+    model[0].weight.requires_grad_(False)
+    model[1](torch.randn(7, 40, device="cuda")).square().sum().backward()
+    grads, norm = [p.grad for p in model.parameters()], torch.empty((), device="cuda")
+    assert grads[0] is None and grads[-1] is None
+    want = math.sqrt(sum(float(g.double().square().sum()) for g in grads if g is not None))
+    scaled = [g.double() * (0.5 / want) for g in grads if g is not None]
+    tfno.clip_grad_norm((p.grad for p in model.parameters()), 0.5, norm)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+    for g, w in zip((g for g in grads if g is not None), scaled):
+        near("clipped", g, w, 2.0 ** -24 * (1 + 2.0 ** -10))
+    tfno.clip_grad_norm(grads, 0.25)                            # a device to go by without a norm
+    near("clipped again", grads[2], scaled[0] / 2, 2.0 ** -23 * (1 + 2.0 ** -10))
+    tfno.clip_grad_norm([None, None], 1.0, norm)
+    assert float(norm) == 0 and tfno.clip_grad_norm([None], 1.0) is None
+    with pytest.raises(TypeError):
+        tfno.clip_grad_norm([None, grads[2], 3.0], 1.0)
