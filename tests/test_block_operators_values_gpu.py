@@ -109,6 +109,78 @@ def test_recurrence_of_a_workgroup_a_cu(tfno, dtype, gates, size):  # noqa: F811
     check_recurrence(tfno, x, f"[case] a workgroup a CU {dtype} {gates} {size}")
 
 
+def recurrence_sizes(x):
+    """What the terms of y, final, and the gradients of x, gate, input_gate, rate and the initial state add up to without their signs.  A float32 result is as far off as its terms'
+    roundings, which oracle.REL and the others count for terms of one size, whatever cancels in it.  A decay exp(l) is |l| times as far off as l: l is a product with a sigmoid, which is
+    (1 + |gate|) 2^-24 off, and 4 2^-24 more, 10 2^-24 in all; so a term that has gone through decays whose l add up to L has 10 L roundings more.  Each decay counts 1 + |l| / 4 times here:
+    their product is 1 + L / 4 at least, and 64 of it the 64 of oracle.REL and 16 L."""
+    live = oracle.live_of(x["lengths"], *x["x"].shape[:2], "cuda")
+    at, gate, into, d_y = (oracle.only(live, x[n]) for n in ("x", "gate", "input_gate", "d_y"))
+    at, d_y = at.abs(), d_y.abs()
+    s = None if x["rate"] is None else torch.sigmoid(gate)
+    l = gate if s is None else -x["rate"].double() * s
+    a, o = l.exp() * (1 - l / 4), torch.ones_like(at) if into is None else torch.sigmoid(into)
+    left = torch.sqrt(-torch.expm1(2 * l)) if x["normalise"] else torch.ones_like(at)
+    h, before, y = x["initial"].double().abs(), [], torch.zeros_like(at)
+    for t in range(at.shape[1]):
+        before.append(h)
+        h = torch.where(live[:, t], a[:, t] * h + at[:, t] * o[:, t] * left[:, t], h)
+        y[:, t] = torch.where(live[:, t], h, 0.0)
+    final, D = h, x["d_final"].double().abs()
+    dx, dl, do = (torch.zeros_like(at) for _ in range(3))
+    for t in reversed(range(at.shape[1])):
+        G = D + d_y[:, t]
+        through = a[:, t] * before[t]
+        if x["normalise"]:
+            through = through + at[:, t] * o[:, t] * a[:, t] ** 2 / left[:, t]
+        for out, v in ((dx, o[:, t] * left[:, t]), (do, at[:, t] * left[:, t]), (dl, through)):
+            out[:, t] = torch.where(live[:, t], G * v, 0.0)
+        D = torch.where(live[:, t], a[:, t] * G, D)
+    return (y, final, dx, dl if s is None else dl * x["rate"].double() * s * (1 - s), None if into is None else do * o * (1 - o), None if s is None else (dl * s).sum((0, 1)), D)
+
+
+def near_by_channel(name, got, want, size, bound):
+    """Every channel of every sequence by itself (of [B, T, C]), or every value, against the size of its terms."""
+    assert torch.isfinite(got).all(), name
+    off = got.double() - want
+    if got.dim() == 3:
+        off, size = off.norm(dim=1), size.norm(dim=1)
+    off = off.abs()
+    worst = float(torch.where(size > 0, off / size, off).max())
+    say(f"   {name}: {worst:.3g} of {bound:.3g} in the worst channel")
+    assert worst <= bound, name
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("gates", ("both", "one", "decay", "decay of inputs"))
+@pytest.mark.parametrize("size", [(3, 300, 70), (7, 130, 33), (1, 1500, 6), (5, 513, 933), (4200, 13, 70), (300, 70, 64)])
+def test_recurrence_every_channel_by_itself(tfno, dtype, gates, size):  # noqa: F811
+    """Channels and sequences whose values, gradients and rates differ by orders of magnitude, and sequences of few tokens among long ones."""
+    B, T, C = size
+    x = recurrence_inputs(dtype, *size, gates, seed=26)
+    gen = torch.Generator("cuda").manual_seed(26)
+
+    def scales(*shape):
+        return 10.0 ** (6 * torch.rand(*shape, generator=gen, device="cuda") - 3)
+
+    for values, state in (("x", "initial"), ("d_y", "d_final")):
+        scale = scales(B, C)
+        x[values], x[state] = (x[values].float() * scale[:, None]).to(dtype), x[state] * scale
+    if x["rate"] is not None:
+        x["rate"] = 10.0 ** (7 * torch.rand(C, generator=gen, device="cuda") - 5)
+    if B > 1:
+        x["lengths"] = torch.tensor([T, 1, *(1 + (b * 101 + 7) % T for b in range(2, B))], dtype=torch.int32, device="cuda")
+    say(f"[case] channels {dtype} {gates} {size}")
+    tape = tfno.gated_recurrence_tape(x["x"])
+    y, final = recur(tfno, x, tape)
+    d = recur_back(tfno, x, tape)
+    bounds = (oracle.REL[dtype], oracle.REL[F32], oracle.REL[dtype], oracle.REL_GATES[dtype], oracle.REL[dtype], oracle.REL_SUMS, oracle.REL[F32])
+    for n, got, w, s, bound in zip(("y", "final", "dx", "dgate", "dinput", "drate", "dinitial"), (y, final, *(d[k] for k in (*INPUTS, "initial"))), recurrence_wanted(x),
+                                   recurrence_sizes(x), bounds):
+        if got is not None:
+            near_by_channel(n, got, w, s, bound)
+
+
 # ---------------------------------------------------------------- norms around a block
 
 def norms_and_gradients(tfno, x):
@@ -189,6 +261,52 @@ def test_norms_and_gradient_of_rows_of_any_size(tfno, types, after, C):  # noqa:
         near_by_row(n, got, want, bound_of(n, got))
     for got in d[3:]:
         assert got is None or torch.isfinite(got).all()
+
+
+def sums_sizes(x):
+    """What the terms of dw_after, dw_before and of the gradient of a gate that tokens share add up to without their signs; the two terms of the slope of z sigmoid(z), which cancel near
+    z = -1.28, among them."""
+    w = x["ways"]
+    live = oracle.live_of(w["lengths"], *x["y"].shape[:2], "cuda")
+    y, r, d_r, d_n = (oracle.only(live, x[n]) for n in ("y", "r", "d_r", "d_n"))
+    wa, wb, gate = (None if x[n] is None else x[n].double() for n in ("w_after", "w_before", "gate"))
+    m = y / torch.sqrt((y * y).mean(-1, keepdim=True) + w["eps"])
+    z, slope = torch.ones_like(m), torch.zeros_like(m)
+    if gate is not None:
+        g = oracle.only(live, gate) if gate.dim() == 3 else gate[:, None].expand_as(m) if gate.dim() == 2 else gate.expand_as(m)
+        o = torch.sigmoid(g)
+        z, slope = {"none": (g, torch.ones_like(g)), "silu": (g * o, o * (1 + g.abs() * (1 - o))), "sigmoid": (o, o * (1 - o))}[w["activation"]]
+    stream, size = w["residual_scale"] * r + z * m * wa, (w["residual_scale"] * r).abs() + (z * m * wa).abs()
+    q = 1 / torch.sqrt((stream * stream).mean(-1, keepdim=True) + w["eps"])
+    b = (d_n * wb).abs()
+    d = d_r.abs() + q * (b + size * q * (q * (b * size).mean(-1, keepdim=True)))
+    of_gate = torch.where(live, d * (m * wa * slope).abs(), 0.0)
+    return (d * (z * m).abs()).sum((0, 1)), (d_n.abs() * size * q).sum((0, 1)), of_gate.sum(1) if gate is not None and gate.dim() == 2 else of_gate.sum((0, 1))
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("gate", ("none", "token", "sequence", "channel"))
+@pytest.mark.parametrize("size", [(2, 30, 40), (3, 700, 64), (900, 5, 40), (2100, 70, 64), (600, 20, 256), (70, 40, 1000), (9, 6, 5000)])
+def test_norms_every_row_and_channel_by_itself(tfno, types, gate, size):  # noqa: F811
+    """Rows whose values and gradients differ by orders of magnitude; many sequences with gates of their own, long and short ones."""
+    B, T, C = size
+    x = between_inputs(*types, *size, gate, "silu", seed=24)
+    gen = torch.Generator("cuda").manual_seed(24)
+    for names in (("y",), ("r",), ("d_r", "d_n")):
+        scale = 10.0 ** (4 * torch.rand(B, T, 1, generator=gen, device="cuda") - 2)
+        for n in names:
+            x[n] = (x[n].float() * scale).to(x[n].dtype)
+    x["ways"]["lengths"] = torch.tensor([T, *(1 + (b * 101 + 7) % T for b in range(1, B))], dtype=torch.int32, device="cuda")
+    say(f"[case] rows by themselves {types} {gate} {size}")
+    got, w = norms_and_gradients(tfno, x), between_wanted(x)
+    sizes = dict(zip(("dw_after", "dw_before", "dgate"), sums_sizes(x)))
+    for (n, t), want in zip(got.items(), w):
+        if t is None:
+            continue
+        if t.dim() == 3:
+            near_by_row(n, t, want, bound_of(n, t))
+        else:
+            near_by_channel(n, t, want, sizes[n], oracle.REL_SUMS)
 
 
 # ---------------------------------------------------------------- clipping
