@@ -15,8 +15,12 @@ namespace {
 constexpr int CLIP_THREADS = 256, CLIP_TENSORS = 128, CLIP_BLOCKS = 2048;
 constexpr int CLIP_ROUND = CLIP_THREADS * 4;        // vectors of 16 bytes in a piece
 
-// Loads and stores that leave the last-level cache alone: what is read next is as large as what it holds (both passes over 510 MB in BF16 314 -> 277 us; the stores alone 293).
 typedef unsigned Vector __attribute__((ext_vector_type(4)));
+
+// Tensors of more bytes than this are loaded and stored past the caches (PAST): more than those hold, so the second pass finds little of them, and whoever wrote them and reads them next
+// neither.  Fewer are kept.  A step that writes gradients, clips and reads them, kept and past: 1 MB 119 and 130 us, 64 MB 191 and 213, 192 MB 407 and 418, 288 MB 615 and 622, 320 MB
+// 666 and 662, 512 MB 1000 and 961; clipping by itself, again and again: 64 MB 39 and 43, 288 MB 148 and 161, 352 MB 186 and 194, 512 MB 294 and 274.
+constexpr unsigned long long CLIP_KEPT = 300ull << 20;
 
 struct ClipTable {
     void *p[CLIP_TENSORS];
@@ -61,10 +65,14 @@ struct Piece {
         to = min(skip + t.n[tensor] - vector * per, (long long)CLIP_ROUND * per);
         whole = from == 0 && to == (long long)CLIP_ROUND * per;
     }
+    template <bool PAST>
     __device__ __forceinline__ void load(Vector (&in)[4]) const
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) in[i] = __builtin_nontemporal_load(p + threadIdx.x + i * CLIP_THREADS);
+        for (int i = 0; i < 4; ++i) {
+            const Vector *at = p + threadIdx.x + i * CLIP_THREADS;
+            in[i] = PAST ? __builtin_nontemporal_load(at) : *at;
+        }
     }
 };
 
@@ -99,6 +107,7 @@ __device__ __forceinline__ double block_sum(double v, double (&meet)[CLIP_THREAD
     return all;
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(CLIP_THREADS) void k_clip_squares(ClipTable t, double *partial)
 {
     __shared__ double meet[CLIP_THREADS / 64];
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_squares(ClipTable t, doub
     unsigned piece = blockIdx.x;
     Piece at(t, piece);
     Vector next[4];
-    if (at.whole) at.load(next);
+    if (at.whole) at.template load<PAST>(next);
     while (piece < end) {
         const Piece now = at;
         Vector in[4];
@@ -115,7 +124,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_squares(ClipTable t, doub
         for (int i = 0; i < 4; ++i) in[i] = next[i];
         if ((piece += gridDim.x) < end) {
             at.go(t, piece);
-            if (at.whole) at.load(next);
+            if (at.whole) at.template load<PAST>(next);
         }
         if (now.whole) {
 #pragma unroll
@@ -131,6 +140,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_squares(ClipTable t, doub
 
 __device__ __forceinline__ float scaled(float x, double scale) { return (float)((double)x * scale); }
 
+template <bool PAST>
 __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(ClipTable t, const double *partial, int partials, double limit, float *norm)
 {
     __shared__ double meet[CLIP_THREADS / 64];
@@ -145,7 +155,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(ClipTable t, const 
     unsigned piece = pieces - 1 - blockIdx.x;
     Piece at(t, piece);
     Vector next[4];
-    if (at.whole) at.load(next);
+    if (at.whole) at.template load<PAST>(next);
     for (;;) {
         const Piece now = at;
         Vector in[4];
@@ -154,7 +164,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(ClipTable t, const 
         const bool more = piece >= gridDim.x;
         if (more) {
             at.go(t, piece -= gridDim.x);
-            if (at.whole) at.load(next);
+            if (at.whole) at.template load<PAST>(next);
         }
         if (now.whole) {
 #pragma unroll
@@ -165,7 +175,9 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_scale(ClipTable t, const 
                     if (now.bf16) w[e] = bf16_pair(scaled(__uint_as_float(w[e] << 16), scale), scaled(__uint_as_float(w[e] & 0xffff0000u), scale));
                     else w[e] = __float_as_uint(scaled(__uint_as_float(w[e]), scale));
                 }
-                __builtin_nontemporal_store(Vector{w[0], w[1], w[2], w[3]}, now.p + threadIdx.x + k * CLIP_THREADS);
+                Vector *to = now.p + threadIdx.x + k * CLIP_THREADS;
+                if (PAST) __builtin_nontemporal_store(Vector{w[0], w[1], w[2], w[3]}, to);
+                else *to = Vector{w[0], w[1], w[2], w[3]};
             }
         } else {
             for (long long k = now.from + threadIdx.x; k < now.to; k += CLIP_THREADS) {
@@ -196,16 +208,15 @@ int fill(ClipTable &t, const tfno_tensor *tensors, int from, int count)
 }
 unsigned blocks_of(const ClipTable &t) { return std::min(t.first[t.count], (unsigned)CLIP_BLOCKS); }
 
-}  // namespace
-
-hipError_t clip_launch(const tfno_tensor *tensors, int count, double limit, float *norm, double *partial, hipStream_t s)
+template <bool PAST>
+hipError_t clip(const tfno_tensor *tensors, int count, double limit, float *norm, double *partial, hipStream_t s)
 {
     ClipTable t;
     int partials = 0;
     for (int from = 0; from < count;) {
         from = fill(t, tensors, from, count);
         if (const unsigned grid = blocks_of(t)) {
-            k_clip_squares<<<grid, CLIP_THREADS, 0, s>>>(t, partial + partials);
+            k_clip_squares<PAST><<<grid, CLIP_THREADS, 0, s>>>(t, partial + partials);
             partials += grid;
         }
     }
@@ -213,15 +224,24 @@ hipError_t clip_launch(const tfno_tensor *tensors, int count, double limit, floa
     for (int from = 0; from < count;) {
         from = fill(t, tensors, from, count);
         if (const unsigned grid = blocks_of(t)) {
-            k_clip_scale<<<std::isinf(limit) ? 1 : grid, CLIP_THREADS, 0, s>>>(t, partial, partials, limit, wrote ? nullptr : norm);
+            k_clip_scale<PAST><<<std::isinf(limit) ? 1 : grid, CLIP_THREADS, 0, s>>>(t, partial, partials, limit, wrote ? nullptr : norm);
             if (wrote = true; std::isinf(limit)) break;
         }
     }
     if (!wrote) {       // no element at all
         t.count = 0, t.first[0] = 0;
-        k_clip_scale<<<1, CLIP_THREADS, 0, s>>>(t, partial, 0, limit, norm);
+        k_clip_scale<PAST><<<1, CLIP_THREADS, 0, s>>>(t, partial, 0, limit, norm);
     }
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t clip_launch(const tfno_tensor *tensors, int count, double limit, float *norm, double *partial, hipStream_t s)
+{
+    unsigned long long bytes = 0;
+    for (int i = 0; i < count; ++i) bytes += (unsigned long long)tensors[i].elements * (tensors[i].dtype == TFNO_BF16 ? 2 : 4);
+    return bytes > CLIP_KEPT ? clip<true>(tensors, count, limit, norm, partial, s) : clip<false>(tensors, count, limit, norm, partial, s);
 }
 
 size_t clip_workspace_bytes(int count) { return sizeof(double) * CLIP_BLOCKS * (size_t)(count / CLIP_TENSORS + 1); }

@@ -330,3 +330,21 @@ def test_clip_skips_parameters_without_a_gradient(tfno):  # noqa: F811
     assert float(norm) == 0 and tfno.clip_grad_norm([None], 1.0) is None
     with pytest.raises(TypeError):
         tfno.clip_grad_norm([None, grads[2], 3.0], 1.0)
+
+
+@pytest.mark.parametrize("million", (70, 90))
+def test_clip_of_what_caches_hold_and_of_more(tfno, million):  # noqa: F811
+    """280 and 360 MB: both ways to load and store, whole pieces and their ends."""
+    n = million * 1000 * 1000
+    gen = torch.Generator("cuda").manual_seed(million)
+    memory = torch.randn(n // 2 + 5, generator=gen, device="cuda")
+    tensors = [memory[1:n // 2 + 1], torch.randn(n + 3, generator=gen, device="cuda").to(BF16)[3:], torch.randn(7, generator=gen, device="cuda")]
+    before, norm = [t.clone() for t in tensors], torch.empty((), device="cuda")
+    ends = memory[[0, -4, -3, -2, -1]].clone()
+    want = math.sqrt(sum(float(t.double().square().sum()) for t in tensors))
+    tfno.clip_grad_norm(tensors, math.inf, norm)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want and all(torch.equal(a, b) for a, b in zip(tensors, before))
+    tfno.clip_grad_norm(tensors, 1.0, norm)
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want and torch.equal(memory[[0, -4, -3, -2, -1]], ends)
+    for t, b in zip(tensors, before):
+        near(str(t.dtype), t, b.double() / want, (2.0 ** -8 if t.dtype == BF16 else 2.0 ** -24) * (1 + 2.0 ** -10))
