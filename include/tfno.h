@@ -410,9 +410,10 @@ tfno_status tfno_gated_delta_rule_step(const tfno_delta_rule_desc *d, const void
  *   u = x, times sigmoid(input_gate) where that is not NULL, times sqrt(1 - exp(2 l)) where `normalise` is set
  *
  * with x, gate, input_gate, y [B, T, C], rate float32 [C], finite and not negative, and states float32 [B, C], contiguous; h starts from `initial` (NULL: zeros).
- * Where exp(l) is 0 in float32 (l = -inf, say) the state is forgotten, whatever it holds.  l should be 0 or less: above that the state grows, which is right as long as the
- * growth over any run of tokens is finite, and `normalise` gives NaN.  `lengths` as for the rule above: tokens past them are not read, their outputs
- * and gradients are zeros.  A NaN or an infinity in a token makes its channel NaN from there to the next decay of 0.
+ * Where exp(l) is 0 in float32 (l = -inf, say) the state is forgotten, whatever it holds; other decays, and products of them, that are below 2^-126 may count
+ * as that.  l should be 0 or less: above that the state grows, which is right as long as the growth over any run of tokens is finite, and `normalise` gives NaN.  `lengths` as for the
+ * rule above: tokens past them are not read, their outputs and gradients are zeros.  A NaN or an infinity in a token makes its channel NaN or infinite from there to the next decay of 0,
+ * and gradients that pass through it as far back as the decay of 0 before.
  *
  * The whole sequence: y, and the last state into `final` where it is not NULL.  With a tape (tfno_gated_recurrence_tape_bytes bytes, aligned to 256) the call leaves there
  * the states (float32) that the backward call starts from.  Both need tfno_gated_recurrence_workspace_bytes(d, backward) bytes of workspace, which may be 0.

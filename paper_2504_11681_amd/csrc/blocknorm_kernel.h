@@ -8,7 +8,8 @@
 // the backward pass makes s again from y, r and the gate instead of reading it back: as many bytes, and s as it was before its rounding.  Sums over
 // tokens (of the weights' gradients, of a gate that tokens share) stay in registers over a group's rows, then a workgroup leaves one row of each in the
 // workspace, which k_column_sums adds up in their order.  A group's rows lie one behind the other, and the next one's values wait in registers as they stand in memory (16 x 1024
-// tokens of 2048 in BF16 with a float32 residual: forward 173 -> 79 us, 403 MB, 5.1 TB/s, with a row a workgroup and its weights read for each; gradient 187 -> 140, 604 MB).
+// tokens of 2048 in BF16 with a float32 residual: forward 82 us, 403 MB, 4.9 TB/s, gradient 143, 604 MB, 4.2 TB/s; with a row a workgroup and its weights read for each 173 and 187).
+// Rows of more than 4096 take sixteen values a lane, for which the gradient has too few registers: 255 or 256, and all but one kernel spill, up to 304 bytes a lane.
 #pragma once
 #include "blocknorm.h"
 #include "gates.h"
@@ -79,7 +80,9 @@ struct Eight<bf16, true> {
     }
     __device__ __forceinline__ static void store(bf16 *p, int, int, const float (&v)[8])
     {
-        // whole lines that nobody reads soon (16 x 8192 heads of 128, both directions: 70 -> 65 us); the two halves of a lane's float32 values would be parts of lines
+        // whole lines, past the caches: 16 x 1024 of 1024 forward 40 us, else 41, gradient 79 and 79, 131072 heads of 128 29 and 30, 52 and 53.  What reads them next is as fast or
+        // faster, but a product behind little: n_out of 16 x 64 of 1024 and a product 25.6 us, else 23.6, of 2 x 256 of 2048 26.9 and 25.6, of 16 x 1024 of 1024 58 and 59, of
+        // 16 x 1024 of 2048 131 and 130.  The two halves of a lane's float32 values would be parts of lines
         typedef unsigned vector __attribute__((ext_vector_type(4)));
         __builtin_nontemporal_store(vector{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, (vector *)p);
     }

@@ -2,21 +2,21 @@
 //
 //   D_t = dy_t + a_{t+1} D_{t+1},   du = D,   dl = D a h_{t-1} - D x sigmoid(input_gate) a^2 / sqrt(1 - a^2).
 //
-// Every input is read once and every output written once; a value takes 46 vector instructions (backward 100), five of them of the slow kind (exp2, 1/x, square root), so with
-// BF16 both sides are near: 256 x 1024 tokens of 128 channels 63 us (269 MB, 4.3 TB/s; vector pipes 50 us).  A workgroup takes 64 or 32 neighbouring channels and walks through a sequence
+// Every input is read once and every output written once; a value takes 46 vector instructions (56 where groups of 32 lanes are joined, backward 100), five of them of the slow kind
+// (exp2, 1/x, square root), so with BF16 both sides are near: 256 x 1024 tokens of 128 channels 62 us (269 MB, 4.3 TB/s; vector pipes busy for 44).  A workgroup takes 64 or 32 neighbouring channels and walks through a sequence
 // in tiles; a tile is shared out over time among groups of as many lanes, each with S tokens in a row, whose loads are all under way while the tile before is worked on.  A
 // group makes of its tokens one map h -> a h + B (backward also e -> a e + R for what comes from later tokens); the maps are joined along the wave by shuffles and along the
 // workgroup in LDS, and each group then walks its tokens from the state that the maps before it give.  Sequences too few to fill the chip are cut into segments, whose maps a
 // kernel of its own finds first.  One channel a lane: with two the maps of a lane are joined twice and the gradient has 256 registers.  Workgroups that are neighbours in memory share an XCD: half lines of
-// channels were read twice otherwise (4 x 2048 tokens of 2048 channels, both directions, 144 -> 131 us).
+// channels were read twice otherwise (4 x 2048 tokens of 2048 channels, both directions, 143 -> 129 us).
 #pragma once
 #include "gates.h"
 #include "recurrence.h"
 
 namespace tfno {
 
-// Tokens of a group in a tile.  Forward four waves a SIMD have registers for that (with 16, which two have, 77 -> 85 us for the batch above); backward two (with 4 and four waves
-// 131 -> 137 us for the two directions above: twice the joining).
+// Tokens of a group in a tile.  Forward four waves a SIMD have registers for that (with 16, which two have, 70 -> 82 us for the batch above, each time on other inputs); backward two
+// (with 4 129 -> 146 us for the two directions above: twice the joining).
 constexpr int RECURRENCE_TOKENS = 8, RECURRENCE_TOKENS_BACK = 8;
 
 // What a kernel knows of its gates: ALL has rates, an input gate and `normalise`, NONE neither, RATES all but an input gate; ANY asks.
